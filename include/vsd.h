@@ -358,6 +358,98 @@ vsd_status vsd_lmhead_backward(const void* hidden, const void* weight, int32_t H
                                const vsd_params* params, float* d_hidden, float* d_weight,
                                void* ws, size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Supervised losses of the draft head: the objectives a draft is trained on
+ * before (or beside) the EM step, each with its gradient.
+ *
+ *   x = hidden . weight^T (the LM-head calls) or the logits given,
+ *   q_r = softmax(x_r / T),
+ *   l_r = sum_k p_rk (log p_rk - log q_r(id_rk)),
+ *   loss = sum_r w_r l_r / sum_r w_r      over the counted rows (0 if the
+ *                                         weights sum to 0),
+ *   d loss / d x_rv = w_r / (T sum w) (q_r(v) - sum_k p_rk [v = id_rk]).
+ *
+ * The target p is the label's one-hot (cross entropy, T = 1), or the teacher's
+ * top logits renormalised over the row's valid entries,
+ * p_rk = softmax_k(teacher_rk / T) (Eq. klv's distribution, from supplied
+ * logits).  A row is counted unless its label is ignore_index, or none of its
+ * teacher entries is valid; rows not counted have loss, logz and gradient 0,
+ * whatever their hidden states or logits hold (NaN included).
+ *   labels         [R]; a label outside [0, V) other than ignore_index sets
+ *                  VSD_STATUS_BAD_TOKEN and its row is not counted.
+ *   teacher_ids    [R][K]; a negative id is no entry (its logit is not looked
+ *                  at); one >= V sets VSD_STATUS_BAD_TOKEN and is no entry.
+ *                  Entries may come in any order; equal ids add.
+ *   teacher_logits [R][K] of teacher_dtype; -inf is an entry without mass; NaN
+ *                  or +inf sets VSD_STATUS_BAD_ROW, the row is not counted.
+ *   row_weight     [R] w_r >= 0, or NULL for 1; a negative or non-finite one
+ *                  sets VSD_STATUS_BAD_ROW, the row is not counted.
+ *   grad_scale     multiplies the gradients (not the loss).
+ * A counted row whose log-partition is not finite (NaN or +inf logits, or all
+ * -inf) sets VSD_STATUS_BAD_ROW; NaN then spreads as in the formulas.
+ * Sums are in fp32 or wider and in a fixed order: a call repeated on the same
+ * inputs gives the same bits.
+ * ------------------------------------------------------------------------ */
+
+/* Outputs (device, caller-owned).  loss, row_loss and logz are required; a NULL
+ * gradient is neither computed nor written. */
+typedef struct {
+    float* loss;     /* [1]                                                       */
+    float* row_loss; /* [R] l_r                                                   */
+    float* logz;     /* [R] log sum_v exp(x_rv / T)                               */
+    void* d_hidden;  /* LM-head calls: [R][H] bf16 (the type of its tensor)       */
+    void* d_weight;  /* LM-head calls: [V][H] bf16                                */
+    void* grad;      /* vsd_topk_distill: [R][V] of the logits' dtype; may be the
+                        logits themselves (then overwritten)                      */
+} vsd_loss_outputs;
+
+/* Bytes of device workspace of the LM-head losses (0 if a size is invalid).
+ * K: entries of a teacher row (1 for labels); grads: whether a gradient is
+ * asked for; piece: vocabulary columns worked on at a time, 0 = the library's
+ * choice.  The logits are never kept whole when R is large: the workspace holds
+ * the gradient of one piece (bf16).  Where a piece spans the vocabulary and its
+ * logits are no larger than the weight (few rows), they are kept and made
+ * once.  A larger piece uses more workspace and fewer launches. */
+size_t vsd_lmhead_loss_workspace_bytes(int32_t R, int32_t V, int32_t H, int32_t K, int32_t grads,
+                                       int32_t piece);
+
+/* Cross entropy of labels under the LM head (T = 1), without keeping the
+ * logits, with the gradients of the hidden states and of the weight.
+ *   hidden  device, bf16 [R][H]; weight  device, bf16 [V][H];
+ *   H a multiple of 8, both pointers and the gradients 16-byte aligned
+ *   (VSD_ERR_INVALID_ARG); 1 <= V <= 1048576, 1 <= R <= 16777216.
+ * Logits are sums of exact products in fp32, never rounded to bf16; their
+ * gradient is rounded to bf16 once, as the operand of the two products that
+ * carry it, and those are summed in fp32 and rounded once to bf16.  ws as for
+ * the other calls (256-byte aligned, its first word the status word, cleared
+ * here). */
+vsd_status vsd_lmhead_cross_entropy(const void* hidden, const void* weight, int32_t R, int32_t V,
+                                    int32_t H, const int32_t* labels, int32_t ignore_index,
+                                    const float* row_weight, float grad_scale, int32_t piece,
+                                    vsd_loss_outputs* out, void* ws, size_t ws_bytes,
+                                    void* stream);
+
+/* The LM head distilled from a teacher's top logits, as above with
+ * 1 <= K <= 128; T finite and > 0. */
+vsd_status vsd_lmhead_distill(const void* hidden, const void* weight, int32_t R, int32_t V,
+                              int32_t H, const int32_t* teacher_ids, const void* teacher_logits,
+                              vsd_dtype teacher_dtype, int32_t K, float T,
+                              const float* row_weight, float grad_scale, int32_t piece,
+                              vsd_loss_outputs* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Bytes of device workspace of vsd_topk_distill (0 if a size is invalid). */
+size_t vsd_topk_distill_workspace_bytes(int32_t R, int32_t V, int32_t K);
+
+/* Distillation from a teacher's top logits on logits in hand, [R][V] of
+ * `dtype` (-inf marks a token without mass), with their gradient.  Any V;
+ * rows that are 16-byte aligned take the bulk-copy path, others a scalar one
+ * with the same results. */
+vsd_status vsd_topk_distill(const void* logits, vsd_dtype dtype, int32_t R, int32_t V,
+                            const int32_t* teacher_ids, const void* teacher_logits,
+                            vsd_dtype teacher_dtype, int32_t K, float T,
+                            const float* row_weight, float grad_scale, vsd_loss_outputs* out,
+                            void* ws, size_t ws_bytes, void* stream);
+
 /* The greedy reference of Algorithm 2 from its own rows: the oracle's z-bar
  * is drawn from the greedy target policy, so its validity log kappa(z-bar)
  * needs the draft and target distributions along z-bar, which the caller

@@ -12,6 +12,7 @@
 
 #include "vsd.h"
 #include "vsd_launch.h"
+#include "vsd_loss.h"
 
 namespace vsd {
 namespace {
@@ -659,6 +660,83 @@ vsd_status vsd_lmhead_backward(const void* hidden, const void* weight, int32_t H
         at<void>(ws, w.bfac), d_hidden, d_weight, at<int>(ws, w.status), p.wait_timeout_ns ? p.wait_timeout_ns : kDefaultTimeoutNs,
         static_cast<cudaStream_t>(stream));
     return from_cuda(e);
+}
+
+// The checks that the supervised losses share; Targets' ws and outputs.
+static vsd_status check_loss_call(const vsd_loss_outputs* out, float T, float grad_scale) {
+    if (!out || !out->loss || !out->row_loss || !out->logz) return VSD_ERR_INVALID_ARG;
+    if (!(T > 0.f) || !isfinite(T) || !isfinite(grad_scale)) return VSD_ERR_INVALID_ARG;
+    return VSD_OK;
+}
+
+static vsd_status lmhead_loss_call(const void* hidden, const void* weight, int32_t H,
+                                   const TargetIn& in, float T, float grad_scale, int32_t piece,
+                                   const vsd_loss_outputs* out, void* ws, size_t ws_bytes,
+                                   void* stream) {
+    vsd_status st = check_loss_call(out, T, grad_scale);
+    if (st) return st;
+    const LmLossShape s{in.R, in.V, H, in.K, out->d_hidden != nullptr, out->d_weight != nullptr,
+                        piece};
+    if (!hidden || !weight || !lmloss_shape_ok(s)) return VSD_ERR_INVALID_ARG;
+    if (((uintptr_t)hidden | (uintptr_t)weight | (uintptr_t)out->d_hidden |
+         (uintptr_t)out->d_weight) & 15)
+        return VSD_ERR_INVALID_ARG;
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < lmloss_workspace_bytes(s))
+        return VSD_ERR_WORKSPACE;
+    return from_cuda(lmloss(s, hidden, weight, in, T, grad_scale, *out, ws,
+                            static_cast<cudaStream_t>(stream)));
+}
+
+size_t vsd_lmhead_loss_workspace_bytes(int32_t R, int32_t V, int32_t H, int32_t K, int32_t grads,
+                                       int32_t piece) {
+    return lmloss_workspace_bytes(LmLossShape{R, V, H, K, grads != 0, grads != 0, piece});
+}
+
+vsd_status vsd_lmhead_cross_entropy(const void* hidden, const void* weight, int32_t R, int32_t V,
+                                    int32_t H, const int32_t* labels, int32_t ignore_index,
+                                    const float* row_weight, float grad_scale, int32_t piece,
+                                    vsd_loss_outputs* out, void* ws, size_t ws_bytes,
+                                    void* stream) {
+    if (!labels) return VSD_ERR_INVALID_ARG;
+    const TargetIn in{labels, ignore_index, nullptr, nullptr, 0, row_weight, R, V, 1, 1.f};
+    return lmhead_loss_call(hidden, weight, H, in, 1.f, grad_scale, piece, out, ws, ws_bytes,
+                            stream);
+}
+
+vsd_status vsd_lmhead_distill(const void* hidden, const void* weight, int32_t R, int32_t V,
+                              int32_t H, const int32_t* teacher_ids, const void* teacher_logits,
+                              vsd_dtype teacher_dtype, int32_t K, float T,
+                              const float* row_weight, float grad_scale, int32_t piece,
+                              vsd_loss_outputs* out, void* ws, size_t ws_bytes, void* stream) {
+    if (!teacher_ids || !teacher_logits) return VSD_ERR_INVALID_ARG;
+    if (teacher_dtype != VSD_F32 && teacher_dtype != VSD_BF16) return VSD_ERR_INVALID_ARG;
+    const TargetIn in{nullptr, 0, teacher_ids, teacher_logits, teacher_dtype == VSD_BF16,
+                      row_weight, R, V, K, 1.f / T};
+    return lmhead_loss_call(hidden, weight, H, in, T, grad_scale, piece, out, ws, ws_bytes,
+                            stream);
+}
+
+size_t vsd_topk_distill_workspace_bytes(int32_t R, int32_t V, int32_t K) {
+    return topk_workspace_bytes(R, V, K);
+}
+
+vsd_status vsd_topk_distill(const void* logits, vsd_dtype dtype, int32_t R, int32_t V,
+                            const int32_t* teacher_ids, const void* teacher_logits,
+                            vsd_dtype teacher_dtype, int32_t K, float T,
+                            const float* row_weight, float grad_scale, vsd_loss_outputs* out,
+                            void* ws, size_t ws_bytes, void* stream) {
+    if (!logits || !teacher_ids || !teacher_logits || !topk_shape_ok(R, V, K))
+        return VSD_ERR_INVALID_ARG;
+    if (dtype != VSD_F32 && dtype != VSD_BF16) return VSD_ERR_INVALID_ARG;
+    if (teacher_dtype != VSD_F32 && teacher_dtype != VSD_BF16) return VSD_ERR_INVALID_ARG;
+    vsd_status st = check_loss_call(out, T, grad_scale);
+    if (st) return st;
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < topk_workspace_bytes(R, V, K))
+        return VSD_ERR_WORKSPACE;
+    const TargetIn in{nullptr, 0, teacher_ids, teacher_logits, teacher_dtype == VSD_BF16,
+                      row_weight, R, V, K, 1.f / T};
+    return from_cuda(topk_distill(logits, dtype == VSD_BF16, in, T, grad_scale, *out, ws,
+                                  static_cast<cudaStream_t>(stream)));
 }
 
 vsd_status vsd_reference_logkappa(const void* ref_draft, const void* ref_target, vsd_dtype dtype,

@@ -1,0 +1,220 @@
+// vsd_target.cuh -- the target distributions of the supervised losses: per row
+// either a label or a teacher's top logits, turned into a short sorted list of
+// (token, probability), and the list of rows that count.
+//
+//   p_k = softmax over the row's valid entries of teacher_k / T
+//   plogp = sum_k p_k log p_k
+//
+// A row is counted when its label is not the ignored one, or when it has a
+// teacher entry with a finite logit, and its weight is finite and >= 0.
+#pragma once
+
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "vsd.h"
+#include "vsd_common.cuh"
+
+namespace vsd {
+
+constexpr int kMaxTeacher = 128;  // entries of a teacher row: four per lane of a warp
+
+// What a call says about its targets (device pointers).
+struct TargetIn {
+    const int32_t* labels;     // [R], or null: ids and logits below
+    int32_t ignore;            // the label that is not counted
+    const int32_t* ids;        // [R][K], negative: no entry
+    const void* teacher;       // [R][K] of float or bf16
+    int teacher_bf16;
+    const float* row_weight;   // [R], or null: 1
+    int R, V, K;
+    float invT;
+};
+
+// The targets in the workspace.  Lists are per original row; the entries of a
+// row are distinct tokens in ascending order (probabilities of equal ids added).
+struct Targets {
+    int32_t* n;       // [R] entries of the list; -1: the row is not counted
+    int32_t* id;      // [R][K]
+    float* p;         // [R][K]
+    float* plogp;     // [R]
+    float* w;         // [R] the row's weight
+    int32_t* rowmap;  // [R] i-th counted row, in row order
+    int32_t* rowinv;  // [R] its inverse, -1: not counted
+    int32_t* nrows;   // counted rows
+    double* wsum;     // sum of their weights, 1 where that is 0
+    int32_t* done;    // block counter, 0 at the start
+    int32_t* status;
+};
+
+__device__ __forceinline__ float teacher_logit(const TargetIn& in, size_t i) {
+    if (in.teacher_bf16)
+        return __uint_as_float(
+            (uint32_t)__ldg(static_cast<const unsigned short*>(in.teacher) + i) << 16);
+    return __ldg(static_cast<const float*>(in.teacher) + i);
+}
+
+// The target of one row, by one warp.
+__device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg, int r,
+                                           int lane) {
+    constexpr unsigned kAll = 0xffffffffu;
+    constexpr int kPer = kMaxTeacher / 32;
+    const float w = in.row_weight ? __ldg(in.row_weight + r) : 1.f;
+    int bits = (w >= 0.f && isfinite(w)) ? 0 : VSD_STATUS_BAD_ROW;
+    const size_t base = (size_t)r * in.K;
+    if (in.labels) {
+        const int lab = __ldg(in.labels + r);
+        bool counted = lab != in.ignore && !bits;
+        if (lab != in.ignore && (lab < 0 || lab >= in.V)) {
+            bits |= VSD_STATUS_BAD_TOKEN;
+            counted = false;
+        }
+        if (lane == 0) {
+            tg.n[r] = counted ? 1 : -1;
+            tg.id[base] = counted ? lab : 0;
+            tg.p[base] = 1.f;
+            tg.plogp[r] = 0.f;
+            tg.w[r] = w;
+            if (bits) atomicOr(tg.status, bits);
+        }
+        return;
+    }
+    int id[kPer];
+    float t[kPer];
+    float m = -INFINITY;
+    bool bad = false, far = false;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+        const int k = lane + 32 * j;
+        id[j] = -1;
+        t[j] = -INFINITY;
+        if (k < in.K) {
+            const int v = __ldg(in.ids + base + k);
+            if (v >= in.V) far = true;
+            if (v >= 0 && v < in.V) {
+                id[j] = v;
+                t[j] = teacher_logit(in, base + k);
+                if (!(t[j] < INFINITY)) bad = true;  // NaN or +inf
+            }
+        }
+        m = fmaxf(m, t[j]);
+    }
+    if (__any_sync(kAll, bad)) bits |= VSD_STATUS_BAD_ROW;
+    if (__any_sync(kAll, far)) bits |= VSD_STATUS_BAD_TOKEN;
+    m = warp_max(m);
+    const bool counted = m > -INFINITY && !(bits & VSD_STATUS_BAD_ROW);
+    int n = 0;
+    float plogp = 0.f;
+    if (counted) {  // (one outcome for the warp)
+        float e[kPer], z = 0.f;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            e[j] = id[j] >= 0 ? expf((t[j] - m) * in.invT) : 0.f;
+            if (!(e[j] > 0.f)) id[j] = -1;  // no mass: not in the list
+            z += e[j];
+        }
+        z = warp_sum(z);
+        const float lz = logf(z);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j)
+            if (id[j] >= 0) plogp += e[j] / z * ((t[j] - m) * in.invT - lz);
+        plogp = warp_sum(plogp);
+        // the mass of equal ids is added at the first of them, whose place is
+        // the number of distinct smaller ids
+        float p[kPer];
+        bool first[kPer];
+        int rank[kPer];
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) p[j] = 0.f, first[j] = id[j] >= 0, rank[j] = 0;
+#pragma unroll
+        for (int jo = 0; jo < kPer; ++jo) {
+            if (32 * jo >= in.K) break;
+            for (int o = 0; o < 32; ++o) {
+                const int oid = __shfl_sync(kAll, id[jo], o);
+                const float oe = __shfl_sync(kAll, e[jo], o);
+                if (oid < 0) continue;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (id[j] == oid) {
+                        p[j] += oe;
+                        if (o + 32 * jo < lane + 32 * j) first[j] = false;
+                    }
+            }
+        }
+#pragma unroll
+        for (int jo = 0; jo < kPer; ++jo) {
+            if (32 * jo >= in.K) break;
+            for (int o = 0; o < 32; ++o) {
+                const int oid = __shfl_sync(kAll, first[jo] ? id[jo] : -1, o);
+                if (oid < 0) continue;
+#pragma unroll
+                for (int j = 0; j < kPer; ++j)
+                    if (oid < id[j]) ++rank[j];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+            if (first[j]) {
+                tg.id[base + rank[j]] = id[j];
+                tg.p[base + rank[j]] = p[j] / z;
+            }
+            n += __popc(__ballot_sync(kAll, first[j]));
+        }
+    }
+    if (lane == 0) {
+        tg.n[r] = counted ? n : -1;
+        tg.plogp[r] = plogp;
+        tg.w[r] = w;
+        if (bits) atomicOr(tg.status, bits);
+    }
+}
+
+// The list of counted rows and the sum of their weights, by one block.  Each
+// thread takes a run of rows; the runs' counts and sums are combined in thread
+// order, so the result does not depend on timing.
+__device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_loss,
+                                          float* logz) {
+    __shared__ int cnt[32];
+    __shared__ double sum[32];
+    const int nt = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int per = (R + nt - 1) / nt;
+    const int64_t r0 = (int64_t)threadIdx.x * per;
+    const int64_t r1 = min((int64_t)R, r0 + per);
+    int c = 0;
+    double ws = 0.0;
+    for (int64_t r = r0; r < r1; ++r)
+        if (ld_cg(tg.n + r) >= 0) {
+            ++c;
+            ws += (double)ld_cg(tg.w + r);
+        }
+    int inc = c;
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, inc, o);
+        if (lane >= o) inc += v;
+    }
+    const double wsw = warp_sum(ws);
+    if (lane == 31) cnt[warp] = inc;
+    if (lane == 0) sum[warp] = wsw;
+    __syncthreads();
+    int at = inc - c;
+    for (int i = 0; i < warp; ++i) at += cnt[i];
+    for (int64_t r = r0; r < r1; ++r) {
+        const bool on = ld_cg(tg.n + r) >= 0;
+        tg.rowinv[r] = on ? at : -1;
+        if (on) {
+            tg.rowmap[at++] = (int)r;
+        } else {
+            row_loss[r] = 0.f;
+            logz[r] = 0.f;
+        }
+    }
+    if (threadIdx.x == 0) {
+        int total = 0;
+        double s = 0.0;
+        for (int i = 0; i < nt / 32; ++i) total += cnt[i], s += sum[i];
+        *tg.nrows = total;
+        *tg.wsum = s > 0.0 ? s : 1.0;
+    }
+}
+
+}  // namespace vsd

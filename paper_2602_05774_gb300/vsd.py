@@ -24,7 +24,9 @@ SYMBOLS = ("vsd_workspace_bytes", "vsd_sample_paths", "vsd_verify_paths",
            "vsd_weighted_loss_fwd_bwd", "vsd_estep_mstep", "vsd_device_status",
            "vsd_status_string", "vsd_version", "vsd_estep_mstep_noalloc",
            "vsd_noalloc_device_status", "vsd_lmhead_logits", "vsd_lmhead_estep_mstep",
-           "vsd_reference_logkappa", "vsd_tree_estep_mstep", "vsd_lmhead_backward")
+           "vsd_reference_logkappa", "vsd_tree_estep_mstep", "vsd_lmhead_backward",
+           "vsd_lmhead_loss_workspace_bytes", "vsd_lmhead_cross_entropy", "vsd_lmhead_distill",
+           "vsd_topk_distill_workspace_bytes", "vsd_topk_distill")
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -56,6 +58,7 @@ LINEAR_FIELDS = ("tokens", "logq_tok", "alpha", "accept", "accept_len", "corr_to
                  "kl_loss")
 TREE_FIELDS = ("alpha", "accept", "path_accept", "logkappa", "corr_tokens", "deepest",
                "accept_len", "bonus", "row_stats")
+LOSS_FIELDS = ("loss", "row_loss", "logz", "d_hidden", "d_weight", "grad")
 TREE_EM_FIELDS = ("corr_tokens", "logq_tok", "logq_corr", "logkappa", "logkappa_corr",
                   "logkappa_ref", "weights", "loss", "grad")
 
@@ -70,6 +73,10 @@ class TreeOutputs(C.Structure):
 
 class TreeEmOutputs(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in TREE_EM_FIELDS]
+
+
+class LossOutputs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in LOSS_FIELDS]
 
 
 _LIB = None
@@ -117,6 +124,17 @@ def _lib():
         lib.vsd_tree_estep_mstep.argtypes = [vp, vp, C.c_int, Layout, C.c_float, vp, vp, vp,
                                              C.POINTER(Params), C.POINTER(TreeEmOutputs), vp,
                                              C.c_size_t, vp]
+        i32, f32 = C.c_int32, C.c_float
+        lib.vsd_lmhead_loss_workspace_bytes.argtypes = [i32] * 6
+        lib.vsd_lmhead_loss_workspace_bytes.restype = C.c_size_t
+        lib.vsd_lmhead_cross_entropy.argtypes = [vp, vp, i32, i32, i32, vp, i32, vp, f32, i32,
+                                                 C.POINTER(LossOutputs), vp, C.c_size_t, vp]
+        lib.vsd_lmhead_distill.argtypes = [vp, vp, i32, i32, i32, vp, vp, C.c_int, i32, f32, vp,
+                                           f32, i32, C.POINTER(LossOutputs), vp, C.c_size_t, vp]
+        lib.vsd_topk_distill_workspace_bytes.argtypes = [i32] * 3
+        lib.vsd_topk_distill_workspace_bytes.restype = C.c_size_t
+        lib.vsd_topk_distill.argtypes = [vp, C.c_int, i32, i32, vp, vp, C.c_int, i32, f32, vp,
+                                         f32, C.POINTER(LossOutputs), vp, C.c_size_t, vp]
         lib.vsd_status_string.argtypes = [C.c_int]
         lib.vsd_status_string.restype = C.c_char_p
         lib.vsd_version.restype = C.c_char_p
@@ -124,7 +142,8 @@ def _lib():
                      "vsd_estep_mstep", "vsd_device_status", "vsd_estep_mstep_noalloc",
                      "vsd_noalloc_device_status", "vsd_reference_logkappa",
                      "vsd_tree_estep_mstep",
-                     "vsd_lmhead_logits", "vsd_lmhead_estep_mstep", "vsd_lmhead_backward"):
+                     "vsd_lmhead_logits", "vsd_lmhead_estep_mstep", "vsd_lmhead_backward",
+                     "vsd_lmhead_cross_entropy", "vsd_lmhead_distill", "vsd_topk_distill"):
             getattr(lib, name).restype = C.c_int
         _LIB = lib
     return _LIB
@@ -487,6 +506,163 @@ def lmhead_backward(hidden, weight, draft_logits, K, D, T, workspace, prm=None,
                                       _ptr(res.get("d_weight")), _ptr(workspace),
                                       workspace.numel(), _stream(dev)), "vsd_lmhead_backward")
     return res
+
+
+def _need_int32(t, shape, name):
+    if t.dtype != torch.int32 or tuple(t.shape) != shape:
+        raise ValueError("%s must be int32 of shape %s" % (name, shape))
+
+
+def _check_teacher(teacher_ids, teacher_logits, row_weight, R):
+    """Shapes and types of a teacher's top logits; returns K."""
+    if teacher_ids.dim() != 2:
+        raise ValueError("teacher_ids must be [R, K]")
+    K = teacher_ids.shape[1]
+    _need_int32(teacher_ids, (R, K), "teacher_ids")
+    if teacher_logits.shape != teacher_ids.shape:
+        raise ValueError("teacher_logits must have the shape of teacher_ids")
+    _check_row_weight(row_weight, R)
+    return K
+
+
+def _check_row_weight(row_weight, R):
+    if row_weight is not None and (row_weight.dtype != torch.float32 or
+                                   tuple(row_weight.shape) != (R,)):
+        raise ValueError("row_weight must be float32 of shape (%d,)" % R)
+
+
+def _same_device(ref, *ts):
+    for t in ts:
+        if t is not None and t.device != ref.device:
+            raise ValueError("tensors must live on one device")
+
+
+def _grad_tensor(want, like, name):
+    """A gradient's tensor: new for True, none for False or None, or the given one."""
+    if want is True:
+        return torch.empty_like(like)
+    if want is False or want is None:
+        return None
+    _need_cuda(want)
+    if want.dtype != like.dtype or want.shape != like.shape:
+        raise ValueError("%s must have the type and shape of the tensor it is the gradient of"
+                         % name)
+    return want
+
+
+def _loss_outputs(R, device):
+    return dict(loss=torch.empty(1, dtype=torch.float32, device=device),
+                row_loss=torch.empty(R, dtype=torch.float32, device=device),
+                logz=torch.empty(R, dtype=torch.float32, device=device))
+
+
+def _loss_workspace(need, workspace, device):
+    if need == 0:
+        raise ValueError("invalid sizes")
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    _need_cuda(workspace)
+    if workspace.numel() * workspace.element_size() < need:
+        raise ValueError("workspace too small")
+    return workspace
+
+
+def lmhead_loss_workspace_bytes(R, V, H, K=1, grads=True, piece=0):
+    """Bytes of workspace of lmhead_cross_entropy (K = 1) and lmhead_distill."""
+    return _lib().vsd_lmhead_loss_workspace_bytes(int(R), int(V), int(H), int(K),
+                                                  int(bool(grads)), int(piece))
+
+
+def _lmhead_loss(hidden, weight, K, d_hidden, d_weight, piece, workspace, others):
+    """What the LM-head losses share: checks, outputs and workspace."""
+    _need_cuda(hidden, weight, *others)
+    _same_device(hidden, weight, workspace, *others)
+    if hidden.dtype != torch.bfloat16 or weight.dtype != torch.bfloat16:
+        raise ValueError("the LM head takes bf16 hidden states and weights")
+    if weight.dim() != 2 or hidden.shape[-1] != weight.shape[1]:
+        raise ValueError("hidden and weight disagree on the hidden size")
+    V, H = weight.shape
+    R = hidden.numel() // H
+    dev = hidden.device
+    out = _loss_outputs(R, dev)
+    dh = _grad_tensor(d_hidden, hidden, "d_hidden")
+    dw = _grad_tensor(d_weight, weight, "d_weight")
+    if dh is not None:
+        out["d_hidden"] = dh
+    if dw is not None:
+        out["d_weight"] = dw
+    ws = _loss_workspace(lmhead_loss_workspace_bytes(R, V, H, K, dh is not None or dw is not None,
+                                                     piece), workspace, dev)
+    st = LossOutputs(out["loss"].data_ptr(), out["row_loss"].data_ptr(), out["logz"].data_ptr(),
+                     None if dh is None else dh.data_ptr(), None if dw is None else dw.data_ptr(),
+                     None)
+    return out, st, ws, R, V, H
+
+
+def lmhead_cross_entropy(hidden, weight, labels, ignore_index=-100, row_weight=None,
+                         grad_scale=1.0, d_hidden=True, d_weight=True, piece=0, workspace=None):
+    """Cross entropy of labels [R] (int32) under logits = hidden [R][H] . weight
+    [V][H]^T, without keeping the logits: {"loss": [1], "row_loss": [R], "logz":
+    [R], "d_hidden", "d_weight"}.  The loss is the mean over the rows whose label
+    is not ignore_index, weighted by row_weight; gradients are bf16, the type of
+    their tensors, times grad_scale.  Pass False to skip one, or a tensor to
+    write into."""
+    R = hidden.numel() // max(1, hidden.shape[-1])
+    _need_int32(labels, (R,), "labels")
+    _check_row_weight(row_weight, R)
+    out, st, ws, R, V, H = _lmhead_loss(hidden, weight, 1, d_hidden, d_weight, piece, workspace,
+                                        (labels, row_weight))
+    _check(_lib().vsd_lmhead_cross_entropy(_ptr(hidden), _ptr(weight), R, V, H, _ptr(labels),
+                                           int(ignore_index), _ptr(row_weight), float(grad_scale),
+                                           int(piece), C.byref(st), _ptr(ws),
+                                           ws.numel() * ws.element_size(), _stream(hidden.device)),
+           "vsd_lmhead_cross_entropy")
+    return out
+
+
+def lmhead_distill(hidden, weight, teacher_ids, teacher_logits, T=1.0, row_weight=None,
+                   grad_scale=1.0, d_hidden=True, d_weight=True, piece=0, workspace=None):
+    """The LM head distilled from a teacher's top logits (ids [R][K] int32, a
+    negative one is no entry; logits [R][K] float32 or bf16):
+    KL(softmax(teacher / T) || softmax(hidden . weight^T / T)) per row, outputs
+    as lmhead_cross_entropy."""
+    R = hidden.numel() // max(1, hidden.shape[-1])
+    K = _check_teacher(teacher_ids, teacher_logits, row_weight, R)
+    out, st, ws, R, V, H = _lmhead_loss(hidden, weight, K, d_hidden, d_weight, piece, workspace,
+                                        (teacher_ids, teacher_logits, row_weight))
+    _check(_lib().vsd_lmhead_distill(_ptr(hidden), _ptr(weight), R, V, H, _ptr(teacher_ids),
+                                     _ptr(teacher_logits), _dtype_code(teacher_logits), K,
+                                     float(T), _ptr(row_weight), float(grad_scale), int(piece),
+                                     C.byref(st), _ptr(ws), ws.numel() * ws.element_size(),
+                                     _stream(hidden.device)), "vsd_lmhead_distill")
+    return out
+
+
+def topk_distill(logits, teacher_ids, teacher_logits, T=1.0, row_weight=None, grad_scale=1.0,
+                 grad=True, workspace=None):
+    """Distillation from a teacher's top logits on logits in hand [R][V]:
+    {"loss": [1], "row_loss": [R], "logz": [R], "grad": [R][V]}.  grad=False
+    leaves the gradient out; a tensor is written into, the logits themselves
+    among them."""
+    _need_cuda(logits, teacher_ids, teacher_logits, row_weight)
+    _same_device(logits, teacher_ids, teacher_logits, row_weight, workspace)
+    V = logits.shape[-1]
+    R = _rows(logits, V)
+    K = _check_teacher(teacher_ids, teacher_logits, row_weight, R)
+    dev = logits.device
+    out = _loss_outputs(R, dev)
+    g = _grad_tensor(grad, logits, "grad")
+    if g is not None:
+        out["grad"] = g
+    ws = _loss_workspace(_lib().vsd_topk_distill_workspace_bytes(R, V, K), workspace, dev)
+    st = LossOutputs(out["loss"].data_ptr(), out["row_loss"].data_ptr(), out["logz"].data_ptr(),
+                     None, None, None if g is None else g.data_ptr())
+    _check(_lib().vsd_topk_distill(_ptr(logits), _dtype_code(logits), R, V, _ptr(teacher_ids),
+                                   _ptr(teacher_logits), _dtype_code(teacher_logits), K, float(T),
+                                   _ptr(row_weight), float(grad_scale), C.byref(st), _ptr(ws),
+                                   ws.numel() * ws.element_size(), _stream(dev)),
+           "vsd_topk_distill")
+    return out
 
 
 def estep_mstep_noalloc(draft, target, u_draft, u_accept, u_correct, K, D, T,

@@ -1,0 +1,478 @@
+"""GPU checks of the draft head's supervised losses (vsd_lmhead_cross_entropy,
+vsd_lmhead_distill, vsd_topk_distill) against a plain float64 implementation.
+
+The float64 side works from the exact bf16 / float32 inputs.  Tolerances:
+
+* row losses and log-partitions: the logits are sums of H exact products in
+  float32, off by at most H 2^-24 sum |h w| (one rounding per addition; the
+  tensor cores' own order and truncation stay within it), a log-partition by
+  no more than its logits are, plus 8 float32 ulps of the largest value that
+  is rounded on the way (the row's log-partition and target logits over T)
+  and the 2^-20 relative error of the exponentials in the sum;
+* gradients of the logits: each element a (q - p): relative error of q from
+  its exponent (the absolute error of its logit and log-partition, above) and
+  of a few float32 steps, then one rounding to the gradient's type (bf16:
+  2^-8 relative);
+* d_hidden and d_weight: that error carried through |W| or |hidden|, plus the
+  float32 summation bound n 2^-24 of the products' absolute sum, plus one bf16
+  rounding of the result.
+"""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module")
+def vsd():
+    from paper_2602_05774_gb300 import build, vsd as v
+    build.build_library()
+    v.load()
+    assert torch.cuda.is_available(), "GPU tests need CUDA"
+    return v
+
+
+def f64(t):
+    return t.detach().double().cpu()
+
+
+def plain(x, ids, p, counted, w, T):
+    """Loss, row losses, log-partitions and d loss / d x of float64 logits x, for
+    targets p on ids (one list per row, float64)."""
+    y = x / T
+    top = y.max(1).values
+    top = torch.where(torch.isfinite(top), top, torch.zeros_like(top))
+    y = y - top[:, None]  # (all further terms relative to the row's maximum)
+    ls = torch.log(torch.exp(y).sum(1))
+    at = torch.gather(y, 1, ids)
+    logp = torch.where(p > 0, torch.log(torch.where(p > 0, p, torch.ones_like(p))), 0.0)
+    terms = torch.where(p > 0, p * (logp - at + ls[:, None]), torch.zeros_like(p))
+    row = torch.where(counted, terms.sum(1), torch.zeros_like(ls))
+    wr = torch.where(counted, w, torch.zeros_like(w))
+    tot = wr.sum() if wr.sum() > 0 else torch.ones(())
+    a = (wr / (tot * T))[:, None]
+    g = torch.exp(y - ls[:, None])
+    g.scatter_add_(1, ids, -p)
+    g = torch.where(counted[:, None], a * g, torch.zeros_like(g))
+    logz = top + ls
+    loss = torch.where(wr > 0, wr * row, torch.zeros_like(row)).sum() / tot
+    return dict(loss=loss, row_loss=row, logz=torch.where(counted, logz, 0.0), g=g, a=a)
+
+
+def teacher_target(ids, t, T, V):
+    """(ids, p, counted) in float64 from a teacher's list with negative ids and
+    -inf logits."""
+    ids = ids.cpu().long()
+    t = f64(t)
+    ok = (ids >= 0) & (ids < V)
+    t = torch.where(ok, t, torch.full_like(t, -np.inf))
+    m = t.max(1).values
+    counted = torch.isfinite(m)
+    e = torch.exp((t - torch.where(counted, m, torch.zeros_like(m))[:, None]) / T)
+    z = torch.where(counted, e.sum(1), torch.ones_like(m))
+    return torch.where(ok, ids, torch.zeros_like(ids)), e / z[:, None], counted
+
+
+U = 2.0 ** -24
+
+
+def logit_bound(h, w):
+    """Per row: how far a float32 sum of the row's products may be off."""
+    if w is None:
+        return None
+    return (h.shape[1] * U) * (h.abs() @ w.abs().T)
+
+
+def check(got, ref, x, xerr, T, dtype, h=None, w=None, ids=None, p=None, scale=1.0):
+    """got: the library's outputs; ref: plain()'s; xerr: bound of each logit's
+    error (0 for logits in hand)."""
+    y = x.abs().where(torch.isfinite(x), torch.zeros_like(x)) / T
+    row_err = xerr.max(1).values / T
+    # values that are rounded on the way to a row's loss and log-partition
+    big = torch.maximum(y.max(1).values, ref["logz"].abs()).clamp(min=1.0)
+    tol = 2 * row_err + 8 * 2 * U * big + 2.0 ** -20
+    for name in ("row_loss", "logz"):
+        a, b = f64(got[name]), ref[name]
+        fin = torch.isfinite(b)
+        assert torch.equal(torch.isnan(a), torch.isnan(b)), name
+        assert torch.equal(a[~fin & ~torch.isnan(b)], b[~fin & ~torch.isnan(b)]), name
+        err = (a - b).abs()[fin]
+        assert (err <= tol[fin]).all(), (name, float((err - tol[fin]).max()), float(err.max()))
+    if torch.isfinite(ref["loss"]):
+        assert abs(float(got["loss"]) - float(ref["loss"])) <= float(tol.max()) + 2 * U * abs(
+            float(ref["loss"]))
+    # d loss / d x: q's relative error, then that of the coefficient and steps
+    q_rel = 2 * (xerr / T + row_err[:, None]) + 16 * 2 * U * big[:, None] + 2.0 ** -20
+    a = ref["a"] * abs(scale)
+    q = (ref["g"] / ref["a"].where(ref["a"] > 0, torch.ones_like(ref["a"])))
+    if ids is not None:
+        q = q.scatter_add(1, ids, p)
+    gerr = a * (q.abs() * q_rel + 8 * U)
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else U
+    g = ref["g"] * scale
+    gerr = gerr + half * (g.abs() + gerr) + 2.0 ** -126
+    if "grad" in got:
+        err = (f64(got["grad"]) - g).abs()
+        assert (err <= gerr).all(), ("grad", float((err / gerr).max()))
+    if h is not None and "d_hidden" in got:
+        b = gerr @ w.abs() + (w.shape[0] * U) * (g.abs() @ w.abs())
+        want = g @ w
+        b = b + 2.0 ** -8 * (want.abs() + b) + 2.0 ** -126
+        err = (f64(got["d_hidden"]) - want).abs()
+        assert (err <= b).all(), ("d_hidden", float((err / b).max()))
+    if h is not None and "d_weight" in got:
+        b = gerr.T @ h.abs() + (h.shape[0] * U) * (g.abs().T @ h.abs())
+        want = g.T @ h
+        b = b + 2.0 ** -8 * (want.abs() + b) + 2.0 ** -126
+        err = (f64(got["d_weight"]) - want).abs()
+        assert (err <= b).all(), ("d_weight", float((err / b).max()))
+
+
+def head(R, V, H, seed, gain=0.05):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    h = torch.randn(R, H, generator=g, device="cuda").to(torch.bfloat16)
+    w = (gain * torch.randn(V, H, generator=g, device="cuda")).to(torch.bfloat16)
+    return h, w, g
+
+
+def teacher(R, V, K, g, dtype=torch.float32, dup=False):
+    if dup:
+        ids = torch.randint(0, V, (R, K), generator=g, device="cuda")
+    else:
+        ids = torch.rand(R, V, generator=g, device="cuda").topk(K, dim=1).indices
+    t = 3.0 * torch.randn(R, K, generator=g, device="cuda")
+    return ids.to(torch.int32), t.to(dtype)
+
+
+XENT = [  # R, V, H, piece
+    (1, 1, 8, 0), (1, 5, 8, 0), (3, 257, 64, 0), (32, 1024, 256, 0), (129, 1000, 72, 256),
+    (257, 2049, 136, 512), (300, 777, 1032, 256), (513, 4096, 64, 1024), (64, 8191, 264, 0),
+    (700, 1536, 512, 768)]
+
+
+@pytest.mark.parametrize("R,V,H,piece", XENT)
+@pytest.mark.parametrize("weighted", [False, True])
+def test_cross_entropy(vsd, R, V, H, piece, weighted):
+    h, w, g = head(R, V, H, 100 + R + V, gain=0.3 / H ** 0.5 + 0.02)
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda").to(torch.int32)
+    if R > 2:
+        labels[torch.randperm(R, generator=g, device="cuda")[: R // 3]] = -100
+    rw = torch.rand(R, generator=g, device="cuda") if weighted else None
+    got = vsd.lmhead_cross_entropy(h, w, labels, row_weight=rw, piece=piece)
+    lab = labels.cpu().long()
+    counted = lab != -100
+    ids, p = lab.clamp(min=0)[:, None], counted.double()[:, None]
+    H64, W64 = f64(h), f64(w)
+    x = H64 @ W64.T
+    ref = plain(x, ids, p, counted, f64(rw) if weighted else torch.ones(R).double(), 1.0)
+    check(got, ref, x, logit_bound(H64, W64), 1.0, torch.bfloat16, H64, W64, ids, p)
+
+
+DISTILL = [  # R, V, H, K, T, teacher type, piece
+    (1, 9, 8, 1, 1.0, torch.float32, 0), (5, 300, 64, 4, 2.0, torch.bfloat16, 0),
+    (33, 1024, 256, 10, 0.7, torch.float32, 0), (200, 1537, 264, 64, 1.0, torch.bfloat16, 512),
+    (260, 600, 128, 128, 2.0, torch.float32, 256), (130, 4100, 520, 33, 1.0, torch.float32, 1024)]
+
+
+@pytest.mark.parametrize("R,V,H,K,T,tdt,piece", DISTILL)
+def test_lmhead_distill(vsd, R, V, H, K, T, tdt, piece):
+    h, w, g = head(R, V, H, 300 + R + V, gain=1.0 / H ** 0.5)
+    ids, t = teacher(R, V, K, g, tdt)
+    if R > 4:  # rows with shorter lists, one with none; what they lack holds NaN
+        n = torch.randint(1, K + 1, (R, 1), generator=g, device="cuda")
+        n[3] = 0
+        lacks = torch.arange(K, device="cuda") >= n
+        ids, t = ids.masked_fill(lacks, -1), t.masked_fill(lacks, NAN)
+    rw = 1.05 ** (torch.arange(R, device="cuda") % 8).float()
+    got = vsd.lmhead_distill(h, w, ids, t, T=T, row_weight=rw, grad_scale=T * T, piece=piece)
+    i64, p, counted = teacher_target(ids, t, T, V)
+    H64, W64 = f64(h), f64(w)
+    x = H64 @ W64.T
+    ref = plain(x, i64, p, counted, f64(rw), T)
+    check(got, ref, x, logit_bound(H64, W64), T, torch.bfloat16, H64, W64, i64, p, scale=T * T)
+
+
+TOPK = [  # R, V, K, T, logits' type, teacher's type
+    (1, 1, 1, 1.0, torch.float32, torch.float32), (2, 7, 3, 1.0, torch.bfloat16, torch.float32),
+    (16, 1024, 10, 1.0, torch.float32, torch.float32), (9, 1031, 128, 0.7, torch.float32, torch.bfloat16),
+    (7, 32003, 100, 2.0, torch.bfloat16, torch.bfloat16), (40, 32000, 32, 1.0, torch.bfloat16, torch.float32),
+    (5, 128256, 10, 0.7, torch.bfloat16, torch.float32), (3, 128256, 64, 1.0, torch.float32, torch.float32),
+    (2, 300008, 16, 1.0, torch.float32, torch.float32), (2, 1048576, 8, 1.0, torch.bfloat16, torch.bfloat16),
+    (611, 520, 5, 1.0, torch.float32, torch.bfloat16)]
+
+
+@pytest.mark.parametrize("R,V,K,T,dt,tdt", TOPK)
+@pytest.mark.parametrize("inplace", [False, True])
+def test_topk_distill(vsd, R, V, K, T, dt, tdt, inplace):
+    g = torch.Generator(device="cuda").manual_seed(500 + R + V)
+    x = (4.0 * torch.randn(R, V, generator=g, device="cuda")).to(dt)
+    ids, t = teacher(R, V, K, g, tdt)
+    rw = torch.rand(R, generator=g, device="cuda")
+    x64 = f64(x)
+    if R > 4:
+        ids[2, K // 2:] = -1
+        ids[4] = -1
+        x[4] = NAN  # a row not counted may hold anything
+    got = vsd.topk_distill(x, ids, t, T=T, row_weight=rw, grad_scale=T * T,
+                           grad=x if inplace else True)
+    i64, p, counted = teacher_target(ids, t, T, V)
+    ref = plain(x64, i64, p, counted, f64(rw), T)
+    check(got, ref, x64, torch.zeros_like(x64), T, dt, ids=i64, p=p, scale=T * T)
+    if inplace:
+        assert got["grad"].data_ptr() == x.data_ptr()
+
+
+def test_gradients_against_differences(vsd):
+    """Central differences of the library's own float32 loss along random
+    directions (topk_distill on float32 logits): truncation of a third-order
+    term, |d|^3 eps^2 / 6 with bounded third derivatives, and the loss's own
+    rounding over 2 eps."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    R, V, K, T = 6, 500, 7, 1.3
+    x = torch.randn(R, V, generator=g, device="cuda")
+    ids, t = teacher(R, V, K, g)
+    rw = torch.rand(R, generator=g, device="cuda") + 0.1
+    grad = f64(vsd.topk_distill(x, ids, t, T=T, row_weight=rw)["grad"])
+    eps = 2.0 ** -5
+    for _ in range(6):
+        d = torch.randint(0, 2, (R, V), generator=g, device="cuda").float() * 2 - 1
+        up = vsd.topk_distill(x + eps * d, ids, t, T=T, row_weight=rw, grad=False)["loss"]
+        dn = vsd.topk_distill(x - eps * d, ids, t, T=T, row_weight=rw, grad=False)["loss"]
+        fd = (float(up) - float(dn)) / (2 * eps)
+        an = float((grad * f64(d)).sum())
+        # |d^3 lse| <= 2 (2 max|d| / T)^3 / 8; x +- eps d is rounded to 2^-24 |x|
+        third = 2 * (2 / T) ** 3 / 8 * eps ** 2 / 6
+        rounding = (2 ** -20 * 8 + 2 ** -22 * float(x.abs().max())) / eps
+        assert abs(fd - an) <= third + rounding, (fd, an, third + rounding)
+
+
+def test_duplicate_ids_add_and_mass_at_the_ends(vsd):
+    """Equal ids add; -inf and lowest-value teacher logits carry no mass; a row
+    of equal lowest values is uniform."""
+    R, V, K, H = 6, 300, 8, 64
+    h, w, g = head(R, V, H, 77, gain=0.1)
+    ids, t = teacher(R, V, K, g, dup=True)
+    ids[0] = 17                      # one token, eight times
+    ids[1, :4] = ids[1, 4:]
+    t[2, 1:] = -float("inf")
+    t[3, 2] = torch.finfo(torch.float32).min
+    t[4] = torch.finfo(torch.float32).min
+    i64, p, counted = teacher_target(ids, t, 1.0, V)
+    assert counted.all()
+    H64, W64 = f64(h), f64(w)
+    x = H64 @ W64.T
+    # p log p is taken entry by entry, as listed
+    ref = plain(x, i64, p, counted, torch.ones(R).double(), 1.0)
+    got = vsd.lmhead_distill(h, w, ids, t)
+    check(got, ref, x, logit_bound(H64, W64), 1.0, torch.bfloat16, H64, W64, i64, p)
+    xb = x.float().cuda()
+    got = vsd.topk_distill(xb, ids, t)
+    ref = plain(f64(xb), i64, p, counted, torch.ones(R).double(), 1.0)
+    check(got, ref, f64(xb), torch.zeros_like(x), 1.0, torch.float32, ids=i64, p=p)
+
+
+@pytest.mark.parametrize("piece", [0, 256])
+def test_rows_not_counted_hold_anything(vsd, piece):
+    """A row with an ignored label may hold NaN or infinities: the others'
+    results do not change by a bit, and its own are zero."""
+    R, V, H = 300, 900, 128
+    h, w, g = head(R, V, H, 5)
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda").to(torch.int32)
+    off = torch.randperm(R, generator=g, device="cuda")[:120]
+    labels[off] = -100
+    ws = torch.empty(vsd.lmhead_loss_workspace_bytes(R, V, H, 1, True, piece), dtype=torch.uint8,
+                     device="cuda")
+    a = vsd.lmhead_cross_entropy(h, w, labels, piece=piece, workspace=ws)
+    h2 = h.clone()
+    h2[off[:60]] = NAN
+    h2[off[60:]] = float("inf")
+    ws.fill_(0xFF)  # NaN in every workspace float
+    b = vsd.lmhead_cross_entropy(h2, w, labels, piece=piece, workspace=ws)
+    assert vsd.device_status(ws) == (0, 0)
+    for name in a:
+        assert torch.equal(a[name], b[name]), name
+        assert torch.isfinite(a[name].float()).all(), name
+    assert (b["row_loss"][off] == 0).all() and (b["d_hidden"][off] == 0).all()
+
+
+@pytest.mark.parametrize("piece", [0, 256])
+def test_no_row_counted(vsd, piece):
+    h, w, g = head(40, 600, 64, 6)
+    labels = torch.full((40,), 7, dtype=torch.int32, device="cuda")
+    ws = torch.full((vsd.lmhead_loss_workspace_bytes(40, 600, 64, 1, True, piece),), 255,
+                    dtype=torch.uint8, device="cuda")
+    out = vsd.lmhead_cross_entropy(h * NAN, w, labels, ignore_index=7, piece=piece, workspace=ws)
+    zero = vsd.lmhead_cross_entropy(h, w, labels, row_weight=torch.zeros(40, device="cuda"),
+                                    piece=piece)
+    ids = torch.full((40, 3), -1, dtype=torch.int32, device="cuda")
+    t = torch.full((40, 3), NAN, device="cuda")
+    x = torch.full((40, 600), NAN, device="cuda")
+    top = vsd.topk_distill(x, ids, t)
+    for o in (out, top):
+        for name, v in o.items():
+            assert (v == 0).all(), name
+    assert float(zero["loss"]) == 0 and (zero["d_weight"] == 0).all()
+    assert (zero["row_loss"] > 0).all()
+
+
+def test_status_bits(vsd):
+    """Bad labels, ids, weights and teacher logits: a status bit, and the row is
+    not counted; a counted row of NaN sets the bit of a bad row."""
+    R, V, H = 20, 300, 64
+    h, w, g = head(R, V, H, 8)
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda").to(torch.int32)
+    ws = torch.empty(vsd.lmhead_loss_workspace_bytes(R, V, H), dtype=torch.uint8, device="cuda")
+    good = labels.clone()
+    good[3] = -100
+    want = vsd.lmhead_cross_entropy(h, w, good, workspace=ws)
+    assert vsd.device_status(ws) == (0, 0)
+    for bad in (V, -1, 2 ** 31 - 1, -2 ** 31):
+        labels[3] = bad
+        got = vsd.lmhead_cross_entropy(h, w, labels, workspace=ws)
+        assert vsd.device_status(ws) == (6, vsd.STATUS_BAD_TOKEN)
+        for name in want:
+            assert torch.equal(got[name], want[name]), name
+    rw = torch.ones(R, device="cuda")
+    for bad in (-1.0, NAN, float("inf")):
+        rw[3] = bad
+        labels[3] = 5
+        got = vsd.lmhead_cross_entropy(h, w, labels, row_weight=rw, workspace=ws)
+        assert vsd.device_status(ws) == (6, vsd.STATUS_BAD_ROW)
+        assert torch.equal(got["loss"], want["loss"])
+    h[7, 5] = NAN
+    got = vsd.lmhead_cross_entropy(h, w, good, workspace=ws)
+    assert vsd.device_status(ws)[1] == vsd.STATUS_BAD_ROW
+    assert torch.isnan(got["row_loss"][7]) and torch.isfinite(got["row_loss"][6])
+    x = torch.randn(R, V, generator=g, device="cuda")
+    ids, t = teacher(R, V, 4, g)
+    wst = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    ids2, t2 = ids.clone(), t.clone()
+    ids2[2, 1] = V
+    got = vsd.topk_distill(x, ids2, t2, workspace=wst)
+    assert vsd.device_status(wst) == (6, vsd.STATUS_BAD_TOKEN)
+    ids2[2, 1] = -1
+    want = vsd.topk_distill(x, ids2, t2, workspace=wst)
+    assert vsd.device_status(wst) == (0, 0)
+    assert torch.equal(got["grad"], want["grad"])
+    t2[6, 0] = float("inf")
+    got = vsd.topk_distill(x, ids, t2, workspace=wst)
+    assert vsd.device_status(wst) == (6, vsd.STATUS_BAD_ROW)
+    assert (got["grad"][6] == 0).all() and float(got["row_loss"][6]) == 0
+    x[5] = -float("inf")
+    got = vsd.topk_distill(x, ids, t, workspace=wst)
+    assert vsd.device_status(wst)[1] == vsd.STATUS_BAD_ROW
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1000, 1003])
+def test_masked_vocabulary(vsd, dt, V):
+    """-inf logits carry no mass and no gradient; one at a token the teacher
+    wants makes the loss infinite and leaves the gradient finite; the type's
+    lowest value is an ordinary logit."""
+    R, K = 8, 5
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn(R, V, generator=g, device="cuda").to(dt)
+    ids, t = teacher(R, V, K, g)
+    x[0, : V // 2] = -float("inf")
+    ids[0] = torch.arange(V - K, V, device="cuda").to(torch.int32)
+    x[1, :] = -float("inf")
+    x[1, 11] = 2.0
+    ids[1] = 11
+    x[2] = torch.finfo(dt).min
+    x[3, 1:] = torch.finfo(dt).min
+    ids[3, 0] = 0
+    t[3, 1:] = -float("inf")
+    x[4, int(ids[4, 2])] = -float("inf")
+    wst = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    got = vsd.topk_distill(x, ids, t, workspace=wst)
+    assert vsd.device_status(wst) == (0, 0)
+    x64 = f64(x)
+    i64, p, counted = teacher_target(ids, t, 1.0, V)
+    ref = plain(x64, i64, p, counted, torch.ones(R).double(), 1.0)
+    assert float(got["row_loss"][4]) == float("inf") and float(got["loss"]) == float("inf")
+    # rows 2 and 3 are at the type's lowest value, where a rounding of the
+    # log-partition is of its size: their gradients are held exactly instead
+    assert torch.allclose(f64(got["grad"][2]), ref["g"][2], rtol=2 ** -8, atol=0)
+    assert float(got["row_loss"][3]) == 0.0
+    keep = torch.tensor([0, 1, 4, 5, 6, 7])
+    sub = {k: (v[keep.cuda()] if v.dim() and v.shape[0] == R else v) for k, v in got.items()}
+    rs = {k: (v[keep] if v.dim() and v.shape[0] == R else v) for k, v in ref.items()}
+    check(sub, rs, x64[keep], torch.zeros_like(x64[keep]), 1.0, dt, ids=i64[keep], p=p[keep])
+
+
+def test_pieces_and_repeats_agree(vsd):
+    """Any piece gives the same row losses within rounding; a repeated call gives
+    the same bits, on another stream and a used workspace too."""
+    R, V, H = 400, 3001, 264
+    h, w, g = head(R, V, H, 21)
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda").to(torch.int32)
+    base = vsd.lmhead_cross_entropy(h, w, labels)
+    for piece in (256, 1024, 4096):
+        a = vsd.lmhead_cross_entropy(h, w, labels, piece=piece)
+        assert torch.allclose(a["row_loss"], base["row_loss"], rtol=1e-5, atol=1e-5)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            ws = torch.full((vsd.lmhead_loss_workspace_bytes(R, V, H, 1, True, piece),), 127,
+                            dtype=torch.uint8, device="cuda")
+            b = vsd.lmhead_cross_entropy(h, w, labels, piece=piece, workspace=ws)
+        s.synchronize()
+        for name in a:
+            assert torch.equal(a[name], b[name]), (piece, name)
+
+
+def test_one_gradient_or_none(vsd):
+    h, w, g = head(70, 700, 128, 3)
+    labels = torch.randint(0, 700, (70,), generator=g, device="cuda").to(torch.int32)
+    both = vsd.lmhead_cross_entropy(h, w, labels)
+    dh = torch.empty_like(h)
+    a = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=dh, d_weight=False)
+    b = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False)
+    n = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False, d_weight=False)
+    assert a["d_hidden"] is dh and torch.equal(dh, both["d_hidden"]) and "d_weight" not in a
+    assert torch.equal(b["d_weight"], both["d_weight"]) and "d_hidden" not in b
+    assert torch.equal(n["loss"], both["loss"]) and set(n) == {"loss", "row_loss", "logz"}
+
+
+def test_refusals(vsd):
+    h, w, g = head(8, 100, 64, 1)
+    labels = torch.zeros(8, dtype=torch.int32, device="cuda")
+    ids, t = teacher(8, 100, 3, g)
+    x = torch.zeros(8, 100, device="cuda")
+    for bad in (lambda: vsd.lmhead_cross_entropy(h.float(), w, labels),
+                lambda: vsd.lmhead_cross_entropy(h, w, labels.long()),
+                lambda: vsd.lmhead_cross_entropy(h, w, labels[:7]),
+                lambda: vsd.lmhead_cross_entropy(h, w[:, :32], labels),
+                lambda: vsd.lmhead_cross_entropy(h, w, labels, d_hidden=h.float()),
+                lambda: vsd.lmhead_cross_entropy(h, w, labels, d_weight=torch.empty_like(h)),
+                lambda: vsd.lmhead_cross_entropy(h, w, labels, row_weight=labels),
+                lambda: vsd.lmhead_cross_entropy(h, w.t().contiguous().t(), labels),
+                lambda: vsd.lmhead_cross_entropy(h, w, labels.cpu()),
+                lambda: vsd.lmhead_cross_entropy(h, w, labels, workspace=torch.empty(
+                    256, dtype=torch.uint8, device="cuda")),
+                lambda: vsd.lmhead_distill(h, w, ids, t[:, :2]),
+                lambda: vsd.lmhead_distill(h, w, ids.long(), t),
+                lambda: vsd.lmhead_distill(h, w, ids[:, :0], t[:, :0]),
+                lambda: vsd.lmhead_distill(h[:, :60].contiguous(), w[:, :60].contiguous(), ids, t),
+                lambda: vsd.topk_distill(x, ids[:4], t[:4]),
+                lambda: vsd.topk_distill(x, ids, t, grad=x.bfloat16()),
+                lambda: vsd.topk_distill(x[:0], ids[:0], t[:0])):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(TypeError):
+        vsd.lmhead_distill(h, w, ids, t.half())
+    with pytest.raises(TypeError):
+        vsd.topk_distill(x.half(), ids, t)
+    for T in (0.0, -1.0, NAN, float("inf")):
+        with pytest.raises(vsd.VsdError) as e:
+            vsd.topk_distill(x, ids, t, T=T)
+        assert e.value.code == 1
+        with pytest.raises(vsd.VsdError) as e:
+            vsd.lmhead_distill(h, w, ids, t, T=T)
+        assert e.value.code == 1
+    with pytest.raises(vsd.VsdError) as e:
+        vsd.lmhead_cross_entropy(h, w, labels, grad_scale=NAN)
+    assert e.value.code == 1

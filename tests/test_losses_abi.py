@@ -1,0 +1,91 @@
+"""CPU checks of the supervised losses' C entry points: workspace sizes and the
+host-side argument checks, which return before anything is enqueued."""
+import ctypes as C
+
+import pytest
+import torch
+
+host_only = pytest.mark.skipif(torch.cuda.is_available(),
+                               reason="fake device pointers: host-only checks")
+
+
+@pytest.fixture(scope="module")
+def vsd():
+    from paper_2602_05774_gb300 import build, vsd as v
+    build.build_library()
+    v.load()
+    return v
+
+
+def test_workspace_bytes(vsd):
+    n = vsd.lmhead_loss_workspace_bytes
+    for bad in ((0, 100, 64), (4, 0, 64), (4, 100, 0), (4, 100, 60), (4, (1 << 20) + 1, 64),
+                ((1 << 24) + 1, 100, 64), (4, 100, 64, 0), (4, 100, 64, 129),
+                (4, 100, 64, 1, True, -1)):
+        assert n(*bad) == 0, bad
+    # the logits are not kept: far less than R V of them, at any vocabulary
+    R, H = 4096, 4096
+    for V in (32000, 128256, 1 << 20):
+        assert 0 < n(R, V, H) < 0.5 * 4 * R * V + (256 << 20), V
+    assert n(R, 32000, H, grads=False) < n(R, 32000, H)
+    assert n(R, 32000, H, piece=4096) < n(R, 32000, H, piece=16384)
+    t = vsd.load().vsd_topk_distill_workspace_bytes
+    for bad in ((0, 10, 1), (1, 0, 1), (1, (1 << 20) + 1, 1), (1, 10, 0), (1, 10, 129)):
+        assert t(*bad) == 0, bad
+    assert 0 < t(4096, 128256, 10) < (4 << 20)
+
+
+@host_only
+def test_argument_checks_before_any_launch(vsd):
+    lib = vsd.load()
+    p = 0x100000  # never dereferenced: every call below fails its checks
+    big = 1 << 40
+    o = vsd.LossOutputs(p, p, p, p, p, None)
+
+    def xent(hidden=p, weight=p, R=4, V=100, H=64, labels=p, scale=1.0, piece=0, out=o, ws=p,
+             n=big):
+        return lib.vsd_lmhead_cross_entropy(hidden, weight, R, V, H, labels, -100, None, scale,
+                                            piece, C.byref(out) if out else None, ws, n, None)
+
+    def distill(ids=p, t=p, dt=0, K=4, T=1.0, H=64, out=o, ws=p, n=big):
+        return lib.vsd_lmhead_distill(p, p, 4, 100, H, ids, t, dt, K, T, None, 1.0, 0,
+                                      C.byref(out), ws, n, None)
+
+    def topk(x=p, dt=0, R=4, V=100, ids=p, t=p, tdt=0, K=4, T=1.0, scale=1.0, out=o, ws=p, n=big):
+        return lib.vsd_topk_distill(x, dt, R, V, ids, t, tdt, K, T, None, scale, C.byref(out), ws,
+                                    n, None)
+
+    nan, inf = float("nan"), float("inf")
+    for kw in (dict(hidden=None), dict(weight=None), dict(labels=None), dict(out=None),
+               dict(R=0), dict(V=0), dict(V=(1 << 20) + 1), dict(H=60), dict(H=0),
+               dict(scale=nan), dict(scale=inf), dict(piece=-1), dict(hidden=p + 8),
+               dict(weight=p + 2), dict(out=vsd.LossOutputs(None, p, p, p, p, None)),
+               dict(out=vsd.LossOutputs(p, None, p, p, p, None)),
+               dict(out=vsd.LossOutputs(p, p, None, p, p, None)),
+               dict(out=vsd.LossOutputs(p, p, p, p + 8, p, None)),
+               dict(out=vsd.LossOutputs(p, p, p, p, p + 8, None))):
+        assert xent(**kw) == 1, kw
+    for kw in (dict(ids=None), dict(t=None), dict(dt=2), dict(K=0), dict(K=129), dict(T=0.0),
+               dict(T=-1.0), dict(T=nan), dict(T=inf), dict(H=4)):
+        assert distill(**kw) == 1, kw
+    for kw in (dict(x=None), dict(ids=None), dict(t=None), dict(dt=2), dict(tdt=-1), dict(R=0),
+               dict(V=0), dict(V=(1 << 20) + 1), dict(K=0), dict(K=129), dict(T=0.0), dict(T=nan),
+               dict(scale=inf)):
+        assert topk(**kw) == 1, kw
+    for call in (xent, distill, topk):
+        assert call(ws=None) == 5
+        assert call(ws=p + 16) == 5
+        assert call(n=16) == 5
+
+
+def test_binding_refuses_cpu_tensors(vsd):
+    h = torch.zeros(4, 64, dtype=torch.bfloat16)
+    w = torch.zeros(100, 64, dtype=torch.bfloat16)
+    i = torch.zeros(4, 2, dtype=torch.int32)
+    t = torch.zeros(4, 2)
+    with pytest.raises(ValueError):
+        vsd.lmhead_cross_entropy(h, w, i[:, 0].contiguous())
+    with pytest.raises(ValueError):
+        vsd.lmhead_distill(h, w, i, t)
+    with pytest.raises(ValueError):
+        vsd.topk_distill(torch.zeros(4, 100), i, t)
