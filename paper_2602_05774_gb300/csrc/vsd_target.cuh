@@ -43,6 +43,7 @@ struct Targets {
     int32_t* rowinv;  // [R] its inverse, -1: not counted
     int32_t* nrows;   // counted rows
     double* wsum;     // sum of their weights, 1 where that is 0
+    float* wmax;      // the largest of them
     int32_t* done;    // block counter, 0 at the start
     int32_t* status;
 };
@@ -169,23 +170,27 @@ __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg
     }
 }
 
-// The list of counted rows and the sum of their weights, by one block.  Each
+// The list of counted rows, the sum and the largest of their weights, by one block.  Each
 // thread takes a run of rows; the runs' counts and sums are combined in thread
 // order, so the result does not depend on timing.
 __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_loss,
                                           float* logz) {
     __shared__ int cnt[32];
     __shared__ double sum[32];
+    __shared__ float top[32];
     const int nt = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = (R + nt - 1) / nt;
     const int64_t r0 = (int64_t)threadIdx.x * per;
     const int64_t r1 = min((int64_t)R, r0 + per);
     int c = 0;
     double ws = 0.0;
+    float wm = 0.f;
     for (int64_t r = r0; r < r1; ++r)
         if (ld_cg(tg.n + r) >= 0) {
+            const float w = ld_cg(tg.w + r);
             ++c;
-            ws += (double)ld_cg(tg.w + r);
+            ws += (double)w;
+            wm = fmaxf(wm, w);
         }
     int inc = c;
     for (int o = 1; o < 32; o <<= 1) {
@@ -194,7 +199,8 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_l
     }
     const double wsw = warp_sum(ws);
     if (lane == 31) cnt[warp] = inc;
-    if (lane == 0) sum[warp] = wsw;
+    wm = warp_max(wm);
+    if (lane == 0) sum[warp] = wsw, top[warp] = wm;
     __syncthreads();
     int at = inc - c;
     for (int i = 0; i < warp; ++i) at += cnt[i];
@@ -211,9 +217,10 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_l
     if (threadIdx.x == 0) {
         int total = 0;
         double s = 0.0;
-        for (int i = 0; i < nt / 32; ++i) total += cnt[i], s += sum[i];
+        for (int i = 0; i < nt / 32; ++i) total += cnt[i], s += sum[i], wm = fmaxf(wm, top[i]);
         *tg.nrows = total;
         *tg.wsum = s > 0.0 ? s : 1.0;
+        *tg.wmax = wm;
     }
 }
 

@@ -143,5 +143,9 @@ __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
 // as zero (vsd_lmhead.cu).
 bool make_map_box(CUtensorMap* m, const void* base, int rows, int cols, int box_cols,
                   int box_rows, int swizzle_bytes);
+// The same in the 128-byte swizzle for bf16 or (f32) float elements, with rows
+// `pitch` elements apart; box_cols elements span 128 bytes.
+bool make_map_sw128(CUtensorMap* m, const void* base, bool f32, int64_t rows, int64_t cols,
+                    int64_t pitch, int box_rows);
 
 }  // namespace vsd_lm

@@ -19,7 +19,7 @@ namespace {
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct TopkWs {
-    size_t status, done, zero_end, nrows, wsum, n, id, p, plogp, w, rowmap, rowinv, total;
+    size_t status, done, zero_end, nrows, wsum, wmax, n, id, p, plogp, w, rowmap, rowinv, total;
 };
 
 TopkWs topk_ws(int R, int K) {
@@ -36,6 +36,7 @@ TopkWs topk_ws(int R, int K) {
     w.zero_end = o;
     w.nrows = take(4);
     w.wsum = take(8);
+    w.wmax = take(4);
     w.n = take(4 * r);
     w.id = take(4 * rk);
     w.p = take(4 * rk);
@@ -166,7 +167,7 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     Targets tg{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
                at<float>(ws, w.plogp), at<float>(ws, w.w), at<int32_t>(ws, w.rowmap),
                at<int32_t>(ws, w.rowinv), at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum),
-               at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
+               at<float>(ws, w.wmax), at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
     const float c = (float)(kLog2e / (double)T);
     cudaError_t e = cudaMemsetAsync(ws, 0, w.zero_end, st);
     if (e != cudaSuccess) return e;
