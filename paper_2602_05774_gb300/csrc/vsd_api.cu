@@ -662,9 +662,15 @@ vsd_status vsd_lmhead_backward(const void* hidden, const void* weight, int32_t H
     return from_cuda(e);
 }
 
-// The checks that the supervised losses share; Targets' ws and outputs.
-static vsd_status check_loss_call(const vsd_loss_outputs* out, float T, float grad_scale) {
+// The checks that the supervised losses share: outputs, scalars and the
+// natural alignment of the small arrays.
+static vsd_status check_loss_call(const vsd_loss_outputs* out, const TargetIn& in, float T,
+                                  float grad_scale) {
     if (!out || !out->loss || !out->row_loss || !out->logz) return VSD_ERR_INVALID_ARG;
+    if (((uintptr_t)out->loss | (uintptr_t)out->row_loss | (uintptr_t)out->logz |
+         (uintptr_t)in.labels | (uintptr_t)in.ids | (uintptr_t)in.row_weight) & 3)
+        return VSD_ERR_INVALID_ARG;
+    if ((uintptr_t)in.teacher & (in.teacher_bf16 ? 1 : 3)) return VSD_ERR_INVALID_ARG;
     if (!(T > 0.f) || !isfinite(T) || !isfinite(grad_scale)) return VSD_ERR_INVALID_ARG;
     return VSD_OK;
 }
@@ -673,7 +679,7 @@ static vsd_status lmhead_loss_call(const void* hidden, const void* weight, int32
                                    const TargetIn& in, float T, float grad_scale, int32_t piece,
                                    const vsd_loss_outputs* out, void* ws, size_t ws_bytes,
                                    void* stream) {
-    vsd_status st = check_loss_call(out, T, grad_scale);
+    vsd_status st = check_loss_call(out, in, T, grad_scale);
     if (st) return st;
     const LmLossShape s{in.R, in.V, H, in.K, out->d_hidden != nullptr, out->d_weight != nullptr,
                         piece};
@@ -729,12 +735,14 @@ vsd_status vsd_topk_distill(const void* logits, vsd_dtype dtype, int32_t R, int3
         return VSD_ERR_INVALID_ARG;
     if (dtype != VSD_F32 && dtype != VSD_BF16) return VSD_ERR_INVALID_ARG;
     if (teacher_dtype != VSD_F32 && teacher_dtype != VSD_BF16) return VSD_ERR_INVALID_ARG;
-    vsd_status st = check_loss_call(out, T, grad_scale);
-    if (st) return st;
-    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < topk_workspace_bytes(R, V, K))
-        return VSD_ERR_WORKSPACE;
     const TargetIn in{nullptr, 0, teacher_ids, teacher_logits, teacher_dtype == VSD_BF16,
                       row_weight, R, V, K, 1.f / T};
+    vsd_status st = check_loss_call(out, in, T, grad_scale);
+    if (st) return st;
+    if (((uintptr_t)logits | (uintptr_t)out->grad) & (dtype == VSD_BF16 ? 1 : 3))
+        return VSD_ERR_INVALID_ARG;
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < topk_workspace_bytes(R, V, K))
+        return VSD_ERR_WORKSPACE;
     return from_cuda(topk_distill(logits, dtype == VSD_BF16, in, T, grad_scale, *out, ws,
                                   static_cast<cudaStream_t>(stream)));
 }

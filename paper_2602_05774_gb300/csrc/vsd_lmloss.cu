@@ -45,7 +45,7 @@ int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct LmWs {
     size_t status, done, zero_end, nrows, wsum, wmax, kappa, n, id, p, plogp, w, rowmap, rowinv,
-        lse2, coef, xk, tab, hid, X, G, dh, total;
+        lse2, coef, xk, tab, part, hid, X, G, dh, total;
     int rpad, piece, npiece, split;
     bool keep;  // the logits are kept (one piece)
 };
@@ -99,7 +99,8 @@ LmWs lm_ws(const LmLossShape& s) {
     w.lse2 = take(4 * (size_t)w.rpad);
     w.coef = take(4 * (size_t)w.rpad);
     w.xk = take(4 * RK);
-    w.tab = take(8 * (size_t)w.rpad * (size_t)units);
+    w.tab = take(8 * (size_t)w.rpad * (size_t)units * 2);
+    w.part = take(8 * ((R + 31) / 32));
     w.hid = take(2 * (size_t)w.rpad * s.H);
     w.X = take(w.keep ? 4 * (size_t)w.rpad * w.piece : 0);
     w.G = take(grads ? 2 * (size_t)w.rpad * w.piece : 0);
@@ -113,25 +114,13 @@ template <typename U> U* at(void* ws, size_t off) {
 }
 
 // ------------------------------------------------------------ rows
-// The rows' targets, then (the last block to finish) the list of counted rows.
-__global__ void k_targets(TargetIn in, Targets tg, float* row_loss, float* logz) {
-    const int lane = threadIdx.x & 31;
-    const int r = (int)((blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5);
-    if (r < in.R) target_row(in, tg, r, lane);
-    __shared__ int last;
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(tg.done, 1) == (int)gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    scan_rows(tg, in.R, row_loss, logz);
-}
-
 // Counted rows of hidden, packed; the rows up to the next K block of d_weight
-// are zero.
-__global__ void k_gather(const bf16* hidden, int H, Targets tg, bf16* hid) {
+// are zero.  Where every row counts the products read hidden itself.
+__global__ void k_gather(const bf16* hidden, int R, int H, Targets tg, bf16* hid) {
+    dep_launch();
+    dep_wait();
     const int n = *tg.nrows;
+    if (n == R) return;
     const int end = (n + 63) / 64 * 64;
     const int vecs = H / 8;
     for (int i = blockIdx.x; i < end; i += gridDim.x) {
@@ -150,10 +139,14 @@ __global__ void k_gather(const bf16* hidden, int H, Targets tg, bf16* hid) {
 //   warp 0     TMA producer: its half of A and of B (16 KB each) per K block,
 //              counted on the leader's barrier;
 //   warp 1     the leader's MMA issuer (one thread, for both CTAs);
-//   warps 2-5  epilogue: 32 rows each, tcgen05.ld, then what the product is for:
+//   warps 4-11 epilogue: 32 rows x 128 columns each, tcgen05.ld, then what the
+//              product is for:
 //     logits   A = hidden rows, B = weight rows, both K-major.  kStats: per row
-//              and tile (max, sum 2^{(x - max) c}) and the target logits in the
-//              tile (kKeep: the logits too).  kGrad: G, rounded to bf16.
+//              and half tile (max, sum 2^{(x - max) c}) and the target logits
+//              in it (kKeep: the logits too).  The tensor cores' running sum
+//              truncates, an error that grows with the number of K steps, so
+//              K is summed in parts of 512 that are added up here in fp32
+//              (round to nearest).  kGrad: G, rounded to bf16.
 //     d_hidden A = G (K-major), B = weight (MN-major, as it lies): fp32 sums,
 //              added up over the pieces of the vocabulary by TMA.
 //     d_weight A = G (MN-major), B = hidden (MN-major): one rounding to bf16.
@@ -164,10 +157,18 @@ __global__ void k_gather(const bf16* hidden, int H, Targets tg, bf16* hid) {
 namespace tc = vsd_pair;
 
 constexpr int BT = 256, BK = 64;
-constexpr int kPairThreads = 192;
+constexpr int kEpiWarps = 8;
+constexpr int kPairThreads = 32 * (4 + kEpiWarps);  // three warpgroups
+constexpr int kHalfN = BT / 2;                 // columns of an epilogue warp
+constexpr int kSumBlocks = 8;                  // K blocks of a partial sum of the logits
+// Registers per thread of the kernels that add partial sums: launched with 168,
+// of which the first warpgroup gives up what the two epilogue groups take
+// (128 (40 + 232 + 232) = 384 * 168).
+constexpr int kRegsFew = 40, kRegsMany = 232;
+static_assert(kRegsFew + 2 * kRegsMany <= 3 * 168, "the launch's registers");
 constexpr int kHalfBytes = 128 * BK * 2;       // one operand's half tile: 16 KB
 constexpr int kStageBytes = 2 * kHalfBytes;
-constexpr int kPairStages = 6;
+constexpr int kPairStages = 5;
 constexpr int kBoxBytes = 64 * BK * 2;         // an MN-major half is two 64-column boxes
 constexpr int kOutBytes = 4096;                // 32 rows x 128 bytes
 constexpr uint32_t kTmemAll = 2 * BT;
@@ -178,24 +179,25 @@ struct PairBars {
     uint64_t full[kPairStages];   // leader: both CTAs' bytes landed
     uint64_t empty[kPairStages];  // the MMAs reading the stage are done
     uint64_t acc_full[2];
-    uint64_t acc_empty[2];        // leader: 8 epilogue warps
+    uint64_t acc_empty[2];        // leader: the epilogue warps of both CTAs
     uint64_t drain;
     uint32_t tmem_base;
     int err;
 };
 constexpr size_t kPairSmem =
-    1024 + (size_t)kPairStages * kStageBytes + 8 * kOutBytes + sizeof(PairBars);
+    1024 + (size_t)kPairStages * kStageBytes + 2 * kEpiWarps * kOutBytes + sizeof(PairBars);
 
 enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3 };
 
 struct PairMaps {
-    CUtensorMap a, b, o;        // logits: hidden, weight, stored tiles
-    CUtensorMap gk, gt, wt, ht; // products: G K- and MN-major, weight and hidden MN-major
+    CUtensorMap a, a0, b, o;         // logits: packed rows, hidden, weight; stored tiles
+    CUtensorMap gk, gt, wt, ht, ht0; // products: G K- and MN-major; MN-major the weight,
+                                     // the packed rows, hidden
     CUtensorMap dw, dh;
 };
 struct PairArgs {
     Targets tg;
-    int K;                 // entries of a target list
+    int R, K;              // rows of the call, entries of a target list
     int H, V, v0, cols;    // this piece: columns v0 .. v0 + cols - 1
     int nkh;               // K blocks of the hidden size
     int64_t rpad;
@@ -329,12 +331,7 @@ __device__ __forceinline__ void read32(uint32_t taddr, int lim, float (&f)[32]) 
     uint32_t u[32];
     tc::tmem_ld32(taddr, u);
 #pragma unroll
-    for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(u[i]);
-    if (lim < 32) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i >= lim) f[i] = -INFINITY;
-    }
+    for (int i = 0; i < 32; ++i) f[i] = i < lim ? __uint_as_float(u[i]) : -INFINITY;
 }
 
 // The warp's staging buffers: `use` counts its stores.
@@ -365,83 +362,75 @@ __device__ __forceinline__ uint4* chunk_at(unsigned char* box, int lane, int j) 
     return reinterpret_cast<uint4*>(box + lane * 128) + (j ^ (lane & 7));
 }
 
+// n0: the warp's first column of the piece; x: its row's 128 logits.
 template <bool KEEP>
-__device__ __forceinline__ void stats_tile(const PairArgs& a, const PairMaps& maps, const Job& j,
-                                           int row0, int lane, int n_rows, uint32_t taddr,
+__device__ __forceinline__ void stats_tile(const PairArgs& a, const PairMaps& maps, int n0,
+                                           int row0, int lane, int n_rows, float (&x)[kHalfN],
                                            Stage& out) {
     const int row = row0 + lane;
     const bool on = row < n_rows;
-    float m = -INFINITY, s = 0.f;
-#pragma unroll 1
-    for (int cc = 0; cc < BT / 32; ++cc) {
-        float f[32];
-        read32(taddr + 32u * cc, a.cols - j.n0 - 32 * cc, f);
-        float gm = f[0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) gm = fmaxf(gm, f[i]);
-        const float nm = fmaxf(m, gm);
-        if (nm > -INFINITY) {
-            const float b = -nm * a.c;
-            float t0 = 0.f, t1 = 0.f;
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-                t0 += ex2(fmaf(f[i], a.c, b));
-                t1 += ex2(fmaf(f[i + 1], a.c, b));
-            }
-            s = s * ex2((m - nm) * a.c) + (t0 + t1);
-            m = nm;
-        } else {  // nothing but -inf and NaN: a NaN has to reach the sum
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (f[i] != f[i]) s = f[i];
-        }
-        if (KEEP) {
-            unsigned char* box = out.acquire();
-#pragma unroll
-            for (int v = 0; v < 8; ++v)
-                *chunk_at(box, lane, v) =
-                    make_uint4(__float_as_uint(f[4 * v]), __float_as_uint(f[4 * v + 1]),
-                               __float_as_uint(f[4 * v + 2]), __float_as_uint(f[4 * v + 3]));
-            out.store(&maps.o, j.n0 + 32 * cc, row0, row0 < n_rows);
-        }
-    }
-    if (on) a.tab[(int64_t)(j.n0 / BT) * a.rpad + row] = make_float2(m, s);
-    // the target logits in this tile: the warp reads each wanted column once
+    const int lim = a.cols - n0;
+    // the target logits among these columns, each read back by its own row's
+    // thread from shared memory (a register array cannot be indexed)
     const RowList list(a, row, on);
-    const int lo = a.v0 + j.n0, hi = lo + min(BT, a.cols - j.n0);
+    const int lo = a.v0 + n0, hi = lo + min(kHalfN, lim);
     int k = lower_bound(list.id, list.n, lo);
     int id = k < list.n ? __ldg(list.id + k) : hi;
-    for (;;) {
-        const unsigned want = __ballot_sync(0xffffffffu, id < hi);
-        if (!want) break;
-        const int col = __shfl_sync(0xffffffffu, id, __ffs(want) - 1);
-        const float x = tc::tmem_ld1(taddr + (uint32_t)(col - lo));
-        if (id == col) {
-            a.xk[(size_t)row * a.K + k] = x;
+#pragma unroll
+    for (int g = 0; g < kHalfN / 32; ++g) {
+        const int end = min(lo + 32 * (g + 1), hi);
+        if (!KEEP && !__any_sync(0xffffffffu, id < end)) continue;
+        unsigned char* box = out.acquire();
+#pragma unroll
+        for (int v = 0; v < 8; ++v)
+            *chunk_at(box, lane, v) = make_uint4(
+                __float_as_uint(x[32 * g + 4 * v]), __float_as_uint(x[32 * g + 4 * v + 1]),
+                __float_as_uint(x[32 * g + 4 * v + 2]), __float_as_uint(x[32 * g + 4 * v + 3]));
+        while (id < end) {
+            const int col = id - lo - 32 * g;
+            a.xk[(size_t)row * a.K + k] =
+                reinterpret_cast<const float*>(chunk_at(box, lane, col >> 2))[col & 3];
             ++k;
             id = k < list.n ? __ldg(list.id + k) : hi;
         }
+        if (KEEP) out.store(&maps.o, n0 + 32 * g, row0, row0 < n_rows);
     }
+    if (lim < kHalfN) {
+#pragma unroll
+        for (int i = 0; i < kHalfN; ++i)
+            if (i >= lim) x[i] = -INFINITY;
+    }
+    float m0 = x[0], m1 = x[1];
+#pragma unroll
+    for (int i = 2; i < kHalfN; i += 2) m0 = fmaxf(m0, x[i]), m1 = fmaxf(m1, x[i + 1]);
+    const float m = fmaxf(m0, m1);
+    const float b = m > -INFINITY ? -m * a.c : 0.f;  // (a NaN still reaches the sum)
+    float t[4] = {};
+#pragma unroll
+    for (int i = 0; i < kHalfN; ++i) t[i & 3] += ex2(fmaf(x[i], a.c, b));
+    if (on)
+        a.tab[(int64_t)(n0 / kHalfN) * a.rpad + row] =
+            make_float2(m, (t[0] + t[1]) + (t[2] + t[3]));
 }
 
-__device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& maps, const Job& j,
+__device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& maps, int n0,
                                           int row0, int lane, int n_rows, uint32_t taddr,
                                           Stage& out) {
     const int row = row0 + lane;
     const bool on = row < n_rows;
     const float cf = on ? __ldg(a.coef + row) : 0.f, l = on ? __ldg(a.lse2 + row) : 0.f;
     const RowList list(a, row, on);
-    const int lo = a.v0 + j.n0;
+    const int lo = a.v0 + n0;
     int k = lower_bound(list.id, list.n, lo);
     // rows up to the next K block of d_weight are written (zero past the last)
     const bool inside = row0 < (n_rows + BK - 1) / BK * BK;
 #pragma unroll 1
-    for (int g = 0; g < BT / 64; ++g) {
+    for (int g = 0; g < kHalfN / 64; ++g) {
         unsigned char* box = out.acquire();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float f[32];
-            read32(taddr + 64u * g + 32u * h, a.cols - j.n0 - 64 * g - 32 * h, f);
+            read32(taddr + 64u * g + 32u * h, a.cols - n0 - 64 * g - 32 * h, f);
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -463,17 +452,17 @@ __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& map
                 __float2bfloat16_rn(cf * (ex2(fmaf(x, a.c, -l)) - __ldg(list.p + k)));
             ++k;
         }
-        out.store(&maps.o, j.n0 + 64 * g, row0, inside);
+        out.store(&maps.o, n0 + 64 * g, row0, inside);
     }
 }
 
 __device__ __forceinline__ void dh_tile(const PairArgs& a, const PairMaps& maps, const Job& j,
-                                        int row0, int lane, int n_rows, uint32_t taddr,
+                                        int n0, int row0, int lane, int n_rows, uint32_t taddr,
                                         Stage& out) {
     const bool none = j.kb0 == j.kb1;
     if (none && !a.first) return;  // nothing to add
 #pragma unroll 1
-    for (int g = 0; g < BT / 32; ++g) {
+    for (int g = 0; g < kHalfN / 32; ++g) {
         unsigned char* box = out.acquire();
         uint32_t u[32];
         tc::tmem_ld32(taddr + 32u * g, u);
@@ -482,17 +471,17 @@ __device__ __forceinline__ void dh_tile(const PairArgs& a, const PairMaps& maps,
             *chunk_at(box, lane, v) =
                 none ? make_uint4(0u, 0u, 0u, 0u)
                      : make_uint4(u[4 * v], u[4 * v + 1], u[4 * v + 2], u[4 * v + 3]);
-        const int x = j.n0 + 32 * g;
+        const int x = n0 + 32 * g;
         out.store(&maps.dh, x, (int)(j.part * a.rpad) + row0, x < a.H && row0 < n_rows, !a.first);
     }
 }
 
 __device__ __forceinline__ void dw_tile(const PairArgs& a, const PairMaps& maps, const Job& j,
-                                        int row0, int lane, uint32_t taddr, Stage& out) {
+                                        int n0, int row0, int lane, uint32_t taddr, Stage& out) {
     const bool none = j.kb0 == j.kb1;
     const float s = none ? 0.f : __ldg(a.kappa);
 #pragma unroll 1
-    for (int g = 0; g < BT / 64; ++g) {
+    for (int g = 0; g < kHalfN / 64; ++g) {
         unsigned char* box = out.acquire();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -509,9 +498,14 @@ __device__ __forceinline__ void dw_tile(const PairArgs& a, const PairMaps& maps,
                 *chunk_at(box, lane, 4 * h + v) =
                     make_uint4(w[4 * v], w[4 * v + 1], w[4 * v + 2], w[4 * v + 3]);
         }
-        const int x = j.n0 + 64 * g, y = a.v0 + row0;
+        const int x = n0 + 64 * g, y = a.v0 + row0;
         out.store(&maps.dw, x, y, x < a.H && y < a.V);
     }
+}
+
+// The first warpgroup's share of the register split, in each of its roles.
+template <bool kSplit> __device__ __forceinline__ void give_registers() {
+    if (kSplit) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kRegsFew));
 }
 
 template <int MODE>
@@ -520,11 +514,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     extern __shared__ unsigned char dsm_raw[];
     unsigned char* dsm = dsm_raw + ((1024u - (smem_u32(dsm_raw) & 1023u)) & 1023u);
     unsigned char* outs = dsm + kPairStages * kStageBytes;
-    PairBars* sb = reinterpret_cast<PairBars*>(outs + 8 * kOutBytes);
+    PairBars* sb = reinterpret_cast<PairBars*>(outs + 2 * kEpiWarps * kOutBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)tc::cluster_rank();
     int* status = a.tg.status;
-    const int n_rows = __ldg(a.tg.nrows);
+    dep_launch();
     if (threadIdx.x == 0) {
         for (int s = 0; s < kPairStages; ++s) {
             mbar_init(&sb->full[s], 1);
@@ -532,7 +526,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&sb->acc_full[b], 1);
-            mbar_init(&sb->acc_empty[b], 8);
+            mbar_init(&sb->acc_empty[b], 2 * kEpiWarps);
         }
         mbar_init(&sb->drain, 1);
         sb->err = 0;
@@ -544,12 +538,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     tc::cluster_sync();
     tc::tc_fence_after();
     const uint32_t tmem = sb->tmem_base;
+    dep_wait();
+    const int n_rows = *(const volatile int*)a.tg.nrows;
+    const bool all = n_rows == a.R;  // hidden as it is
+    // K blocks summed at a time: the logits' parts, or all of a product's
+    constexpr bool kParts = MODE == kStats || MODE == kKeep;
     Jobs<MODE> jobs(a, n_rows);
     Job j;
-
     if (warp == 0) {
+        give_registers<kParts>();
         // ------------------------------------------------------ TMA producer
         if (lane == 0) {
+            // what earlier kernels stored is read through the async proxy
+            asm volatile("fence.proxy.async;" ::: "memory");
+            const CUtensorMap* ma = all ? &maps.a0 : &maps.a;
+            const CUtensorMap* mh = all ? &maps.ht0 : &maps.ht;
             uint32_t it = 0;
             bool ok = true;
             while (ok && !*(volatile int*)&sb->err && jobs.next(j)) {
@@ -566,7 +569,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     const uint32_t bar = tc::leader_addr(&sb->full[s]);
                     if (rank == 0) mbar_expect_tx(&sb->full[s], 2 * kStageBytes);
                     if (MODE != kProd) {
-                        tc::load_2d(A, &maps.a, kb * BK, j.m0 + 128 * rank, bar);
+                        tc::load_2d(A, ma, kb * BK, j.m0 + 128 * rank, bar);
                         tc::load_2d(B, &maps.b, kb * BK, a.v0 + j.n0 + 128 * rank, bar);
                     } else {
                         const int n = j.n0 + 128 * rank;
@@ -578,8 +581,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                             const int m = j.m0 + 128 * rank;
                             tc::load_2d(A, &maps.gt, m, kb * BK, bar);
                             tc::load_2d(A + kBoxBytes, &maps.gt, m + 64, kb * BK, bar);
-                            tc::load_2d(B, &maps.ht, n, kb * BK, bar);
-                            tc::load_2d(B + kBoxBytes, &maps.ht, n + 64, kb * BK, bar);
+                            tc::load_2d(B, mh, n, kb * BK, bar);
+                            tc::load_2d(B + kBoxBytes, mh, n + 64, kb * BK, bar);
                         }
                     }
                     ++it;
@@ -591,68 +594,112 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     drain_pair(&sb->full[i % kPairStages], (i / kPairStages) & 1u);
         }
     } else if (warp == 1) {
+        give_registers<kParts>();
         // ------------------------------------------------------ MMA issuer
         if (lane == 0 && rank == 0) {
             uint32_t it = 0;
             int lt = 0;
             bool ok = true;
-            for (; ok && !*(volatile int*)&sb->err && jobs.next(j); ++lt) {
-                const int buf = lt & 1;
-                const uint32_t use = (uint32_t)lt >> 1;
-                if (use > 0 && !wait_pair(&sb->acc_empty[buf], (use - 1) & 1u, sb, status)) break;
-                tc::tc_fence_after();
-                const uint32_t d = tmem + (uint32_t)(buf * BT);
+            while (ok && !*(volatile int*)&sb->err && jobs.next(j)) {
                 const bool amn = MODE == kProd && j.kind == 2, bmn = MODE == kProd;
                 const uint32_t idesc = tc::idesc_bf16(256, BT) | (amn ? 1u << 15 : 0u) |
                                        (bmn ? 1u << 16 : 0u);
                 const int kb1 = MODE == kProd ? j.kb1 : a.nkh;
-                for (int kb = j.kb0; kb < kb1; ++kb) {
-                    const int s = (int)(it % kPairStages);
-                    if (!wait_pair(&sb->full[s], (it / kPairStages) & 1u, sb, status)) {
+                int kb = j.kb0;
+                do {  // (a job without K blocks hands on its accumulator unread)
+                    const int end = kParts ? min(kb1, kb + kSumBlocks) : kb1;
+                    const int buf = lt & 1;
+                    const uint32_t use = (uint32_t)lt >> 1;
+                    if (use > 0 && !wait_pair(&sb->acc_empty[buf], (use - 1) & 1u, sb, status)) {
                         ok = false;
                         break;
                     }
                     tc::tc_fence_after();
-                    const uint32_t A = smem_u32(dsm + s * kStageBytes), B = A + kHalfBytes;
+                    const uint32_t d = tmem + (uint32_t)(buf * BT);
+                    uint32_t more = 0;
+                    for (; kb < end; ++kb) {
+                        const int s = (int)(it % kPairStages);
+                        if (!wait_pair(&sb->full[s], (it / kPairStages) & 1u, sb, status)) {
+                            ok = false;
+                            break;
+                        }
+                        tc::tc_fence_after();
+                        const uint32_t A = smem_u32(dsm + s * kStageBytes), B = A + kHalfBytes;
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k)
-                        tc::mma_pair(d,
-                                     amn ? tc::desc_mn(A + 2048u * k, kBoxBytes)
-                                         : tc::sdesc_sw128(A + 32u * k),
-                                     bmn ? tc::desc_mn(B + 2048u * k, kBoxBytes)
-                                         : tc::sdesc_sw128(B + 32u * k),
-                                     idesc, (kb != j.kb0 || k != 0) ? 1u : 0u);
-                    tc::commit_pair(&sb->empty[s]);
-                    ++it;
-                }
-                if (!ok) break;
-                tc::commit_pair(&sb->acc_full[buf]);
+                        for (int k = 0; k < BK / 16; ++k) {
+                            tc::mma_pair(d,
+                                         amn ? tc::desc_mn(A + 2048u * k, kBoxBytes)
+                                             : tc::sdesc_sw128(A + 32u * k),
+                                         bmn ? tc::desc_mn(B + 2048u * k, kBoxBytes)
+                                             : tc::sdesc_sw128(B + 32u * k),
+                                         idesc, more);
+                            more = 1;
+                        }
+                        tc::commit_pair(&sb->empty[s]);
+                        ++it;
+                    }
+                    if (!ok) break;
+                    tc::commit_pair(&sb->acc_full[buf]);
+                    ++lt;
+                } while (kb < kb1);
             }
             tc::commit_pair(&sb->drain);  // every MMA issued is done once it arrives
             drain_pair(&sb->drain, 0);
         }
+    } else if (warp < 4) {
+        give_registers<kParts>();
     } else {
         // ------------------------------------------------------ epilogue
-        const int q = warp & 3;  // TMEM lanes 32q .. 32q + 31
-        Stage out{outs + (warp - 2) * 2 * kOutBytes, 0, lane};
-        for (int lt = 0; jobs.next(j); ++lt) {
-            const int buf = lt & 1;
-            const uint32_t use = (uint32_t)lt >> 1;
-            if (!__all_sync(0xffffffffu, wait_pair(&sb->acc_full[buf], use & 1u, sb, status)))
-                break;
+        if (kParts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kRegsMany));
+        const int q = warp & 3;               // TMEM lanes 32q .. 32q + 31
+        const int h0 = (warp - 4) / 4 * kHalfN;  // its columns of the tile
+        Stage out{outs + (warp - 4) * 2 * kOutBytes, 0, lane};
+        const uint32_t empty = tc::leader_addr(&sb->acc_empty[0]);
+        int lt = 0;
+        auto ready = [&]() {
+            const bool ok = __all_sync(0xffffffffu, wait_pair(&sb->acc_full[lt & 1],
+                                                              ((uint32_t)lt >> 1) & 1u, sb, status));
             tc::tc_fence_after();
-            const uint32_t taddr = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * BT);
-            const int row0 = j.m0 + 128 * rank + 32 * q;
-            if (MODE == kStats) stats_tile<false>(a, maps, j, row0, lane, n_rows, taddr, out);
-            if (MODE == kKeep) stats_tile<true>(a, maps, j, row0, lane, n_rows, taddr, out);
-            if (MODE == kGrad) grad_tile(a, maps, j, row0, lane, n_rows, taddr, out);
-            if (MODE == kProd) {
-                if (j.kind == 1) dh_tile(a, maps, j, row0, lane, n_rows, taddr, out);
-                else dw_tile(a, maps, j, row0, lane, taddr, out);
-            }
+            return ok;
+        };
+        auto release = [&]() {
             tc::tc_fence_before();
             __syncwarp();
-            if (lane == 0) tc::arrive_remote(tc::leader_addr(&sb->acc_empty[buf]));
+            if (lane == 0) tc::arrive_remote(empty + 8u * (lt & 1));
+            ++lt;
+        };
+        auto acc_addr = [&]() {
+            return tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)((lt & 1) * BT + h0);
+        };
+        while (jobs.next(j)) {
+            const int row0 = j.m0 + 128 * rank + 32 * q, n0 = j.n0 + h0;
+            if (kParts) {
+                float x[kHalfN];
+                bool ok = true;
+                for (int kb = 0; ok && kb < a.nkh; kb += kSumBlocks) {
+                    if (!(ok = ready())) break;
+                    const uint32_t t = acc_addr();
+#pragma unroll
+                    for (int g = 0; g < kHalfN / 32; ++g) {
+                        uint32_t u[32];
+                        tc::tmem_ld32(t + 32u * g, u);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            x[32 * g + i] = kb ? x[32 * g + i] + __uint_as_float(u[i])
+                                               : __uint_as_float(u[i]);
+                    }
+                    release();
+                }
+                if (!ok) break;
+                stats_tile<MODE == kKeep>(a, maps, n0, row0, lane, n_rows, x, out);
+            } else {
+                if (!ready()) break;
+                const uint32_t t = acc_addr();
+                if (MODE == kGrad) grad_tile(a, maps, n0, row0, lane, n_rows, t, out);
+                else if (j.kind == 1) dh_tile(a, maps, j, n0, row0, lane, n_rows, t, out);
+                else dw_tile(a, maps, j, n0, row0, lane, t, out);
+                release();
+            }
         }
         if (lane == 0) tc::bulk_wait_all();
     }
@@ -666,57 +713,92 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
 }
 
-// One warp per counted row: its log-partition, loss and gradient coefficient;
-// the last block to finish sums the losses in row order.
-__global__ void k_rows(const float2* tab, int ntab, int64_t stride, Targets tg, int K, float c,
-                       float T, float grad_scale, const float* xk, float* lse2, float* coef,
-                       float* kappa, float* row_loss, float* logz, float* loss, int R) {
-    const int n_rows = *tg.nrows;
+// 32 counted rows per block: log-partition, loss and gradient coefficient.  The
+// warps share out the row's parts (a lane per row, so the reads coalesce), then
+// the rows' target lists.  The blocks' weighted losses are added in block order
+// by the last block to finish.
+__global__ void __launch_bounds__(256)
+    k_rows(const float2* tab, int ntab, int64_t stride, Targets tg, int K, float c, float T,
+           float grad_scale, const float* xk, float* lse2, float* coef, float* kappa,
+           float* row_loss, float* logz, double* part, float* loss) {
+    __shared__ float2 ms[8][32];
+    __shared__ double dots[32], wl[32];
+    __shared__ int last;
+    dep_launch();
+    dep_wait();
+    const int n_rows = *(const volatile int*)tg.nrows;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int i = (int)((blockIdx.x * (int64_t)blockDim.x + threadIdx.x) >> 5);
-    if (i < n_rows) {
-        float m = -INFINITY;
-        for (int t = lane; t < ntab; t += 32) m = fmaxf(m, tab[t * stride + i].x);
-        m = warp_max(m);
-        float s = 0.f;
-        for (int t = lane; t < ntab; t += 32) {
-            const float2 e = tab[t * stride + i];
-            // (a part of no mass has maximum -inf and sum 0, or NaN)
-            s += e.x > -INFINITY ? e.y * ex2((e.x - m) * c) : e.y;
+    const int i0 = blockIdx.x * 32, i = i0 + lane;
+    if (i0 < n_rows) {
+        float m = -INFINITY, s = 0.f;
+        if (i < n_rows) {
+            for (int t = warp; t < ntab; t += 32) {  // (four parts' loads at a time)
+                float2 e[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    e[u] = t + 8 * u < ntab ? ld_cg(tab + (t + 8 * u) * stride + i)
+                                            : make_float2(-INFINITY, 0.f);
+                const float nm =
+                    fmaxf(fmaxf(fmaxf(e[0].x, e[1].x), fmaxf(e[2].x, e[3].x)), m);
+                const float z = nm > -INFINITY ? nm : 0.f;
+                s *= ex2((m - z) * c);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) s += e[u].y * ex2((e[u].x - z) * c);
+                m = nm;
+            }
         }
-        s = warp_sum(s);
-        const int r = tg.rowmap[i], n = tg.n[r];
-        double dot = 0.0;
-        for (int k = lane; k < n; k += 32)
-            dot += (double)tg.p[(size_t)r * K + k] * (double)xk[(size_t)i * K + k];
-        dot = warp_sum(dot);
-        if (lane == 0) {
-            const double lz = (double)m / (double)T + log((double)s);
-            if (!isfinite(lz)) atomicOr(tg.status, VSD_STATUS_BAD_ROW);
-            logz[r] = (float)lz;
-            row_loss[r] = (float)((double)tg.plogp[r] + lz - dot / (double)T);
-            lse2[i] = (float)(lz * kLog2e);
-            const float wm = *tg.wmax;
-            coef[i] = wm > 0.f ? kTopMantissa * (tg.w[r] / wm) : 0.f;
+        ms[warp][lane] = make_float2(m, s);
+        for (int q = warp * 4; q < warp * 4 + 4; ++q) {
+            double dot = 0.0;
+            if (i0 + q < n_rows) {
+                const int r = tg.rowmap[i0 + q], n = tg.n[r];
+                for (int k = lane; k < n; k += 32)
+                    dot += (double)tg.p[(size_t)r * K + k] *
+                           (double)xk[(size_t)(i0 + q) * K + k];
+            }
+            dot = warp_sum(dot);
+            if (lane == 0) dots[q] = dot;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            double wloss = 0.0;
+            if (i < n_rows) {
+                m = ms[0][lane].x;
+                for (int w = 1; w < 8; ++w) m = fmaxf(m, ms[w][lane].x);
+                const float z = m > -INFINITY ? m : 0.f;
+                s = 0.f;
+                for (int w = 0; w < 8; ++w) s += ms[w][lane].y * ex2((ms[w][lane].x - z) * c);
+                const int r = tg.rowmap[i];
+                const double lz = (double)m / (double)T + log((double)s);
+                if (!isfinite(lz)) atomicOr(tg.status, VSD_STATUS_BAD_ROW);
+                const float rl = (float)((double)tg.plogp[r] + lz - dots[lane] / (double)T);
+                const float w = tg.w[r], wm = *tg.wmax;
+                logz[r] = (float)lz;
+                row_loss[r] = rl;
+                lse2[i] = (float)(lz * kLog2e);
+                coef[i] = wm > 0.f ? kTopMantissa * (w / wm) : 0.f;
+                if (w != 0.f) wloss = (double)w * (double)rl;
+            }
+            wloss = warp_sum(wloss);
+            if (lane == 0) part[blockIdx.x] = wloss;
         }
     }
-    __shared__ int last;
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(tg.done + 1, 1) == (int)gridDim.x - 1;
+    if (threadIdx.x == 0) {
+        __threadfence();
+        last = atomicAdd(tg.done + 1, 1) == (int)gridDim.x - 1;
+    }
     __syncthreads();
     if (!last) return;
     __threadfence();
+    const int nb = (n_rows + 31) / 32;
     double sum = 0.0;
-    for (int r = threadIdx.x; r < R; r += blockDim.x)
-        if (tg.rowinv[r] >= 0 && tg.w[r] != 0.f) sum += (double)tg.w[r] * (double)ld_cg(row_loss + r);
-    __shared__ double part[8];
+    for (int b = threadIdx.x; b < nb; b += blockDim.x) sum += ld_cg(part + b);
     sum = warp_sum(sum);
-    if (lane == 0) part[warp] = sum;
+    if (lane == 0) wl[warp] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         sum = 0.0;
-        for (int w = 0; w < (int)blockDim.x / 32; ++w) sum += part[w];
+        for (int w = 0; w < 8; ++w) sum += wl[w];
         *loss = (float)(sum / *tg.wsum);
         *kappa = (float)((double)grad_scale * (double)*tg.wmax /
                          ((double)kTopMantissa * *tg.wsum * (double)T));
@@ -730,6 +812,8 @@ constexpr int kMakeCols = 2048;
 __global__ void __launch_bounds__(256)
     k_make_g(const float* X, int64_t ldx, int V, int K, Targets tg, float c, const float* lse2,
              const float* coef, const float* xk, bf16* G, int64_t ldg) {
+    dep_launch();
+    dep_wait();
     const int i = blockIdx.y, n_rows = *tg.nrows;
     if (i >= (n_rows + BK - 1) / BK * BK) return;
     const int c0 = blockIdx.x * kMakeCols, v = c0 + threadIdx.x * 8;
@@ -765,12 +849,16 @@ __global__ void __launch_bounds__(256)
 // in rows not counted.
 __global__ void k_dh_out(const float* dh, int split, int64_t rpad, int H, Targets tg,
                          const float* kappa, bf16* out) {
+    dep_launch();
+    dep_wait();
     const int r = blockIdx.x, i = tg.rowinv[r];
     const float s = *kappa;
-    for (int h = threadIdx.x * 8; h < H; h += blockDim.x * 8) {
+    for (int h = (blockIdx.y * blockDim.x + threadIdx.x) * 8; h < H;
+         h += gridDim.y * blockDim.x * 8) {
         uint4 w = make_uint4(0u, 0u, 0u, 0u);
         if (i >= 0) {
             float f[8] = {};
+#pragma unroll 4
             for (int q = 0; q < split; ++q) {
                 const float4* p =
                     reinterpret_cast<const float4*>(dh + ((size_t)q * rpad + i) * H + h);
@@ -804,8 +892,8 @@ static cudaError_t launch_pair(const PairMaps& maps, const PairArgs& a, int64_t 
     cudaError_t e = ensure_dyn_smem((const void*)k_pair<MODE>, kPairSmem);
     if (e != cudaSuccess) return e;
     const int64_t pairs = std::max<int64_t>(1, std::min<int64_t>(jobs, device_sm_count() / 2));
-    k_pair<MODE><<<(unsigned)(2 * pairs), kPairThreads, kPairSmem, st>>>(maps, a);
-    return cudaGetLastError();
+    return launch_dep(k_pair<MODE>, dim3((unsigned)(2 * pairs)), kPairThreads, kPairSmem, 1, st,
+                      maps, a);
 }
 
 cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
@@ -813,6 +901,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
                    void* ws, cudaStream_t st) {
     const LmWs w = lm_ws(s);
     const int R = s.R, V = s.V, H = s.H, K = s.K;
+    const bool grads = s.dh || s.dw;
     Targets tg{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
                at<float>(ws, w.plogp), at<float>(ws, w.w), at<int32_t>(ws, w.rowmap),
                at<int32_t>(ws, w.rowinv), at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum),
@@ -824,21 +913,22 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     float *xk = at<float>(ws, w.xk), *lse2 = at<float>(ws, w.lse2), *coef = at<float>(ws, w.coef),
           *kappa = at<float>(ws, w.kappa), *dh = at<float>(ws, w.dh);
     const float c = (float)(kLog2e / (double)T);
-    // rows of the packed hidden states that may be read: up to a K block
+    // packed rows that may be read: up to a K block
     const int64_t hrows = round_up(R, BK);
     PairMaps maps;
     memset(&maps, 0, sizeof(maps));
     using vsd_lm::make_map_sw128;
     bool ok = make_map_sw128(&maps.a, hid, false, hrows, H, H, 128) &&
+              make_map_sw128(&maps.a0, hidden, false, R, H, H, 128) &&
               make_map_sw128(&maps.b, weight, false, V, H, H, 128);
-    if (s.dh || s.dw)
+    if (grads)
         ok = ok && make_map_sw128(&maps.gk, G, false, w.rpad, w.piece, w.piece, 128) &&
              make_map_sw128(&maps.gt, G, false, w.rpad, w.piece, w.piece, BK) &&
              make_map_sw128(&maps.wt, weight, false, V, H, H, BK) &&
-             make_map_sw128(&maps.ht, hid, false, hrows, H, H, BK);
+             make_map_sw128(&maps.ht, hid, false, hrows, H, H, BK) &&
+             make_map_sw128(&maps.ht0, hidden, false, R, H, H, BK);
     if (w.keep) ok = ok && make_map_sw128(&maps.o, X, true, w.rpad, w.piece, w.piece, 32);
-    else if (s.dh || s.dw)
-        ok = ok && make_map_sw128(&maps.o, G, false, w.rpad, w.piece, w.piece, 32);
+    else if (grads) ok = ok && make_map_sw128(&maps.o, G, false, w.rpad, w.piece, w.piece, 32);
     if (s.dw) ok = ok && make_map_sw128(&maps.dw, out.d_weight, false, V, H, H, 32);
     if (s.dh)
         ok = ok && make_map_sw128(&maps.dh, dh, true, (int64_t)w.rpad * w.split, H, H, 32);
@@ -846,6 +936,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
 
     PairArgs a{};
     a.tg = tg;
+    a.R = R;
     a.K = K;
     a.H = H;
     a.V = V;
@@ -863,20 +954,20 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     a.want_dh = s.dh;
     a.want_dw = s.dw;
 
-    cudaError_t e = cudaMemsetAsync(ws, 0, w.zero_end, st);
+    cudaError_t e = launch_targets(in, tg, out.row_loss, out.logz, w.zero_end, st);
     if (e != cudaSuccess) return e;
-    k_targets<<<(R + 7) / 8, 256, 0, st>>>(in, tg, out.row_loss, out.logz);
-    k_gather<<<std::min(w.rpad, 4 * device_sm_count()), 256, 0, st>>>(
-        static_cast<const bf16*>(hidden), H, tg, hid);
-    if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    e = launch_dep(k_gather, dim3((unsigned)std::min<int64_t>(hrows, 4 * device_sm_count())), 256,
+                   0, 1, st, static_cast<const bf16*>(hidden), R, H, tg, hid);
+    if (e != cudaSuccess) return e;
     const int64_t mt = w.rpad / kRowPad, units = (V + kPieceUnit - 1) / kPieceUnit;
     const int64_t ht = (H + BT - 1) / BT;
     e = w.keep ? launch_pair<kKeep>(maps, a, mt * units, st)
                : launch_pair<kStats>(maps, a, mt * units, st);
     if (e != cudaSuccess) return e;
-    k_rows<<<(R + 7) / 8, 256, 0, st>>>(tab, (int)units, w.rpad, tg, K, c, T, grad_scale, xk, lse2,
-                                        coef, kappa, out.row_loss, out.logz, out.loss, R);
-    if ((e = cudaGetLastError()) != cudaSuccess || !(s.dh || s.dw)) return e;
+    e = launch_dep(k_rows, dim3((unsigned)((R + 31) / 32)), 256, 0, 1, st, tab, (int)(2 * units),
+                   (int64_t)w.rpad, tg, K, c, T, grad_scale, xk, lse2, coef, kappa, out.row_loss,
+                   out.logz, at<double>(ws, w.part), out.loss);
+    if (e != cudaSuccess || !grads) return e;
     for (int q = 0; q < w.npiece; ++q) {
         a.v0 = q * w.piece;
         a.cols = std::min(w.piece, V - a.v0);
@@ -884,8 +975,8 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         const int64_t nu = (a.cols + kPieceUnit - 1) / kPieceUnit;
         if (w.keep) {
             const dim3 grid((unsigned)((w.piece + kMakeCols - 1) / kMakeCols), (unsigned)hrows);
-            k_make_g<<<grid, 256, 0, st>>>(X, w.piece, V, K, tg, c, lse2, coef, xk, G, w.piece);
-            e = cudaGetLastError();
+            e = launch_dep(k_make_g, grid, 256, 0, 1, st, X, (int64_t)w.piece, V, K, tg, c, lse2,
+                           coef, xk, G, (int64_t)w.piece);
         } else {
             e = launch_pair<kGrad>(maps, a, mt * nu, st);
         }
@@ -894,9 +985,9 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         if (e != cudaSuccess) return e;
     }
     if (s.dh) {
-        k_dh_out<<<R, 256, 0, st>>>(dh, w.split, w.rpad, H, tg, kappa,
-                                    static_cast<bf16*>(out.d_hidden));
-        e = cudaGetLastError();
+        const unsigned y = (unsigned)std::min<int64_t>(((int64_t)H + 2047) / 2048, 16);
+        e = launch_dep(k_dh_out, dim3((unsigned)R, y), 256, 0, 1, st, dh, w.split, (int64_t)w.rpad,
+                       H, tg, kappa, static_cast<bf16*>(out.d_hidden));
     }
     return e;
 }

@@ -19,6 +19,34 @@ namespace vsd {
 
 constexpr int kMaxTeacher = 128;  // entries of a teacher row: four per lane of a warp
 
+// Programmatic dependent launch: a kernel started this way may begin before
+// the one ahead of it in the stream has ended, and reads what that one wrote
+// only after dep_wait().  Every kernel of a chain calls dep_wait(), so each
+// one's end implies the end of all before it.
+__device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// The kernel after this one may be brought in.
+__device__ __forceinline__ void dep_launch() {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename... P, typename... A>
+cudaError_t launch_dep(void (*kern)(P...), dim3 grid, int threads, size_t smem, int cluster,
+                       cudaStream_t st, A&&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = (unsigned)cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, P(args)...);
+}
+
 // What a call says about its targets (device pointers).
 struct TargetIn {
     const int32_t* labels;     // [R], or null: ids and logits below
@@ -55,11 +83,11 @@ __device__ __forceinline__ float teacher_logit(const TargetIn& in, size_t i) {
     return __ldg(static_cast<const float*>(in.teacher) + i);
 }
 
-// The target of one row, by one warp.
+// The target of one row, by one warp; kPer entries of the list per lane.
+template <int kPer>
 __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg, int r,
                                            int lane) {
     constexpr unsigned kAll = 0xffffffffu;
-    constexpr int kPer = kMaxTeacher / 32;
     const float w = in.row_weight ? __ldg(in.row_weight + r) : 1.f;
     int bits = (w >= 0.f && isfinite(w)) ? 0 : VSD_STATUS_BAD_ROW;
     const size_t base = (size_t)r * in.K;
@@ -170,9 +198,9 @@ __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg
     }
 }
 
-// The list of counted rows, the sum and the largest of their weights, by one block.  Each
-// thread takes a run of rows; the runs' counts and sums are combined in thread
-// order, so the result does not depend on timing.
+// The list of counted rows, the sum and the largest of their weights, by one
+// block.  Each thread takes a run of rows; the runs' counts and sums are
+// combined in thread order, so the result does not depend on timing.
 __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_loss,
                                           float* logz) {
     __shared__ int cnt[32];
@@ -185,13 +213,22 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_l
     int c = 0;
     double ws = 0.0;
     float wm = 0.f;
-    for (int64_t r = r0; r < r1; ++r)
-        if (ld_cg(tg.n + r) >= 0) {
-            const float w = ld_cg(tg.w + r);
-            ++c;
-            ws += (double)w;
-            wm = fmaxf(wm, w);
+    for (int64_t b = r0; b < r1; b += 8) {  // (eight rows' loads at a time)
+        int n[8];
+        float w[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            n[i] = b + i < r1 ? ld_cg(tg.n + b + i) : -1;
+            w[i] = b + i < r1 ? ld_cg(tg.w + b + i) : 0.f;
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (n[i] >= 0) {
+                ++c;
+                ws += (double)w[i];
+                wm = fmaxf(wm, w[i]);
+            }
+    }
     int inc = c;
     for (int o = 1; o < 32; o <<= 1) {
         const int v = __shfl_up_sync(0xffffffffu, inc, o);
@@ -204,14 +241,23 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_l
     __syncthreads();
     int at = inc - c;
     for (int i = 0; i < warp; ++i) at += cnt[i];
-    for (int64_t r = r0; r < r1; ++r) {
-        const bool on = ld_cg(tg.n + r) >= 0;
-        tg.rowinv[r] = on ? at : -1;
-        if (on) {
-            tg.rowmap[at++] = (int)r;
-        } else {
-            row_loss[r] = 0.f;
-            logz[r] = 0.f;
+    for (int64_t b = r0; b < r1; b += 8) {
+        int n[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n[i] = b + i < r1 ? ld_cg(tg.n + b + i) : -1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (b + i >= r1) break;
+            const int r = (int)(b + i);
+            const bool on = n[i] >= 0;
+            if (tg.rowinv) tg.rowinv[r] = on ? at : -1;
+            if (on) {
+                if (tg.rowmap) tg.rowmap[at] = r;
+                ++at;
+            } else {
+                row_loss[r] = 0.f;
+                logz[r] = 0.f;
+            }
         }
     }
     if (threadIdx.x == 0) {
@@ -223,5 +269,57 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_l
         *tg.wmax = wm;
     }
 }
+
+// Whether a call's targets are made by a single block, which then also clears
+// the status word and the counters: one launch less where latency counts.  Each
+// of its 32 warps takes up to 32 labels, or two teacher lists.
+inline bool targets_in_one_block(const TargetIn& in) { return in.R <= (in.labels ? 1024 : 64); }
+
+namespace {
+
+// All rows' targets, then (the last block to finish) the list of counted rows.
+template <int kPer, bool kOneBlock>
+__global__ void __launch_bounds__(kOneBlock ? 1024 : 256)
+    k_targets(TargetIn in, Targets tg, float* row_loss, float* logz) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    dep_launch();
+    if (kOneBlock) {
+        if (threadIdx.x < 4) tg.done[threadIdx.x] = 0;
+        if (threadIdx.x == 0) *tg.status = 0;
+        __syncthreads();
+        for (int r = warp; r < in.R; r += 32) target_row<kPer>(in, tg, r, lane);
+        __syncthreads();
+    } else {
+        const int r = (int)(blockIdx.x * 8 + warp);
+        if (r < in.R) target_row<kPer>(in, tg, r, lane);
+        __shared__ int last;
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) last = atomicAdd(tg.done, 1) == (int)gridDim.x - 1;
+        __syncthreads();
+        if (!last) return;
+        __threadfence();
+    }
+    scan_rows(tg, in.R, row_loss, logz);
+}
+
+// `zero_bytes` of the workspace from its start (status word, counters) are
+// cleared, then the targets made.
+inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, float* row_loss,
+                                  float* logz, size_t zero_bytes, cudaStream_t st) {
+    const int per = in.labels || in.K <= 32 ? 1 : in.K <= 64 ? 2 : 4;
+    if (targets_in_one_block(in)) {
+        auto k = per == 1 ? k_targets<1, true> : per == 2 ? k_targets<2, true> : k_targets<4, true>;
+        k<<<1, 1024, 0, st>>>(in, tg, row_loss, logz);
+        return cudaGetLastError();
+    }
+    cudaError_t e = cudaMemsetAsync(tg.status, 0, zero_bytes, st);
+    if (e != cudaSuccess) return e;
+    auto k = per == 1 ? k_targets<1, false> : per == 2 ? k_targets<2, false> : k_targets<4, false>;
+    k<<<(unsigned)((in.R + 7) / 8), 256, 0, st>>>(in, tg, row_loss, logz);
+    return cudaGetLastError();
+}
+
+}  // namespace
 
 }  // namespace vsd
