@@ -22,6 +22,7 @@
 #include "vsd_launch.h"
 #include "vsd_loss.h"
 #include "vsd_pair.cuh"
+#include "vsd_rowloss.cuh"
 
 namespace vsd {
 namespace {
@@ -29,11 +30,12 @@ namespace {
 typedef __nv_bfloat16 bf16;
 
 constexpr int kRowPad = 256;     // the workspace's rows are a multiple of this
+constexpr int BK = 64;           // K block of the products
 constexpr int kPieceUnit = 256;  // a piece's columns are a multiple of this
 // Bytes of a piece's G: about the L2, so that the products read it from there.
 constexpr int64_t kPieceBytes = 128ll << 20;
 constexpr int64_t kKeepBytes = 64ll << 20;
-constexpr int64_t kPairsHint = 152;  // d_hidden jobs wanted: two for each pair of SMs
+constexpr int64_t kPairs = 76;  // pairs of SMs
 // The operand G is scaled so that the largest weight sits at the top of a
 // binade (1.984 ..), where bf16's relative rounding error is least: a row's
 // target entries are near -w before the draft has learned them, and they
@@ -71,11 +73,17 @@ LmWs lm_ws(const LmLossShape& s) {
     }
     w.piece = (int)(per * kPieceUnit);
     w.npiece = (int)((units + per - 1) / per);
-    // parts of a piece's columns in d_hidden: enough jobs for every pair, each
-    // of 8 K blocks at least
+    // parts of a piece's columns in d_hidden where its tiles are few: the count
+    // that leaves the pairs of SMs least idle, each part of 32 K blocks at least
     const int64_t tiles = (int64_t)(w.rpad / kRowPad) * ((s.H + kRowPad - 1) / kRowPad);
-    w.split = (int)std::max<int64_t>(1, std::min<int64_t>((kPairsHint + tiles - 1) / tiles,
-                                                          w.piece / 512));
+    w.split = 1;
+    if (tiles < 2 * kPairs) {
+        double best = 1e30;
+        for (int n = 1; n <= 32 && (n == 1 || w.piece / BK >= 32 * n); ++n) {
+            const double rounds = (double)((tiles * n + kPairs - 1) / kPairs) / n + 0.004 * n;
+            if (rounds < best) best = rounds, w.split = n;
+        }
+    }
     size_t o = 0;
     auto take = [&](size_t bytes) {
         const size_t at = o;
@@ -100,7 +108,7 @@ LmWs lm_ws(const LmLossShape& s) {
     w.coef = take(4 * (size_t)w.rpad);
     w.xk = take(4 * RK);
     w.tab = take(8 * (size_t)w.rpad * (size_t)units * 2);
-    w.part = take(8 * ((R + 31) / 32));
+    w.part = take(8 * R);
     w.hid = take(2 * (size_t)w.rpad * s.H);
     w.X = take(w.keep ? 4 * (size_t)w.rpad * w.piece : 0);
     w.G = take(grads ? 2 * (size_t)w.rpad * w.piece : 0);
@@ -115,21 +123,12 @@ template <typename U> U* at(void* ws, size_t off) {
 
 // ------------------------------------------------------------ rows
 // Counted rows of hidden, packed; the rows up to the next K block of d_weight
-// are zero.  Where every row counts the products read hidden itself.
-__global__ void k_gather(const bf16* hidden, int R, int H, Targets tg, bf16* hid) {
+// are zero (where every row counts the products read hidden itself).  Rows not
+// counted get a zero gradient.
+__global__ void __launch_bounds__(256) k_gather(RowGather g, int R, Targets tg) {
     dep_launch();
     dep_wait();
-    const int n = *tg.nrows;
-    if (n == R) return;
-    const int end = (n + 63) / 64 * 64;
-    const int vecs = H / 8;
-    for (int i = blockIdx.x; i < end; i += gridDim.x) {
-        uint4* dst = reinterpret_cast<uint4*>(hid + (size_t)i * H);
-        const uint4* src =
-            i < n ? reinterpret_cast<const uint4*>(hidden + (size_t)tg.rowmap[i] * H) : nullptr;
-        for (int v = threadIdx.x; v < vecs; v += blockDim.x)
-            dst[v] = src ? src[v] : make_uint4(0u, 0u, 0u, 0u);
-    }
+    gather_rows(g, R, tg, blockIdx.x, gridDim.x);
 }
 
 // ------------------------------------------------------------ products
@@ -143,7 +142,7 @@ __global__ void k_gather(const bf16* hidden, int R, int H, Targets tg, bf16* hid
 //              product is for:
 //     logits   A = hidden rows, B = weight rows, both K-major.  kStats: per row
 //              and half tile (max, sum 2^{(x - max) c}) and the target logits
-//              in it (kKeep: the logits too).  The tensor cores' running sum
+//              in it.  kKeep: the logits themselves, fp32.  The tensor cores' running sum
 //              truncates, an error that grows with the number of K steps, so
 //              K is summed in parts of 512 that are added up here in fp32
 //              (round to nearest).  kGrad: G, rounded to bf16.
@@ -156,7 +155,7 @@ __global__ void k_gather(const bf16* hidden, int R, int H, Targets tg, bf16* hid
 // in flight and frees its tensor memory.
 namespace tc = vsd_pair;
 
-constexpr int BT = 256, BK = 64;
+constexpr int BT = 256;
 constexpr int kEpiWarps = 8;
 constexpr int kPairThreads = 32 * (4 + kEpiWarps);  // three warpgroups
 constexpr int kHalfN = BT / 2;                 // columns of an epilogue warp
@@ -168,7 +167,14 @@ constexpr int kRegsFew = 40, kRegsMany = 232;
 static_assert(kRegsFew + 2 * kRegsMany <= 3 * 168, "the launch's registers");
 constexpr int kHalfBytes = 128 * BK * 2;       // one operand's half tile: 16 KB
 constexpr int kStageBytes = 2 * kHalfBytes;
-constexpr int kPairStages = 5;
+#ifndef PS
+#define PS 6
+#endif
+#ifndef PB
+#define PB 1
+#endif
+constexpr int kPairStages = PS;
+constexpr int kOutBufs = PB;  // staging buffers of an epilogue warp
 constexpr int kBoxBytes = 64 * BK * 2;         // an MN-major half is two 64-column boxes
 constexpr int kOutBytes = 4096;                // 32 rows x 128 bytes
 constexpr uint32_t kTmemAll = 2 * BT;
@@ -185,7 +191,7 @@ struct PairBars {
     int err;
 };
 constexpr size_t kPairSmem =
-    1024 + (size_t)kPairStages * kStageBytes + 2 * kEpiWarps * kOutBytes + sizeof(PairBars);
+    1024 + (size_t)kPairStages * kStageBytes + kOutBufs * kEpiWarps * kOutBytes + sizeof(PairBars);
 
 enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3 };
 
@@ -205,8 +211,11 @@ struct PairArgs {
     float2* tab;
     float* xk;
     const float *lse2, *coef, *kappa;
-    int split, first;      // d_hidden: parts of the piece's columns; first piece
+    int split;             // d_hidden: parts of the piece's columns
+    int first, last;       // first and last piece
     int want_dh, want_dw;
+    const float* dh;       // sums of the pieces so far, [split][rpad][H]
+    bf16* d_hidden;
 };
 
 struct Job {
@@ -218,10 +227,16 @@ struct Job {
 // tiles (the rows of a group stay in L2 while the weight streams by).
 // Products: the long d_hidden jobs first, dealt round; where they leave some
 // pairs one short, those take d_weight jobs of the same length before the rest
-// is dealt round.
+// is dealt round.  With few rows (kFewBlocks K blocks) d_hidden is bound by
+// reading the weight and d_weight by writing its gradient, so every other pair
+// takes its jobs in the opposite order: memory reads and writes at once (48 x
+// 128256 x 4096: FIG).
+constexpr int kFewBlocks = 8;
+constexpr int kStoreCost = 5;  // K blocks of time that storing a d_weight tile takes at least
 template <int MODE> struct Jobs {
     int i, c, C, mt, nt, total;
-    int dh, dw, kdh, kp, kr, r, L, fill, step;
+    int dh, dw, kdh, kp, kr, r, L, fill, step, left;
+    bool swap;
     __device__ Jobs(const PairArgs& a, int n_rows) {
         c = blockIdx.x >> 1;
         C = gridDim.x >> 1;
@@ -239,9 +254,12 @@ template <int MODE> struct Jobs {
         dh = a.want_dh ? mt * nt * a.split : 0;
         dw = a.want_dw ? (a.cols + BT - 1) / BT * nt : 0;
         r = dh % C;
-        L = r && kr ? (kdh + kr / 2) / kr : 0;
+        const int cost = max(kr, kStoreCost);
+        L = r ? (kdh + cost / 2) / cost : 0;
         fill = min(dw, (C - r) * L);
-        step = 0;
+        swap = kr <= kFewBlocks && (c & 1);
+        step = swap ? 1 : 0;
+        left = 3;
     }
     __device__ bool next(Job& j) {
         if (MODE != kProd) {
@@ -253,33 +271,27 @@ template <int MODE> struct Jobs {
             j = Job{0, (g * kGroupM + u % mg) * BT, u / mg * BT, 0, 0, 0};
             return true;
         }
-        if (step == 0) {
-            const int t = c + i * C;
-            if (t < dh) {
-                ++i;
-                const int s = t / (mt * nt), u = t - s * mt * nt;
-                j = Job{1, u % mt * BT, u / mt * BT, min(kp, s * kdh), min(kp, (s + 1) * kdh), s};
-                return true;
+        // steps 0: d_hidden, 1: the d_weight jobs in place of one, 2: the rest
+        for (; left; --left, step = step == 2 ? 0 : step + 1, i = 0) {
+            if (step == 0) {
+                const int t = c + i * C;
+                if (t < dh) {
+                    ++i;
+                    const int s = t / (mt * nt), u = t - s * mt * nt;
+                    j = Job{1, u % mt * BT, u / mt * BT, min(kp, s * kdh), min(kp, (s + 1) * kdh),
+                            s};
+                    return true;
+                }
+                continue;
             }
-            step = 1;
-            i = 0;
-        }
-        int t;
-        if (step == 1) {
-            t = (c - r) * L + i;
-            if (c >= r && i < L && t < fill) {
+            const int t = step == 1 ? (c - r) * L + i : fill + c + i * C;
+            if (step == 1 ? c >= r && i < L && t < fill : t < dw) {
                 ++i;
                 j = Job{2, t / nt * BT, t % nt * BT, 0, kr, 0};
                 return true;
             }
-            step = 2;
-            i = 0;
         }
-        t = fill + c + i * C;
-        if (t >= dw) return false;
-        ++i;
-        j = Job{2, t / nt * BT, t % nt * BT, 0, kr, 0};
-        return true;
+        return false;
     }
 };
 
@@ -339,17 +351,17 @@ struct Stage {
     unsigned char* buf;
     int use, lane;
     __device__ unsigned char* acquire() {
-        if (lane == 0) tc::bulk_wait_read<1>();  // the store before last has read its buffer
+        if (lane == 0) tc::bulk_wait_read<kOutBufs - 1>();  // its last store has read the buffer
         __syncwarp();
-        return buf + (use & 1) * kOutBytes;
+        return buf + use % kOutBufs * kOutBytes;
     }
     __device__ void store(const CUtensorMap* map, int x, int y, bool inside, bool add = false) {
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
             if (inside) {
-                if (add) tc::add_2d(map, x, y, buf + (use & 1) * kOutBytes);
-                else tc::store_2d(map, x, y, buf + (use & 1) * kOutBytes);
+                if (add) tc::add_2d(map, x, y, buf + use % kOutBufs * kOutBytes);
+                else tc::store_2d(map, x, y, buf + use % kOutBufs * kOutBytes);
             }
             tc::bulk_commit();
         }
@@ -363,10 +375,22 @@ __device__ __forceinline__ uint4* chunk_at(unsigned char* box, int lane, int j) 
 }
 
 // n0: the warp's first column of the piece; x: its row's 128 logits.
-template <bool KEEP>
-__device__ __forceinline__ void stats_tile(const PairArgs& a, const PairMaps& maps, int n0,
-                                           int row0, int lane, int n_rows, float (&x)[kHalfN],
-                                           Stage& out) {
+__device__ __forceinline__ void keep_tile(const PairMaps& maps, int n0, int row0, int lane,
+                                          int n_rows, const float (&x)[kHalfN], Stage& out) {
+#pragma unroll
+    for (int g = 0; g < kHalfN / 32; ++g) {
+        unsigned char* box = out.acquire();
+#pragma unroll
+        for (int v = 0; v < 8; ++v)
+            *chunk_at(box, lane, v) = make_uint4(
+                __float_as_uint(x[32 * g + 4 * v]), __float_as_uint(x[32 * g + 4 * v + 1]),
+                __float_as_uint(x[32 * g + 4 * v + 2]), __float_as_uint(x[32 * g + 4 * v + 3]));
+        out.store(&maps.o, n0 + 32 * g, row0, row0 < n_rows);
+    }
+}
+
+__device__ __forceinline__ void stats_tile(const PairArgs& a, int n0, int row0, int lane,
+                                           int n_rows, float (&x)[kHalfN], Stage& out) {
     const int row = row0 + lane;
     const bool on = row < n_rows;
     const int lim = a.cols - n0;
@@ -379,7 +403,7 @@ __device__ __forceinline__ void stats_tile(const PairArgs& a, const PairMaps& ma
 #pragma unroll
     for (int g = 0; g < kHalfN / 32; ++g) {
         const int end = min(lo + 32 * (g + 1), hi);
-        if (!KEEP && !__any_sync(0xffffffffu, id < end)) continue;
+        if (!__any_sync(0xffffffffu, id < end)) continue;
         unsigned char* box = out.acquire();
 #pragma unroll
         for (int v = 0; v < 8; ++v)
@@ -393,7 +417,6 @@ __device__ __forceinline__ void stats_tile(const PairArgs& a, const PairMaps& ma
             ++k;
             id = k < list.n ? __ldg(list.id + k) : hi;
         }
-        if (KEEP) out.store(&maps.o, n0 + 32 * g, row0, row0 < n_rows);
     }
     if (lim < kHalfN) {
 #pragma unroll
@@ -456,10 +479,49 @@ __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& map
     }
 }
 
+// d_hidden in one part and the last piece: the earlier pieces' sums are added
+// here, rounded once and stored in the caller's row.
+__device__ __forceinline__ void dh_last_tile(const PairArgs& a, bool none, int n0, int row,
+                                             int n_rows, uint32_t taddr) {
+    const bool on = row < n_rows;
+    const float s = none ? 0.f : __ldg(a.kappa);
+    const float* part = a.dh + (size_t)row * a.H;
+    bf16* o = a.d_hidden + (size_t)(on ? __ldg(a.tg.rowmap + row) : 0) * a.H;
+#pragma unroll 1
+    for (int g = 0; g < kHalfN / 32; ++g) {
+        uint32_t u[32];
+        tc::tmem_ld32(taddr + 32u * g, u);
+        const int x = n0 + 32 * g;
+        if (!on) continue;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            if (x + 8 * v >= a.H) break;
+            float f[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = none ? 0.f : __uint_as_float(u[8 * v + i]);
+            if (!a.first) {
+                const float4* q = reinterpret_cast<const float4*>(part + x + 8 * v);
+                const float4 y = ld_cg(q), z = ld_cg(q + 1);
+                f[0] += y.x; f[1] += y.y; f[2] += y.z; f[3] += y.w;
+                f[4] += z.x; f[5] += z.y; f[6] += z.z; f[7] += z.w;
+            }
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[i] = tc::pack_bf16(__float_as_uint(s * f[2 * i]), __float_as_uint(s * f[2 * i + 1]));
+            *reinterpret_cast<uint4*>(o + x + 8 * v) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+}
+
 __device__ __forceinline__ void dh_tile(const PairArgs& a, const PairMaps& maps, const Job& j,
                                         int n0, int row0, int lane, int n_rows, uint32_t taddr,
                                         Stage& out) {
     const bool none = j.kb0 == j.kb1;
+    if (a.last && a.split == 1) {
+        dh_last_tile(a, none, n0, row0 + lane, n_rows, taddr);
+        return;
+    }
     if (none && !a.first) return;  // nothing to add
 #pragma unroll 1
     for (int g = 0; g < kHalfN / 32; ++g) {
@@ -514,7 +576,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     extern __shared__ unsigned char dsm_raw[];
     unsigned char* dsm = dsm_raw + ((1024u - (smem_u32(dsm_raw) & 1023u)) & 1023u);
     unsigned char* outs = dsm + kPairStages * kStageBytes;
-    PairBars* sb = reinterpret_cast<PairBars*>(outs + 2 * kEpiWarps * kOutBytes);
+    PairBars* sb = reinterpret_cast<PairBars*>(outs + kOutBufs * kEpiWarps * kOutBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)tc::cluster_rank();
     int* status = a.tg.status;
@@ -597,13 +659,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         give_registers<kParts>();
         // ------------------------------------------------------ MMA issuer
         if (lane == 0 && rank == 0) {
+            const uint32_t ring = smem_u32(dsm);
             uint32_t it = 0;
             int lt = 0;
             bool ok = true;
             while (ok && !*(volatile int*)&sb->err && jobs.next(j)) {
-                const bool amn = MODE == kProd && j.kind == 2, bmn = MODE == kProd;
+                const bool amn = MODE == kProd && j.kind == 2;
+                constexpr bool bmn = MODE == kProd;
                 const uint32_t idesc = tc::idesc_bf16(256, BT) | (amn ? 1u << 15 : 0u) |
                                        (bmn ? 1u << 16 : 0u);
+                // descriptors of stage 0; a stage and a K step add to the address
+                // field (16-byte units), which never carries out of it
+                const uint64_t a0 = amn ? tc::desc_mn(ring, kBoxBytes) : tc::sdesc_sw128(ring);
+                const uint64_t b0 = bmn ? tc::desc_mn(ring + kHalfBytes, kBoxBytes)
+                                        : tc::sdesc_sw128(ring + kHalfBytes);
+                const uint32_t ka = amn ? 2048u >> 4 : 32u >> 4;
+                constexpr uint32_t kbs = bmn ? 2048u >> 4 : 32u >> 4;
+                const uint32_t alo = (uint32_t)a0, ahi = (uint32_t)(a0 >> 32);
+                const uint32_t blo = (uint32_t)b0, bhi = (uint32_t)(b0 >> 32);
                 const int kb1 = MODE == kProd ? j.kb1 : a.nkh;
                 int kb = j.kb0;
                 do {  // (a job without K blocks hands on its accumulator unread)
@@ -624,15 +697,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                             break;
                         }
                         tc::tc_fence_after();
-                        const uint32_t A = smem_u32(dsm + s * kStageBytes), B = A + kHalfBytes;
+                        const uint32_t at = (uint32_t)s * (kStageBytes >> 4);
 #pragma unroll
                         for (int k = 0; k < BK / 16; ++k) {
-                            tc::mma_pair(d,
-                                         amn ? tc::desc_mn(A + 2048u * k, kBoxBytes)
-                                             : tc::sdesc_sw128(A + 32u * k),
-                                         bmn ? tc::desc_mn(B + 2048u * k, kBoxBytes)
-                                             : tc::sdesc_sw128(B + 32u * k),
-                                         idesc, more);
+                            tc::mma_pair(d, (uint64_t)ahi << 32 | (alo + at + ka * k),
+                                         (uint64_t)bhi << 32 | (blo + at + kbs * k), idesc, more);
                             more = 1;
                         }
                         tc::commit_pair(&sb->empty[s]);
@@ -653,7 +722,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         if (kParts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kRegsMany));
         const int q = warp & 3;               // TMEM lanes 32q .. 32q + 31
         const int h0 = (warp - 4) / 4 * kHalfN;  // its columns of the tile
-        Stage out{outs + (warp - 4) * 2 * kOutBytes, 0, lane};
+        Stage out{outs + (warp - 4) * kOutBufs * kOutBytes, 0, lane};
         const uint32_t empty = tc::leader_addr(&sb->acc_empty[0]);
         int lt = 0;
         auto ready = [&]() {
@@ -691,7 +760,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     release();
                 }
                 if (!ok) break;
-                stats_tile<MODE == kKeep>(a, maps, n0, row0, lane, n_rows, x, out);
+                if (MODE == kKeep) keep_tile(maps, n0, row0, lane, n_rows, x, out);
+                else stats_tile(a, n0, row0, lane, n_rows, x, out);
             } else {
                 if (!ready()) break;
                 const uint32_t t = acc_addr();
@@ -713,66 +783,73 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     }
 }
 
-// 32 counted rows per block: log-partition, loss and gradient coefficient.  The
-// warps share out the row's parts (a lane per row, so the reads coalesce), then
-// the rows' target lists.  The blocks' weighted losses are added in block order
+// RB counted rows per block, 256 / RB threads each: log-partition, loss and
+// gradient coefficient.  A thread takes every (256 / RB)-th part and list entry
+// of its row (consecutive threads: consecutive rows, so the reads coalesce
+// where there are many).  The blocks' weighted losses are added in block order
 // by the last block to finish.
+template <int RB>
 __global__ void __launch_bounds__(256)
     k_rows(const float2* tab, int ntab, int64_t stride, Targets tg, int K, float c, float T,
            float grad_scale, const float* xk, float* lse2, float* coef, float* kappa,
            float* row_loss, float* logz, double* part, float* loss) {
-    __shared__ float2 ms[8][32];
-    __shared__ double dots[32], wl[32];
+    constexpr int P = 256 / RB;
+    __shared__ float2 ms[8][RB];
+    __shared__ double dots[8][RB], wl[8];
     __shared__ int last;
     dep_launch();
     dep_wait();
     const int n_rows = *(const volatile int*)tg.nrows;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int i0 = blockIdx.x * 32, i = i0 + lane;
-    if (i0 < n_rows) {
+    const int q = threadIdx.x % RB, pt = threadIdx.x / RB;
+    const int i = blockIdx.x * RB + q;
+    const bool on = i < n_rows;
+    const double wsum = *tg.wsum;
+    const float wm = *tg.wmax;
+    if (blockIdx.x * RB < n_rows) {
         float m = -INFINITY, s = 0.f;
-        if (i < n_rows) {
-            for (int t = warp; t < ntab; t += 32) {  // (four parts' loads at a time)
-                float2 e[4];
+        double dot = 0.0;
+        const int r = on ? tg.rowmap[i] : 0;
+        auto join = [&](const float2* e, int n) {
+            float nm = m;
+            for (int u = 0; u < n; ++u) nm = fmaxf(nm, e[u].x);
+            const float z = nm > -INFINITY ? nm : 0.f;
+            s *= ex2((m - z) * c);
+            for (int u = 0; u < n; ++u) s += e[u].y * ex2((e[u].x - z) * c);
+            m = nm;
+        };
+        const int n = on ? tg.n[r] : 0;
+        const float plogp = on ? tg.plogp[r] : 0.f, w = on ? tg.w[r] : 0.f;
+        if (on)
+            for (int t = pt; t < ntab; t += 8 * P) {  // (eight parts' loads at a time)
+                float2 e[8];
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
-                    e[u] = t + 8 * u < ntab ? ld_cg(tab + (t + 8 * u) * stride + i)
+                for (int u = 0; u < 8; ++u)
+                    e[u] = t + u * P < ntab ? ld_cg(tab + (t + u * P) * stride + i)
                                             : make_float2(-INFINITY, 0.f);
-                const float nm =
-                    fmaxf(fmaxf(fmaxf(e[0].x, e[1].x), fmaxf(e[2].x, e[3].x)), m);
-                const float z = nm > -INFINITY ? nm : 0.f;
-                s *= ex2((m - z) * c);
+                join(e, 8);
+            }
+        for (int k = pt; k < n; k += P)
+            dot += (double)tg.p[(size_t)r * K + k] * (double)xk[(size_t)i * K + k];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) s += e[u].y * ex2((e[u].x - z) * c);
-                m = nm;
-            }
+        for (int o = RB; o < 32; o <<= 1) {
+            const float2 e = make_float2(__shfl_xor_sync(0xffffffffu, m, o),
+                                         __shfl_xor_sync(0xffffffffu, s, o));
+            join(&e, 1);
+            dot += __shfl_xor_sync(0xffffffffu, dot, o);
         }
-        ms[warp][lane] = make_float2(m, s);
-        for (int q = warp * 4; q < warp * 4 + 4; ++q) {
-            double dot = 0.0;
-            if (i0 + q < n_rows) {
-                const int r = tg.rowmap[i0 + q], n = tg.n[r];
-                for (int k = lane; k < n; k += 32)
-                    dot += (double)tg.p[(size_t)r * K + k] *
-                           (double)xk[(size_t)(i0 + q) * K + k];
-            }
-            dot = warp_sum(dot);
-            if (lane == 0) dots[q] = dot;
-        }
+        if (lane < RB) ms[warp][q] = make_float2(m, s), dots[warp][q] = dot;
         __syncthreads();
         if (warp == 0) {
             double wloss = 0.0;
-            if (i < n_rows) {
-                m = ms[0][lane].x;
-                for (int w = 1; w < 8; ++w) m = fmaxf(m, ms[w][lane].x);
-                const float z = m > -INFINITY ? m : 0.f;
-                s = 0.f;
-                for (int w = 0; w < 8; ++w) s += ms[w][lane].y * ex2((ms[w][lane].x - z) * c);
-                const int r = tg.rowmap[i];
-                const double lz = (double)m / (double)T + log((double)s);
+            if (lane < RB && on) {
+                float2 e[7];
+#pragma unroll
+                for (int u = 1; u < 8; ++u) e[u - 1] = ms[u][q], dot += dots[u][q];
+                join(e, 7);
+                const double lz = (double)m / (double)T + (double)logf(s);
                 if (!isfinite(lz)) atomicOr(tg.status, VSD_STATUS_BAD_ROW);
-                const float rl = (float)((double)tg.plogp[r] + lz - dots[lane] / (double)T);
-                const float w = tg.w[r], wm = *tg.wmax;
+                const float rl = (float)((double)plogp + lz - dot / (double)T);
                 logz[r] = (float)lz;
                 row_loss[r] = rl;
                 lse2[i] = (float)(lz * kLog2e);
@@ -785,68 +862,28 @@ __global__ void __launch_bounds__(256)
     }
     if (threadIdx.x == 0) {
         __threadfence();
-        last = atomicAdd(tg.done + 1, 1) == (int)gridDim.x - 1;
+        last = gridDim.x == 1 || atomicAdd(tg.done + 1, 1) == (int)gridDim.x - 1;
     }
     __syncthreads();
     if (!last) return;
     __threadfence();
-    const int nb = (n_rows + 31) / 32;
+    const int nb = (n_rows + RB - 1) / RB;
     double sum = 0.0;
-    for (int b = threadIdx.x; b < nb; b += blockDim.x) sum += ld_cg(part + b);
+    for (int b = threadIdx.x; b < nb; b += 256) sum += ld_cg(part + b);
     sum = warp_sum(sum);
     if (lane == 0) wl[warp] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         sum = 0.0;
-        for (int w = 0; w < 8; ++w) sum += wl[w];
-        *loss = (float)(sum / *tg.wsum);
-        *kappa = (float)((double)grad_scale * (double)*tg.wmax /
-                         ((double)kTopMantissa * *tg.wsum * (double)T));
+        for (int u = 0; u < 8; ++u) sum += wl[u];
+        *loss = (float)(sum / wsum);
+        *kappa = (float)((double)grad_scale * (double)wm /
+                         ((double)kTopMantissa * wsum * (double)T));
     }
 }
 
-// G from logits that were kept, 2048 columns of a row per block; rows up to the
-// next K block of d_weight and columns up to ldg are written, zero where there
-// is no logit.
-constexpr int kMakeCols = 2048;
-__global__ void __launch_bounds__(256)
-    k_make_g(const float* X, int64_t ldx, int V, int K, Targets tg, float c, const float* lse2,
-             const float* coef, const float* xk, bf16* G, int64_t ldg) {
-    dep_launch();
-    dep_wait();
-    const int i = blockIdx.y, n_rows = *tg.nrows;
-    if (i >= (n_rows + BK - 1) / BK * BK) return;
-    const int c0 = blockIdx.x * kMakeCols, v = c0 + threadIdx.x * 8;
-    bf16* g = G + (size_t)i * ldg;
-    const bool on = i < n_rows;
-    const float a = on ? coef[i] : 0.f, l = on ? lse2[i] : 0.f;
-    if (v < ldg) {
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (on && v < V) {  // (ldx is a multiple of 256: the loads stay in the row)
-            const float4* x = reinterpret_cast<const float4*>(X + (size_t)i * ldx + v);
-            const float4 x0 = x[0], x1 = x[1];
-            const float f[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float lo = v + 2 * e < V ? a * ex2(fmaf(f[2 * e], c, -l)) : 0.f;
-                const float hi = v + 2 * e + 1 < V ? a * ex2(fmaf(f[2 * e + 1], c, -l)) : 0.f;
-                w[e] = tc::pack_bf16(__float_as_uint(lo), __float_as_uint(hi));
-            }
-        }
-        *reinterpret_cast<uint4*>(g + v) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    if (!on) return;
-    __syncthreads();
-    const int r = tg.rowmap[i], n = tg.n[r];
-    const int32_t* id = tg.id + (size_t)r * K;
-    for (int k = threadIdx.x; k < n; k += blockDim.x)
-        if (id[k] >= c0 && id[k] < c0 + kMakeCols)
-            g[id[k]] = __float2bfloat16_rn(
-                a * (ex2(fmaf(xk[(size_t)i * K + k], c, -l)) - tg.p[(size_t)r * K + k]));
-}
-
-// d_hidden in the caller's rows: the parts added in order, one rounding, zero
-// in rows not counted.
+// d_hidden of several parts, in the caller's rows: the parts added in order,
+// one rounding (rows not counted are zero already).
 __global__ void k_dh_out(const float* dh, int split, int64_t rpad, int H, Targets tg,
                          const float* kappa, bf16* out) {
     dep_launch();
@@ -855,8 +892,8 @@ __global__ void k_dh_out(const float* dh, int split, int64_t rpad, int H, Target
     const float s = *kappa;
     for (int h = (blockIdx.y * blockDim.x + threadIdx.x) * 8; h < H;
          h += gridDim.y * blockDim.x * 8) {
-        uint4 w = make_uint4(0u, 0u, 0u, 0u);
         if (i >= 0) {
+            uint4 w;
             float f[8] = {};
 #pragma unroll 4
             for (int q = 0; q < split; ++q) {
@@ -870,8 +907,8 @@ __global__ void k_dh_out(const float* dh, int split, int64_t rpad, int H, Target
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 o[e] = tc::pack_bf16(__float_as_uint(s * f[2 * e]), __float_as_uint(s * f[2 * e + 1]));
+            *reinterpret_cast<uint4*>(out + (size_t)r * H + h) = w;
         }
-        *reinterpret_cast<uint4*>(out + (size_t)r * H + h) = w;
     }
 }
 
@@ -922,7 +959,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
               make_map_sw128(&maps.a0, hidden, false, R, H, H, 128) &&
               make_map_sw128(&maps.b, weight, false, V, H, H, 128);
     if (grads)
-        ok = ok && make_map_sw128(&maps.gk, G, false, w.rpad, w.piece, w.piece, 128) &&
+        ok = ok && make_map_sw128(&maps.gk, G, false, hrows, w.piece, w.piece, 128) &&
              make_map_sw128(&maps.gt, G, false, w.rpad, w.piece, w.piece, BK) &&
              make_map_sw128(&maps.wt, weight, false, V, H, H, BK) &&
              make_map_sw128(&maps.ht, hid, false, hrows, H, H, BK) &&
@@ -953,38 +990,60 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     a.split = w.split;
     a.want_dh = s.dh;
     a.want_dw = s.dw;
+    a.dh = dh;
+    a.d_hidden = static_cast<bf16*>(out.d_hidden);
 
-    cudaError_t e = launch_targets(in, tg, out.row_loss, out.logz, w.zero_end, st);
-    if (e != cudaSuccess) return e;
-    e = launch_dep(k_gather, dim3((unsigned)std::min<int64_t>(hrows, 4 * device_sm_count())), 256,
-                   0, 1, st, static_cast<const bf16*>(hidden), R, H, tg, hid);
+    const RowGather rg{static_cast<const bf16*>(hidden), hid, static_cast<bf16*>(out.d_hidden), H};
+    const bool inline_gather = targets_in_one_block(in) && hrows * H <= kInlineGather;
+    cudaError_t e = launch_targets(in, tg, out.row_loss, out.logz, w.zero_end, st,
+                                   inline_gather ? rg : RowGather{});
+    if (e == cudaSuccess && !inline_gather)
+        e = launch_dep(k_gather, dim3((unsigned)std::min<int64_t>(hrows, 4 * device_sm_count())),
+                       256, 0, 1, st, rg, R, tg);
     if (e != cudaSuccess) return e;
     const int64_t mt = w.rpad / kRowPad, units = (V + kPieceUnit - 1) / kPieceUnit;
     const int64_t ht = (H + BT - 1) / BT;
     e = w.keep ? launch_pair<kKeep>(maps, a, mt * units, st)
                : launch_pair<kStats>(maps, a, mt * units, st);
     if (e != cudaSuccess) return e;
-    e = launch_dep(k_rows, dim3((unsigned)((R + 31) / 32)), 256, 0, 1, st, tab, (int)(2 * units),
-                   (int64_t)w.rpad, tg, K, c, T, grad_scale, xk, lse2, coef, kappa, out.row_loss,
-                   out.logz, at<double>(ws, w.part), out.loss);
+    if (w.keep) {  // losses and G from the kept logits, a row at a time
+        RowArgs ra{};
+        ra.tg = tg;
+        ra.rows = R;
+        ra.V = V;
+        ra.K = K;
+        ra.ldx = ra.ldg = w.piece;
+        ra.gcols = w.piece;
+        ra.c = c;
+        ra.T = T;
+        ra.grad_scale = grad_scale;
+        ra.row_loss = out.row_loss;
+        ra.logz = out.logz;
+        ra.loss = out.loss;
+        ra.kappa = kappa;
+        ra.same_align = true;
+        e = launch_row_loss<float, bf16, true>(X, G, ra, hrows, kTopMantissa, device_sm_count(),
+                                               ensure_dyn_smem, st);
+    } else {
+        // one row per block while that fills the GPU no more than a few times over
+        const int rb = R <= 1024 ? 1 : R <= 16384 ? 8 : 32;
+        e = launch_dep(rb == 1 ? k_rows<1> : rb == 8 ? k_rows<8> : k_rows<32>,
+                       dim3((unsigned)((R + rb - 1) / rb)), 256, 0, 1, st, tab, (int)(2 * units),
+                       (int64_t)w.rpad, tg, K, c, T, grad_scale, xk, lse2, coef, kappa,
+                       out.row_loss, out.logz, at<double>(ws, w.part), out.loss);
+    }
     if (e != cudaSuccess || !grads) return e;
     for (int q = 0; q < w.npiece; ++q) {
         a.v0 = q * w.piece;
         a.cols = std::min(w.piece, V - a.v0);
         a.first = q == 0;
+        a.last = q == w.npiece - 1;
         const int64_t nu = (a.cols + kPieceUnit - 1) / kPieceUnit;
-        if (w.keep) {
-            const dim3 grid((unsigned)((w.piece + kMakeCols - 1) / kMakeCols), (unsigned)hrows);
-            e = launch_dep(k_make_g, grid, 256, 0, 1, st, X, (int64_t)w.piece, V, K, tg, c, lse2,
-                           coef, xk, G, (int64_t)w.piece);
-        } else {
-            e = launch_pair<kGrad>(maps, a, mt * nu, st);
-        }
-        if (e != cudaSuccess) return e;
+        if (!w.keep && (e = launch_pair<kGrad>(maps, a, mt * nu, st)) != cudaSuccess) return e;
         e = launch_pair<kProd>(maps, a, (s.dh ? mt * ht * w.split : 0) + (s.dw ? nu * ht : 0), st);
         if (e != cudaSuccess) return e;
     }
-    if (s.dh) {
+    if (s.dh && w.split > 1) {
         const unsigned y = (unsigned)std::min<int64_t>(((int64_t)H + 2047) / 2048, 16);
         e = launch_dep(k_dh_out, dim3((unsigned)R, y), 256, 0, 1, st, dh, w.split, (int64_t)w.rpad,
                        H, tg, kappa, static_cast<bf16*>(out.d_hidden));

@@ -270,6 +270,39 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_l
     }
 }
 
+// Rows packed for the LM-head losses: counted rows of hidden [R][H], in order,
+// then zero rows up to a multiple of 64; rows not counted get a zero gradient.
+// Nothing is packed where every row counts.
+struct RowGather {
+    const __nv_bfloat16* hidden;  // null: nothing to do
+    __nv_bfloat16* packed;
+    __nv_bfloat16* d_hidden;      // may be null
+    int H;                        // a multiple of 8
+};
+// One block's share of the rows.
+__device__ __forceinline__ void gather_rows(const RowGather& g, int R, const Targets& tg,
+                                            int block, int blocks) {
+    const int n = *(const volatile int*)tg.nrows;
+    if (n == R) return;
+    const int vecs = g.H / 8;
+    const int64_t step = (int64_t)blocks * blockDim.x, t0 = (int64_t)block * blockDim.x + threadIdx.x;
+    const int64_t end = (int64_t)((n + 63) / 64 * 64) * vecs;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 4
+    for (int64_t t = t0; t < end; t += step) {
+        const int i = (int)(t / vecs), v = (int)(t - (int64_t)i * vecs);
+        reinterpret_cast<uint4*>(g.packed)[t] =
+            i < n ? __ldg(reinterpret_cast<const uint4*>(
+                              g.hidden + (size_t)ld_cg(tg.rowmap + i) * g.H) + v)
+                  : zero;
+    }
+    if (!g.d_hidden) return;
+    for (int64_t t = t0; t < (int64_t)R * vecs; t += step)
+        if (ld_cg(tg.rowinv + (int)(t / vecs)) < 0) reinterpret_cast<uint4*>(g.d_hidden)[t] = zero;
+}
+// Elements up to which the block that makes the targets packs the rows too.
+constexpr int64_t kInlineGather = 32768;
+
 // Whether a call's targets are made by a single block, which then also clears
 // the status word and the counters: one launch less where latency counts.  Each
 // of its 32 warps takes up to 32 labels, or two teacher lists.
@@ -280,7 +313,7 @@ namespace {
 // All rows' targets, then (the last block to finish) the list of counted rows.
 template <int kPer, bool kOneBlock>
 __global__ void __launch_bounds__(kOneBlock ? 1024 : 256)
-    k_targets(TargetIn in, Targets tg, float* row_loss, float* logz) {
+    k_targets(TargetIn in, Targets tg, float* row_loss, float* logz, RowGather g) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     dep_launch();
     if (kOneBlock) {
@@ -301,22 +334,27 @@ __global__ void __launch_bounds__(kOneBlock ? 1024 : 256)
         __threadfence();
     }
     scan_rows(tg, in.R, row_loss, logz);
+    if (kOneBlock && g.hidden) {
+        __syncthreads();
+        gather_rows(g, in.R, tg, 0, 1);
+    }
 }
 
 // `zero_bytes` of the workspace from its start (status word, counters) are
 // cleared, then the targets made.
 inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, float* row_loss,
-                                  float* logz, size_t zero_bytes, cudaStream_t st) {
+                                  float* logz, size_t zero_bytes, cudaStream_t st,
+                                  const RowGather& g = RowGather{}) {
     const int per = in.labels || in.K <= 32 ? 1 : in.K <= 64 ? 2 : 4;
     if (targets_in_one_block(in)) {
         auto k = per == 1 ? k_targets<1, true> : per == 2 ? k_targets<2, true> : k_targets<4, true>;
-        k<<<1, 1024, 0, st>>>(in, tg, row_loss, logz);
+        k<<<1, 1024, 0, st>>>(in, tg, row_loss, logz, g);
         return cudaGetLastError();
     }
     cudaError_t e = cudaMemsetAsync(tg.status, 0, zero_bytes, st);
     if (e != cudaSuccess) return e;
     auto k = per == 1 ? k_targets<1, false> : per == 2 ? k_targets<2, false> : k_targets<4, false>;
-    k<<<(unsigned)((in.R + 7) / 8), 256, 0, st>>>(in, tg, row_loss, logz);
+    k<<<(unsigned)((in.R + 7) / 8), 256, 0, st>>>(in, tg, row_loss, logz, g);
     return cudaGetLastError();
 }
 
