@@ -12,6 +12,7 @@
 // them into G (bf16) and adds the piece's products.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <limits.h>
 #include <stdint.h>
 
 #include <algorithm>
@@ -46,7 +47,7 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct LmWs {
-    size_t status, done, zero_end, nrows, wsum, wmax, kappa, n, id, p, plogp, w, rowmap, rowinv,
+    size_t status, done, zero_end, nrows, wsum, wmax, kappa, share, n, id, p, plogp, w, rowmap, rowinv,
         lse2, coef, xk, tab, part, hid, X, G, dh, total;
     int rpad, piece, npiece, split;
     bool keep;  // the logits are kept (one piece)
@@ -97,6 +98,7 @@ LmWs lm_ws(const LmLossShape& s) {
     w.wsum = take(8);
     w.wmax = take(4);
     w.kappa = take(4);
+    w.share = take(4);
     w.n = take(4 * R);
     w.id = take(4 * RK);
     w.p = take(4 * RK);
@@ -149,15 +151,14 @@ __global__ void __launch_bounds__(256) k_gather(RowGather g, int R, Targets tg) 
 //     d_hidden A = G (K-major), B = weight (MN-major, as it lies): fp32 sums,
 //              added up over the pieces of the vocabulary by TMA.
 //     d_weight A = G (MN-major), B = hidden (MN-major): one rounding to bf16.
-// What is stored goes through 4 KB of swizzled shared memory per warp (double
-// buffered) and a TMA store.  Every wait is bounded: one that runs out sets
+// What is stored goes through 4 KB of swizzled shared memory per warp and a TMA
+// store.  Every wait is bounded: one that runs out sets
 // VSD_STATUS_TIMEOUT, and the pair winds down, waits for its copies and MMAs
 // in flight and frees its tensor memory.
 namespace tc = vsd_pair;
 
 constexpr int BT = 256;
-constexpr int kEpiWarps = 8;
-constexpr int kPairThreads = 32 * (4 + kEpiWarps);  // three warpgroups
+constexpr int kTileWarps = 8;                  // epilogue warps of a tile
 constexpr int kHalfN = BT / 2;                 // columns of an epilogue warp
 constexpr int kSumBlocks = 8;                  // K blocks of a partial sum of the logits
 // Registers per thread of the kernels that add partial sums: launched with 168,
@@ -166,34 +167,45 @@ constexpr int kSumBlocks = 8;                  // K blocks of a partial sum of t
 constexpr int kRegsFew = 40, kRegsMany = 232;
 static_assert(kRegsFew + 2 * kRegsMany <= 3 * 168, "the launch's registers");
 constexpr int kHalfBytes = 128 * BK * 2;       // one operand's half tile: 16 KB
-constexpr int kStageBytes = 2 * kHalfBytes;
-#ifndef PS
-#define PS 6
-#endif
-#ifndef PB
-#define PB 1
-#endif
-constexpr int kPairStages = PS;
-constexpr int kOutBufs = PB;  // staging buffers of an epilogue warp
 constexpr int kBoxBytes = 64 * BK * 2;         // an MN-major half is two 64-column boxes
 constexpr int kOutBytes = 4096;                // 32 rows x 128 bytes
+constexpr int kMaxStages = 9;
 constexpr uint32_t kTmemAll = 2 * BT;
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr int kGroupM = 16;                    // M tiles that share B tiles in L2
 
 struct PairBars {
-    uint64_t full[kPairStages];   // leader: both CTAs' bytes landed
-    uint64_t empty[kPairStages];  // the MMAs reading the stage are done
+    uint64_t full[kMaxStages];    // leader: both CTAs' bytes landed
+    uint64_t empty[kMaxStages];   // the MMAs reading the stage are done
     uint64_t acc_full[2];
     uint64_t acc_empty[2];        // leader: the epilogue warps of both CTAs
     uint64_t drain;
     uint32_t tmem_base;
     int err;
 };
-constexpr size_t kPairSmem =
-    1024 + (size_t)kPairStages * kStageBytes + kOutBufs * kEpiWarps * kOutBytes + sizeof(PairBars);
-
 enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3 };
+
+// Few rows (NF = 64 or 128 at most): the products with the rows' side are turned
+// round, so that the weight's side is the 256-wide M of the tile and the rows
+// are its N, and no part of the tile is empty:
+//     logits^T  A = weight rows (K-major), B = hidden rows (K-major)
+//     d_hidden^T  A = weight (MN-major, M = hidden size), B = G rows (K-major)
+// What the tile costs then is bringing the weight in.  NF = 0: rows are M.
+template <int MODE, int NF> struct PairCfg {
+    static constexpr bool kFew = NF > 0;
+    // the products' epilogues (store 64 KB per SM) take as long as eight K
+    // blocks: two sets of warps, one for each accumulator
+    static constexpr int kSets = MODE == kProd ? 2 : 1;
+    static constexpr int kThreads = 32 * (4 + kSets * kTileWarps);
+    static constexpr int kFewB = NF / 2 * BK * 2;  // the rows' half of a turned stage
+    static constexpr int kStageBytes = MODE == kKeep && kFew ? kHalfBytes + kFewB : 2 * kHalfBytes;
+    static constexpr int kStages =
+        MODE == kKeep && kFew ? (NF == 64 ? 9 : 8) : MODE == kProd ? 5 : 6;
+    static constexpr size_t kSmem =
+        1024 + (size_t)kStages * kStageBytes + kSets * kTileWarps * kOutBytes +
+        sizeof(PairBars);
+    static_assert(kStages <= kMaxStages && kSmem <= 232448, "shared memory");
+};
 
 struct PairMaps {
     CUtensorMap a, a0, b, o;         // logits: packed rows, hidden, weight; stored tiles
@@ -214,8 +226,12 @@ struct PairArgs {
     int split;             // d_hidden: parts of the piece's columns
     int first, last;       // first and last piece
     int want_dh, want_dw;
-    const float* dh;       // sums of the pieces so far, [split][rpad][H]
-    bf16* d_hidden;
+    float* dh;             // sums of the pieces so far, [split][rpad][H]
+    const float* row_loss; // for the mean, written by the first product that has `loss`
+    float* loss;
+    float* X;              // kept logits
+    int64_t ldx;
+    bf16 *d_hidden, *d_weight;
 };
 
 struct Job {
@@ -233,7 +249,7 @@ struct Job {
 // 128256 x 4096: FIG).
 constexpr int kFewBlocks = 8;
 constexpr int kStoreCost = 5;  // K blocks of time that storing a d_weight tile takes at least
-template <int MODE> struct Jobs {
+template <int MODE, bool FEW> struct Jobs {
     int i, c, C, mt, nt, total;
     int dh, dw, kdh, kp, kr, r, L, fill, step, left;
     bool swap;
@@ -244,7 +260,7 @@ template <int MODE> struct Jobs {
         mt = (n_rows + BT - 1) / BT;
         if (MODE != kProd) {
             nt = (a.cols + BT - 1) / BT;
-            total = mt * nt;
+            total = mt * nt;  // (few rows: mt is 1, or 0 where no row counts)
             return;
         }
         nt = (a.H + BT - 1) / BT;
@@ -266,6 +282,10 @@ template <int MODE> struct Jobs {
             const int t = c + i * C;
             if (t >= total) return false;
             ++i;
+            if (FEW) {
+                j = Job{0, t * BT, 0, 0, 0, 0};
+                return true;
+            }
             const int g = t / (kGroupM * nt), u = t - g * kGroupM * nt;
             const int mg = min(kGroupM, mt - g * kGroupM);
             j = Job{0, (g * kGroupM + u % mg) * BT, u / mg * BT, 0, 0, 0};
@@ -278,8 +298,8 @@ template <int MODE> struct Jobs {
                 if (t < dh) {
                     ++i;
                     const int s = t / (mt * nt), u = t - s * mt * nt;
-                    j = Job{1, u % mt * BT, u / mt * BT, min(kp, s * kdh), min(kp, (s + 1) * kdh),
-                            s};
+                    j = Job{1, (FEW ? u : u % mt) * BT, FEW ? 0 : u / mt * BT, min(kp, s * kdh),
+                            min(kp, (s + 1) * kdh), s};
                     return true;
                 }
                 continue;
@@ -325,16 +345,19 @@ __device__ __forceinline__ int lower_bound(const int32_t* id, int n, int v) {
     return lo;
 }
 
-// A row's target list, for one epilogue thread.
+// A row's target list, for one epilogue thread: entry k is the first from token
+// `lo` on, next its token.  (Made before the tile's accumulator is waited for.)
 struct RowList {
     const int32_t* id;
     const float* p;
-    int n;
-    __device__ RowList(const PairArgs& a, int row, bool on) {
+    int n, k, next;
+    __device__ RowList(const PairArgs& a, int row, bool on, int lo) {
         const int r = on ? __ldg(a.tg.rowmap + row) : 0;
         id = a.tg.id + (size_t)r * a.K;
         p = a.tg.p + (size_t)r * a.K;
         n = on ? __ldg(a.tg.n + r) : 0;
+        k = lower_bound(id, n, lo);
+        next = k < n ? __ldg(id + k) : INT_MAX;
     }
 };
 
@@ -346,26 +369,25 @@ __device__ __forceinline__ void read32(uint32_t taddr, int lim, float (&f)[32]) 
     for (int i = 0; i < 32; ++i) f[i] = i < lim ? __uint_as_float(u[i]) : -INFINITY;
 }
 
-// The warp's staging buffers: `use` counts its stores.
+// The warp's staging buffer.
 struct Stage {
     unsigned char* buf;
-    int use, lane;
+    int lane;
     __device__ unsigned char* acquire() {
-        if (lane == 0) tc::bulk_wait_read<kOutBufs - 1>();  // its last store has read the buffer
+        if (lane == 0) tc::bulk_wait_read<0>();  // the last store has read it
         __syncwarp();
-        return buf + use % kOutBufs * kOutBytes;
+        return buf;
     }
     __device__ void store(const CUtensorMap* map, int x, int y, bool inside, bool add = false) {
         fence_proxy_async();
         __syncwarp();
         if (lane == 0) {
             if (inside) {
-                if (add) tc::add_2d(map, x, y, buf + use % kOutBufs * kOutBytes);
-                else tc::store_2d(map, x, y, buf + use % kOutBufs * kOutBytes);
+                if (add) tc::add_2d(map, x, y, buf);
+                else tc::store_2d(map, x, y, buf);
             }
             tc::bulk_commit();
         }
-        ++use;
     }
 };
 
@@ -390,16 +412,15 @@ __device__ __forceinline__ void keep_tile(const PairMaps& maps, int n0, int row0
 }
 
 __device__ __forceinline__ void stats_tile(const PairArgs& a, int n0, int row0, int lane,
-                                           int n_rows, float (&x)[kHalfN], Stage& out) {
+                                           int n_rows, float (&x)[kHalfN], const RowList& list,
+                                           Stage& out) {
     const int row = row0 + lane;
     const bool on = row < n_rows;
     const int lim = a.cols - n0;
     // the target logits among these columns, each read back by its own row's
     // thread from shared memory (a register array cannot be indexed)
-    const RowList list(a, row, on);
     const int lo = a.v0 + n0, hi = lo + min(kHalfN, lim);
-    int k = lower_bound(list.id, list.n, lo);
-    int id = k < list.n ? __ldg(list.id + k) : hi;
+    int k = list.k, id = min(list.next, hi);
 #pragma unroll
     for (int g = 0; g < kHalfN / 32; ++g) {
         const int end = min(lo + 32 * (g + 1), hi);
@@ -438,13 +459,11 @@ __device__ __forceinline__ void stats_tile(const PairArgs& a, int n0, int row0, 
 
 __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& maps, int n0,
                                           int row0, int lane, int n_rows, uint32_t taddr,
-                                          Stage& out) {
+                                          const RowList& list, float cf, float l, Stage& out) {
     const int row = row0 + lane;
     const bool on = row < n_rows;
-    const float cf = on ? __ldg(a.coef + row) : 0.f, l = on ? __ldg(a.lse2 + row) : 0.f;
-    const RowList list(a, row, on);
     const int lo = a.v0 + n0;
-    int k = lower_bound(list.id, list.n, lo);
+    int k = list.k;
     // rows up to the next K block of d_weight are written (zero past the last)
     const bool inside = row0 < (n_rows + BK - 1) / BK * BK;
 #pragma unroll 1
@@ -471,9 +490,10 @@ __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& map
             const int col = __ldg(list.id + k) - base;
             if (col >= 64) break;
             const float x = __ldg(a.xk + (size_t)row * a.K + k);
+            float p = __ldg(list.p + k++);
+            while (k < list.n && __ldg(list.id + k) == base + col) p += __ldg(list.p + k++);
             reinterpret_cast<bf16*>(chunk_at(box, lane, col >> 3))[col & 7] =
-                __float2bfloat16_rn(cf * (ex2(fmaf(x, a.c, -l)) - __ldg(list.p + k)));
-            ++k;
+                __float2bfloat16_rn(cf * (ex2(fmaf(x, a.c, -l)) - p));
         }
         out.store(&maps.o, n0 + 64 * g, row0, inside);
     }
@@ -538,31 +558,91 @@ __device__ __forceinline__ void dh_tile(const PairArgs& a, const PairMaps& maps,
     }
 }
 
-__device__ __forceinline__ void dw_tile(const PairArgs& a, const PairMaps& maps, const Job& j,
-                                        int n0, int row0, int lane, uint32_t taddr, Stage& out) {
+// The turned tiles: this thread's row of the tile is column `col` of the output,
+// u the accumulators of rows i0 .. i0 + 31.
+__device__ __forceinline__ void few_keep_tile(const PairArgs& a, int col, int i0, int n_rows,
+                                              const float* u) {
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+        if (i0 + c < n_rows) a.X[(size_t)(i0 + c) * a.ldx + col] = u[c];
+}
+__device__ __forceinline__ void few_dh_tile(const PairArgs& a, const Job& j, int col, int i0,
+                                            int n_rows, uint32_t taddr) {
+    uint32_t u[32];
+    tc::tmem_ld32(taddr, u);
+    if (col >= a.H) return;
+    if (a.split == 1) {
+        const float s = __ldg(a.kappa);
+#pragma unroll
+        for (int c = 0; c < 32; ++c)
+            if (i0 + c < n_rows)
+                a.d_hidden[(size_t)__ldg(a.tg.rowmap + i0 + c) * a.H + col] =
+                    __float2bfloat16_rn(s * __uint_as_float(u[c]));
+        return;
+    }
+    float* o = a.dh + ((size_t)j.part * a.rpad + i0) * a.H + col;
+    const bool none = j.kb0 == j.kb1;
+#pragma unroll
+    for (int c = 0; c < 32; ++c)
+        if (i0 + c < n_rows) o[(size_t)c * a.H] = none ? 0.f : __uint_as_float(u[c]);
+}
+
+// The accumulator is read and handed back first, so that the next product runs
+// while this one is stored: an SM's stores leave at 32 bytes a cycle at most.
+template <typename Release>
+__device__ __forceinline__ void dw_tile(const PairArgs& a, const Job& j, int n0, int row0,
+                                        int lane, uint32_t taddr, unsigned char* box,
+                                        Release release) {
     const bool none = j.kb0 == j.kb1;
     const float s = none ? 0.f : __ldg(a.kappa);
-#pragma unroll 1
-    for (int g = 0; g < kHalfN / 64; ++g) {
-        unsigned char* box = out.acquire();
+    uint32_t w[kHalfN / 2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t u[32];
-            tc::tmem_ld32(taddr + 64u * g + 32u * h, u);
-            uint32_t w[16];
+    for (int g = 0; g < kHalfN / 32; ++g) {
+        uint32_t u[32];
+        tc::tmem_ld32(taddr + 32u * g, u);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                w[i] = none ? 0u
-                            : tc::pack_bf16(__float_as_uint(s * __uint_as_float(u[2 * i])),
-                                            __float_as_uint(s * __uint_as_float(u[2 * i + 1])));
-#pragma unroll
-            for (int v = 0; v < 4; ++v)
-                *chunk_at(box, lane, 4 * h + v) =
-                    make_uint4(w[4 * v], w[4 * v + 1], w[4 * v + 2], w[4 * v + 3]);
-        }
-        const int x = n0 + 64 * g, y = a.v0 + row0;
-        out.store(&maps.dw, x, y, x < a.H && y < a.V);
+        for (int i = 0; i < 16; ++i)
+            w[16 * g + i] = none ? 0u
+                                 : tc::pack_bf16(__float_as_uint(s * __uint_as_float(u[2 * i])),
+                                                 __float_as_uint(s * __uint_as_float(u[2 * i + 1])));
     }
+    release();
+#pragma unroll
+    for (int g = 0; g < kHalfN / 64; ++g) {
+        __syncwarp();  // the box has been read
+#pragma unroll
+        for (int v = 0; v < 8; ++v)
+            *chunk_at(box, lane, v) = make_uint4(w[32 * g + 4 * v], w[32 * g + 4 * v + 1],
+                                                 w[32 * g + 4 * v + 2], w[32 * g + 4 * v + 3]);
+        __syncwarp();
+        const int x = n0 + 64 * g + 8 * (lane & 7);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int rr = 4 * i + (lane >> 3), y = a.v0 + row0 + rr;
+            const uint4 v = *chunk_at(box, rr, lane & 7);
+            if (x < a.H && y < a.V)
+                *reinterpret_cast<uint4*>(a.d_weight + (size_t)y * a.H + x) = v;
+        }
+    }
+}
+
+// The weighted mean of the rows' losses, in row order, by one warp.
+__device__ __forceinline__ void mean_loss(const PairArgs& a, int n_rows, int lane) {
+    double sum = 0.0;
+    for (int b = lane; b < n_rows; b += 32 * 8) {
+        float w[8], l[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const int r = b + 32 * u < n_rows ? __ldg(a.tg.rowmap + b + 32 * u) : -1;
+            w[u] = r >= 0 ? __ldg(a.tg.w + r) : 0.f;
+            l[u] = r >= 0 ? ld_cg(a.row_loss + r) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+            if (w[u] != 0.f) sum += (double)w[u] * (double)l[u];
+    }
+    sum = warp_sum(sum);
+    if (lane == 0) *a.loss = (float)(sum / *a.tg.wsum);
 }
 
 // The first warpgroup's share of the register split, in each of its roles.
@@ -570,13 +650,16 @@ template <bool kSplit> __device__ __forceinline__ void give_registers() {
     if (kSplit) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kRegsFew));
 }
 
-template <int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+template <int MODE, int NF>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::kThreads, 1)
     k_pair(const __grid_constant__ PairMaps maps, const PairArgs a) {
+    using Cfg = PairCfg<MODE, NF>;
+    constexpr bool kFew = Cfg::kFew;
+    constexpr int kPairStages = Cfg::kStages, kStageBytes = Cfg::kStageBytes;
     extern __shared__ unsigned char dsm_raw[];
     unsigned char* dsm = dsm_raw + ((1024u - (smem_u32(dsm_raw) & 1023u)) & 1023u);
     unsigned char* outs = dsm + kPairStages * kStageBytes;
-    PairBars* sb = reinterpret_cast<PairBars*>(outs + kOutBufs * kEpiWarps * kOutBytes);
+    PairBars* sb = reinterpret_cast<PairBars*>(outs + Cfg::kSets * kTileWarps * kOutBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)tc::cluster_rank();
     int* status = a.tg.status;
@@ -588,7 +671,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&sb->acc_full[b], 1);
-            mbar_init(&sb->acc_empty[b], 2 * kEpiWarps);
+            mbar_init(&sb->acc_empty[b], 2 * kTileWarps);
         }
         mbar_init(&sb->drain, 1);
         sb->err = 0;
@@ -605,10 +688,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
     const bool all = n_rows == a.R;  // hidden as it is
     // K blocks summed at a time: the logits' parts, or all of a product's
     constexpr bool kParts = MODE == kStats || MODE == kKeep;
-    Jobs<MODE> jobs(a, n_rows);
+    constexpr bool kSplitRegs = kParts && !kFew;
+    Jobs<MODE, kFew> jobs(a, n_rows);
     Job j;
     if (warp == 0) {
-        give_registers<kParts>();
+        give_registers<kSplitRegs>();
         // ------------------------------------------------------ TMA producer
         if (lane == 0) {
             // what earlier kernels stored is read through the async proxy
@@ -629,13 +713,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     unsigned char* A = dsm + s * kStageBytes;
                     unsigned char* B = A + kHalfBytes;
                     const uint32_t bar = tc::leader_addr(&sb->full[s]);
-                    if (rank == 0) mbar_expect_tx(&sb->full[s], 2 * kStageBytes);
-                    if (MODE != kProd) {
+                    if (rank == 0) {
+                        const bool turned = kFew && (MODE == kKeep || j.kind == 1);
+                        mbar_expect_tx(&sb->full[s],
+                                       2 * (kHalfBytes + (turned ? Cfg::kFewB : kHalfBytes)));
+                    }
+                    if (MODE == kKeep && kFew) {
+                        tc::load_2d(A, &maps.b, kb * BK, j.m0 + 128 * rank, bar);
+                        tc::load_2d(B, ma, kb * BK, NF / 2 * rank, bar);
+                    } else if (MODE != kProd) {
                         tc::load_2d(A, ma, kb * BK, j.m0 + 128 * rank, bar);
                         tc::load_2d(B, &maps.b, kb * BK, a.v0 + j.n0 + 128 * rank, bar);
                     } else {
                         const int n = j.n0 + 128 * rank;
-                        if (j.kind == 1) {
+                        if (kFew && j.kind == 1) {
+                            const int m = j.m0 + 128 * rank;
+                            tc::load_2d(A, &maps.wt, m, a.v0 + kb * BK, bar);
+                            tc::load_2d(A + kBoxBytes, &maps.wt, m + 64, a.v0 + kb * BK, bar);
+                            tc::load_2d(B, &maps.gk, kb * BK, NF / 2 * rank, bar);
+                        } else if (j.kind == 1) {
                             tc::load_2d(A, &maps.gk, kb * BK, j.m0 + 128 * rank, bar);
                             tc::load_2d(B, &maps.wt, n, a.v0 + kb * BK, bar);
                             tc::load_2d(B + kBoxBytes, &maps.wt, n + 64, a.v0 + kb * BK, bar);
@@ -656,7 +752,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                     drain_pair(&sb->full[i % kPairStages], (i / kPairStages) & 1u);
         }
     } else if (warp == 1) {
-        give_registers<kParts>();
+        give_registers<kSplitRegs>();
         // ------------------------------------------------------ MMA issuer
         if (lane == 0 && rank == 0) {
             const uint32_t ring = smem_u32(dsm);
@@ -664,17 +760,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             int lt = 0;
             bool ok = true;
             while (ok && !*(volatile int*)&sb->err && jobs.next(j)) {
-                const bool amn = MODE == kProd && j.kind == 2;
-                constexpr bool bmn = MODE == kProd;
-                const uint32_t idesc = tc::idesc_bf16(256, BT) | (amn ? 1u << 15 : 0u) |
-                                       (bmn ? 1u << 16 : 0u);
+                const bool turned = kFew && (MODE == kKeep || j.kind == 1);
+                const bool amn = MODE == kProd && (kFew || j.kind == 2);
+                const bool bmn = MODE == kProd && !turned;
+                const uint32_t idesc = (turned ? tc::idesc_bf16(256, NF) : tc::idesc_bf16(256, BT)) |
+                                       (amn ? 1u << 15 : 0u) | (bmn ? 1u << 16 : 0u);
                 // descriptors of stage 0; a stage and a K step add to the address
                 // field (16-byte units), which never carries out of it
                 const uint64_t a0 = amn ? tc::desc_mn(ring, kBoxBytes) : tc::sdesc_sw128(ring);
                 const uint64_t b0 = bmn ? tc::desc_mn(ring + kHalfBytes, kBoxBytes)
                                         : tc::sdesc_sw128(ring + kHalfBytes);
                 const uint32_t ka = amn ? 2048u >> 4 : 32u >> 4;
-                constexpr uint32_t kbs = bmn ? 2048u >> 4 : 32u >> 4;
+                const uint32_t kbs = bmn ? 2048u >> 4 : 32u >> 4;
                 const uint32_t alo = (uint32_t)a0, ahi = (uint32_t)(a0 >> 32);
                 const uint32_t blo = (uint32_t)b0, bhi = (uint32_t)(b0 >> 32);
                 const int kb1 = MODE == kProd ? j.kb1 : a.nkh;
@@ -716,13 +813,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             drain_pair(&sb->drain, 0);
         }
     } else if (warp < 4) {
-        give_registers<kParts>();
+        give_registers<kSplitRegs>();
+        if (MODE == kProd && a.loss && blockIdx.x == 0 && warp == 2) mean_loss(a, n_rows, lane);
     } else {
         // ------------------------------------------------------ epilogue
-        if (kParts) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kRegsMany));
+        if (kSplitRegs) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(kRegsMany));
         const int q = warp & 3;               // TMEM lanes 32q .. 32q + 31
-        const int h0 = (warp - 4) / 4 * kHalfN;  // its columns of the tile
-        Stage out{outs + (warp - 4) * kOutBufs * kOutBytes, 0, lane};
+        const int h0 = ((warp - 4) >> 2 & 1) * kHalfN;  // its columns of the tile
+        const int set = (warp - 4) / kTileWarps;  // its accumulator, where there are two sets
+        Stage out{outs + (warp - 4) * kOutBytes, lane};
         const uint32_t empty = tc::leader_addr(&sb->acc_empty[0]);
         int lt = 0;
         auto ready = [&]() {
@@ -737,17 +836,44 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
             if (lane == 0) tc::arrive_remote(empty + 8u * (lt & 1));
             ++lt;
         };
-        auto acc_addr = [&]() {
-            return tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)((lt & 1) * BT + h0);
+        auto acc_addr = [&](int col) {
+            return tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)((lt & 1) * BT + col);
         };
+        const int f0 = ((warp - 4) >> 2 & 1) * (NF / 2);  // its rows of a turned tile
         while (jobs.next(j)) {
+            if (Cfg::kSets == 2 && (lt & 1) != set) {
+                ++lt;
+                continue;
+            }
             const int row0 = j.m0 + 128 * rank + 32 * q, n0 = j.n0 + h0;
-            if (kParts) {
+            if (MODE == kKeep && kFew) {
+                float x[kFew ? NF / 2 : 1];
+                bool ok = true;
+                for (int kb = 0; ok && kb < a.nkh; kb += kSumBlocks) {
+                    if (!(ok = ready())) break;
+#pragma unroll
+                    for (int g = 0; g < NF / 64; ++g) {
+                        uint32_t u[32];
+                        tc::tmem_ld32(acc_addr(f0 + 32 * g), u);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            x[32 * g + i] = kb ? x[32 * g + i] + __uint_as_float(u[i])
+                                               : __uint_as_float(u[i]);
+                    }
+                    release();
+                }
+                if (!ok) break;
+#pragma unroll
+                for (int g = 0; g < NF / 64; ++g)
+                    few_keep_tile(a, row0 + lane, f0 + 32 * g, n_rows, x + 32 * g);
+            } else if (kParts) {
+                const RowList list(a, row0 + lane, MODE == kStats && row0 + lane < n_rows,
+                                   a.v0 + n0);
                 float x[kHalfN];
                 bool ok = true;
                 for (int kb = 0; ok && kb < a.nkh; kb += kSumBlocks) {
                     if (!(ok = ready())) break;
-                    const uint32_t t = acc_addr();
+                    const uint32_t t = acc_addr(h0);
 #pragma unroll
                     for (int g = 0; g < kHalfN / 32; ++g) {
                         uint32_t u[32];
@@ -761,13 +887,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
                 }
                 if (!ok) break;
                 if (MODE == kKeep) keep_tile(maps, n0, row0, lane, n_rows, x, out);
-                else stats_tile(a, n0, row0, lane, n_rows, x, out);
+                else stats_tile(a, n0, row0, lane, n_rows, x, list, out);
+            } else if (MODE == kGrad) {
+                const int row = row0 + lane;
+                const bool on = row < n_rows;
+                const RowList list(a, row, on, a.v0 + n0);
+                const float cf = on ? __ldg(a.coef + row) : 0.f, l = on ? __ldg(a.lse2 + row) : 0.f;
+                if (!ready()) break;
+                grad_tile(a, maps, n0, row0, lane, n_rows, acc_addr(h0), list, cf, l, out);
+                release();
             } else {
                 if (!ready()) break;
-                const uint32_t t = acc_addr();
-                if (MODE == kGrad) grad_tile(a, maps, n0, row0, lane, n_rows, t, out);
-                else if (j.kind == 1) dh_tile(a, maps, j, n0, row0, lane, n_rows, t, out);
-                else dw_tile(a, maps, j, n0, row0, lane, t, out);
+                const uint32_t t = acc_addr(h0);
+                if (kFew && j.kind == 1) {
+#pragma unroll
+                    for (int g = 0; g < NF / 64; ++g)
+                        few_dh_tile(a, j, row0 + lane, f0 + 32 * g, n_rows, acc_addr(f0 + 32 * g));
+                } else if (j.kind == 1) {
+                    dh_tile(a, maps, j, n0, row0, lane, n_rows, t, out);
+                } else {
+                    // (a TMA store may still read the box)
+                    if (!kFew && a.want_dh) out.acquire();
+                    dw_tile(a, j, n0, row0, lane, t, out.buf, release);
+                    continue;
+                }
                 release();
             }
         }
@@ -786,13 +929,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 // RB counted rows per block, 256 / RB threads each: log-partition, loss and
 // gradient coefficient.  A thread takes every (256 / RB)-th part and list entry
 // of its row (consecutive threads: consecutive rows, so the reads coalesce
-// where there are many).  The blocks' weighted losses are added in block order
-// by the last block to finish.
+// where there are many).  With `loss` the blocks' weighted losses are added in
+// block order by the last block to finish.
 template <int RB>
 __global__ void __launch_bounds__(256)
     k_rows(const float2* tab, int ntab, int64_t stride, Targets tg, int K, float c, float T,
-           float grad_scale, const float* xk, float* lse2, float* coef, float* kappa,
-           float* row_loss, float* logz, double* part, float* loss) {
+           const float* xk, float* lse2, float* coef, float* row_loss, float* logz, double* part,
+           float* loss) {
     constexpr int P = 256 / RB;
     __shared__ float2 ms[8][RB];
     __shared__ double dots[8][RB], wl[8];
@@ -860,6 +1003,7 @@ __global__ void __launch_bounds__(256)
             if (lane == 0) part[blockIdx.x] = wloss;
         }
     }
+    if (!loss) return;
     if (threadIdx.x == 0) {
         __threadfence();
         last = gridDim.x == 1 || atomicAdd(tg.done + 1, 1) == (int)gridDim.x - 1;
@@ -877,8 +1021,6 @@ __global__ void __launch_bounds__(256)
         sum = 0.0;
         for (int u = 0; u < 8; ++u) sum += wl[u];
         *loss = (float)(sum / wsum);
-        *kappa = (float)((double)grad_scale * (double)wm /
-                         ((double)kTopMantissa * wsum * (double)T));
     }
 }
 
@@ -923,13 +1065,14 @@ size_t lmloss_workspace_bytes(const LmLossShape& s) {
     return lmloss_shape_ok(s) ? lm_ws(s).total : 0;
 }
 
-template <int MODE>
+template <int MODE, int NF = 0>
 static cudaError_t launch_pair(const PairMaps& maps, const PairArgs& a, int64_t jobs,
                                cudaStream_t st) {
-    cudaError_t e = ensure_dyn_smem((const void*)k_pair<MODE>, kPairSmem);
+    constexpr size_t smem = PairCfg<MODE, NF>::kSmem;
+    cudaError_t e = ensure_dyn_smem((const void*)k_pair<MODE, NF>, smem);
     if (e != cudaSuccess) return e;
     const int64_t pairs = std::max<int64_t>(1, std::min<int64_t>(jobs, device_sm_count() / 2));
-    return launch_dep(k_pair<MODE>, dim3((unsigned)(2 * pairs)), kPairThreads, kPairSmem, 1, st,
+    return launch_dep(k_pair<MODE, NF>, dim3((unsigned)(2 * pairs)), PairCfg<MODE, NF>::kThreads, smem, 1, st,
                       maps, a);
 }
 
@@ -942,7 +1085,8 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     Targets tg{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
                at<float>(ws, w.plogp), at<float>(ws, w.w), at<int32_t>(ws, w.rowmap),
                at<int32_t>(ws, w.rowinv), at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum),
-               at<float>(ws, w.wmax), at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
+               at<float>(ws, w.wmax), at<float>(ws, w.kappa), at<float>(ws, w.share),
+               at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
     bf16* hid = at<bf16>(ws, w.hid);
     float* X = at<float>(ws, w.X);
     bf16* G = at<bf16>(ws, w.G);
@@ -955,11 +1099,13 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     PairMaps maps;
     memset(&maps, 0, sizeof(maps));
     using vsd_lm::make_map_sw128;
-    bool ok = make_map_sw128(&maps.a, hid, false, hrows, H, H, 128) &&
-              make_map_sw128(&maps.a0, hidden, false, R, H, H, 128) &&
+    const int nf = !w.keep ? 0 : R <= 64 ? 64 : R <= 128 ? 128 : 0;  // few rows: turned products
+    const int rbox = nf ? nf / 2 : 128;                              // rows of a K-major half tile
+    bool ok = make_map_sw128(&maps.a, hid, false, hrows, H, H, rbox) &&
+              make_map_sw128(&maps.a0, hidden, false, R, H, H, rbox) &&
               make_map_sw128(&maps.b, weight, false, V, H, H, 128);
     if (grads)
-        ok = ok && make_map_sw128(&maps.gk, G, false, hrows, w.piece, w.piece, 128) &&
+        ok = ok && make_map_sw128(&maps.gk, G, false, hrows, w.piece, w.piece, rbox) &&
              make_map_sw128(&maps.gt, G, false, w.rpad, w.piece, w.piece, BK) &&
              make_map_sw128(&maps.wt, weight, false, V, H, H, BK) &&
              make_map_sw128(&maps.ht, hid, false, hrows, H, H, BK) &&
@@ -991,11 +1137,16 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     a.want_dh = s.dh;
     a.want_dw = s.dw;
     a.dh = dh;
+    a.row_loss = out.row_loss;
+    a.X = X;
+    a.ldx = w.piece;
     a.d_hidden = static_cast<bf16*>(out.d_hidden);
+    a.d_weight = static_cast<bf16*>(out.d_weight);
 
     const RowGather rg{static_cast<const bf16*>(hidden), hid, static_cast<bf16*>(out.d_hidden), H};
     const bool inline_gather = targets_in_one_block(in) && hrows * H <= kInlineGather;
-    cudaError_t e = launch_targets(in, tg, out.row_loss, out.logz, w.zero_end, st,
+    const double scale = (double)grad_scale / ((double)kTopMantissa * (double)T);
+    cudaError_t e = launch_targets(in, tg, scale, out.row_loss, out.logz, w.zero_end, st,
                                    inline_gather ? rg : RowGather{});
     if (e == cudaSuccess && !inline_gather)
         e = launch_dep(k_gather, dim3((unsigned)std::min<int64_t>(hrows, 4 * device_sm_count())),
@@ -1003,8 +1154,10 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     if (e != cudaSuccess) return e;
     const int64_t mt = w.rpad / kRowPad, units = (V + kPieceUnit - 1) / kPieceUnit;
     const int64_t ht = (H + BT - 1) / BT;
-    e = w.keep ? launch_pair<kKeep>(maps, a, mt * units, st)
-               : launch_pair<kStats>(maps, a, mt * units, st);
+    e = nf == 64    ? launch_pair<kKeep, 64>(maps, a, units, st)
+        : nf == 128 ? launch_pair<kKeep, 128>(maps, a, units, st)
+        : w.keep    ? launch_pair<kKeep>(maps, a, mt * units, st)
+                    : launch_pair<kStats>(maps, a, mt * units, st);
     if (e != cudaSuccess) return e;
     if (w.keep) {  // losses and G from the kept logits, a row at a time
         RowArgs ra{};
@@ -1015,22 +1168,19 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         ra.ldx = ra.ldg = w.piece;
         ra.gcols = w.piece;
         ra.c = c;
-        ra.T = T;
-        ra.grad_scale = grad_scale;
+        ra.invT = 1.f / T;
         ra.row_loss = out.row_loss;
         ra.logz = out.logz;
-        ra.loss = out.loss;
-        ra.kappa = kappa;
         ra.same_align = true;
         e = launch_row_loss<float, bf16, true>(X, G, ra, hrows, kTopMantissa, device_sm_count(),
                                                ensure_dyn_smem, st);
     } else {
         // one row per block while that fills the GPU no more than a few times over
-        const int rb = R <= 1024 ? 1 : R <= 16384 ? 8 : 32;
+        const int rb = R <= 256 ? 1 : R <= 16384 ? 8 : 32;
         e = launch_dep(rb == 1 ? k_rows<1> : rb == 8 ? k_rows<8> : k_rows<32>,
                        dim3((unsigned)((R + rb - 1) / rb)), 256, 0, 1, st, tab, (int)(2 * units),
-                       (int64_t)w.rpad, tg, K, c, T, grad_scale, xk, lse2, coef, kappa,
-                       out.row_loss, out.logz, at<double>(ws, w.part), out.loss);
+                       (int64_t)w.rpad, tg, K, c, T, xk, lse2, coef, out.row_loss, out.logz,
+                       at<double>(ws, w.part), grads ? nullptr : out.loss);
     }
     if (e != cudaSuccess || !grads) return e;
     for (int q = 0; q < w.npiece; ++q) {
@@ -1038,9 +1188,13 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         a.cols = std::min(w.piece, V - a.v0);
         a.first = q == 0;
         a.last = q == w.npiece - 1;
+        a.loss = q == 0 ? out.loss : nullptr;
         const int64_t nu = (a.cols + kPieceUnit - 1) / kPieceUnit;
         if (!w.keep && (e = launch_pair<kGrad>(maps, a, mt * nu, st)) != cudaSuccess) return e;
-        e = launch_pair<kProd>(maps, a, (s.dh ? mt * ht * w.split : 0) + (s.dw ? nu * ht : 0), st);
+        const int64_t jobs = (s.dh ? mt * ht * w.split : 0) + (s.dw ? nu * ht : 0);
+        e = nf == 64    ? launch_pair<kProd, 64>(maps, a, jobs, st)
+            : nf == 128 ? launch_pair<kProd, 128>(maps, a, jobs, st)
+                        : launch_pair<kProd>(maps, a, jobs, st);
         if (e != cudaSuccess) return e;
     }
     if (s.dh && w.split > 1) {

@@ -30,8 +30,10 @@ __device__ __forceinline__ uint32_t leader_addr(const void* p) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(smem_u32(p)));
     return a;
 }
+// Relaxed: it hands back tensor memory, which tcgen05.fence orders, and a
+// release would wait for the thread's outstanding global stores.
 __device__ __forceinline__ void arrive_remote(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar)
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar)
                  : "memory");
 }
 __device__ __forceinline__ bool try_wait_cluster(uint64_t* bar, uint32_t parity) {

@@ -47,9 +47,8 @@ struct RowArgs {
     int vper;            // vectors of a block's segment
     int64_t ldx, ldg;    // row pitches in elements
     int gcols;           // columns of a gradient row that are written (zero from V on)
-    float c, T, grad_scale;
-    float *row_loss, *logz, *loss;
-    float* kappa;        // packed rows: what the products are multiplied by
+    float c, invT;
+    float *row_loss, *logz;
     bool same_align;     // gradient rows start where logits rows do, modulo 16 bytes
 };
 
@@ -87,7 +86,6 @@ __global__ void __launch_bounds__(kRowThreads)
     __shared__ uint64_t bars[kRowBars];
     __shared__ float2 part[kRowWarps], cpart[kMaxCluster];
     __shared__ float xs[kMaxTeacher];
-    __shared__ int last;
     uint32_t rank, C;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
@@ -137,13 +135,12 @@ __global__ void __launch_bounds__(kRowThreads)
     } else {
         dep_wait();
     }
-    const int n_rows = LM ? *(const volatile int*)a.tg.nrows : a.rows;
-    const bool real = i < n_rows;
-    if (LM && real) {
-        // the kernel before this one stored the logits
+    if (LM) {  // the kernel before this one stored the logits (all rows' space may be read)
         if (tid == 0) asm volatile("fence.proxy.async;" ::: "memory");
         load(0);
     }
+    const int n_rows = LM ? *(const volatile int*)a.tg.nrows : a.rows;
+    const bool real = i < n_rows;
     const int r = LM ? (real ? a.tg.rowmap[i] : 0) : i;
     const int n = real ? a.tg.n[r] : -1;
     const int32_t* id = a.tg.id + (size_t)r * a.K;
@@ -164,7 +161,8 @@ __global__ void __launch_bounds__(kRowThreads)
     float M = 0.f, S = 1.f;
     int loads = 0;  // of this block so far
     if (n >= 0) {
-        if (tid < n) xs[tid] = row_value(x[id[tid]]);  // (before any gradient is written)
+        // the target logits (read before any gradient is written, used after)
+        const float xv = tid < n ? row_value(x[id[tid]]) : 0.f;
         float m = -INFINITY, s = 0.f;
         for (int rd = 0; rd < a.rounds; ++rd) {
             if (rd) {
@@ -205,6 +203,7 @@ __global__ void __launch_bounds__(kRowThreads)
             }
             ++loads;
         }
+        if (tid < n) xs[tid] = xv;
         const float wm = warp_max(m), wz = wm > -INFINITY ? wm : 0.f;
         s = warp_sum(s * ex2(((m > -INFINITY ? m : wz) - wz) * a.c));
         if (lane == 0) part[warp] = make_float2(wm, s);
@@ -232,18 +231,18 @@ __global__ void __launch_bounds__(kRowThreads)
         }
     } else {
         // (copies of a row that does not count land before the block may exit)
-        if (!LM)
-            for (int q = 0; q < kRowBars; ++q) arrived(q, 0);
+        for (int q = 0; q < kRowBars; ++q) arrived(q, 0);
         if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     }
     const float inv = 1.f / S;
     float coef = 0.f;
     if (n >= 0) {
+        const float w = a.tg.w[r];
         if (LM) {
             const float wm = *a.tg.wmax;
-            coef = wm > 0.f ? top * (a.tg.w[r] / wm) : 0.f;
+            coef = wm > 0.f ? top * (w / wm) : 0.f;
         } else {
-            coef = (float)((double)a.grad_scale * (double)a.tg.w[r] / (*a.tg.wsum * (double)a.T));
+            coef = w * *a.tg.share;
         }
     }
     if (g && (!LM || i < (n_rows + 63) / 64 * 64)) {
@@ -285,59 +284,56 @@ __global__ void __launch_bounds__(kRowThreads)
         if (LM && rank == C - 1)
             for (int v = V + tid; v < a.gcols; v += kRowThreads) row_put(g + v, 0.f);
         __syncthreads();
-        if (tid < n) {  // the target entries this block wrote as dense ones
-            const int j = (id[tid] + off) / PV % stride;
-            if (j / a.vper == (int)rank)
-                row_put(g + id[tid], coef * (ex2((xs[tid] - M) * a.c) * inv - p[tid]));
+        if (tid < n && (tid == 0 || id[tid - 1] != id[tid])) {
+            // the target entries this block wrote as dense ones; equal tokens add
+            const int v = id[tid], j = (v + off) / PV % stride;
+            if (j / a.vper == (int)rank) {
+                float q = p[tid];
+                for (int k = tid + 1; k < n && id[k] == v; ++k) q += p[k];
+                row_put(g + v, coef * (ex2((xs[tid] - M) * a.c) * inv - q));
+            }
         }
     }
-    // the row's loss, then (the last row) their weighted mean in row order
-    if (rank != 0) return;
-    if (warp == 0 && n >= 0) {
-        double dot = 0.0;
-        for (int k = lane; k < n; k += 32) dot += (double)p[k] * ((double)xs[k] - (double)M);
-        dot = warp_sum(dot);
-        if (lane == 0) {
-            const double l = (double)logf(S), lz = (double)M / (double)a.T + l;
-            if (!isfinite(lz)) atomicOr(a.tg.status, VSD_STATUS_BAD_ROW);
-            a.logz[r] = (float)lz;
-            a.row_loss[r] = (float)((double)a.tg.plogp[r] + l - dot / (double)a.T);
-        }
+    // the row's loss
+    if (rank != 0 || warp != 0 || n < 0) return;
+    float dot = 0.f;
+    for (int k = lane; k < n; k += 32) dot = fmaf(p[k], xs[k] - M, dot);
+    dot = warp_sum(dot);
+    if (lane == 0) {
+        const float l = logf(S), lz = fmaf(M, a.invT, l);
+        if (!isfinite(lz)) atomicOr(a.tg.status, VSD_STATUS_BAD_ROW);
+        a.logz[r] = lz;
+        a.row_loss[r] = a.tg.plogp[r] + (l - dot * a.invT);
     }
-    if (tid == 0) {
-        __threadfence();
-        last = atomicAdd(a.tg.done + 1, 1) == (int)(gridDim.x / C) - 1;
-    }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
+}
+
+// The weighted mean of the rows' losses, in row order, by one block.
+__global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const float* row_loss,
+                                                    float* loss) {
+    __shared__ double part[32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    dep_launch();
+    dep_wait();
     double sum = 0.0;
-    for (int b = tid; b < n_rows; b += kRowThreads * 8) {
-        float w[8], l[8];
+    for (int64_t b = threadIdx.x; b < R; b += 1024 * 4) {
+        float w[4], l[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            const int q = b + u * kRowThreads;
-            int t = q < n_rows ? q : -1;
-            if (LM && t >= 0) t = ld_cg(a.tg.rowmap + t);
-            if (!LM && t >= 0 && ld_cg(a.tg.n + t) < 0) t = -1;
-            w[u] = t >= 0 ? ld_cg(a.tg.w + t) : 0.f;
-            l[u] = t >= 0 ? ld_cg(a.row_loss + t) : 0.f;
+        for (int u = 0; u < 4; ++u) {
+            const int64_t r = min(b + u * 1024, (int64_t)R - 1);
+            const bool on = ld_cg(tg.n + r) >= 0 && b + u * 1024 < R;
+            w[u] = on ? ld_cg(tg.w + r) : 0.f;
+            l[u] = ld_cg(row_loss + r);
         }
 #pragma unroll
-        for (int u = 0; u < 8; ++u)
+        for (int u = 0; u < 4; ++u)
             if (w[u] != 0.f) sum += (double)w[u] * (double)l[u];
     }
-    __shared__ double dpart[kRowWarps];
     sum = warp_sum(sum);
-    if (lane == 0) dpart[warp] = sum;
+    if (lane == 0) part[warp] = sum;
     __syncthreads();
-    if (tid == 0) {
-        sum = 0.0;
-        for (int w = 0; w < kRowWarps; ++w) sum += dpart[w];
-        *a.loss = (float)(sum / *a.tg.wsum);
-        if (LM)
-            *a.kappa = (float)((double)a.grad_scale * (double)*a.tg.wmax /
-                               ((double)top * *a.tg.wsum * (double)a.T));
+    if (warp == 0) {
+        sum = warp_sum(lane < (int)blockDim.x / 32 ? part[lane] : 0.0);
+        if (lane == 0) *loss = (float)(sum / *tg.wsum);
     }
 }
 

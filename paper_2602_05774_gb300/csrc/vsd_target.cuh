@@ -12,6 +12,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "vsd.h"
 #include "vsd_common.cuh"
 
@@ -60,7 +62,7 @@ struct TargetIn {
 };
 
 // The targets in the workspace.  Lists are per original row; the entries of a
-// row are distinct tokens in ascending order (probabilities of equal ids added).
+// row are in ascending order of their tokens (equal ones next to each other).
 struct Targets {
     int32_t* n;       // [R] entries of the list; -1: the row is not counted
     int32_t* id;      // [R][K]
@@ -72,6 +74,8 @@ struct Targets {
     int32_t* nrows;   // counted rows
     double* wsum;     // sum of their weights, 1 where that is 0
     float* wmax;      // the largest of them
+    float* kappa;     // a constant of the call times wmax / wsum
+    float* share;     // the same constant / wsum
     int32_t* done;    // block counter, 0 at the start
     int32_t* status;
 };
@@ -83,7 +87,7 @@ __device__ __forceinline__ float teacher_logit(const TargetIn& in, size_t i) {
     return __ldg(static_cast<const float*>(in.teacher) + i);
 }
 
-// The target of one row, by one warp; kPer entries of the list per lane.
+// The target of one teacher row, by one warp; kPer entries of the list per lane.
 template <int kPer>
 __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg, int r,
                                            int lane) {
@@ -91,23 +95,6 @@ __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg
     const float w = in.row_weight ? __ldg(in.row_weight + r) : 1.f;
     int bits = (w >= 0.f && isfinite(w)) ? 0 : VSD_STATUS_BAD_ROW;
     const size_t base = (size_t)r * in.K;
-    if (in.labels) {
-        const int lab = __ldg(in.labels + r);
-        bool counted = lab != in.ignore && !bits;
-        if (lab != in.ignore && (lab < 0 || lab >= in.V)) {
-            bits |= VSD_STATUS_BAD_TOKEN;
-            counted = false;
-        }
-        if (lane == 0) {
-            tg.n[r] = counted ? 1 : -1;
-            tg.id[base] = counted ? lab : 0;
-            tg.p[base] = 1.f;
-            tg.plogp[r] = 0.f;
-            tg.w[r] = w;
-            if (bits) atomicOr(tg.status, bits);
-        }
-        return;
-    }
     int id[kPer];
     float t[kPer];
     float m = -INFINITY;
@@ -148,46 +135,30 @@ __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg
         for (int j = 0; j < kPer; ++j)
             if (id[j] >= 0) plogp += e[j] / z * ((t[j] - m) * in.invT - lz);
         plogp = warp_sum(plogp);
-        // the mass of equal ids is added at the first of them, whose place is
-        // the number of distinct smaller ids
-        float p[kPer];
-        bool first[kPer];
+        // an entry's place: the number of entries before it by (id, position)
         int rank[kPer];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) p[j] = 0.f, first[j] = id[j] >= 0, rank[j] = 0;
+        for (int j = 0; j < kPer; ++j) rank[j] = 0;
 #pragma unroll
         for (int jo = 0; jo < kPer; ++jo) {
             if (32 * jo >= in.K) break;
+#pragma unroll 8
             for (int o = 0; o < 32; ++o) {
-                const int oid = __shfl_sync(kAll, id[jo], o);
-                const float oe = __shfl_sync(kAll, e[jo], o);
-                if (oid < 0) continue;
+                // (absent entries, -1, sort behind all: as unsigned, the largest)
+                const uint32_t oid = (uint32_t)__shfl_sync(kAll, id[jo], o);
 #pragma unroll
                 for (int j = 0; j < kPer; ++j)
-                    if (id[j] == oid) {
-                        p[j] += oe;
-                        if (o + 32 * jo < lane + 32 * j) first[j] = false;
-                    }
-            }
-        }
-#pragma unroll
-        for (int jo = 0; jo < kPer; ++jo) {
-            if (32 * jo >= in.K) break;
-            for (int o = 0; o < 32; ++o) {
-                const int oid = __shfl_sync(kAll, first[jo] ? id[jo] : -1, o);
-                if (oid < 0) continue;
-#pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    if (oid < id[j]) ++rank[j];
+                    rank[j] += oid < (uint32_t)id[j] ||
+                               (oid == (uint32_t)id[j] && o + 32 * jo < lane + 32 * j);
             }
         }
 #pragma unroll
         for (int j = 0; j < kPer; ++j) {
-            if (first[j]) {
+            if (id[j] >= 0) {
                 tg.id[base + rank[j]] = id[j];
-                tg.p[base + rank[j]] = p[j] / z;
+                tg.p[base + rank[j]] = e[j] / z;
             }
-            n += __popc(__ballot_sync(kAll, first[j]));
+            n += __popc(__ballot_sync(kAll, id[j] >= 0));
         }
     }
     if (lane == 0) {
@@ -199,57 +170,73 @@ __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg
 }
 
 // The list of counted rows, the sum and the largest of their weights, by one
-// block.  Each thread takes a run of rows; the runs' counts and sums are
-// combined in thread order, so the result does not depend on timing.
-__device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_loss,
-                                          float* logz) {
+// block of whole warps.  A thread takes a run of rows, 16 at a time; the runs'
+// counts and sums are combined in an order that timing does not change.
+// look(b, n, w): flags (n >= 0) and weights of rows b .. b + 15 that the thread
+// owns.
+template <int kBatch, typename Look>
+__device__ __forceinline__ void scan_rows(const Targets& tg, int R, double scale, float* row_loss,
+                                          float* logz, Look look) {
     __shared__ int cnt[32];
     __shared__ double sum[32];
     __shared__ float top[32];
-    const int nt = blockDim.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int nt = blockDim.x, nw = nt / 32, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int per = (R + nt - 1) / nt;
-    const int64_t r0 = (int64_t)threadIdx.x * per;
+    const int64_t r0 = min((int64_t)R, (int64_t)threadIdx.x * per);
     const int64_t r1 = min((int64_t)R, r0 + per);
     int c = 0;
     double ws = 0.0;
     float wm = 0.f;
-    for (int64_t b = r0; b < r1; b += 8) {  // (eight rows' loads at a time)
-        int n[8];
-        float w[8];
+    uint32_t mask = 0;  // the last batch's flags
+    auto batch = [&](int64_t b) {
+        int n[kBatch];
+        float w[kBatch];
+        look(b, r1, n, w);
+        mask = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            n[i] = b + i < r1 ? ld_cg(tg.n + b + i) : -1;
-            w[i] = b + i < r1 ? ld_cg(tg.w + b + i) : 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < kBatch; ++i)
             if (n[i] >= 0) {
+                mask |= 1u << i;
                 ++c;
                 ws += (double)w[i];
                 wm = fmaxf(wm, w[i]);
             }
-    }
+    };
+    for (int64_t b = r0; b < r1; b += kBatch) batch(b);
     int inc = c;
     for (int o = 1; o < 32; o <<= 1) {
         const int v = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += v;
     }
-    const double wsw = warp_sum(ws);
-    if (lane == 31) cnt[warp] = inc;
-    wm = warp_max(wm);
-    if (lane == 0) sum[warp] = wsw, top[warp] = wm;
-    __syncthreads();
     int at = inc - c;
-    for (int i = 0; i < warp; ++i) at += cnt[i];
-    for (int64_t b = r0; b < r1; b += 8) {
-        int n[8];
+    ws = warp_sum(ws);
+    wm = warp_max(wm);
+    if (lane == 31) cnt[warp] = inc;
+    if (lane == 0) sum[warp] = ws, top[warp] = wm;
+    __syncthreads();
+    // every warp: the count of the warps before it
+    int others = lane < nw ? cnt[lane] : 0;
+    const int all = __reduce_add_sync(0xffffffffu, others);
+    at += __reduce_add_sync(0xffffffffu, lane < warp ? others : 0);
+    if (warp == 0) {
+        ws = warp_sum(lane < nw ? sum[lane] : 0.0);
+        wm = warp_max(lane < nw ? top[lane] : 0.f);
+        if (lane == 0) {
+            ws = ws > 0.0 ? ws : 1.0;
+            *tg.nrows = all;
+            *tg.wsum = ws;
+            *tg.wmax = wm;
+            *tg.kappa = (float)(scale * (double)wm / ws);
+            *tg.share = (float)(scale / ws);
+        }
+    }
+    for (int64_t b = r0; b < r1; b += kBatch) {
+        if (per > kBatch) batch(b);  // (else still held)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) n[i] = b + i < r1 ? ld_cg(tg.n + b + i) : -1;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kBatch; ++i) {
             if (b + i >= r1) break;
             const int r = (int)(b + i);
-            const bool on = n[i] >= 0;
+            const bool on = mask >> i & 1;
             if (tg.rowinv) tg.rowinv[r] = on ? at : -1;
             if (on) {
                 if (tg.rowmap) tg.rowmap[at] = r;
@@ -259,14 +246,6 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, float* row_l
                 logz[r] = 0.f;
             }
         }
-    }
-    if (threadIdx.x == 0) {
-        int total = 0;
-        double s = 0.0;
-        for (int i = 0; i < nt / 32; ++i) total += cnt[i], s += sum[i], wm = fmaxf(wm, top[i]);
-        *tg.nrows = total;
-        *tg.wsum = s > 0.0 ? s : 1.0;
-        *tg.wmax = wm;
     }
 }
 
@@ -304,27 +283,87 @@ __device__ __forceinline__ void gather_rows(const RowGather& g, int R, const Tar
 constexpr int64_t kInlineGather = 32768;
 
 // Whether a call's targets are made by a single block, which then also clears
-// the status word and the counters: one launch less where latency counts.  Each
-// of its 32 warps takes up to 32 labels, or two teacher lists.
-inline bool targets_in_one_block(const TargetIn& in) { return in.R <= (in.labels ? 1024 : 64); }
+// the status word and the counters: one launch less where latency counts.  A
+// thread takes up to 8 labels, or a warp two teacher lists.
+inline bool targets_in_one_block(const TargetIn& in) { return in.R <= (in.labels ? 8192 : 64); }
 
 namespace {
 
+// The targets of up to kBatch labels from row b on, to r1; all loads first.
+template <int kBatch>
+__device__ __forceinline__ void label_rows(const TargetIn& in, const Targets& tg, int64_t b,
+                                           int64_t r1, int (&n)[kBatch], float (&w)[kBatch],
+                                           int* bits) {
+    int lab[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) lab[i] = __ldg(in.labels + min(b + i, r1 - 1));
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i)
+        w[i] = in.row_weight ? __ldg(in.row_weight + min(b + i, r1 - 1)) : 1.f;
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+        n[i] = -1;
+        if (b + i >= r1) continue;
+        const bool bad_w = !(w[i] >= 0.f && isfinite(w[i]));
+        const bool far = lab[i] != in.ignore && (lab[i] < 0 || lab[i] >= in.V);
+        if (bad_w) *bits |= VSD_STATUS_BAD_ROW;
+        if (far) *bits |= VSD_STATUS_BAD_TOKEN;
+        n[i] = lab[i] != in.ignore && !far && !bad_w ? 1 : -1;
+        tg.n[b + i] = n[i];
+        tg.id[b + i] = n[i] > 0 ? lab[i] : 0;
+        tg.p[b + i] = 1.f;
+        tg.plogp[b + i] = 0.f;
+        tg.w[b + i] = w[i];
+    }
+}
+
 // All rows' targets, then (the last block to finish) the list of counted rows.
-template <int kPer, bool kOneBlock>
-__global__ void __launch_bounds__(kOneBlock ? 1024 : 256)
-    k_targets(TargetIn in, Targets tg, float* row_loss, float* logz, RowGather g) {
+// kPer: entries of a teacher row per lane, or the batch of labels of a thread.
+template <int kPer, bool kLabels, bool kOneBlock>
+__global__ void __launch_bounds__(1024)
+    k_targets(TargetIn in, Targets tg, double scale, float* row_loss, float* logz, RowGather g) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     dep_launch();
-    if (kOneBlock) {
+    int bits = 0;
+    auto made = [&](int64_t b, int64_t r1, int (&n)[16], float (&w)[16]) {  // by any block
+#pragma unroll
+        for (int i = 0; i < 16; ++i) n[i] = ld_cg(tg.n + min(b + i, r1 - 1));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = ld_cg(tg.w + min(b + i, r1 - 1));
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (b + i >= r1) n[i] = -1;
+    };
+    if constexpr (kOneBlock) {
         if (threadIdx.x < 4) tg.done[threadIdx.x] = 0;
         if (threadIdx.x == 0) *tg.status = 0;
         __syncthreads();
-        for (int r = warp; r < in.R; r += 32) target_row<kPer>(in, tg, r, lane);
-        __syncthreads();
+        if constexpr (kLabels) {
+            scan_rows<kPer>(tg, in.R, scale, row_loss, logz,
+                            [&](int64_t b, int64_t r1, int (&n)[kPer], float (&w)[kPer]) {
+                                label_rows<kPer>(in, tg, b, r1, n, w, &bits);
+                            });
+            if (bits) atomicOr(tg.status, bits);
+        } else {
+            for (int r = warp; r < in.R; r += blockDim.x / 32) target_row<kPer>(in, tg, r, lane);
+            __syncthreads();
+            scan_rows<16>(tg, in.R, scale, row_loss, logz, made);
+        }
+        if (g.hidden) {
+            __syncthreads();
+            gather_rows(g, in.R, tg, 0, 1);
+        }
     } else {
-        const int r = (int)(blockIdx.x * 8 + warp);
-        if (r < in.R) target_row<kPer>(in, tg, r, lane);
+        if constexpr (kLabels) {
+            const int64_t r = blockIdx.x * (int64_t)256 + threadIdx.x;
+            int n[1];
+            float w[1];
+            if (r < in.R) label_rows<1>(in, tg, r, r + 1, n, w, &bits);
+            if (bits) atomicOr(tg.status, bits);
+        } else {
+            const int64_t r = blockIdx.x * (int64_t)8 + warp;
+            if (r < in.R) target_row<kPer>(in, tg, (int)r, lane);
+        }
         __shared__ int last;
         __threadfence();
         __syncthreads();
@@ -332,29 +371,35 @@ __global__ void __launch_bounds__(kOneBlock ? 1024 : 256)
         __syncthreads();
         if (!last) return;
         __threadfence();
-    }
-    scan_rows(tg, in.R, row_loss, logz);
-    if (kOneBlock && g.hidden) {
-        __syncthreads();
-        gather_rows(g, in.R, tg, 0, 1);
+        scan_rows<16>(tg, in.R, scale, row_loss, logz, made);
     }
 }
 
 // `zero_bytes` of the workspace from its start (status word, counters) are
-// cleared, then the targets made.
-inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, float* row_loss,
-                                  float* logz, size_t zero_bytes, cudaStream_t st,
+// cleared, then the targets made; scale: of kappa.
+inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, double scale,
+                                  float* row_loss, float* logz, size_t zero_bytes, cudaStream_t st,
                                   const RowGather& g = RowGather{}) {
-    const int per = in.labels || in.K <= 32 ? 1 : in.K <= 64 ? 2 : 4;
+    const int per = in.K <= 32 ? 1 : in.K <= 64 ? 2 : 4;
     if (targets_in_one_block(in)) {
-        auto k = per == 1 ? k_targets<1, true> : per == 2 ? k_targets<2, true> : k_targets<4, true>;
-        k<<<1, 1024, 0, st>>>(in, tg, row_loss, logz, g);
+        // threads: a label each while they reach, then four at a time; a warp per list
+        const int threads = in.labels ? (in.R <= 256 ? 256 : 1024)
+                                      : std::max(64, std::min(1024, 32 * in.R));
+        auto k = in.labels ? (in.R <= 1024 ? k_targets<1, true, true> : k_targets<4, true, true>)
+                 : per == 1 ? k_targets<1, false, true>
+                 : per == 2 ? k_targets<2, false, true>
+                            : k_targets<4, false, true>;
+        k<<<1, threads, 0, st>>>(in, tg, scale, row_loss, logz, g);
         return cudaGetLastError();
     }
     cudaError_t e = cudaMemsetAsync(tg.status, 0, zero_bytes, st);
     if (e != cudaSuccess) return e;
-    auto k = per == 1 ? k_targets<1, false> : per == 2 ? k_targets<2, false> : k_targets<4, false>;
-    k<<<(unsigned)((in.R + 7) / 8), 256, 0, st>>>(in, tg, row_loss, logz, g);
+    auto k = in.labels  ? k_targets<1, true, false>
+             : per == 1 ? k_targets<1, false, false>
+             : per == 2 ? k_targets<2, false, false>
+                        : k_targets<4, false, false>;
+    const int rows = in.labels ? 256 : 8;  // per block
+    k<<<(unsigned)((in.R + rows - 1) / rows), 256, 0, st>>>(in, tg, scale, row_loss, logz, g);
     return cudaGetLastError();
 }
 

@@ -23,7 +23,7 @@ namespace {
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct TopkWs {
-    size_t status, done, zero_end, nrows, wsum, wmax, n, id, p, plogp, w, total;
+    size_t status, done, zero_end, nrows, wsum, wmax, kappa, share, n, id, p, plogp, w, total;
 };
 
 TopkWs topk_ws(int R, int K) {
@@ -41,6 +41,8 @@ TopkWs topk_ws(int R, int K) {
     w.nrows = take(4);
     w.wsum = take(8);
     w.wmax = take(4);
+    w.kappa = take(4);
+    w.share = take(4);
     w.n = take(4 * r);
     w.id = take(4 * rk);
     w.p = take(4 * rk);
@@ -71,7 +73,8 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     RowArgs a{};
     a.tg = Targets{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
                    at<float>(ws, w.plogp), at<float>(ws, w.w), nullptr, nullptr,
-                   at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum), at<float>(ws, w.wmax),
+                   at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum), at<float>(ws, w.wmax), at<float>(ws, w.kappa),
+                   at<float>(ws, w.share),
                    at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
     a.rows = in.R;
     a.V = in.V;
@@ -79,22 +82,24 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     a.ldx = a.ldg = in.V;
     a.gcols = in.V;
     a.c = (float)(kLog2e / (double)T);
-    a.T = T;
-    a.grad_scale = grad_scale;
+    a.invT = 1.f / T;
     a.row_loss = out.row_loss;
     a.logz = out.logz;
-    a.loss = out.loss;
     a.same_align = (((uintptr_t)logits ^ (uintptr_t)out.grad) & 15) == 0;
-    cudaError_t e = launch_targets(in, a.tg, out.row_loss, out.logz, w.zero_end, st);
+    cudaError_t e = launch_targets(in, a.tg, (double)grad_scale / (double)T, out.row_loss,
+                                   out.logz, w.zero_end, st);
     if (e != cudaSuccess) return e;
     const int sms = device_sm_count();
     if (bf16)
-        return launch_row_loss<__nv_bfloat16, __nv_bfloat16, false>(
+        e = launch_row_loss<__nv_bfloat16, __nv_bfloat16, false>(
             static_cast<const __nv_bfloat16*>(logits), static_cast<__nv_bfloat16*>(out.grad), a,
             in.R, 1.f, sms, ensure_dyn_smem, st);
-    return launch_row_loss<float, float, false>(static_cast<const float*>(logits),
-                                                static_cast<float*>(out.grad), a, in.R, 1.f, sms,
-                                                ensure_dyn_smem, st);
+    else
+        e = launch_row_loss<float, float, false>(static_cast<const float*>(logits),
+                                                 static_cast<float*>(out.grad), a, in.R, 1.f, sms,
+                                                 ensure_dyn_smem, st);
+    if (e != cudaSuccess) return e;
+    return launch_dep(k_mean_loss, dim3(1), 1024, 0, 1, st, a.tg, in.R, out.row_loss, out.loss);
 }
 
 }  // namespace vsd

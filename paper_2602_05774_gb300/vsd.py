@@ -8,6 +8,7 @@ streams.  There is no CPU fallback: if libvsd.so is missing or fails to load,
 every call raises.
 """
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -551,9 +552,8 @@ def _grad_tensor(want, like, name):
 
 
 def _loss_outputs(R, device):
-    return dict(loss=torch.empty(1, dtype=torch.float32, device=device),
-                row_loss=torch.empty(R, dtype=torch.float32, device=device),
-                logz=torch.empty(R, dtype=torch.float32, device=device))
+    f = dict(dtype=torch.float32, device=device)
+    return dict(loss=torch.empty(1, **f), row_loss=torch.empty(R, **f), logz=torch.empty(R, **f))
 
 
 def _loss_workspace(need, workspace, device):
@@ -569,6 +569,11 @@ def _loss_workspace(need, workspace, device):
 
 def lmhead_loss_workspace_bytes(R, V, H, K=1, grads=True, piece=0):
     """Bytes of workspace of lmhead_cross_entropy (K = 1) and lmhead_distill."""
+    return _lmhead_loss_bytes(R, V, H, K, grads, piece)
+
+
+@functools.lru_cache(maxsize=256)
+def _lmhead_loss_bytes(R, V, H, K, grads, piece):
     return _lib().vsd_lmhead_loss_workspace_bytes(int(R), int(V), int(H), int(K),
                                                   int(bool(grads)), int(piece))
 
@@ -591,8 +596,8 @@ def _lmhead_loss(hidden, weight, K, d_hidden, d_weight, piece, workspace, others
         out["d_hidden"] = dh
     if dw is not None:
         out["d_weight"] = dw
-    ws = _loss_workspace(lmhead_loss_workspace_bytes(R, V, H, K, dh is not None or dw is not None,
-                                                     piece), workspace, dev)
+    ws = _loss_workspace(_lmhead_loss_bytes(R, V, H, K, dh is not None or dw is not None, piece),
+                         workspace, dev)
     st = LossOutputs(out["loss"].data_ptr(), out["row_loss"].data_ptr(), out["logz"].data_ptr(),
                      None if dh is None else dh.data_ptr(), None if dw is None else dw.data_ptr(),
                      None)
@@ -638,6 +643,11 @@ def lmhead_distill(hidden, weight, teacher_ids, teacher_logits, T=1.0, row_weigh
     return out
 
 
+@functools.lru_cache(maxsize=256)
+def _topk_bytes(R, V, K):
+    return _lib().vsd_topk_distill_workspace_bytes(R, V, K)
+
+
 def topk_distill(logits, teacher_ids, teacher_logits, T=1.0, row_weight=None, grad_scale=1.0,
                  grad=True, workspace=None):
     """Distillation from a teacher's top logits on logits in hand [R][V]:
@@ -654,7 +664,7 @@ def topk_distill(logits, teacher_ids, teacher_logits, T=1.0, row_weight=None, gr
     g = _grad_tensor(grad, logits, "grad")
     if g is not None:
         out["grad"] = g
-    ws = _loss_workspace(_lib().vsd_topk_distill_workspace_bytes(R, V, K), workspace, dev)
+    ws = _loss_workspace(_topk_bytes(R, V, K), workspace, dev)
     st = LossOutputs(out["loss"].data_ptr(), out["row_loss"].data_ptr(), out["logz"].data_ptr(),
                      None, None, None if g is None else g.data_ptr())
     _check(_lib().vsd_topk_distill(_ptr(logits), _dtype_code(logits), R, V, _ptr(teacher_ids),

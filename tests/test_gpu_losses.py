@@ -150,7 +150,8 @@ def teacher(R, V, K, g, dtype=torch.float32, dup=False):
 XENT = [  # R, V, H, piece
     (1, 1, 8, 0), (1, 5, 8, 0), (3, 257, 64, 0), (32, 1024, 256, 0), (129, 1000, 72, 256),
     (257, 2049, 136, 512), (300, 777, 1032, 256), (513, 4096, 64, 1024), (64, 8191, 264, 0),
-    (700, 1536, 512, 768)]
+    (700, 1536, 512, 768), (100, 3000, 520, 0), (128, 700, 264, 0), (65, 33000, 40, 0),
+    (17, 20011, 1000, 0)]
 
 
 @pytest.mark.parametrize("R,V,H,piece", XENT)
