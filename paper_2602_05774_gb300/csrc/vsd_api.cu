@@ -349,6 +349,39 @@ int blocks_per_sm(const void* kernel, int threads, size_t smem) {
     return n;
 }
 
+int resident_clusters(const void* kernel, int threads, size_t smem, int cluster) {
+    if (cluster == 1) return blocks_per_sm(kernel, threads, smem) * device_sm_count();
+    struct Entry { const void* kernel; int dev, threads, cluster; size_t smem; int n; };
+    static Entry seen[256];  // (the oldest makes room)
+    static int used = 0;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    {
+        std::lock_guard<std::mutex> lock(g_cache_mu);
+        for (int i = 0; i < used && i < 256; ++i)
+            if (seen[i].kernel == kernel && seen[i].dev == dev && seen[i].threads == threads &&
+                seen[i].cluster == cluster && seen[i].smem == smem)
+                return seen[i].n;
+    }
+    if (ensure_dyn_smem(kernel, smem) != cudaSuccess) return 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)cluster);
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) return 0;
+    std::lock_guard<std::mutex> lock(g_cache_mu);
+    seen[used % 256] = Entry{kernel, dev, threads, cluster, smem, n};
+    used = used < 511 ? used + 1 : 256;  // (256 entries are in use from then on)
+    return n;
+}
+
 namespace {
 
 // ------------------------------------------------------------ entry bodies

@@ -50,6 +50,9 @@ cudaError_t ensure_dyn_smem(const void* kernel, size_t smem);
 // of dynamic shared memory on the current device (0 on error).
 int blocks_per_sm(const void* kernel, int threads, size_t smem);
 
+// Clusters of `cluster` such blocks that can be resident at once (0 on error).
+int resident_clusters(const void* kernel, int threads, size_t smem, int cluster);
+
 inline size_t table_smem_bytes(int nch) { return (size_t)nch * sizeof(float4); }
 // Dynamic shared memory of a streaming kernel: the TMA ring (vector rows
 // only) followed by the chunk table.

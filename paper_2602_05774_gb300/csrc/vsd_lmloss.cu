@@ -160,7 +160,7 @@ namespace tc = vsd_pair;
 constexpr int BT = 256;
 constexpr int kTileWarps = 8;                  // epilogue warps of a tile
 constexpr int kHalfN = BT / 2;                 // columns of an epilogue warp
-constexpr int kSumBlocks = 8;                  // K blocks of a partial sum of the logits
+constexpr int kSumBlocks = 8;                  // K blocks of a partial sum, at most
 // Registers per thread of the kernels that add partial sums: launched with 168,
 // of which the first warpgroup gives up what the two epilogue groups take
 // (128 (40 + 232 + 232) = 384 * 168).
@@ -211,13 +211,13 @@ struct PairMaps {
     CUtensorMap a, a0, b, o;         // logits: packed rows, hidden, weight; stored tiles
     CUtensorMap gk, gt, wt, ht, ht0; // products: G K- and MN-major; MN-major the weight,
                                      // the packed rows, hidden
-    CUtensorMap dw, dh;
+    CUtensorMap dh;
 };
 struct PairArgs {
     Targets tg;
     int R, K;              // rows of the call, entries of a target list
     int H, V, v0, cols;    // this piece: columns v0 .. v0 + cols - 1
-    int nkh;               // K blocks of the hidden size
+    int nkh, part;         // K blocks of the hidden size, of a partial sum of the logits
     int64_t rpad;
     float c;
     float2* tab;
@@ -317,22 +317,17 @@ template <int MODE, bool FEW> struct Jobs {
 
 __device__ __forceinline__ bool wait_pair(uint64_t* bar, uint32_t parity, PairBars* sb,
                                           int* status) {
-    if (tc::try_wait_cluster(bar, parity)) return true;
-    const uint64_t t0 = global_timer_ns();
-    for (;;) {
-        if (tc::try_wait_cluster(bar, parity)) return true;
-        if (*(volatile int*)&sb->err) return false;
-        if (global_timer_ns() - t0 > kWaitNs) {
-            sb->err = 1;
-            atomicOr(status, VSD_STATUS_TIMEOUT);
-            return false;
-        }
+    if (bounded_wait([&] { return tc::try_wait_cluster(bar, parity); },
+                     [&] { return *(volatile int*)&sb->err != 0; }, kWaitNs))
+        return true;
+    if (!*(volatile int*)&sb->err) {
+        sb->err = 1;
+        atomicOr(status, VSD_STATUS_TIMEOUT);
     }
+    return false;
 }
 __device__ __forceinline__ void drain_pair(uint64_t* bar, uint32_t parity) {
-    const uint64_t t0 = global_timer_ns();
-    while (!tc::try_wait_cluster(bar, parity))
-        if (global_timer_ns() - t0 > kWaitNs) return;
+    bounded_wait([&] { return tc::try_wait_cluster(bar, parity); }, [] { return false; }, kWaitNs);
 }
 
 // First place of a list not below v.
@@ -777,7 +772,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
                 const int kb1 = MODE == kProd ? j.kb1 : a.nkh;
                 int kb = j.kb0;
                 do {  // (a job without K blocks hands on its accumulator unread)
-                    const int end = kParts ? min(kb1, kb + kSumBlocks) : kb1;
+                    const int end = kParts ? min(kb1, kb + a.part) : kb1;
                     const int buf = lt & 1;
                     const uint32_t use = (uint32_t)lt >> 1;
                     if (use > 0 && !wait_pair(&sb->acc_empty[buf], (use - 1) & 1u, sb, status)) {
@@ -849,7 +844,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
             if (MODE == kKeep && kFew) {
                 float x[kFew ? NF / 2 : 1];
                 bool ok = true;
-                for (int kb = 0; ok && kb < a.nkh; kb += kSumBlocks) {
+                for (int kb = 0; ok && kb < a.nkh; kb += a.part) {
                     if (!(ok = ready())) break;
 #pragma unroll
                     for (int g = 0; g < NF / 64; ++g) {
@@ -871,7 +866,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
                                    a.v0 + n0);
                 float x[kHalfN];
                 bool ok = true;
-                for (int kb = 0; ok && kb < a.nkh; kb += kSumBlocks) {
+                for (int kb = 0; ok && kb < a.nkh; kb += a.part) {
                     if (!(ok = ready())) break;
                     const uint32_t t = acc_addr(h0);
 #pragma unroll
@@ -1072,7 +1067,7 @@ static cudaError_t launch_pair(const PairMaps& maps, const PairArgs& a, int64_t 
     cudaError_t e = ensure_dyn_smem((const void*)k_pair<MODE, NF>, smem);
     if (e != cudaSuccess) return e;
     const int64_t pairs = std::max<int64_t>(1, std::min<int64_t>(jobs, device_sm_count() / 2));
-    return launch_dep(k_pair<MODE, NF>, dim3((unsigned)(2 * pairs)), PairCfg<MODE, NF>::kThreads, smem, 1, st,
+        return launch_dep(true, k_pair<MODE, NF>, dim3((unsigned)(2 * pairs)), PairCfg<MODE, NF>::kThreads, smem, 1, st,
                       maps, a);
 }
 
@@ -1083,7 +1078,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     const int R = s.R, V = s.V, H = s.H, K = s.K;
     const bool grads = s.dh || s.dw;
     Targets tg{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
-               at<float>(ws, w.plogp), at<float>(ws, w.w), at<int32_t>(ws, w.rowmap),
+               at<float>(ws, w.plogp), at<float>(ws, w.w), nullptr, at<int32_t>(ws, w.rowmap),
                at<int32_t>(ws, w.rowinv), at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum),
                at<float>(ws, w.wmax), at<float>(ws, w.kappa), at<float>(ws, w.share),
                at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
@@ -1112,7 +1107,6 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
              make_map_sw128(&maps.ht0, hidden, false, R, H, H, BK);
     if (w.keep) ok = ok && make_map_sw128(&maps.o, X, true, w.rpad, w.piece, w.piece, 32);
     else if (grads) ok = ok && make_map_sw128(&maps.o, G, false, w.rpad, w.piece, w.piece, 32);
-    if (s.dw) ok = ok && make_map_sw128(&maps.dw, out.d_weight, false, V, H, H, 32);
     if (s.dh)
         ok = ok && make_map_sw128(&maps.dh, dh, true, (int64_t)w.rpad * w.split, H, H, 32);
     if (!ok) return cudaErrorInvalidValue;
@@ -1126,6 +1120,8 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     a.v0 = 0;
     a.cols = V;
     a.nkh = (H + BK - 1) / BK;
+    const int parts = (a.nkh + kSumBlocks - 1) / kSumBlocks;
+    a.part = (a.nkh + parts - 1) / parts;  // parts of about the same size
     a.rpad = w.rpad;
     a.c = c;
     a.tab = tab;
@@ -1149,7 +1145,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     cudaError_t e = launch_targets(in, tg, scale, out.row_loss, out.logz, w.zero_end, st,
                                    inline_gather ? rg : RowGather{});
     if (e == cudaSuccess && !inline_gather)
-        e = launch_dep(k_gather, dim3((unsigned)std::min<int64_t>(hrows, 4 * device_sm_count())),
+        e = launch_dep(true, k_gather, dim3((unsigned)std::min<int64_t>(hrows, 4 * device_sm_count())),
                        256, 0, 1, st, rg, R, tg);
     if (e != cudaSuccess) return e;
     const int64_t mt = w.rpad / kRowPad, units = (V + kPieceUnit - 1) / kPieceUnit;
@@ -1162,7 +1158,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     if (w.keep) {  // losses and G from the kept logits, a row at a time
         RowArgs ra{};
         ra.tg = tg;
-        ra.rows = R;
+        ra.rows = (int)hrows;
         ra.V = V;
         ra.K = K;
         ra.ldx = ra.ldg = w.piece;
@@ -1172,12 +1168,12 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         ra.row_loss = out.row_loss;
         ra.logz = out.logz;
         ra.same_align = true;
-        e = launch_row_loss<float, bf16, true>(X, G, ra, hrows, kTopMantissa, device_sm_count(),
-                                               ensure_dyn_smem, st);
+        e = launch_row_loss<float, bf16, true>(X, G, ra, kTopMantissa, device_sm_count(),
+                                               resident_clusters, st);
     } else {
         // one row per block while that fills the GPU no more than a few times over
         const int rb = R <= 256 ? 1 : R <= 16384 ? 8 : 32;
-        e = launch_dep(rb == 1 ? k_rows<1> : rb == 8 ? k_rows<8> : k_rows<32>,
+        e = launch_dep(true, rb == 1 ? k_rows<1> : rb == 8 ? k_rows<8> : k_rows<32>,
                        dim3((unsigned)((R + rb - 1) / rb)), 256, 0, 1, st, tab, (int)(2 * units),
                        (int64_t)w.rpad, tg, K, c, T, xk, lse2, coef, out.row_loss, out.logz,
                        at<double>(ws, w.part), grads ? nullptr : out.loss);
@@ -1199,7 +1195,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     }
     if (s.dh && w.split > 1) {
         const unsigned y = (unsigned)std::min<int64_t>(((int64_t)H + 2047) / 2048, 16);
-        e = launch_dep(k_dh_out, dim3((unsigned)R, y), 256, 0, 1, st, dh, w.split, (int64_t)w.rpad,
+        e = launch_dep(true, k_dh_out, dim3((unsigned)R, y), 256, 0, 1, st, dh, w.split, (int64_t)w.rpad,
                        H, tg, kappa, static_cast<bf16*>(out.d_hidden));
     }
     return e;

@@ -6,19 +6,18 @@
 //   g_v = a (2^{(x_v - m) c} / s - sum_k p_k [v = id_k]).
 //
 // Bound by memory: one read of the row, one write of its gradient.  A cluster of
-// up to 8 blocks holds a row in shared memory between the two, a segment each
-// (bulk copies, four barriers so that the first part is worked on while the rest
-// arrives); the blocks' partial sums meet in distributed shared memory.  Small
-// segments keep several blocks on an SM, so that some load while others wait
-// for their cluster or write.  A row too long for the cluster is read twice, in
-// rounds.  A row that does not start on 16 bytes is laid out from the vector
-// boundary below it; its ragged first and last vectors are filled element by
-// element.
+// up to 8 blocks holds a row in shared memory between the two, a segment each;
+// the blocks' partial sums meet in distributed shared memory.  The clusters are
+// persistent, several to an SM, so that some load while others sum or write.  A row too long for the cluster is read twice, in rounds.  A row that
+// does not start on 16 bytes is laid out from the vector boundary below it; its
+// ragged first and last vectors are filled element by element.
 #pragma once
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "vsd.h"
 #include "vsd_common.cuh"
@@ -27,24 +26,19 @@
 namespace vsd {
 namespace {
 
-#ifndef ROW_T
-#define ROW_T 128
-#endif
-#ifndef ROW_SEG
-#define ROW_SEG 32768
-#endif
-constexpr int kRowThreads = ROW_T;
+constexpr int kRowThreads = 128;
 constexpr int kRowWarps = kRowThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kRowBars = 4;
-constexpr int kSegBytes = ROW_SEG;    // a block's segment, where the cluster reaches over the row
+constexpr int kSegBytes = 32768;    // a block's segment, where the cluster reaches over the row
 constexpr int kSegMax = 200 << 10;  // at most
 constexpr uint64_t kRowWaitNs = 2000000000ull;
+static_assert(kRowThreads >= kMaxTeacher, "a thread per target entry");
 
 struct RowArgs {
     Targets tg;
     int rows, V, K, rounds;
-    int vper;            // vectors of a block's segment
+    int vper;            // vectors of a block's segment, whole rounds of its threads
+    bool by4;            // rounds of four vectors
     int64_t ldx, ldg;    // row pitches in elements
     int gcols;           // columns of a gradient row that are written (zero from V on)
     float c, invT;
@@ -82,44 +76,45 @@ __global__ void __launch_bounds__(kRowThreads)
     k_row_loss(const TI* logits, TO* grad, RowArgs a, float top) {
     constexpr int PV = Traits<TI>::kPerVec;
     extern __shared__ __align__(128) unsigned char row_smem[];
+    __shared__ uint64_t bar, xbars[2];
+    __shared__ float2 part[kRowWarps], cpart[2][kMaxCluster];
+    __shared__ float xs[2][kMaxTeacher], ps[2][kMaxTeacher];
+    __shared__ int ids[2][kMaxTeacher];
     uint4* seg = reinterpret_cast<uint4*>(row_smem);
-    __shared__ uint64_t bars[kRowBars];
-    __shared__ float2 part[kRowWarps], cpart[kMaxCluster];
-    __shared__ float xs[kMaxTeacher];
     uint32_t rank, C;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int i = (int)(blockIdx.x / C);
-    const int V = a.V;
-    const TI* x = logits + (size_t)i * a.ldx;
-    const int off = (int)(((uintptr_t)x / sizeof(TI)) % PV);
-    const int nvec = (V + off + PV - 1) / PV;
-    const int in0 = off ? 1 : 0, in1 = (V + off) / PV;  // whole vectors
-    const int stride = (int)C * a.vper;
+    const int V = a.V, stride = (int)C * a.vper;
+    const int first = (int)(blockIdx.x / C), step = (int)(gridDim.x / C);
+    const uint4 none = make_uint4(Traits<TI>::kNegInf, Traits<TI>::kNegInf, Traits<TI>::kNegInf,
+                                  Traits<TI>::kNegInf);
     dep_launch();
     if (tid == 0) {
-        for (int b = 0; b < kRowBars; ++b) mbar_init(&bars[b], 1);
+        mbar_init(&bar, 1);
+        mbar_init(&xbars[0], 1);
+        mbar_init(&xbars[1], 1);
         mbar_init_fence();
     }
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
-    // vectors v0 .. v1 - 1 of the row are this block's in round rd; quarter q of
-    // them is counted on barrier q
-    const int vq = (a.vper + kRowBars - 1) / kRowBars;
-    auto load = [&](int rd) {
+    auto row_of = [&](int i) { return logits + (size_t)i * a.ldx; };
+    auto off_of = [&](const TI* x) { return (int)(((uintptr_t)x / sizeof(TI)) % PV); };
+    // vectors rd stride + rank vper .. of row i, and -inf in the segment's rest
+    // (all of it the first time: a later row's part is at most a vector shorter)
+    auto load = [&](int i, int rd, bool all) {
+        const TI* x = row_of(i);
+        const int off = off_of(x), nvec = (V + off + PV - 1) / PV;
+        const int in0 = off ? 1 : 0, in1 = (V + off) / PV;  // whole vectors
         const int v0 = rd * stride + (int)rank * a.vper, v1 = min(nvec, v0 + a.vper);
         if (tid == 0) {
-            const uint64_t pol = policy_evict_first();
-            for (int q = 0; q < kRowBars; ++q) {
-                const int b = max(v0 + q * vq, in0), e = min(min(v0 + (q + 1) * vq, v0 + a.vper), in1);
-                const uint32_t bytes = e > b ? 16u * (uint32_t)(e - b) : 0u;
-                mbar_expect_tx(&bars[q], bytes);
-                if (bytes)
-                    bulk_g2s(seg + (b - v0), x + ((int64_t)b * PV - off), bytes, &bars[q], pol);
-            }
+            const int lo = max(v0, in0), hi = min(v1, in1);
+            const uint32_t bytes = hi > lo ? 16u * (uint32_t)(hi - lo) : 0u;
+            mbar_expect_tx(&bar, bytes);
+            if (bytes)
+                bulk_g2s(seg + (lo - v0), x + ((int64_t)lo * PV - off), bytes, &bar,
+                         policy_evict_first());
         }
-        // the ragged ends
-        if (warp == 1 && lane < 2 * PV) {
+        if (warp == 1 && lane < 2 * PV) {  // the ragged ends
             const int v = lane < PV ? 0 : nvec - 1, el = lane % PV;
             const int col = v * PV - off + el;
             if (v >= v0 && v < v1 && (v < in0 || v >= in1)) {
@@ -128,86 +123,120 @@ __global__ void __launch_bounds__(kRowThreads)
                 else row_put(d, -INFINITY);
             }
         }
+        const int cnt = max(v1 - v0, 0);
+        if (all || a.rounds > 1) {
+            for (int j = cnt + tid; j < a.vper; j += kRowThreads) seg[j] = none;
+        } else if (tid == 2 && cnt < a.vper) {
+            seg[cnt] = none;
+        }
     };
-    if (!LM) {
-        load(0);  // (these logits were there before the targets' kernel began)
+    auto wait_bounded = [&](uint64_t* bar, uint32_t parity) {
+        if (!bounded_wait([&] { return mbar_try_wait(bar, parity); }, [] { return false; },
+                          kRowWaitNs))
+            atomicOr(a.tg.status, VSD_STATUS_TIMEOUT);
+    };
+    uint32_t phase = 0;  // parity of the next load
+    auto arrived = [&]() {
+        wait_bounded(&bar, phase);
+        phase ^= 1u;
+    };
+    int rows = a.rows, n_rows = a.rows;
+    if (LM) {  // the kernel before this one stored the logits
         dep_wait();
-    } else {
-        dep_wait();
-    }
-    if (LM) {  // the kernel before this one stored the logits (all rows' space may be read)
         if (tid == 0) asm volatile("fence.proxy.async;" ::: "memory");
-        load(0);
+        n_rows = *(const volatile int*)a.tg.nrows;
+        rows = (n_rows + 63) / 64 * 64;
     }
-    const int n_rows = LM ? *(const volatile int*)a.tg.nrows : a.rows;
-    const bool real = i < n_rows;
-    const int r = LM ? (real ? a.tg.rowmap[i] : 0) : i;
-    const int n = real ? a.tg.n[r] : -1;
-    const int32_t* id = a.tg.id + (size_t)r * a.K;
-    const float* p = a.tg.p + (size_t)r * a.K;
-    TO* g = grad ? grad + (size_t)i * a.ldg : nullptr;
-    __syncthreads();  // the barriers and the ragged ends are set
-    bool ok = true;
-    auto arrived = [&](int q, int rd) {
-        if (mbar_try_wait(&bars[q], rd & 1)) return;
-        const uint64_t t0 = global_timer_ns();
-        while (!mbar_try_wait(&bars[q], rd & 1))
-            if (global_timer_ns() - t0 > kRowWaitNs) {
-                ok = false;
-                atomicOr(a.tg.status, VSD_STATUS_TIMEOUT);
-                return;
-            }
+    // (logits in hand were there before the targets' kernel began: the first rows
+    // are loaded and summed while it runs)
+    if (first < rows) load(first, 0, true);
+    if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // all have begun
+
+    // A row's target: thread k holds entry k.  Looked up for the next row while
+    // one is worked on (first the entry, then its logit).
+    int r = 0, n = -1, my_id = 0;
+    float my_p = 0.f, w = 0.f, plogp = 0.f, xv = 0.f, scale = 0.f;
+    auto look = [&](int i) {
+        n = -1;
+        if (i >= n_rows) return;
+        r = LM ? a.tg.rowmap[i] : i;
+        if (tid < a.K) {
+            my_id = a.tg.id[(size_t)r * a.K + tid];
+            my_p = a.tg.p[(size_t)r * a.K + tid];
+        }
+        n = a.tg.n[r];
+        w = a.tg.w[r];
+        plogp = a.tg.plogp[r];
     };
-    float M = 0.f, S = 1.f;
-    int loads = 0;  // of this block so far
-    if (n >= 0) {
-        // the target logits (read before any gradient is written, used after)
-        const float xv = tid < n ? row_value(x[id[tid]]) : 0.f;
+    // (read before the cluster writes any of the row's gradient, used after)
+    auto look_logit = [&](int i) { xv = tid < n ? row_value(row_of(i)[my_id]) : 0.f; };
+
+    for (int i = first, it = 0; i < rows; i += step, ++it) {
+        const int par = it & 1;
+        const TI* x = row_of(i);
+        const int off = off_of(x), nvec = (V + off + PV - 1) / PV;
         float m = -INFINITY, s = 0.f;
+        // N of the segment's vectors, N rounds of threads apart
+        auto take = [&](int j, auto count) {
+            constexpr int N = decltype(count)::value;
+            uint4 q[N];
+#pragma unroll
+            for (int u = 0; u < N; ++u) q[u] = seg[j + u * kRowThreads];
+            float nm = vec_max<TI>(q[0]);
+#pragma unroll
+            for (int u = 1; u < N; ++u) nm = fmaxf(nm, vec_max<TI>(q[u]));
+            nm = fmaxf(nm, m);
+            const float z = nm > -INFINITY ? nm : 0.f;  // (a NaN still reaches the sum)
+            const uint64_t z2 = f2(z, z), c2 = f2(a.c, a.c);
+            uint64_t acc[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                uint64_t v[PV / 2];
+                vec_pairs<TI>(q[u], v);
+#pragma unroll
+                for (int e = 0; e < PV / 2; ++e)
+                    acc[e & 1] = f2add(acc[e & 1], f2_mass(v[e], z2, c2));
+            }
+            float lo, hi;
+            f2split(f2add(acc[0], acc[1]), lo, hi);
+            s = s * ex2((m - z) * a.c) + (lo + hi);
+            m = nm;
+        };
         for (int rd = 0; rd < a.rounds; ++rd) {
             if (rd) {
                 __syncthreads();  // the segment has been read
                 if (tid == 0) fence_proxy_async();
-                load(rd);
-                __syncthreads();
+                load(i, rd, false);
             }
-            const int v0 = rd * stride + (int)rank * a.vper, cnt = min(nvec, v0 + a.vper) - v0;
-            for (int q = 0; q < kRowBars; ++q) {
-                arrived(q, loads);
-                const int e = min((q + 1) * vq, cnt);
-                for (int j = q * vq + tid; j < e; j += 4 * kRowThreads) {
-                    uint4 b[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-                        b[u] = j + u * kRowThreads < e
-                                   ? seg[j + u * kRowThreads]
-                                   : make_uint4(Traits<TI>::kNegInf, Traits<TI>::kNegInf,
-                                                Traits<TI>::kNegInf, Traits<TI>::kNegInf);
-                    const float nm = fmaxf(fmaxf(fmaxf(vec_max<TI>(b[0]), vec_max<TI>(b[1])),
-                                                 fmaxf(vec_max<TI>(b[2]), vec_max<TI>(b[3]))), m);
-                    const float z = nm > -INFINITY ? nm : 0.f;  // (a NaN still reaches the sum)
-                    const uint64_t z2 = f2(z, z), c2 = f2(a.c, a.c);
-                    uint64_t acc = f2(0.f, 0.f);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        uint64_t v[PV / 2];
-                        vec_pairs<TI>(b[u], v);
-#pragma unroll
-                        for (int w = 0; w < PV / 2; ++w) acc = f2add(acc, f2_mass(v[w], z2, c2));
-                    }
-                    float lo, hi;
-                    f2split(acc, lo, hi);
-                    s = s * ex2((m - z) * a.c) + (lo + hi);
-                    m = nm;
-                }
-            }
-            ++loads;
+            __syncthreads();  // what the threads wrote of the segment
+            arrived();
+            if (a.by4)
+                for (int j = tid; j < a.vper; j += 4 * kRowThreads)
+                    take(j, std::integral_constant<int, 4>());
+            else
+                for (int j = tid; j < a.vper; j += kRowThreads)
+                    take(j, std::integral_constant<int, 1>());
         }
-        if (tid < n) xs[tid] = xv;
+        if (it == 0) {
+            if (!LM) dep_wait();
+            scale = LM ? *a.tg.wmax : *a.tg.share;
+            look(i);
+            look_logit(i);
+        }
+        // this row's target
+        const int row = r, cnt_n = n;
+        const float row_w = w, row_plogp = plogp;
+        if (tid < cnt_n) {
+            xs[par][tid] = xv;
+            ps[par][tid] = my_p;
+            ids[par][tid] = my_id;
+        }
         const float wm = warp_max(m), wz = wm > -INFINITY ? wm : 0.f;
         s = warp_sum(s * ex2(((m > -INFINITY ? m : wz) - wz) * a.c));
         if (lane == 0) part[warp] = make_float2(wm, s);
         __syncthreads();
+        if (i + step < rows) look(i + step);
+        float M, S;
         auto join = [&](const float2* e, int cnt) {
             M = e[0].x;
             for (int k = 1; k < cnt; ++k) M = fmaxf(M, e[k].x);
@@ -217,100 +246,116 @@ __global__ void __launch_bounds__(kRowThreads)
         };
         join(part, kRowWarps);
         if (C > 1) {
-            asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // the others have begun
+            // every block's pair to every block, counted in bytes on the
+            // receiver's barrier (a cluster barrier would also wait for this
+            // block's gradient stores); two sets, as a block may be a row ahead
+            // of one still reading
+            if (tid == 0) mbar_expect_tx(&xbars[par], 8u * C);
             if (tid < (int)C) {
-                uint32_t dst;
+                uint32_t dst, bar;
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
-                             : "=r"(dst) : "r"(smem_u32(&cpart[rank])), "r"(tid));
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};"
-                             :: "r"(dst), "f"(M), "f"(S) : "memory");
+                             : "=r"(dst) : "r"(smem_u32(&cpart[par][rank])), "r"(tid));
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                             : "=r"(bar) : "r"(smem_u32(&xbars[par])), "r"(tid));
+                asm volatile(
+                    "st.async.shared::cluster.mbarrier::complete_tx::bytes.b64 [%0], %1, [%2];"
+                    :: "r"(dst), "l"(f2(M, S)), "r"(bar) : "memory");
             }
-            asm volatile("barrier.cluster.arrive.release.aligned;\n\t"
-                         "barrier.cluster.wait.acquire.aligned;" ::: "memory");
-            join(cpart, (int)C);
+            wait_bounded(&xbars[par], (uint32_t)it >> 1 & 1);
+            join(cpart[par], (int)C);
         }
-    } else {
-        // (copies of a row that does not count land before the block may exit)
-        for (int q = 0; q < kRowBars; ++q) arrived(q, 0);
-        if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-    }
-    const float inv = 1.f / S;
-    float coef = 0.f;
-    if (n >= 0) {
-        const float w = a.tg.w[r];
-        if (LM) {
-            const float wm = *a.tg.wmax;
-            coef = wm > 0.f ? top * (w / wm) : 0.f;
-        } else {
-            coef = w * *a.tg.share;
-        }
-    }
-    if (g && (!LM || i < (n_rows + 63) / 64 * 64)) {
-        const bool on = n >= 0;
-        const float cs = coef * inv;
-        const uint64_t m2 = f2(M, M), c2 = f2(a.c, a.c), cs2 = f2(cs, cs);
-        for (int rd = 0; rd < a.rounds; ++rd) {
-            if (on && a.rounds > 1) {
-                __syncthreads();
-                if (tid == 0) fence_proxy_async();
-                load(rd);
-                __syncthreads();
-                for (int q = 0; q < kRowBars; ++q) arrived(q, loads);
-                ++loads;
-            }
-            const int v0 = rd * stride + (int)rank * a.vper, cnt = min(nvec, v0 + a.vper) - v0;
+        const float inv = 1.f / S;
+        const bool on = cnt_n >= 0;
+        const float coef = !on ? 0.f : LM ? (scale > 0.f ? top * (row_w / scale) : 0.f)
+                                          : row_w * scale;
+        TO* g = grad ? grad + (size_t)i * a.ldg : nullptr;
+        if (g) {
+            const float cs = coef * inv;
+            const uint64_t m2 = f2(M, M), c2 = f2(a.c, a.c), cs2 = f2(cs, cs);
+            for (int rd = 0; rd < a.rounds; ++rd) {
+                if (a.rounds > 1) {
+                    __syncthreads();
+                    if (tid == 0) fence_proxy_async();
+                    load(i, rd, false);
+                    __syncthreads();
+                    arrived();
+                }
+                const int v0 = rd * stride + (int)rank * a.vper;
+                const int cnt = min(nvec, v0 + a.vper) - v0;
+                auto vec = [&](int j, float (&o)[PV]) {
+                    uint64_t v[PV / 2];
+                    vec_pairs<TI>(seg[j], v);
+#pragma unroll
+                    for (int e = 0; e < PV / 2; ++e)
+                        f2split(f2mul(f2_mass(v[e], m2, c2), cs2), o[2 * e], o[2 * e + 1]);
+                };
+                // whole vectors, then the ragged ends (or all) by element
+                const int lo = max(0, (off ? 1 : 0) - v0);
+                const int hi = a.same_align ? min(cnt, (V + off) / PV - v0) : lo;
+                TO* gv = g + (int64_t)v0 * PV - off;
+                if (on) {
 #pragma unroll 4
-            for (int j = tid; j < cnt; j += kRowThreads) {
-                uint64_t v[PV / 2];
-                vec_pairs<TI>(on ? seg[j] : make_uint4(0u, 0u, 0u, 0u), v);
-                float o[PV];
-#pragma unroll
-                for (int w = 0; w < PV / 2; ++w) {
-                    float lo, hi;
-                    f2split(f2mul(f2_mass(v[w], m2, c2), cs2), lo, hi);
-                    o[2 * w] = on ? lo : 0.f;
-                    o[2 * w + 1] = on ? hi : 0.f;
-                }
-                const int e0 = (v0 + j) * PV - off;
-                if (a.same_align && e0 >= 0 && e0 + PV <= V) {
-                    row_store<PV>(g + e0, o);
+                    for (int j = lo + tid; j < hi; j += kRowThreads) {
+                        float o[PV];
+                        vec(j, o);
+                        row_store<PV>(gv + j * PV, o);
+                    }
                 } else {
+                    const float o[PV] = {};
+                    for (int j = lo + tid; j < hi; j += kRowThreads) row_store<PV>(gv + j * PV, o);
+                }
+                for (int j = tid; j < cnt; j += kRowThreads) {
+                    if (j >= lo && j < hi) {  // (only the ends are left)
+                        j += (hi - 1 - j) / kRowThreads * kRowThreads;
+                        continue;
+                    }
+                    float o[PV] = {};
+                    if (on) vec(j, o);
+                    const int e0 = (v0 + j) * PV - off;
 #pragma unroll
-                    for (int w = 0; w < PV; ++w)
-                        if (e0 + w >= 0 && e0 + w < V) row_put(g + e0 + w, o[w]);
+                    for (int e = 0; e < PV; ++e)
+                        if (e0 + e >= 0 && e0 + e < V) row_put(g + e0 + e, o[e]);
                 }
             }
+            if (LM && rank == C - 1)
+                for (int v = V + tid; v < a.gcols; v += kRowThreads) row_put(g + v, 0.f);
         }
-        if (LM && rank == C - 1)
-            for (int v = V + tid; v < a.gcols; v += kRowThreads) row_put(g + v, 0.f);
-        __syncthreads();
-        if (tid < n && (tid == 0 || id[tid - 1] != id[tid])) {
+        __syncthreads();  // the segment has been read
+        if (i + step < rows) {
+            if (tid == 0) fence_proxy_async();
+            load(i + step, 0, false);
+        }
+        if (i + step < rows) look_logit(i + step);
+        if (g && tid < cnt_n && (tid == 0 || ids[par][tid - 1] != ids[par][tid])) {
             // the target entries this block wrote as dense ones; equal tokens add
-            const int v = id[tid], j = (v + off) / PV % stride;
+            const int v = ids[par][tid], j = (v + off) / PV % stride;
             if (j / a.vper == (int)rank) {
-                float q = p[tid];
-                for (int k = tid + 1; k < n && id[k] == v; ++k) q += p[k];
-                row_put(g + v, coef * (ex2((xs[tid] - M) * a.c) * inv - q));
+                float q = ps[par][tid];
+                for (int k = tid + 1; k < cnt_n && ids[par][k] == v; ++k) q += ps[par][k];
+                row_put(g + v, coef * (ex2((xs[par][tid] - M) * a.c) * inv - q));
+            }
+        }
+        // the row's loss
+        if (rank == 0 && warp == 0 && on) {
+            float dot = 0.f;
+            for (int k = lane; k < cnt_n; k += 32) dot = fmaf(ps[par][k], xs[par][k] - M, dot);
+            dot = warp_sum(dot);
+            if (lane == 0) {
+                const float l = logf(S), lz = fmaf(M, a.invT, l);
+                if (!isfinite(lz)) atomicOr(a.tg.status, VSD_STATUS_BAD_ROW);
+                a.logz[row] = lz;
+                a.row_loss[row] = row_plogp + (l - dot * a.invT);
             }
         }
     }
-    // the row's loss
-    if (rank != 0 || warp != 0 || n < 0) return;
-    float dot = 0.f;
-    for (int k = lane; k < n; k += 32) dot = fmaf(p[k], xs[k] - M, dot);
-    dot = warp_sum(dot);
-    if (lane == 0) {
-        const float l = logf(S), lz = fmaf(M, a.invT, l);
-        if (!isfinite(lz)) atomicOr(a.tg.status, VSD_STATUS_BAD_ROW);
-        a.logz[r] = lz;
-        a.row_loss[r] = a.tg.plogp[r] + (l - dot * a.invT);
-    }
+    // (a cluster without rows still waits for the kernels before)
+    if (!LM && first >= rows) dep_wait();
 }
 
 // The weighted mean of the rows' losses, in row order, by one block.
 __global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const float* row_loss,
                                                     float* loss) {
-    __shared__ double part[32];
+    __shared__ float part[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     dep_launch();
     dep_wait();
@@ -328,35 +373,42 @@ __global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const flo
         for (int u = 0; u < 4; ++u)
             if (w[u] != 0.f) sum += (double)w[u] * (double)l[u];
     }
-    sum = warp_sum(sum);
-    if (lane == 0) part[warp] = sum;
+    // (a thread's sum in 64 bits, the tree over threads in 32: no long chain)
+    const float t = warp_sum((float)sum);
+    if (lane == 0) part[warp] = t;
     __syncthreads();
     if (warp == 0) {
-        sum = warp_sum(lane < (int)blockDim.x / 32 ? part[lane] : 0.0);
-        if (lane == 0) *loss = (float)(sum / *tg.wsum);
+        const float all = warp_sum(part[lane]);
+        if (lane == 0) *loss = all / (float)*tg.wsum;
     }
 }
 
-// Launches `rows` rows (a.rounds and a.vper are set here).
+// Launches a.rows rows (a.vper, a.by4 and a.rounds are set here).
+// resident: clusters of a kernel's blocks of so many threads and bytes that can
+// be resident at once.
 template <typename TI, typename TO, bool LM>
-cudaError_t launch_row_loss(const TI* logits, TO* grad, RowArgs a, int64_t rows, float top,
-                            int sms, cudaError_t (*smem_opt_in)(const void*, size_t),
+cudaError_t launch_row_loss(const TI* logits, TO* grad, RowArgs a, float top, int sms,
+                            int (*resident)(const void*, int, size_t, int),
                             cudaStream_t st) {
     constexpr int PV = Traits<TI>::kPerVec;
     const int64_t need = ((int64_t)a.V + 2 * PV - 2) / PV;  // vectors, whatever the offset
     int64_t C = 1;
     while (C < kMaxCluster && C * kSegBytes < 16 * need) C *= 2;
     // few rows: spread each over more SMs, while a thread has a vector
-    while (C < kMaxCluster && rows * C < 2 * sms && C * kRowThreads < need) C *= 2;
-    const int64_t vper = std::min<int64_t>((need + C - 1) / C, kSegMax / 16);
+    while (C < kMaxCluster && a.rows * C < 2 * sms && C * kRowThreads < need) C *= 2;
+    int64_t vper = std::min<int64_t>((need + C - 1) / C, kSegMax / 16);
+    a.by4 = vper > 2 * kRowThreads;
+    const int64_t unit = kRowThreads * (a.by4 ? 4 : 1);
+    vper = (vper + unit - 1) / unit * unit;
     a.vper = (int)vper;
     a.rounds = (int)((need + C * vper - 1) / (C * vper));
-    const size_t smem = (size_t)vper * 16;
     auto k = k_row_loss<TI, TO, LM>;
-    cudaError_t e = smem_opt_in((const void*)k, smem);
-    if (e != cudaSuccess) return e;
-    return launch_dep(k, dim3((unsigned)(rows * C)), kRowThreads, smem, (int)C, st, logits, grad, a,
-                      top);
+    const size_t smem = (size_t)vper * 16;
+    const int64_t clusters = resident((const void*)k, kRowThreads, smem, (int)C);
+    if (clusters < 1) return cudaErrorInvalidConfiguration;
+    return launch_dep(a.rows <= clusters, k,
+                      dim3((unsigned)(std::min<int64_t>(clusters, a.rows) * C)), kRowThreads, smem,
+                      (int)C, st, logits, grad, a, top);
 }
 
 }  // namespace

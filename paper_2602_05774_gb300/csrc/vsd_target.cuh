@@ -30,9 +30,12 @@ __device__ __forceinline__ void dep_wait() { asm volatile("griddepcontrol.wait;"
 __device__ __forceinline__ void dep_launch() {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+// early: whether it may.  A persistent grid of clusters that fills the GPU may
+// not: placed around the blocks of the kernel before, not all of its clusters
+// would fit at once, and the rest would run after them.
 template <typename... P, typename... A>
-cudaError_t launch_dep(void (*kern)(P...), dim3 grid, int threads, size_t smem, int cluster,
-                       cudaStream_t st, A&&... args) {
+cudaError_t launch_dep(bool early, void (*kern)(P...), dim3 grid, int threads, size_t smem,
+                       int cluster, cudaStream_t st, A&&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3((unsigned)threads);
@@ -40,13 +43,29 @@ cudaError_t launch_dep(void (*kern)(P...), dim3 grid, int threads, size_t smem, 
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = (unsigned)cluster;
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, P(args)...);
+}
+
+// Waits until done(), at most until give_up() or for limit_ns; whether done()
+// held.  The clock is read once in 256 tries: reading it is slow,
+// and a warp that reads it is late for what it waits for.
+template <typename Done, typename GiveUp>
+__device__ __forceinline__ bool bounded_wait(Done done, GiveUp give_up, uint64_t limit_ns) {
+    uint64_t t0 = 0;
+    for (uint32_t n = 1;; ++n) {
+        if (done()) return true;
+        if (n & 255u) continue;
+        if (give_up()) return false;
+        const uint64_t now = global_timer_ns();
+        if (t0 == 0) t0 = now;
+        else if (now - t0 > limit_ns) return false;
+    }
 }
 
 // What a call says about its targets (device pointers).
@@ -69,7 +88,8 @@ struct Targets {
     float* p;         // [R][K]
     float* plogp;     // [R]
     float* w;         // [R] the row's weight
-    int32_t* rowmap;  // [R] i-th counted row, in row order
+    double* part;     // [R / 4 + 1] scratch where rowmap is null
+    int32_t* rowmap;  // [R] i-th counted row, in row order; null: no list is made
     int32_t* rowinv;  // [R] its inverse, -1: not counted
     int32_t* nrows;   // counted rows
     double* wsum;     // sum of their weights, 1 where that is 0
@@ -88,8 +108,9 @@ __device__ __forceinline__ float teacher_logit(const TargetIn& in, size_t i) {
 }
 
 // The target of one teacher row, by one warp; kPer entries of the list per lane.
+// Returns the row's weight, or -1 where the row does not count.
 template <int kPer>
-__device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg, int r,
+__device__ __forceinline__ float target_row(const TargetIn& in, const Targets& tg, int r,
                                            int lane) {
     constexpr unsigned kAll = 0xffffffffu;
     const float w = in.row_weight ? __ldg(in.row_weight + r) : 1.f;
@@ -106,11 +127,12 @@ __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg
         t[j] = -INFINITY;
         if (k < in.K) {
             const int v = __ldg(in.ids + base + k);
+            const float x = teacher_logit(in, base + k);  // (loaded beside the id)
             if (v >= in.V) far = true;
             if (v >= 0 && v < in.V) {
                 id[j] = v;
-                t[j] = teacher_logit(in, base + k);
-                if (!(t[j] < INFINITY)) bad = true;  // NaN or +inf
+                t[j] = x;
+                if (!(x < INFINITY)) bad = true;  // NaN or +inf
             }
         }
         m = fmaxf(m, t[j]);
@@ -135,21 +157,24 @@ __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg
         for (int j = 0; j < kPer; ++j)
             if (id[j] >= 0) plogp += e[j] / z * ((t[j] - m) * in.invT - lz);
         plogp = warp_sum(plogp);
-        // an entry's place: the number of entries before it by (id, position)
+        // an entry's place: the number of entries before it by (id, position),
+        // packed into one key (an absent entry has the largest)
+        static_assert(kMaxTeacher == 128, "seven bits of position");
+        uint32_t key[kPer];
         int rank[kPer];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) rank[j] = 0;
+        for (int j = 0; j < kPer; ++j) {
+            key[j] = id[j] >= 0 ? (uint32_t)id[j] << 7 | (uint32_t)(lane + 32 * j) : 0xffffffffu;
+            rank[j] = 0;
+        }
 #pragma unroll
         for (int jo = 0; jo < kPer; ++jo) {
             if (32 * jo >= in.K) break;
 #pragma unroll 8
             for (int o = 0; o < 32; ++o) {
-                // (absent entries, -1, sort behind all: as unsigned, the largest)
-                const uint32_t oid = (uint32_t)__shfl_sync(kAll, id[jo], o);
+                const uint32_t other = __shfl_sync(kAll, key[jo], o);
 #pragma unroll
-                for (int j = 0; j < kPer; ++j)
-                    rank[j] += oid < (uint32_t)id[j] ||
-                               (oid == (uint32_t)id[j] && o + 32 * jo < lane + 32 * j);
+                for (int j = 0; j < kPer; ++j) rank[j] += other < key[j];
             }
         }
 #pragma unroll
@@ -167,6 +192,7 @@ __device__ __forceinline__ void target_row(const TargetIn& in, const Targets& tg
         tg.w[r] = w;
         if (bits) atomicOr(tg.status, bits);
     }
+    return counted ? w : -1.f;
 }
 
 // The list of counted rows, the sum and the largest of their weights, by one
@@ -323,6 +349,8 @@ template <int kPer, bool kLabels, bool kOneBlock>
 __global__ void __launch_bounds__(1024)
     k_targets(TargetIn in, Targets tg, double scale, float* row_loss, float* logz, RowGather g) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ float ws[8];
+    __shared__ double sums[8];
     dep_launch();
     int bits = 0;
     auto made = [&](int64_t b, int64_t r1, int (&n)[16], float (&w)[16]) {  // by any block
@@ -361,8 +389,21 @@ __global__ void __launch_bounds__(1024)
             if (r < in.R) label_rows<1>(in, tg, r, r + 1, n, w, &bits);
             if (bits) atomicOr(tg.status, bits);
         } else {
-            const int64_t r = blockIdx.x * (int64_t)8 + warp;
-            if (r < in.R) target_row<kPer>(in, tg, (int)r, lane);
+            const int64_t r = blockIdx.x * (int64_t)(blockDim.x / 32) + warp;
+            const float w = r < in.R ? target_row<kPer>(in, tg, (int)r, lane) : -1.f;
+            if (!tg.rowmap) {  // no list: the blocks' sums are enough
+                if (lane == 0) {
+                    ws[warp] = w;
+                    if (r < in.R && w < 0.f) row_loss[r] = logz[r] = 0.f;
+                }
+                __syncthreads();
+                if (threadIdx.x == 0) {
+                    double sum = 0.0;
+                    for (int i = 0; i < (int)blockDim.x / 32; ++i)
+                        if (ws[i] > 0.f) sum += (double)ws[i];
+                    tg.part[blockIdx.x] = sum;
+                }
+            }
         }
         __shared__ int last;
         __threadfence();
@@ -371,7 +412,22 @@ __global__ void __launch_bounds__(1024)
         __syncthreads();
         if (!last) return;
         __threadfence();
-        scan_rows<16>(tg, in.R, scale, row_loss, logz, made);
+        if (tg.rowmap) {
+            scan_rows<16>(tg, in.R, scale, row_loss, logz, made);
+            return;
+        }
+        double sum = 0.0;
+        for (int b = threadIdx.x; b < (int)gridDim.x; b += blockDim.x) sum += ld_cg(tg.part + b);
+        sum = warp_sum(sum);
+        if (lane == 0) sums[warp] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            sum = 0.0;
+            for (int i = 0; i < (int)blockDim.x / 32; ++i) sum += sums[i];
+            sum = sum > 0.0 ? sum : 1.0;
+            *tg.wsum = sum;
+            *tg.share = (float)(scale / sum);
+        }
     }
 }
 
@@ -398,8 +454,8 @@ inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, double 
              : per == 1 ? k_targets<1, false, false>
              : per == 2 ? k_targets<2, false, false>
                         : k_targets<4, false, false>;
-    const int rows = in.labels ? 256 : 8;  // per block
-    k<<<(unsigned)((in.R + rows - 1) / rows), 256, 0, st>>>(in, tg, scale, row_loss, logz, g);
+    const int threads = in.labels ? 256 : 128, rows = in.labels ? 256 : 4;  // of a block
+    k<<<(unsigned)((in.R + rows - 1) / rows), threads, 0, st>>>(in, tg, scale, row_loss, logz, g);
     return cudaGetLastError();
 }
 

@@ -23,7 +23,7 @@ namespace {
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct TopkWs {
-    size_t status, done, zero_end, nrows, wsum, wmax, kappa, share, n, id, p, plogp, w, total;
+    size_t status, done, zero_end, nrows, wsum, wmax, kappa, share, n, id, p, plogp, w, part, total;
 };
 
 TopkWs topk_ws(int R, int K) {
@@ -48,6 +48,7 @@ TopkWs topk_ws(int R, int K) {
     w.p = take(4 * rk);
     w.plogp = take(4 * r);
     w.w = take(4 * r);
+    w.part = take(8 * (r / 4 + 1));
     w.total = o;
     return w;
 }
@@ -72,7 +73,8 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     const TopkWs w = topk_ws(in.R, in.K);
     RowArgs a{};
     a.tg = Targets{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
-                   at<float>(ws, w.plogp), at<float>(ws, w.w), nullptr, nullptr,
+                   at<float>(ws, w.plogp), at<float>(ws, w.w), at<double>(ws, w.part), nullptr,
+                   nullptr,
                    at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum), at<float>(ws, w.wmax), at<float>(ws, w.kappa),
                    at<float>(ws, w.share),
                    at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
@@ -93,13 +95,13 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     if (bf16)
         e = launch_row_loss<__nv_bfloat16, __nv_bfloat16, false>(
             static_cast<const __nv_bfloat16*>(logits), static_cast<__nv_bfloat16*>(out.grad), a,
-            in.R, 1.f, sms, ensure_dyn_smem, st);
+            1.f, sms, resident_clusters, st);
     else
         e = launch_row_loss<float, float, false>(static_cast<const float*>(logits),
-                                                 static_cast<float*>(out.grad), a, in.R, 1.f, sms,
-                                                 ensure_dyn_smem, st);
+                                                 static_cast<float*>(out.grad), a, 1.f, sms,
+                                                 resident_clusters, st);
     if (e != cudaSuccess) return e;
-    return launch_dep(k_mean_loss, dim3(1), 1024, 0, 1, st, a.tg, in.R, out.row_loss, out.loss);
+    return launch_dep(true, k_mean_loss, dim3(1), 1024, 0, 1, st, a.tg, in.R, out.row_loss, out.loss);
 }
 
 }  // namespace vsd

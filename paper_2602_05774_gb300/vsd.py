@@ -620,7 +620,8 @@ def lmhead_cross_entropy(hidden, weight, labels, ignore_index=-100, row_weight=N
     _check(_lib().vsd_lmhead_cross_entropy(_ptr(hidden), _ptr(weight), R, V, H, _ptr(labels),
                                            int(ignore_index), _ptr(row_weight), float(grad_scale),
                                            int(piece), C.byref(st), _ptr(ws),
-                                           ws.numel() * ws.element_size(), _stream(hidden.device)),
+                                           ws.numel() * ws.element_size(),
+                                           _stream(hidden.device.index)),
            "vsd_lmhead_cross_entropy")
     return out
 
@@ -639,7 +640,7 @@ def lmhead_distill(hidden, weight, teacher_ids, teacher_logits, T=1.0, row_weigh
                                      _ptr(teacher_logits), _dtype_code(teacher_logits), K,
                                      float(T), _ptr(row_weight), float(grad_scale), int(piece),
                                      C.byref(st), _ptr(ws), ws.numel() * ws.element_size(),
-                                     _stream(hidden.device)), "vsd_lmhead_distill")
+                                     _stream(hidden.device.index)), "vsd_lmhead_distill")
     return out
 
 
@@ -670,7 +671,7 @@ def topk_distill(logits, teacher_ids, teacher_logits, T=1.0, row_weight=None, gr
     _check(_lib().vsd_topk_distill(_ptr(logits), _dtype_code(logits), R, V, _ptr(teacher_ids),
                                    _ptr(teacher_logits), _dtype_code(teacher_logits), K, float(T),
                                    _ptr(row_weight), float(grad_scale), C.byref(st), _ptr(ws),
-                                   ws.numel() * ws.element_size(), _stream(dev)),
+                                   ws.numel() * ws.element_size(), _stream(dev.index)),
            "vsd_topk_distill")
     return out
 

@@ -226,6 +226,97 @@ def test_topk_distill(vsd, R, V, K, T, dt, tdt, inplace):
         assert got["grad"].data_ptr() == x.data_ptr()
 
 
+@pytest.mark.parametrize("R,V,dt", [(3000, 301, torch.float32), (2500, 1000, torch.bfloat16),
+                                    (260, 100003, torch.bfloat16), (40, 500009, torch.float32)])
+def test_topk_distill_many_rows(vsd, R, V, dt):
+    """More rows than are resident at once (a cluster takes several in turn, the
+    last ones in rounds), some not counted and full of NaN."""
+    g = torch.Generator(device="cuda").manual_seed(R + V)
+    K, T = 6, 1.5
+    x = (3.0 * torch.randn(R, V, generator=g, device="cuda")).to(dt)
+    ids = torch.randint(0, V, (R, K), generator=g, device="cuda").to(torch.int32)
+    t = 3.0 * torch.randn(R, K, generator=g, device="cuda")
+    x64 = f64(x)
+    off = torch.randperm(R, generator=g, device="cuda")[: R // 4]
+    ids[off] = -1
+    x[off] = NAN
+    got = vsd.topk_distill(x, ids, t, T=T)
+    i64, p, counted = teacher_target(ids, t, T, V)
+    ref = plain(x64, i64, p, counted, torch.ones(R).double(), T)
+    check(got, ref, x64, torch.zeros(()).expand(R, 1).double(), T, dt, ids=i64, p=p)
+    assert (got["grad"][off] == 0).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,skip,gskip", [(1000, 1, 1), (1003, 3, 3), (1000, 1, 0), (1003, 2, 5),
+                                          (16, 1, 0), (2, 1, 1)])
+def test_alignment(vsd, dt, V, skip, gskip):
+    """Logits and gradients that start anywhere (contiguous views into larger
+    tensors), on the same offset from a 16-byte boundary or not: the values of
+    the aligned call, and nothing written outside."""
+    R, K = 9, 2
+    g = torch.Generator(device="cuda").manual_seed(V + skip)
+    pool = torch.randn(R * V + 64, generator=g, device="cuda").to(dt)
+    x = pool[skip:skip + R * V].view(R, V)
+    ids, t = teacher(R, V, K, g)
+    want = vsd.topk_distill(x.clone(), ids, t)
+    gpool = torch.full((R * V + 64,), 7.0, device="cuda", dtype=dt)
+    out = gpool[gskip:gskip + R * V].view(R, V)
+    got = vsd.topk_distill(x, ids, t, grad=out)
+    for name in ("row_loss", "logz", "grad"):
+        a, b = got[name].float(), want[name].float()
+        assert torch.allclose(a, b, rtol=2e-2 if dt == torch.bfloat16 and name == "grad" else 1e-5,
+                              atol=1e-6), name
+    assert (gpool[:gskip] == 7.0).all() and (gpool[gskip + R * V:] == 7.0).all()
+
+
+def test_topk_offsets_past_32_bits(vsd):
+    R, V, K = 20000, 128256, 4
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.empty(R, V, dtype=torch.bfloat16, device="cuda")
+    for r in range(0, R, 1000):
+        x[r:r + 1000] = 3.0 * torch.randn(1000, V, generator=g, device="cuda")
+    ids = torch.randint(0, V, (R, K), generator=g, device="cuda").to(torch.int32)
+    t = torch.randn(R, K, generator=g, device="cuda")
+    got = vsd.topk_distill(x, ids, t)
+    rows = torch.tensor([0, 1, 16743, 16744, R - 2, R - 1], device="cuda")
+    i64, p, counted = teacher_target(ids[rows], t[rows], 1.0, V)
+    x64 = f64(x[rows])
+    ref = plain(x64, i64, p, counted, torch.ones(len(rows)).double(), 1.0)
+    # the mean is over all R rows
+    for name in ("g", "a"):
+        ref[name] = ref[name] * (len(rows) / R)
+    ref["loss"] = torch.tensor(NAN)
+    sub = dict(loss=got["loss"], row_loss=got["row_loss"][rows], logz=got["logz"][rows],
+               grad=got["grad"][rows])
+    check(sub, ref, x64, torch.zeros(()).expand(len(rows), 1).double(), 1.0, torch.bfloat16,
+          ids=i64, p=p)
+
+
+def test_lmhead_offsets_past_32_bits(vsd):
+    """The largest vocabulary with a hidden size that takes the weight past 2^31
+    elements; the last rows of its gradient against float64."""
+    R, V, H = 5, 1 << 20, 2056
+    g = torch.Generator(device="cuda").manual_seed(11)
+    h = torch.randn(R, H, generator=g, device="cuda").to(torch.bfloat16)
+    w = torch.empty(V, H, dtype=torch.bfloat16, device="cuda")
+    for v in range(0, V, 1 << 17):
+        w[v:v + (1 << 17)] = 0.02 * torch.randn(1 << 17, H, generator=g, device="cuda")
+    labels = torch.tensor([0, V - 1, 5, V - 300, 1044479], dtype=torch.int32, device="cuda")
+    got = vsd.lmhead_cross_entropy(h, w, labels)
+    x = torch.cat([(h.double() @ w[v:v + (1 << 17)].double().T).cpu() for v in range(0, V, 1 << 17)],
+                  dim=1)
+    lab = labels.cpu().long()[:, None]
+    ref = plain(x, lab, torch.ones(R, 1).double(), torch.ones(R).bool(), torch.ones(R).double(), 1.0)
+    H64 = f64(h)
+    rows = slice(V - 400, V)
+    tol = 2 * float((H * U) * (H64.abs() @ f64(w[rows]).abs().T).max()) + 2.0 ** -18
+    assert ((f64(got["row_loss"]) - ref["row_loss"]).abs() <= tol).all()
+    want = ref["g"][:, rows].T @ H64
+    bound = 2.0 ** -7 * (ref["g"][:, rows].abs().T @ H64.abs()) + 2.0 ** -126
+    assert ((f64(got["d_weight"][rows]) - want).abs() <= bound).all()
+
+
 def test_gradients_against_differences(vsd):
     """Central differences of the library's own float32 loss along random
     directions (topk_distill on float32 logits): truncation of a third-order
