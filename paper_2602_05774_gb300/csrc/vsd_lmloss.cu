@@ -49,7 +49,7 @@ int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 struct LmWs {
     size_t status, done, zero_end, nrows, wsum, wmax, kappa, share, n, id, p, plogp, w, rowmap, rowinv,
         lse2, coef, xk, tab, part, hid, X, G, dh, total;
-    int rpad, piece, npiece, split;
+    int rpad, hrows, piece, npiece, split;  // rows padded to a tile, to a K block
     bool keep;  // the logits are kept (one piece)
 };
 
@@ -58,11 +58,12 @@ LmWs lm_ws(const LmLossShape& s) {
     const size_t R = (size_t)s.R, RK = R * (size_t)s.K;
     const bool grads = s.dh || s.dw;
     w.rpad = (int)round_up(s.R, kRowPad);
+    w.hrows = (int)round_up(s.R, BK);
     const int64_t vpad = round_up(s.V, kPieceUnit);
-    const int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * (int64_t)w.rpad * kPieceUnit));
+    const int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * (int64_t)w.hrows * kPieceUnit));
     // few rows: the whole vocabulary's logits (4 bytes) and G (2) fit the space
     // of the weight, or are small; they are made once
-    const int64_t whole = 6 * (int64_t)w.rpad * vpad;
+    const int64_t whole = 6 * (int64_t)w.hrows * vpad;
     w.keep = grads && (s.piece ? s.piece >= s.V : true) && w.rpad <= 65280 &&  // (a grid's rows)
              whole <= std::max<int64_t>(2 * (int64_t)s.V * s.H, kKeepBytes);
     int64_t units = vpad / kPieceUnit, per;
@@ -74,15 +75,18 @@ LmWs lm_ws(const LmLossShape& s) {
     }
     w.piece = (int)(per * kPieceUnit);
     w.npiece = (int)((units + per - 1) / per);
-    // parts of a piece's columns in d_hidden where its tiles are few: the count
-    // that leaves the pairs of SMs least idle, each part of 32 K blocks at least
+    // parts of a piece's columns in d_hidden where its tiles are few: the least
+    // time by 0.3 us a K block and 0.1 us to add a part up, each part of 8 K
+    // blocks at least
     const int64_t tiles = (int64_t)(w.rpad / kRowPad) * ((s.H + kRowPad - 1) / kRowPad);
     w.split = 1;
     if (tiles < 2 * kPairs) {
+        const int64_t kp = w.piece / BK;
         double best = 1e30;
-        for (int n = 1; n <= 32 && (n == 1 || w.piece / BK >= 32 * n); ++n) {
-            const double rounds = (double)((tiles * n + kPairs - 1) / kPairs) / n + 0.004 * n;
-            if (rounds < best) best = rounds, w.split = n;
+        for (int64_t n = 1; n <= kPairs && (n == 1 || kp >= 8 * n); ++n) {
+            const double us =
+                0.3 * (double)((kp + n - 1) / n * ((tiles * n + kPairs - 1) / kPairs)) + 0.1 * (double)n;
+            if (us < best) best = us, w.split = (int)n;
         }
     }
     size_t o = 0;
@@ -111,9 +115,9 @@ LmWs lm_ws(const LmLossShape& s) {
     w.xk = take(4 * RK);
     w.tab = take(8 * (size_t)w.rpad * (size_t)units * 2);
     w.part = take(8 * R);
-    w.hid = take(2 * (size_t)w.rpad * s.H);
-    w.X = take(w.keep ? 4 * (size_t)w.rpad * w.piece : 0);
-    w.G = take(grads ? 2 * (size_t)w.rpad * w.piece : 0);
+    w.hid = take(2 * (size_t)w.hrows * s.H);
+    w.X = take(w.keep ? 4 * (size_t)w.hrows * w.piece : 0);
+    w.G = take(grads ? 2 * (size_t)w.hrows * w.piece : 0);
     w.dh = take(s.dh ? 4 * (size_t)w.rpad * s.H * w.split : 0);
     w.total = o;
     return w;
@@ -183,7 +187,8 @@ struct PairBars {
     uint32_t tmem_base;
     int err;
 };
-enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3 };
+// kStats1: kStats where one partial sum spans the hidden size
+enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3, kStats1 = 4 };
 
 // Few rows (NF = 64 or 128 at most): the products with the rows' side are turned
 // round, so that the weight's side is the 256-wide M of the tile and the rows
@@ -193,14 +198,14 @@ enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3 };
 // What the tile costs then is bringing the weight in.  NF = 0: rows are M.
 template <int MODE, int NF> struct PairCfg {
     static constexpr bool kFew = NF > 0;
-    // the products' epilogues (store 64 KB per SM) take as long as eight K
-    // blocks: two sets of warps, one for each accumulator
-    static constexpr int kSets = MODE == kProd ? 2 : 1;
+    // an epilogue takes as long as some ten K blocks: two sets of warps, one for
+    // each accumulator (but where the registers hold partial sums)
+    static constexpr int kSets = MODE == kStats || MODE == kKeep ? 1 : 2;
     static constexpr int kThreads = 32 * (4 + kSets * kTileWarps);
     static constexpr int kFewB = NF / 2 * BK * 2;  // the rows' half of a turned stage
     static constexpr int kStageBytes = MODE == kKeep && kFew ? kHalfBytes + kFewB : 2 * kHalfBytes;
     static constexpr int kStages =
-        MODE == kKeep && kFew ? (NF == 64 ? 9 : 8) : MODE == kProd ? 5 : 6;
+        MODE == kKeep && kFew ? (NF == 64 ? 9 : 8) : kSets == 2 ? 5 : 6;
     static constexpr size_t kSmem =
         1024 + (size_t)kStages * kStageBytes + kSets * kTileWarps * kOutBytes +
         sizeof(PairBars);
@@ -450,6 +455,53 @@ __device__ __forceinline__ void stats_tile(const PairArgs& a, int n0, int row0, 
     if (on)
         a.tab[(int64_t)(n0 / kHalfN) * a.rpad + row] =
             make_float2(m, (t[0] + t[1]) + (t[2] + t[3]));
+}
+
+// The same straight from the accumulator, 32 columns at a time with a running
+// maximum; it is handed back once read.
+template <typename Release>
+__device__ __forceinline__ void stats1_tile(const PairArgs& a, int n0, int row0, int lane,
+                                            int n_rows, uint32_t taddr, const RowList& list,
+                                            Stage& out, Release release) {
+    const int row = row0 + lane;
+    const int lim = a.cols - n0;
+    const int lo = a.v0 + n0, hi = lo + min(kHalfN, lim);
+    int k = list.k, id = min(list.next, hi);
+    float m = -INFINITY, s = 0.f;
+#pragma unroll 1
+    for (int g = 0; g < kHalfN / 32; ++g) {
+        float f[32];
+        read32(taddr + 32u * g, lim - 32 * g, f);
+        if (g == kHalfN / 32 - 1) release();
+        const int end = min(lo + 32 * (g + 1), hi);
+        if (__any_sync(0xffffffffu, id < end)) {
+            unsigned char* box = out.buf;
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+                *chunk_at(box, lane, v) = make_uint4(
+                    __float_as_uint(f[4 * v]), __float_as_uint(f[4 * v + 1]),
+                    __float_as_uint(f[4 * v + 2]), __float_as_uint(f[4 * v + 3]));
+            while (id < end) {
+                const int col = id - lo - 32 * g;
+                a.xk[(size_t)row * a.K + k] =
+                    reinterpret_cast<const float*>(chunk_at(box, lane, col >> 2))[col & 3];
+                ++k;
+                id = k < list.n ? __ldg(list.id + k) : hi;
+            }
+        }
+        float m0 = f[0], m1 = f[1];
+#pragma unroll
+        for (int i = 2; i < 32; i += 2) m0 = fmaxf(m0, f[i]), m1 = fmaxf(m1, f[i + 1]);
+        const float nm = fmaxf(fmaxf(m0, m1), m);
+        const float z = nm > -INFINITY ? nm : 0.f;  // (a NaN still reaches the sum)
+        const float b = -z * a.c;
+        float t[4] = {};
+#pragma unroll
+        for (int i = 0; i < 32; ++i) t[i & 3] += ex2(fmaf(f[i], a.c, b));
+        s = s * ex2((m - z) * a.c) + ((t[0] + t[1]) + (t[2] + t[3]));
+        m = nm;
+    }
+    if (row < n_rows) a.tab[(int64_t)(n0 / kHalfN) * a.rpad + row] = make_float2(m, s);
 }
 
 __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& maps, int n0,
@@ -883,6 +935,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
                 if (!ok) break;
                 if (MODE == kKeep) keep_tile(maps, n0, row0, lane, n_rows, x, out);
                 else stats_tile(a, n0, row0, lane, n_rows, x, list, out);
+            } else if (MODE == kStats1) {
+                const RowList list(a, row0 + lane, row0 + lane < n_rows, a.v0 + n0);
+                if (!ready()) break;
+                stats1_tile(a, n0, row0, lane, n_rows, acc_addr(h0), list, out, release);
             } else if (MODE == kGrad) {
                 const int row = row0 + lane;
                 const bool on = row < n_rows;
@@ -898,6 +954,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
 #pragma unroll
                     for (int g = 0; g < NF / 64; ++g)
                         few_dh_tile(a, j, row0 + lane, f0 + 32 * g, n_rows, acc_addr(f0 + 32 * g));
+                } else if (n0 >= a.H) {
+                    // no column of the output
                 } else if (j.kind == 1) {
                     dh_tile(a, maps, j, n0, row0, lane, n_rows, t, out);
                 } else {
@@ -1019,34 +1077,41 @@ __global__ void __launch_bounds__(256)
     }
 }
 
-// d_hidden of several parts, in the caller's rows: the parts added in order,
-// one rounding (rows not counted are zero already).
-__global__ void k_dh_out(const float* dh, int split, int64_t rpad, int H, Targets tg,
-                         const float* kappa, bf16* out) {
+// d_hidden of several parts, in the caller's rows: the parts added in a fixed
+// order, one rounding (rows not counted are zero already).  A block takes 256
+// columns of a row; warp q every eighth part from q on.
+__global__ void __launch_bounds__(256)
+    k_dh_out(const float* dh, int split, int64_t rpad, int H, Targets tg, const float* kappa,
+             bf16* out) {
+    __shared__ float4 sum[8][2][32];
     dep_launch();
     dep_wait();
     const int r = blockIdx.x, i = tg.rowinv[r];
     const float s = *kappa;
-    for (int h = (blockIdx.y * blockDim.x + threadIdx.x) * 8; h < H;
-         h += gridDim.y * blockDim.x * 8) {
-        if (i >= 0) {
-            uint4 w;
-            float f[8] = {};
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int h = blockIdx.y * 256 + lane * 8;
+    if (i < 0) return;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+    auto add = [](float4& a, const float4& b) { a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w; };
+    if (h < H) {
 #pragma unroll 4
-            for (int q = 0; q < split; ++q) {
-                const float4* p =
-                    reinterpret_cast<const float4*>(dh + ((size_t)q * rpad + i) * H + h);
-                const float4 x = p[0], y = p[1];
-                f[0] += x.x; f[1] += x.y; f[2] += x.z; f[3] += x.w;
-                f[4] += y.x; f[5] += y.y; f[6] += y.z; f[7] += y.w;
-            }
-            uint32_t* o = reinterpret_cast<uint32_t*>(&w);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                o[e] = tc::pack_bf16(__float_as_uint(s * f[2 * e]), __float_as_uint(s * f[2 * e + 1]));
-            *reinterpret_cast<uint4*>(out + (size_t)r * H + h) = w;
+        for (int q = warp; q < split; q += 8) {
+            const float4* p = reinterpret_cast<const float4*>(dh + ((size_t)q * rpad + i) * H + h);
+            add(x, p[0]);
+            add(y, p[1]);
         }
     }
+    sum[warp][0][lane] = x;
+    sum[warp][1][lane] = y;
+    __syncthreads();
+    if (warp || h >= H) return;
+    for (int q = 1; q < 8; ++q) add(x, sum[q][0][lane]), add(y, sum[q][1][lane]);
+    const float f[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        w[e] = tc::pack_bf16(__float_as_uint(s * f[2 * e]), __float_as_uint(s * f[2 * e + 1]));
+    *reinterpret_cast<uint4*>(out + (size_t)r * H + h) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 }  // namespace
@@ -1089,8 +1154,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     float *xk = at<float>(ws, w.xk), *lse2 = at<float>(ws, w.lse2), *coef = at<float>(ws, w.coef),
           *kappa = at<float>(ws, w.kappa), *dh = at<float>(ws, w.dh);
     const float c = (float)(kLog2e / (double)T);
-    // packed rows that may be read: up to a K block
-    const int64_t hrows = round_up(R, BK);
+    const int64_t hrows = w.hrows;
     PairMaps maps;
     memset(&maps, 0, sizeof(maps));
     using vsd_lm::make_map_sw128;
@@ -1101,12 +1165,12 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
               make_map_sw128(&maps.b, weight, false, V, H, H, 128);
     if (grads)
         ok = ok && make_map_sw128(&maps.gk, G, false, hrows, w.piece, w.piece, rbox) &&
-             make_map_sw128(&maps.gt, G, false, w.rpad, w.piece, w.piece, BK) &&
+             make_map_sw128(&maps.gt, G, false, hrows, w.piece, w.piece, BK) &&
              make_map_sw128(&maps.wt, weight, false, V, H, H, BK) &&
              make_map_sw128(&maps.ht, hid, false, hrows, H, H, BK) &&
              make_map_sw128(&maps.ht0, hidden, false, R, H, H, BK);
-    if (w.keep) ok = ok && make_map_sw128(&maps.o, X, true, w.rpad, w.piece, w.piece, 32);
-    else if (grads) ok = ok && make_map_sw128(&maps.o, G, false, w.rpad, w.piece, w.piece, 32);
+    if (w.keep) ok = ok && make_map_sw128(&maps.o, X, true, hrows, w.piece, w.piece, 32);
+    else if (grads) ok = ok && make_map_sw128(&maps.o, G, false, hrows, w.piece, w.piece, 32);
     if (s.dh)
         ok = ok && make_map_sw128(&maps.dh, dh, true, (int64_t)w.rpad * w.split, H, H, 32);
     if (!ok) return cudaErrorInvalidValue;
@@ -1153,7 +1217,8 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     e = nf == 64    ? launch_pair<kKeep, 64>(maps, a, units, st)
         : nf == 128 ? launch_pair<kKeep, 128>(maps, a, units, st)
         : w.keep    ? launch_pair<kKeep>(maps, a, mt * units, st)
-                    : launch_pair<kStats>(maps, a, mt * units, st);
+        : parts == 1 ? launch_pair<kStats1>(maps, a, mt * units, st)
+                     : launch_pair<kStats>(maps, a, mt * units, st);
     if (e != cudaSuccess) return e;
     if (w.keep) {  // losses and G from the kept logits, a row at a time
         RowArgs ra{};
@@ -1194,8 +1259,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         if (e != cudaSuccess) return e;
     }
     if (s.dh && w.split > 1) {
-        const unsigned y = (unsigned)std::min<int64_t>(((int64_t)H + 2047) / 2048, 16);
-        e = launch_dep(true, k_dh_out, dim3((unsigned)R, y), 256, 0, 1, st, dh, w.split, (int64_t)w.rpad,
+        e = launch_dep(true, k_dh_out, dim3((unsigned)R, (unsigned)((H + 255) / 256)), 256, 0, 1, st, dh, w.split, (int64_t)w.rpad,
                        H, tg, kappa, static_cast<bf16*>(out.d_hidden));
     }
     return e;
