@@ -5,6 +5,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <vector>
 
@@ -728,7 +729,12 @@ static vsd_status lmhead_loss_call(const void* hidden, const void* weight, int32
 
 size_t vsd_lmhead_loss_workspace_bytes(int32_t R, int32_t V, int32_t H, int32_t K, int32_t grads,
                                        int32_t piece) {
-    return lmloss_workspace_bytes(LmLossShape{R, V, H, K, grads != 0, grads != 0, piece});
+    // (one gradient alone may be cut into more parts than both together)
+    size_t most = 0;
+    for (int g = grads ? 1 : 0; g <= (grads ? 3 : 0); ++g)
+        most = std::max(most, lmloss_workspace_bytes(
+                                  LmLossShape{R, V, H, K, (g & 1) != 0, (g & 2) != 0, piece}));
+    return most;
 }
 
 vsd_status vsd_lmhead_cross_entropy(const void* hidden, const void* weight, int32_t R, int32_t V,

@@ -37,6 +37,7 @@ constexpr int kPieceUnit = 256;  // a piece's columns are a multiple of this
 constexpr int64_t kPieceBytes = 128ll << 20;
 constexpr int64_t kKeepBytes = 64ll << 20;
 constexpr int64_t kPairs = 76;  // pairs of SMs
+constexpr int kStoreCost = 5;    // K blocks of time that storing a d_weight tile takes at least
 // The operand G is scaled so that the largest weight sits at the top of a
 // binade (1.984 ..), where bf16's relative rounding error is least: a row's
 // target entries are near -w before the draft has learned them, and they
@@ -76,16 +77,21 @@ LmWs lm_ws(const LmLossShape& s) {
     w.piece = (int)(per * kPieceUnit);
     w.npiece = (int)((units + per - 1) / per);
     // parts of a piece's columns in d_hidden where its tiles are few: the least
-    // time by 0.3 us a K block and 0.1 us to add a part up, each part of 8 K
-    // blocks at least
-    const int64_t tiles = (int64_t)(w.rpad / kRowPad) * ((s.H + kRowPad - 1) / kRowPad);
+    // time by 0.3 us a K block (its own rounds, or where d_weight's jobs fill in
+    // the pairs' share of all and part of a job) and, for a part, 0.1 us and its
+    // bytes' way out and back at 6 TB/s; each part of 8 K blocks at least
+    const int64_t ht = (s.H + kRowPad - 1) / kRowPad, tiles = (int64_t)(w.rpad / kRowPad) * ht;
     w.split = 1;
     if (tiles < 2 * kPairs) {
-        const int64_t kp = w.piece / BK;
+        const int64_t kp = w.piece / BK, kr = std::max(w.hrows / BK, kStoreCost);
+        const double share = (double)(tiles * kp + per * ht * kr) / kPairs;
+        const double part_us = 0.1 + 8e-6 / 6.0 * (double)w.hrows * s.H;
         double best = 1e30;
         for (int64_t n = 1; n <= kPairs && (n == 1 || kp >= 8 * n); ++n) {
-            const double us =
-                0.3 * (double)((kp + n - 1) / n * ((tiles * n + kPairs - 1) / kPairs)) + 0.1 * (double)n;
+            const double job = (double)((kp + n - 1) / n);
+            const double blocks = s.dw ? std::max(job, share + 0.25 * job)
+                                       : job * (double)((tiles * n + kPairs - 1) / kPairs);
+            const double us = 0.3 * blocks + part_us * (double)n;
             if (us < best) best = us, w.split = (int)n;
         }
     }
@@ -253,7 +259,6 @@ struct Job {
 // takes its jobs in the opposite order: memory reads and writes at once (48 x
 // 128256 x 4096: FIG).
 constexpr int kFewBlocks = 8;
-constexpr int kStoreCost = 5;  // K blocks of time that storing a d_weight tile takes at least
 template <int MODE, bool FEW> struct Jobs {
     int i, c, C, mt, nt, total;
     int dh, dw, kdh, kp, kr, r, L, fill, step, left;

@@ -516,15 +516,21 @@ def test_pieces_and_repeats_agree(vsd):
             assert torch.equal(a[name], b[name]), (piece, name)
 
 
-def test_one_gradient_or_none(vsd):
-    h, w, g = head(70, 700, 128, 3)
-    labels = torch.randint(0, 700, (70,), generator=g, device="cuda").to(torch.int32)
+@pytest.mark.parametrize("R,V,H", [(70, 700, 128), (40, 60000, 264), (300, 30000, 72)])
+def test_one_gradient_or_none(vsd, R, V, H):
+    """One gradient alone (its sums may be cut into other parts than with both,
+    so d_hidden agrees to a rounding), on a workspace of the size asked for."""
+    h, w, g = head(R, V, H, 3)
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda").to(torch.int32)
+    ws = torch.empty(vsd.lmhead_loss_workspace_bytes(R, V, H), dtype=torch.uint8, device="cuda")
     both = vsd.lmhead_cross_entropy(h, w, labels)
     dh = torch.empty_like(h)
-    a = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=dh, d_weight=False)
-    b = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False)
+    a = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=dh, d_weight=False, workspace=ws)
+    b = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False, workspace=ws)
     n = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False, d_weight=False)
-    assert a["d_hidden"] is dh and torch.equal(dh, both["d_hidden"]) and "d_weight" not in a
+    assert a["d_hidden"] is dh and "d_weight" not in a
+    scale = float(both["d_hidden"].float().abs().max())
+    assert torch.allclose(dh.float(), both["d_hidden"].float(), rtol=2.0 ** -7, atol=1e-5 * scale)
     assert torch.equal(b["d_weight"], both["d_weight"]) and "d_hidden" not in b
     assert torch.equal(n["loss"], both["loss"]) and set(n) == {"loss", "row_loss", "logz"}
 
