@@ -204,9 +204,12 @@ enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3, kStats1 = 4 };
 // What the tile costs then is bringing the weight in.  NF = 0: rows are M.
 template <int MODE, int NF> struct PairCfg {
     static constexpr bool kFew = NF > 0;
-    // an epilogue takes as long as some ten K blocks: two sets of warps, one for
-    // each accumulator (but where the registers hold partial sums)
-    static constexpr int kSets = MODE == kStats || MODE == kKeep ? 1 : 2;
+    // Epilogues that exponentiate take as long as some ten K blocks: two sets of
+    // warps, one for each accumulator, for the gradient and for kStats1 (1715 x
+    // 105611 x 104: 387 us, 418 with one).  kStats and kKeep have no registers
+    // for it; the products gain more from the stage it costs (300 x 32000 x
+    // 4096: 258 us with one set, 266 with two).
+    static constexpr int kSets = MODE == kGrad || MODE == kStats1 ? 2 : 1;
     static constexpr int kThreads = 32 * (4 + kSets * kTileWarps);
     static constexpr int kFewB = NF / 2 * BK * 2;  // the rows' half of a turned stage
     static constexpr int kStageBytes = MODE == kKeep && kFew ? kHalfBytes + kFewB : 2 * kHalfBytes;
@@ -254,15 +257,10 @@ struct Job {
 // tiles (the rows of a group stay in L2 while the weight streams by).
 // Products: the long d_hidden jobs first, dealt round; where they leave some
 // pairs one short, those take d_weight jobs of the same length before the rest
-// is dealt round.  With few rows (kFewBlocks K blocks) d_hidden is bound by
-// reading the weight and d_weight by writing its gradient, so every other pair
-// takes its jobs in the opposite order: memory reads and writes at once (48 x
-// 128256 x 4096: FIG).
-constexpr int kFewBlocks = 8;
+// is dealt round.
 template <int MODE, bool FEW> struct Jobs {
     int i, c, C, mt, nt, total;
-    int dh, dw, kdh, kp, kr, r, L, fill, step, left;
-    bool swap;
+    int dh, dw, kdh, kp, kr, r, L, fill, step;
     __device__ Jobs(const PairArgs& a, int n_rows) {
         c = blockIdx.x >> 1;
         C = gridDim.x >> 1;
@@ -283,9 +281,7 @@ template <int MODE, bool FEW> struct Jobs {
         const int cost = max(kr, kStoreCost);
         L = r ? (kdh + cost / 2) / cost : 0;
         fill = min(dw, (C - r) * L);
-        swap = kr <= kFewBlocks && (c & 1);
-        step = swap ? 1 : 0;
-        left = 3;
+        step = 0;
     }
     __device__ bool next(Job& j) {
         if (MODE != kProd) {
@@ -302,7 +298,7 @@ template <int MODE, bool FEW> struct Jobs {
             return true;
         }
         // steps 0: d_hidden, 1: the d_weight jobs in place of one, 2: the rest
-        for (; left; --left, step = step == 2 ? 0 : step + 1, i = 0) {
+        for (; step < 3; ++step, i = 0) {
             if (step == 0) {
                 const int t = c + i * C;
                 if (t < dh) {
@@ -1241,9 +1237,10 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         e = launch_row_loss<float, bf16, true>(X, G, ra, kTopMantissa, device_sm_count(),
                                                resident_clusters, st);
     } else {
-        // one row per block while that fills the GPU no more than a few times over
-        const int rb = R <= 256 ? 1 : R <= 16384 ? 8 : 32;
-        e = launch_dep(true, rb == 1 ? k_rows<1> : rb == 8 ? k_rows<8> : k_rows<32>,
+        // rows of a block: the 32 threads of each of 8 rows share out its parts; 32
+        // rows (whose reads coalesce fully) once there are blocks enough
+        const int rb = R <= 16384 ? 8 : 32;
+        e = launch_dep(true, rb == 8 ? k_rows<8> : k_rows<32>,
                        dim3((unsigned)((R + rb - 1) / rb)), 256, 0, 1, st, tab, (int)(2 * units),
                        (int64_t)w.rpad, tg, K, c, T, xk, lse2, coef, out.row_loss, out.logz,
                        at<double>(ws, w.part), grads ? nullptr : out.loss);
