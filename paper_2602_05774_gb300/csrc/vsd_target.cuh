@@ -275,39 +275,6 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, double scale
     }
 }
 
-// Rows packed for the LM-head losses: counted rows of hidden [R][H], in order,
-// then zero rows up to a multiple of 64; rows not counted get a zero gradient.
-// Nothing is packed where every row counts.
-struct RowGather {
-    const __nv_bfloat16* hidden;  // null: nothing to do
-    __nv_bfloat16* packed;
-    __nv_bfloat16* d_hidden;      // may be null
-    int H;                        // a multiple of 8
-};
-// One block's share of the rows.
-__device__ __forceinline__ void gather_rows(const RowGather& g, int R, const Targets& tg,
-                                            int block, int blocks) {
-    const int n = *(const volatile int*)tg.nrows;
-    if (n == R) return;
-    const int vecs = g.H / 8;
-    const int64_t step = (int64_t)blocks * blockDim.x, t0 = (int64_t)block * blockDim.x + threadIdx.x;
-    const int64_t end = (int64_t)((n + 63) / 64 * 64) * vecs;
-    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll 4
-    for (int64_t t = t0; t < end; t += step) {
-        const int i = (int)(t / vecs), v = (int)(t - (int64_t)i * vecs);
-        reinterpret_cast<uint4*>(g.packed)[t] =
-            i < n ? __ldg(reinterpret_cast<const uint4*>(
-                              g.hidden + (size_t)ld_cg(tg.rowmap + i) * g.H) + v)
-                  : zero;
-    }
-    if (!g.d_hidden) return;
-    for (int64_t t = t0; t < (int64_t)R * vecs; t += step)
-        if (ld_cg(tg.rowinv + (int)(t / vecs)) < 0) reinterpret_cast<uint4*>(g.d_hidden)[t] = zero;
-}
-// Elements up to which the block that makes the targets packs the rows too.
-constexpr int64_t kInlineGather = 32768;
-
 // Whether a call's targets are made by a single block, which then also clears
 // the status word and the counters: one launch less where latency counts.  A
 // thread takes up to 8 labels, or a warp two teacher lists.
@@ -347,7 +314,7 @@ __device__ __forceinline__ void label_rows(const TargetIn& in, const Targets& tg
 // kPer: entries of a teacher row per lane, or the batch of labels of a thread.
 template <int kPer, bool kLabels, bool kOneBlock>
 __global__ void __launch_bounds__(1024)
-    k_targets(TargetIn in, Targets tg, double scale, float* row_loss, float* logz, RowGather g) {
+    k_targets(TargetIn in, Targets tg, double scale, float* row_loss, float* logz) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __shared__ float ws[8];
     __shared__ double sums[8];
@@ -376,10 +343,6 @@ __global__ void __launch_bounds__(1024)
             for (int r = warp; r < in.R; r += blockDim.x / 32) target_row<kPer>(in, tg, r, lane);
             __syncthreads();
             scan_rows<16>(tg, in.R, scale, row_loss, logz, made);
-        }
-        if (g.hidden) {
-            __syncthreads();
-            gather_rows(g, in.R, tg, 0, 1);
         }
     } else {
         if constexpr (kLabels) {
@@ -434,8 +397,7 @@ __global__ void __launch_bounds__(1024)
 // `zero_bytes` of the workspace from its start (status word, counters) are
 // cleared, then the targets made; scale: of kappa.
 inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, double scale,
-                                  float* row_loss, float* logz, size_t zero_bytes, cudaStream_t st,
-                                  const RowGather& g = RowGather{}) {
+                                  float* row_loss, float* logz, size_t zero_bytes, cudaStream_t st) {
     const int per = in.K <= 32 ? 1 : in.K <= 64 ? 2 : 4;
     if (targets_in_one_block(in)) {
         // threads: a label each while they reach, then four at a time; a warp per list
@@ -445,7 +407,7 @@ inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, double 
                  : per == 1 ? k_targets<1, false, true>
                  : per == 2 ? k_targets<2, false, true>
                             : k_targets<4, false, true>;
-        k<<<1, threads, 0, st>>>(in, tg, scale, row_loss, logz, g);
+        k<<<1, threads, 0, st>>>(in, tg, scale, row_loss, logz);
         return cudaGetLastError();
     }
     cudaError_t e = cudaMemsetAsync(tg.status, 0, zero_bytes, st);
@@ -455,7 +417,7 @@ inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, double 
              : per == 2 ? k_targets<2, false, false>
                         : k_targets<4, false, false>;
     const int threads = in.labels ? 256 : 128, rows = in.labels ? 256 : 4;  // of a block
-    k<<<(unsigned)((in.R + rows - 1) / rows), threads, 0, st>>>(in, tg, scale, row_loss, logz, g);
+    k<<<(unsigned)((in.R + rows - 1) / rows), threads, 0, st>>>(in, tg, scale, row_loss, logz);
     return cudaGetLastError();
 }
 

@@ -91,14 +91,13 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     cudaError_t e = launch_targets(in, a.tg, (double)grad_scale / (double)T, out.row_loss,
                                    out.logz, w.zero_end, st);
     if (e != cudaSuccess) return e;
-    const int sms = device_sm_count();
     if (bf16)
         e = launch_row_loss<__nv_bfloat16, __nv_bfloat16, false>(
             static_cast<const __nv_bfloat16*>(logits), static_cast<__nv_bfloat16*>(out.grad), a,
-            1.f, sms, resident_clusters, st);
+            1.f, resident_clusters, st);
     else
         e = launch_row_loss<float, float, false>(static_cast<const float*>(logits),
-                                                 static_cast<float*>(out.grad), a, 1.f, sms,
+                                                 static_cast<float*>(out.grad), a, 1.f,
                                                  resident_clusters, st);
     if (e != cudaSuccess) return e;
     return launch_dep(true, k_mean_loss, dim3(1), 1024, 0, 1, st, a.tg, in.R, out.row_loss, out.loss);
