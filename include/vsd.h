@@ -388,7 +388,10 @@ vsd_status vsd_lmhead_backward(const void* hidden, const void* weight, int32_t H
  * A counted row whose log-partition is not finite (NaN or +inf logits, or all
  * -inf) sets VSD_STATUS_BAD_ROW; NaN then spreads as in the formulas.
  * Sums are in fp32 or wider and in a fixed order: a call repeated on the same
- * inputs gives the same bits.
+ * inputs gives the same bits.  Outputs may not overlap inputs (but for
+ * vsd_topk_distill's gradient, see there).  An LM-head call's kernels wait for
+ * one another's blocks on the device; a wait that runs out (2 s) sets
+ * VSD_STATUS_TIMEOUT.
  * ------------------------------------------------------------------------ */
 
 /* Outputs (device, caller-owned).  loss, row_loss and logz are required; a NULL
@@ -430,7 +433,7 @@ vsd_status vsd_lmhead_cross_entropy(const void* hidden, const void* weight, int3
                                     void* stream);
 
 /* The LM head distilled from a teacher's top logits, as above with
- * 1 <= K <= 128; T finite and > 0. */
+ * 1 <= K <= 128; T and 1.5 / T finite, T > 0. */
 vsd_status vsd_lmhead_distill(const void* hidden, const void* weight, int32_t R, int32_t V,
                               int32_t H, const int32_t* teacher_ids, const void* teacher_logits,
                               vsd_dtype teacher_dtype, int32_t K, float T,

@@ -705,7 +705,9 @@ static vsd_status check_loss_call(const vsd_loss_outputs* out, const TargetIn& i
          (uintptr_t)in.labels | (uintptr_t)in.ids | (uintptr_t)in.row_weight) & 3)
         return VSD_ERR_INVALID_ARG;
     if ((uintptr_t)in.teacher & (in.teacher_bf16 ? 1 : 3)) return VSD_ERR_INVALID_ARG;
-    if (!(T > 0.f) || !isfinite(T) || !isfinite(grad_scale)) return VSD_ERR_INVALID_ARG;
+    // (log2(e) / T has to be a float too)
+    if (!(T > 0.f) || !isfinite(T) || !isfinite(1.5f / T) || !isfinite(grad_scale))
+        return VSD_ERR_INVALID_ARG;
     return VSD_OK;
 }
 

@@ -86,8 +86,9 @@ LmWs lm_ws(const LmLossShape& s) {
     w.npiece = (int)((units + per - 1) / per);
     // parts of a piece's columns in d_hidden where its tiles are few: the least
     // time by 0.3 us a K block (its own rounds, or where d_weight's jobs fill in
-    // the pairs' share of all and part of a job) and, for a part, 0.1 us and its
-    // bytes' way out and back at 6 TB/s; each part of 8 K blocks at least
+    // the pairs' share of all and part of a job), 6 us for the launch that adds
+    // parts up and, for a part, 0.1 us and its bytes' way out and back at 6 TB/s;
+    // each part of 8 K blocks at least
     const int64_t ht = (s.H + kRowPad - 1) / kRowPad, tiles = (int64_t)(w.rpad / kRowPad) * ht;
     w.split = 1;
     if (tiles < 2 * kPairs) {
@@ -99,7 +100,7 @@ LmWs lm_ws(const LmLossShape& s) {
             const double job = (double)((kp + n - 1) / n);
             const double blocks = s.dw ? std::max(job, share + 0.25 * job)
                                        : job * (double)((tiles * n + kPairs - 1) / kPairs);
-            const double us = 0.3 * blocks + part_us * (double)n;
+            const double us = 0.3 * blocks + (n > 1 ? 6.0 + part_us * (double)n : 0.0);
             if (us < best) best = us, w.split = (int)n;
         }
     }

@@ -42,13 +42,19 @@ cudaError_t launch_dep(bool early, void (*kern)(P...), dim3 grid, int threads, s
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = (unsigned)cluster;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    unsigned n = 0;
+    if (early) {
+        at[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        at[n].id = cudaLaunchAttributeClusterDimension;
+        at[n].val.clusterDim.x = (unsigned)cluster;
+        at[n].val.clusterDim.y = at[n].val.clusterDim.z = 1;
+        ++n;
+    }
     cfg.attrs = at;
-    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kern, P(args)...);
 }
 
@@ -407,8 +413,7 @@ inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, double 
                  : per == 1 ? k_targets<1, false, true>
                  : per == 2 ? k_targets<2, false, true>
                             : k_targets<4, false, true>;
-        k<<<1, threads, 0, st>>>(in, tg, scale, row_loss, logz);
-        return cudaGetLastError();
+        return launch_dep(false, k, dim3(1), threads, 0, 1, st, in, tg, scale, row_loss, logz);
     }
     cudaError_t e = cudaMemsetAsync(tg.status, 0, zero_bytes, st);
     if (e != cudaSuccess) return e;
@@ -417,8 +422,8 @@ inline cudaError_t launch_targets(const TargetIn& in, const Targets& tg, double 
              : per == 2 ? k_targets<2, false, false>
                         : k_targets<4, false, false>;
     const int threads = in.labels ? 256 : 128, rows = in.labels ? 256 : 4;  // of a block
-    k<<<(unsigned)((in.R + rows - 1) / rows), threads, 0, st>>>(in, tg, scale, row_loss, logz);
-    return cudaGetLastError();
+    return launch_dep(false, k, dim3((unsigned)((in.R + rows - 1) / rows)), threads, 0, 1, st, in,
+                      tg, scale, row_loss, logz);
 }
 
 }  // namespace

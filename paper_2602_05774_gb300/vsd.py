@@ -172,6 +172,10 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+def _data_ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _stream(device):
     return C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
 
@@ -562,7 +566,7 @@ def _loss_workspace(need, workspace, device):
     if workspace is None:
         return torch.empty(need, dtype=torch.uint8, device=device)
     _need_cuda(workspace)
-    if workspace.numel() * workspace.element_size() < need:
+    if workspace.nbytes < need:
         raise ValueError("workspace too small")
     return workspace
 
@@ -617,10 +621,10 @@ def lmhead_cross_entropy(hidden, weight, labels, ignore_index=-100, row_weight=N
     _check_row_weight(row_weight, R)
     out, st, ws, R, V, H = _lmhead_loss(hidden, weight, 1, d_hidden, d_weight, piece, workspace,
                                         (labels, row_weight))
-    _check(_lib().vsd_lmhead_cross_entropy(_ptr(hidden), _ptr(weight), R, V, H, _ptr(labels),
-                                           int(ignore_index), _ptr(row_weight), float(grad_scale),
-                                           int(piece), C.byref(st), _ptr(ws),
-                                           ws.numel() * ws.element_size(),
+    _check(_lib().vsd_lmhead_cross_entropy(hidden.data_ptr(), weight.data_ptr(), R, V, H,
+                                           labels.data_ptr(), int(ignore_index),
+                                           _data_ptr(row_weight), float(grad_scale), int(piece),
+                                           C.byref(st), ws.data_ptr(), ws.nbytes,
                                            _stream(hidden.device.index)),
            "vsd_lmhead_cross_entropy")
     return out
@@ -636,10 +640,11 @@ def lmhead_distill(hidden, weight, teacher_ids, teacher_logits, T=1.0, row_weigh
     K = _check_teacher(teacher_ids, teacher_logits, row_weight, R)
     out, st, ws, R, V, H = _lmhead_loss(hidden, weight, K, d_hidden, d_weight, piece, workspace,
                                         (teacher_ids, teacher_logits, row_weight))
-    _check(_lib().vsd_lmhead_distill(_ptr(hidden), _ptr(weight), R, V, H, _ptr(teacher_ids),
-                                     _ptr(teacher_logits), _dtype_code(teacher_logits), K,
-                                     float(T), _ptr(row_weight), float(grad_scale), int(piece),
-                                     C.byref(st), _ptr(ws), ws.numel() * ws.element_size(),
+    _check(_lib().vsd_lmhead_distill(hidden.data_ptr(), weight.data_ptr(), R, V, H,
+                                     teacher_ids.data_ptr(), teacher_logits.data_ptr(),
+                                     _dtype_code(teacher_logits), K, float(T),
+                                     _data_ptr(row_weight), float(grad_scale), int(piece),
+                                     C.byref(st), ws.data_ptr(), ws.nbytes,
                                      _stream(hidden.device.index)), "vsd_lmhead_distill")
     return out
 
@@ -668,10 +673,11 @@ def topk_distill(logits, teacher_ids, teacher_logits, T=1.0, row_weight=None, gr
     ws = _loss_workspace(_topk_bytes(R, V, K), workspace, dev)
     st = LossOutputs(out["loss"].data_ptr(), out["row_loss"].data_ptr(), out["logz"].data_ptr(),
                      None, None, None if g is None else g.data_ptr())
-    _check(_lib().vsd_topk_distill(_ptr(logits), _dtype_code(logits), R, V, _ptr(teacher_ids),
-                                   _ptr(teacher_logits), _dtype_code(teacher_logits), K, float(T),
-                                   _ptr(row_weight), float(grad_scale), C.byref(st), _ptr(ws),
-                                   ws.numel() * ws.element_size(), _stream(dev.index)),
+    _check(_lib().vsd_topk_distill(logits.data_ptr(), _dtype_code(logits), R, V,
+                                   teacher_ids.data_ptr(), teacher_logits.data_ptr(),
+                                   _dtype_code(teacher_logits), K, float(T),
+                                   _data_ptr(row_weight), float(grad_scale), C.byref(st),
+                                   ws.data_ptr(), ws.nbytes, _stream(dev.index)),
            "vsd_topk_distill")
     return out
 

@@ -535,6 +535,25 @@ def test_one_gradient_or_none(vsd, R, V, H):
     assert torch.equal(n["loss"], both["loss"]) and set(n) == {"loss", "row_loss", "logz"}
 
 
+def test_hidden_states_of_paths(vsd):
+    """Hidden states as [B, K, D, H]: rows in their order, the gradient in their
+    shape; a graph that holds a call gives the call's bits."""
+    h, w, g = head(2 * 3 * 8, 500, 64, 12)
+    labels = torch.randint(0, 500, (48,), generator=g, device="cuda").to(torch.int32)
+    flat = vsd.lmhead_cross_entropy(h, w, labels)
+    got = vsd.lmhead_cross_entropy(h.view(2, 3, 8, 64), w, labels)
+    assert got["d_hidden"].shape == (2, 3, 8, 64)
+    assert torch.equal(got["d_hidden"].view(48, 64), flat["d_hidden"])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = vsd.lmhead_cross_entropy(h, w, labels)
+    h.add_(1.0)
+    graph.replay()
+    want = vsd.lmhead_cross_entropy(h, w, labels)
+    for name in want:
+        assert torch.equal(held[name], want[name]), name
+
+
 def test_refusals(vsd):
     h, w, g = head(8, 100, 64, 1)
     labels = torch.zeros(8, dtype=torch.int32, device="cuda")
@@ -564,7 +583,7 @@ def test_refusals(vsd):
         vsd.lmhead_distill(h, w, ids, t.half())
     with pytest.raises(TypeError):
         vsd.topk_distill(x.half(), ids, t)
-    for T in (0.0, -1.0, NAN, float("inf")):
+    for T in (0.0, -1.0, NAN, float("inf"), 1e-39):
         with pytest.raises(vsd.VsdError) as e:
             vsd.topk_distill(x, ids, t, T=T)
         assert e.value.code == 1

@@ -66,9 +66,11 @@ def test_argument_checks_before_any_launch(vsd):
                dict(out=vsd.LossOutputs(p, p, p, p, p + 8, None))):
         assert xent(**kw) == 1, kw
     for kw in (dict(ids=None), dict(t=None), dict(dt=2), dict(K=0), dict(K=129), dict(T=0.0),
-               dict(T=-1.0), dict(T=nan), dict(T=inf), dict(H=4)):
+               dict(T=-1.0), dict(T=nan), dict(T=inf), dict(T=1e-39), dict(H=4),
+               dict(ids=p + 2), dict(t=p + 2)):
         assert distill(**kw) == 1, kw
-    for kw in (dict(x=None), dict(ids=None), dict(t=None), dict(dt=2), dict(tdt=-1), dict(R=0),
+    for kw in (dict(x=None), dict(x=p + 2), dict(ids=None), dict(t=None), dict(dt=2), dict(tdt=-1),
+               dict(R=0),
                dict(V=0), dict(V=(1 << 20) + 1), dict(K=0), dict(K=129), dict(T=0.0), dict(T=nan),
                dict(scale=inf)):
         assert topk(**kw) == 1, kw
