@@ -389,9 +389,9 @@ vsd_status vsd_lmhead_backward(const void* hidden, const void* weight, int32_t H
  * -inf) sets VSD_STATUS_BAD_ROW; NaN then spreads as in the formulas.
  * Sums are in fp32 or wider and in a fixed order: a call repeated on the same
  * inputs gives the same bits.  Outputs may not overlap inputs (but for
- * vsd_topk_distill's gradient, see there).  An LM-head call's kernels wait for
- * one another's blocks on the device; a wait that runs out (2 s) sets
- * VSD_STATUS_TIMEOUT.
+ * vsd_topk_distill's gradient, see there).  The kernels' waits for copies, matrix
+ * instructions and the other blocks of a cluster end after 2 s at most; one that
+ * runs out sets VSD_STATUS_TIMEOUT.
  * ------------------------------------------------------------------------ */
 
 /* Outputs (device, caller-owned).  loss, row_loss and logz are required; a NULL
@@ -444,9 +444,8 @@ vsd_status vsd_lmhead_distill(const void* hidden, const void* weight, int32_t R,
 size_t vsd_topk_distill_workspace_bytes(int32_t R, int32_t V, int32_t K);
 
 /* Distillation from a teacher's top logits on logits in hand, [R][V] of
- * `dtype` (-inf marks a token without mass), with their gradient.  Any V;
- * rows that are 16-byte aligned take the bulk-copy path, others a scalar one
- * with the same results. */
+ * `dtype` (-inf marks a token without mass), with their gradient.  Any
+ * V <= 1048576, rows at any alignment of their type; K and T as above. */
 vsd_status vsd_topk_distill(const void* logits, vsd_dtype dtype, int32_t R, int32_t V,
                             const int32_t* teacher_ids, const void* teacher_logits,
                             vsd_dtype teacher_dtype, int32_t K, float T,

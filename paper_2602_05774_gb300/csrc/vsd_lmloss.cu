@@ -55,8 +55,8 @@ size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct LmWs {
-    size_t status, done, zero_end, nrows, wsum, wmax, kappa, share, n, id, p, plogp, w, rowmap, rowinv,
-        lse2, coef, xk, tab, part, hid, X, G, dh, total;
+    size_t status, done, zero_end, nrows, wsum, wmax, kappa, unit, share, n, id, p, plogp, w,
+        rowmap, rowinv, lse2, coef, xk, tab, part, hid, X, G, dh, total;
     int rpad, hrows, piece, npiece, split;  // rows padded to a tile, to a K block
     bool keep;  // the logits are kept (one piece)
 };
@@ -117,6 +117,7 @@ LmWs lm_ws(const LmLossShape& s) {
     w.wsum = take(8);
     w.wmax = take(4);
     w.kappa = take(4);
+    w.unit = take(4);
     w.share = take(4);
     w.n = take(4 * R);
     w.id = take(4 * RK);
@@ -180,17 +181,17 @@ __global__ void __launch_bounds__(256)
 //              product is for:
 //     logits   A = hidden rows, B = weight rows, both K-major.  kStats: per row
 //              and half tile (max, sum 2^{(x - max) c}) and the target logits
-//              in it.  kKeep: the logits themselves, fp32.  The tensor cores' running sum
-//              truncates, an error that grows with the number of K steps, so
-//              K is summed in parts of 512 that are added up here in fp32
-//              (round to nearest).  kGrad: G, rounded to bf16.
+//              in it.  kKeep: the logits themselves, fp32.  kGrad: G, rounded to
+//              bf16.  The tensor cores' running sum truncates, an error that
+//              grows with the number of K steps, so K is summed in parts of 512
+//              that are added up here in fp32 (round to nearest).
 //     d_hidden A = G (K-major), B = weight (MN-major, as it lies): fp32 sums,
 //              added up over the pieces of the vocabulary by TMA.
 //     d_weight A = G (MN-major), B = hidden (MN-major): one rounding to bf16.
 // What is stored goes through 4 KB of swizzled shared memory per warp and a TMA
-// store.  Every wait is bounded: one that runs out sets
-// VSD_STATUS_TIMEOUT, and the pair winds down, waits for its copies and MMAs
-// in flight and frees its tensor memory.
+// store.  Every wait is bounded: one that runs out sets VSD_STATUS_TIMEOUT, and
+// the pair winds down, waits for its copies and MMAs in flight and frees its
+// tensor memory.
 namespace tc = vsd_pair;
 
 constexpr int BT = 256;
@@ -603,7 +604,8 @@ __device__ __forceinline__ void dh_last_tile(const PairArgs& a, bool none, int n
             uint32_t w[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                w[i] = tc::pack_bf16(__float_as_uint(s * f[2 * i]), __float_as_uint(s * f[2 * i + 1]));
+                w[i] = tc::pack_bf16(__float_as_uint(s * f[2 * i]),
+                                     __float_as_uint(s * f[2 * i + 1]));
             *reinterpret_cast<uint4*>(o + x + 8 * v) = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
@@ -1162,8 +1164,8 @@ static cudaError_t launch_pair(const PairMaps& maps, const PairArgs& a, int64_t 
     cudaError_t e = ensure_dyn_smem((const void*)k_pair<MODE, NF>, smem);
     if (e != cudaSuccess) return e;
     const int64_t pairs = std::max<int64_t>(1, std::min<int64_t>(jobs, device_sm_count() / 2));
-        return launch_dep(true, k_pair<MODE, NF>, dim3((unsigned)(2 * pairs)), PairCfg<MODE, NF>::kThreads, smem, 1, st,
-                      maps, a);
+    return launch_dep(true, k_pair<MODE, NF>, dim3((unsigned)(2 * pairs)),
+                      PairCfg<MODE, NF>::kThreads, smem, 1, st, maps, a);
 }
 
 cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
@@ -1175,8 +1177,8 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     Targets tg{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
                at<float>(ws, w.plogp), at<float>(ws, w.w), nullptr, at<int32_t>(ws, w.rowmap),
                at<int32_t>(ws, w.rowinv), at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum),
-               at<float>(ws, w.wmax), at<float>(ws, w.kappa), at<float>(ws, w.share),
-               at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
+               at<float>(ws, w.wmax), at<float>(ws, w.kappa), at<float>(ws, w.unit),
+               at<float>(ws, w.share), at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
     bf16* hid = at<bf16>(ws, w.hid);
     float* X = at<float>(ws, w.X);
     bf16* G = at<bf16>(ws, w.G);
@@ -1267,9 +1269,8 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         e = launch_row_loss<float, bf16, true>(X, G, ra, kTopMantissa, resident_clusters, st);
     } else {
         e = launch_dep(true, k_rows, dim3((unsigned)((R + kRowsOf - 1) / kRowsOf)), 256, 0, 1, st,
-                       tab, (int)(2 * units),
-                       (int64_t)w.rpad, tg, K, c, T, xk, lse2, coef, out.row_loss, out.logz,
-                       at<double>(ws, w.part), grads ? nullptr : out.loss);
+                       tab, (int)(2 * units), (int64_t)w.rpad, tg, K, c, T, xk, lse2, coef,
+                       out.row_loss, out.logz, at<double>(ws, w.part), grads ? nullptr : out.loss);
     }
     if (e != cudaSuccess || !grads) return e;
     for (int q = 0; q < w.npiece; ++q) {
@@ -1287,8 +1288,9 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         if (e != cudaSuccess) return e;
     }
     if (s.dh && w.split > 1) {
-        e = launch_dep(true, k_dh_out, dim3((unsigned)R, (unsigned)((H + 255) / 256)), 256, 0, 1, st, dh, w.split, (int64_t)w.rpad,
-                       H, tg, kappa, static_cast<bf16*>(out.d_hidden));
+        e = launch_dep(true, k_dh_out, dim3((unsigned)R, (unsigned)((H + 255) / 256)), 256, 0, 1,
+                       st, dh, w.split, (int64_t)w.rpad, H, tg, kappa,
+                       static_cast<bf16*>(out.d_hidden));
     }
     return e;
 }

@@ -10,9 +10,10 @@
 // the blocks' partial sums meet in distributed shared memory.  The clusters are
 // persistent, several to an SM, so that some load while others sum or write.
 // 4096 x 128256 bf16: 0.36 ms a call, 5.9 TB/s (0.86 of a copy); instruction issue
-// is 61 % busy beside it.  A row too long for the cluster is read twice, in rounds.  A row that
-// does not start on 16 bytes is laid out from the vector boundary below it; its
-// ragged first and last vectors are filled element by element.
+// is 61 % busy beside it.  A row too long for the cluster is read twice, in
+// rounds.  A row that does not start on 16 bytes is laid out from the vector
+// boundary below it; its ragged first and last vectors are filled element by
+// element.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -50,7 +51,9 @@ struct RowArgs {
 
 template <typename T> __device__ __forceinline__ float row_value(T x);
 template <> __device__ __forceinline__ float row_value(float x) { return x; }
-template <> __device__ __forceinline__ float row_value(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <> __device__ __forceinline__ float row_value(__nv_bfloat16 x) {
+    return __bfloat162float(x);
+}
 __device__ __forceinline__ void row_put(float* x, float f) { *x = f; }
 __device__ __forceinline__ void row_put(__nv_bfloat16* x, float f) { *x = __float2bfloat16_rn(f); }
 
@@ -66,8 +69,10 @@ template <int N> __device__ __forceinline__ void row_store(__nv_bfloat16* g, con
         const __nv_bfloat162 h = __floats2bfloat162_rn(o[2 * i], o[2 * i + 1]);
         w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
-    if (N == 8) *reinterpret_cast<uint4*>(g) = make_uint4(w[0], w[1], w[2 % (N / 2)], w[3 % (N / 2)]);
-    else *reinterpret_cast<uint2*>(g) = make_uint2(w[0], w[1]);
+    if (N == 8)
+        *reinterpret_cast<uint4*>(g) = make_uint4(w[0], w[1], w[2 % (N / 2)], w[3 % (N / 2)]);
+    else
+        *reinterpret_cast<uint2*>(g) = make_uint2(w[0], w[1]);
 }
 
 // LM: the rows are the LM head's packed ones (row i is original row rowmap[i],
@@ -82,6 +87,7 @@ __global__ void __launch_bounds__(kRowThreads)
     __shared__ float2 part[kRowWarps], cpart[2][kMaxCluster];
     __shared__ float xs[2][kMaxTeacher], ps[2][kMaxTeacher];
     __shared__ int ids[2][kMaxTeacher];
+    __shared__ int dead;  // a wait of this block ran out
     uint4* seg = reinterpret_cast<uint4*>(row_smem);
     uint32_t rank, C;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -96,11 +102,27 @@ __global__ void __launch_bounds__(kRowThreads)
         mbar_init(&bar, 1);
         mbar_init(&xbars[0], 1);
         mbar_init(&xbars[1], 1);
+        dead = 0;
         mbar_init_fence();
     }
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     auto row_of = [&](int i) { return logits + (size_t)i * a.ldx; };
     auto off_of = [&](const TI* x) { return (int)(((uintptr_t)x / sizeof(TI)) % PV); };
+    // Once a wait has run out the results are void: the thread waits and copies
+    // no more, after one more wait for what it had in flight (before a wait for
+    // other blocks none of its copies are).
+    bool lost = false;
+    auto wait_bounded = [&](uint64_t* b, uint32_t parity) {
+        auto done = [&] { return mbar_try_wait(b, parity); };
+        if (lost || bounded_wait(done, [&] { return *(volatile int*)&dead != 0; }, kRowWaitNs))
+            return;
+        lost = true;
+        if (!*(volatile int*)&dead) {
+            dead = 1;
+            atomicOr(a.tg.status, VSD_STATUS_TIMEOUT);
+        }
+        if (tid == 0) bounded_wait(done, [] { return false; }, kRowWaitNs);
+    };
     // vectors rd stride + rank vper .. of row i, and -inf in the segment's rest
     // (all of it the first time: a later row's part is at most a vector shorter)
     auto load = [&](int i, int rd, bool all) {
@@ -108,7 +130,7 @@ __global__ void __launch_bounds__(kRowThreads)
         const int off = off_of(x), nvec = (V + off + PV - 1) / PV;
         const int in0 = off ? 1 : 0, in1 = (V + off) / PV;  // whole vectors
         const int v0 = rd * stride + (int)rank * a.vper, v1 = min(nvec, v0 + a.vper);
-        if (tid == 0) {
+        if (tid == 0 && !lost) {
             const int lo = max(v0, in0), hi = min(v1, in1);
             const uint32_t bytes = hi > lo ? 16u * (uint32_t)(hi - lo) : 0u;
             mbar_expect_tx(&bar, bytes);
@@ -132,11 +154,6 @@ __global__ void __launch_bounds__(kRowThreads)
             seg[cnt] = none;
         }
     };
-    auto wait_bounded = [&](uint64_t* bar, uint32_t parity) {
-        if (!bounded_wait([&] { return mbar_try_wait(bar, parity); }, [] { return false; },
-                          kRowWaitNs))
-            atomicOr(a.tg.status, VSD_STATUS_TIMEOUT);
-    };
     uint32_t phase = 0;  // parity of the next load
     auto arrived = [&]() {
         wait_bounded(&bar, phase);
@@ -157,7 +174,7 @@ __global__ void __launch_bounds__(kRowThreads)
     // A row's target: thread k holds entry k.  Looked up for the next row while
     // one is worked on (first the entry, then its logit).
     int r = 0, n = -1, my_id = 0;
-    float my_p = 0.f, w = 0.f, plogp = 0.f, xv = 0.f, scale = 0.f;
+    float my_p = 0.f, w = 0.f, plogp = 0.f, xv = 0.f, scale = 0.f, unit = 1.f;
     auto look = [&](int i) {
         n = -1;
         if (i >= n_rows) return;
@@ -222,6 +239,7 @@ __global__ void __launch_bounds__(kRowThreads)
         if (it == 0) {
             if (!LM) dep_wait();
             scale = LM ? *a.tg.wmax : *a.tg.share;
+            if (!LM) unit = *a.tg.unit;
             look(i);
             look_logit(i);
         }
@@ -252,8 +270,8 @@ __global__ void __launch_bounds__(kRowThreads)
             // receiver's barrier (a cluster barrier would also wait for this
             // block's gradient stores); two sets, as a block may be a row ahead
             // of one still reading
-            if (tid == 0) mbar_expect_tx(&xbars[par], 8u * C);
-            if (tid < (int)C) {
+            if (tid == 0 && !lost) mbar_expect_tx(&xbars[par], 8u * C);
+            if (tid < (int)C && !lost) {
                 uint32_t dst, bar;
                 asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
                              : "=r"(dst) : "r"(smem_u32(&cpart[par][rank])), "r"(tid));
@@ -269,7 +287,7 @@ __global__ void __launch_bounds__(kRowThreads)
         const float inv = 1.f / S;
         const bool on = cnt_n >= 0;
         const float coef = !on ? 0.f : LM ? (scale > 0.f ? top * (row_w / scale) : 0.f)
-                                          : row_w * scale;
+                                          : row_w * unit * scale;
         TO* g = grad ? grad + (size_t)i * a.ldg : nullptr;
         if (g) {
             const float cs = coef * inv;
@@ -352,6 +370,12 @@ __global__ void __launch_bounds__(kRowThreads)
     }
     // (a cluster without rows still waits for the kernels before)
     if (!LM && first >= rows) dep_wait();
+    // no block ends while another may write to it
+    if (C > 1) {
+        __syncwarp();
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    }
 }
 
 // The weighted mean of the rows' losses, in row order, by one block.
@@ -361,6 +385,7 @@ __global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const flo
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     dep_launch();
     dep_wait();
+    const float unit = *tg.unit;
     double sum = 0.0;
     for (int64_t b = threadIdx.x; b < R; b += 1024 * 4) {
         float w[4], l[4];
@@ -373,7 +398,7 @@ __global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const flo
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (w[u] != 0.f) sum += (double)w[u] * (double)l[u];
+            if (w[u] != 0.f) sum += (double)(w[u] * unit) * (double)l[u];
     }
     // (a thread's sum in 64 bits, the tree over threads in 32: no long chain)
     const float t = warp_sum((float)sum);
@@ -381,7 +406,7 @@ __global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const flo
     __syncthreads();
     if (warp == 0) {
         const float all = warp_sum(part[lane]);
-        if (lane == 0) *loss = all / (float)*tg.wsum;
+        if (lane == 0) *loss = all / (float)(*tg.wsum * (double)unit);
     }
 }
 

@@ -101,10 +101,19 @@ struct Targets {
     double* wsum;     // sum of their weights, 1 where that is 0
     float* wmax;      // the largest of them
     float* kappa;     // a constant of the call times wmax / wsum
-    float* share;     // the same constant / wsum
+    float* unit;      // about 1 / wsum: a power of two, by which weights and their
+                      // sum may be multiplied without rounding
+    float* share;     // that constant / (wsum unit)
     int32_t* done;    // block counter, 0 at the start
     int32_t* status;
 };
+
+// The power of two, within what a float and its inverse reach.
+__device__ __forceinline__ void put_share(const Targets& tg, double scale, double wsum) {
+    const double unit = ldexp(1.0, -max(-126, min(126, ilogb(wsum))));
+    *tg.unit = (float)unit;
+    *tg.share = (float)(scale / (wsum * unit));
+}
 
 __device__ __forceinline__ float teacher_logit(const TargetIn& in, size_t i) {
     if (in.teacher_bf16)
@@ -259,7 +268,7 @@ __device__ __forceinline__ void scan_rows(const Targets& tg, int R, double scale
             *tg.wsum = ws;
             *tg.wmax = wm;
             *tg.kappa = (float)(scale * (double)wm / ws);
-            *tg.share = (float)(scale / ws);
+            put_share(tg, scale, ws);
         }
     }
     for (int64_t b = r0; b < r1; b += kBatch) {
@@ -395,7 +404,7 @@ __global__ void __launch_bounds__(1024)
             for (int i = 0; i < (int)blockDim.x / 32; ++i) sum += sums[i];
             sum = sum > 0.0 ? sum : 1.0;
             *tg.wsum = sum;
-            *tg.share = (float)(scale / sum);
+            put_share(tg, scale, sum);
         }
     }
 }

@@ -23,7 +23,8 @@ namespace {
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 struct TopkWs {
-    size_t status, done, zero_end, nrows, wsum, wmax, kappa, share, n, id, p, plogp, w, part, total;
+    size_t status, done, zero_end, nrows, wsum, wmax, kappa, unit, share, n, id, p, plogp, w, part,
+        total;
 };
 
 TopkWs topk_ws(int R, int K) {
@@ -42,6 +43,7 @@ TopkWs topk_ws(int R, int K) {
     w.wsum = take(8);
     w.wmax = take(4);
     w.kappa = take(4);
+    w.unit = take(4);
     w.share = take(4);
     w.n = take(4 * r);
     w.id = take(4 * rk);
@@ -74,10 +76,9 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     RowArgs a{};
     a.tg = Targets{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
                    at<float>(ws, w.plogp), at<float>(ws, w.w), at<double>(ws, w.part), nullptr,
-                   nullptr,
-                   at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum), at<float>(ws, w.wmax), at<float>(ws, w.kappa),
-                   at<float>(ws, w.share),
-                   at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
+                   nullptr, at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum),
+                   at<float>(ws, w.wmax), at<float>(ws, w.kappa), at<float>(ws, w.unit),
+                   at<float>(ws, w.share), at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
     a.rows = in.R;
     a.V = in.V;
     a.K = in.K;
@@ -100,7 +101,8 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
                                                  static_cast<float*>(out.grad), a, 1.f,
                                                  resident_clusters, st);
     if (e != cudaSuccess) return e;
-    return launch_dep(true, k_mean_loss, dim3(1), 1024, 0, 1, st, a.tg, in.R, out.row_loss, out.loss);
+    return launch_dep(true, k_mean_loss, dim3(1), 1024, 0, 1, st, a.tg, in.R, out.row_loss,
+                      out.loss);
 }
 
 }  // namespace vsd

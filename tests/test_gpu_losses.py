@@ -535,6 +535,29 @@ def test_one_gradient_or_none(vsd, R, V, H):
     assert torch.equal(n["loss"], both["loss"]) and set(n) == {"loss", "row_loss", "logz"}
 
 
+@pytest.mark.parametrize("R", [40, 700])
+@pytest.mark.parametrize("exponent", [-140, -60, 100, 120])
+def test_weights_by_a_factor(vsd, exponent, R):
+    """Weights times a power of two, down to where only denormals hold them and up
+    to where their sum passes a float: the same bits."""
+    g = torch.Generator(device="cuda").manual_seed(R)
+    w = torch.randint(1, 9, (R,), generator=g, device="cuda").float()
+    far = w * 2.0 ** (exponent // 2) * 2.0 ** (exponent - exponent // 2)
+    assert (far > 0).all() and torch.isfinite(far).all()
+    x = torch.randn(R, 333, generator=g, device="cuda")
+    ids = torch.randint(0, 333, (R, 5), generator=g, device="cuda").to(torch.int32)
+    t = torch.randn(R, 5, generator=g, device="cuda")
+    h = torch.randn(R, 64, generator=g, device="cuda").bfloat16()
+    head_w = torch.randn(333, 64, generator=g, device="cuda").bfloat16()
+    for call in (lambda rw: vsd.topk_distill(x, ids, t, row_weight=rw),
+                 lambda rw: vsd.lmhead_distill(h, head_w, ids, t, row_weight=rw),
+                 lambda rw: vsd.lmhead_cross_entropy(h, head_w, ids[:, 0].contiguous(),
+                                                     row_weight=rw)):
+        a, b = call(w), call(far)
+        for name in a:
+            assert torch.equal(a[name], b[name]), name
+
+
 def test_hidden_states_of_paths(vsd):
     """Hidden states as [B, K, D, H]: rows in their order, the gradient in their
     shape; a graph that holds a call gives the call's bits."""
