@@ -13,11 +13,13 @@
 // kept and made once.
 //
 // Bound by the tensor cores for many rows (4096 x 32000 x 4096 with gradients:
-// 2.52 ms for 4.29 TFLOP, 1.70 PFLOP/s, where cuBLAS sustains 1.69), by memory
-// for few (48 x 128256 x 4096: 0.54 ms for the weight read twice and its
-// gradient written, 3.15 GB).
+// 2.51 to 2.56 ms from GPU to GPU for 4.29 TFLOP, 1.68 to 1.71 PFLOP/s, where
+// cuBLAS sustains 1.69), by memory
+// for few (48 x 128256 x 4096: 0.54 ms for the weight read twice and its gradient
+// written, 3.15 GB).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <limits.h>
 #include <stdint.h>
 
@@ -440,6 +442,12 @@ __device__ __forceinline__ void keep_tile(const PairMaps& maps, int n0, int row0
     }
 }
 
+// What is added to x c so that the largest x of a part comes to 0.  Kept finite: a
+// part whose logits are all near a float's lowest value then has no mass, not NaN.
+__device__ __forceinline__ float lift(float m, float c) {
+    return m > -INFINITY ? fminf(-m * c, FLT_MAX) : 0.f;
+}
+
 __device__ __forceinline__ void stats_tile(const PairArgs& a, int n0, int row0, int lane,
                                            int n_rows, float (&x)[kHalfN], const RowList& list,
                                            Stage& out) {
@@ -477,7 +485,7 @@ __device__ __forceinline__ void stats_tile(const PairArgs& a, int n0, int row0, 
 #pragma unroll
     for (int i = 2; i < kHalfN; i += 2) m0 = fmaxf(m0, x[i]), m1 = fmaxf(m1, x[i + 1]);
     const float m = fmaxf(m0, m1);
-    const float b = m > -INFINITY ? -m * a.c : 0.f;  // (a NaN still reaches the sum)
+    const float b = lift(m, a.c);  // (a NaN still reaches the sum)
     float t[4] = {};
 #pragma unroll
     for (int i = 0; i < kHalfN; ++i) t[i & 3] += ex2(fmaf(x[i], a.c, b));
@@ -523,7 +531,7 @@ __device__ __forceinline__ void stats1_tile(const PairArgs& a, int n0, int row0,
         for (int i = 2; i < 32; i += 2) m0 = fmaxf(m0, f[i]), m1 = fmaxf(m1, f[i + 1]);
         const float nm = fmaxf(fmaxf(m0, m1), m);
         const float z = nm > -INFINITY ? nm : 0.f;  // (a NaN still reaches the sum)
-        const float b = -z * a.c;
+        const float b = lift(nm, a.c);
         float t[4] = {};
 #pragma unroll
         for (int i = 0; i < 32; ++i) t[i & 3] += ex2(fmaf(f[i], a.c, b));

@@ -9,7 +9,7 @@
 // up to 8 blocks holds a row in shared memory between the two, a segment each;
 // the blocks' partial sums meet in distributed shared memory.  The clusters are
 // persistent, several to an SM, so that some load while others sum or write.
-// 4096 x 128256 bf16: 0.36 ms a call, 5.9 TB/s (0.86 of a copy); instruction issue
+// 4096 x 128256 bf16: 0.36 ms a call, 5.8 TB/s (0.85 of a copy); instruction issue
 // is 61 % busy beside it.  A row too long for the cluster is read twice, in
 // rounds.  A row that does not start on 16 bytes is laid out from the vector
 // boundary below it; its ragged first and last vectors are filled element by

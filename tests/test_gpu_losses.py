@@ -558,6 +558,36 @@ def test_weights_by_a_factor(vsd, exponent, R):
             assert torch.equal(a[name], b[name]), name
 
 
+@pytest.mark.parametrize("H", [64, 1024])
+@pytest.mark.parametrize("grads", [False, True])
+@pytest.mark.parametrize("piece", [0, 256])
+def test_logits_at_the_lowest_value(vsd, H, grads, piece):
+    """Tokens whose logits come to bfloat16's lowest value, whole tiles of them: as
+    if the vocabulary did not have them."""
+    R, V = 70, 700
+    h, w, g = head(R, V, H, 21)
+    h[:, 0] = 1
+    w[:, 0] = 0
+    labels = torch.randint(0, 128, (R,), generator=g, device="cuda").to(torch.int32)
+    masked = torch.cat((w, w))
+    masked[128:V] = 0
+    masked[V:] = 0
+    masked[128:, 0] = torch.finfo(torch.bfloat16).min
+    got = vsd.lmhead_cross_entropy(h, masked, labels, d_hidden=grads, d_weight=grads, piece=piece)
+    x = f64(h) @ f64(w[:128]).T
+    lz = torch.logsumexp(x, 1)
+    want = lz - x.gather(1, labels.long()[:, None].to(x.device))[:, 0]
+    scale = (f64(h).abs() @ f64(w[:128]).abs().T).max(1).values
+    # fp32 sums of H products, of 128 exponentials, and the logarithm's rounding
+    bound = 2.0 ** -24 * (2 * H * scale + 300 + 8 * lz.abs())
+    assert ((f64(got["row_loss"]) - want).abs() <= bound).all()
+    assert torch.isfinite(got["loss"]).all() and torch.isfinite(got["logz"]).all()
+    if grads:
+        assert torch.isfinite(got["d_hidden"].float()).all()
+        assert torch.isfinite(got["d_weight"].float()).all()
+        assert (got["d_weight"][128:] == 0).all()
+
+
 def test_hidden_states_of_paths(vsd):
     """Hidden states as [B, K, D, H]: rows in their order, the gradient in their
     shape; a graph that holds a call gives the call's bits."""
