@@ -14,9 +14,8 @@
 //
 // Bound by the tensor cores for many rows (4096 x 32000 x 4096 with gradients:
 // 2.51 to 2.56 ms from GPU to GPU for 4.29 TFLOP, 1.68 to 1.71 PFLOP/s, where
-// cuBLAS sustains 1.69), by memory
-// for few (48 x 128256 x 4096: 0.54 ms for the weight read twice and its gradient
-// written, 3.15 GB).
+// cuBLAS sustains 1.69), by memory for few (48 x 128256 x 4096: 0.54 ms for the
+// weight read twice and its gradient written, 3.15 GB).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <float.h>
