@@ -524,6 +524,7 @@ __device__ __forceinline__ void stats1_tile(const PairArgs& a, int n0, int row0,
                 ++k;
                 id = k < list.n ? __ldg(list.id + k) : hi;
             }
+            __syncwarp();  // (the lanes' entries differ; tensor memory is read by whole warps)
         }
         float m0 = f[0], m1 = f[1];
 #pragma unroll
@@ -593,6 +594,7 @@ __device__ __forceinline__ void dh_last_tile(const PairArgs& a, bool none, int n
 #pragma unroll 1
     for (int g = 0; g < kHalfN / 32; ++g) {
         uint32_t u[32];
+        __syncwarp();  // (rows past the last leave the rest out)
         tc::tmem_ld32(taddr + 32u * g, u);
         const int x = n0 + 32 * g;
         if (!on) continue;
@@ -653,6 +655,7 @@ __device__ __forceinline__ void few_keep_tile(const PairArgs& a, int col, int i0
 __device__ __forceinline__ void few_dh_tile(const PairArgs& a, const Job& j, int col, int i0,
                                             int n_rows, uint32_t taddr) {
     uint32_t u[32];
+    __syncwarp();  // (columns past the last leave the rest out)
     tc::tmem_ld32(taddr, u);
     if (col >= a.H) return;
     if (a.split == 1) {

@@ -105,6 +105,7 @@ __global__ void __launch_bounds__(kRowThreads)
         dead = 0;
         mbar_init_fence();
     }
+    __syncwarp();  // (the barrier is one instruction of the whole warp)
     if (C > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
     auto row_of = [&](int i) { return logits + (size_t)i * a.ldx; };
     auto off_of = [&](const TI* x) { return (int)(((uintptr_t)x / sizeof(TI)) % PV); };
@@ -169,6 +170,7 @@ __global__ void __launch_bounds__(kRowThreads)
     // (logits in hand were there before the targets' kernel began: the first rows
     // are loaded and summed while it runs)
     if (first < rows) load(first, 0, true);
+    __syncwarp();
     if (C > 1) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");  // all have begun
 
     // A row's target: thread k holds entry k.  Looked up for the next row while

@@ -646,3 +646,20 @@ def test_refusals(vsd):
     with pytest.raises(vsd.VsdError) as e:
         vsd.lmhead_cross_entropy(h, w, labels, grad_scale=NAN)
     assert e.value.code == 1
+
+
+@pytest.mark.parametrize("R,V,H,K,piece", [(130, 600, 200, 3, 256), (100, 700, 200, 3, 0),
+                                           (65, 520, 72, 1, 0), (33, 3000, 456, 9, 1024)])
+def test_lanes_that_differ(vsd, R, V, H, K, piece):
+    """Warps whose lanes part ways between two reads of tensor memory: a list entry
+    in one row of 32 alone, rows past the last, columns past the hidden size."""
+    h, w, g = head(R, V, H, 700 + R, gain=1.0 / H ** 0.5)
+    ids, t = teacher(R, V, K, g)
+    r = torch.arange(R, device="cuda")[:, None]
+    ids = torch.where(r % 32 == 5, ids, ids % 8)  # the others' entries: the first columns
+    got = vsd.lmhead_distill(h, w, ids, t, piece=piece)
+    i64, p, counted = teacher_target(ids, t, 1.0, V)
+    H64, W64 = f64(h), f64(w)
+    x = H64 @ W64.T
+    ref = plain(x, i64, p, counted, torch.ones(R).double(), 1.0)
+    check(got, ref, x, logit_bound(H64, W64), 1.0, torch.bfloat16, H64, W64, i64, p)
