@@ -18,7 +18,6 @@
 // weight read twice and its gradient written, 3.15 GB).
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
-#include <float.h>
 #include <limits.h>
 #include <stdint.h>
 
@@ -57,7 +56,7 @@ int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct LmWs {
     size_t status, done, zero_end, nrows, wsum, wmax, kappa, unit, share, n, id, p, plogp, w,
-        rowmap, rowinv, lse2, coef, xk, tab, part, hid, X, G, dh, total;
+        rowmap, rowinv, top, coef, coefs, xk, tab, part, hid, X, G, dh, total;
     int rpad, hrows, piece, npiece, split;  // rows padded to a tile, to a K block
     bool keep;  // the logits are kept (one piece)
 };
@@ -127,8 +126,9 @@ LmWs lm_ws(const LmLossShape& s) {
     w.w = take(4 * R);
     w.rowmap = take(4 * R);
     w.rowinv = take(4 * R);
-    w.lse2 = take(4 * (size_t)w.rpad);
+    w.top = take(4 * (size_t)w.rpad);
     w.coef = take(4 * (size_t)w.rpad);
+    w.coefs = take(4 * (size_t)w.rpad);
     w.xk = take(4 * RK);
     w.tab = take(8 * (size_t)w.rpad * (size_t)units * 2);
     w.part = take(8 * R);
@@ -265,7 +265,7 @@ struct PairArgs {
     float c;
     float2* tab;
     float* xk;
-    const float *lse2, *coef, *kappa;
+    const float *top, *coef, *coefs, *kappa;  // a row's largest logit, coefficient, the same / S
     int split;             // d_hidden: parts of the piece's columns
     int first, last;       // first and last piece
     int want_dh, want_dw;
@@ -441,10 +441,18 @@ __device__ __forceinline__ void keep_tile(const PairMaps& maps, int n0, int row0
     }
 }
 
-// What is added to x c so that the largest x of a part comes to 0.  Kept finite: a
-// part whose logits are all near a float's lowest value then has no mass, not NaN.
-__device__ __forceinline__ float lift(float m, float c) {
-    return m > -INFINITY ? fminf(-m * c, FLT_MAX) : 0.f;
+// sum 2^{(x - z) c} of N logits.  The difference is taken first, as it is exact near
+// the maximum z: a product z c rounded by itself is off by half an ulp of z c, which
+// the table's z would not know of.
+template <int N> __device__ __forceinline__ float masses(const float (&x)[N], float z, float c) {
+    const uint64_t z2 = f2(z, z), c2 = f2(c, c);
+    uint64_t t[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+#pragma unroll
+    for (int i = 0; i < N; i += 2)
+        t[i >> 1 & 1] = f2add(t[i >> 1 & 1], f2_mass(f2(x[i], x[i + 1]), z2, c2));
+    float lo, hi;
+    f2split(f2add(t[0], t[1]), lo, hi);
+    return lo + hi;
 }
 
 __device__ __forceinline__ void stats_tile(const PairArgs& a, int n0, int row0, int lane,
@@ -484,13 +492,8 @@ __device__ __forceinline__ void stats_tile(const PairArgs& a, int n0, int row0, 
 #pragma unroll
     for (int i = 2; i < kHalfN; i += 2) m0 = fmaxf(m0, x[i]), m1 = fmaxf(m1, x[i + 1]);
     const float m = fmaxf(m0, m1);
-    const float b = lift(m, a.c);  // (a NaN still reaches the sum)
-    float t[4] = {};
-#pragma unroll
-    for (int i = 0; i < kHalfN; ++i) t[i & 3] += ex2(fmaf(x[i], a.c, b));
-    if (on)
-        a.tab[(int64_t)(n0 / kHalfN) * a.rpad + row] =
-            make_float2(m, (t[0] + t[1]) + (t[2] + t[3]));
+    const float s = masses(x, m > -INFINITY ? m : 0.f, a.c);  // (a NaN still reaches the sum)
+    if (on) a.tab[(int64_t)(n0 / kHalfN) * a.rpad + row] = make_float2(m, s);
 }
 
 // The same straight from the accumulator, 32 columns at a time with a running
@@ -531,21 +534,21 @@ __device__ __forceinline__ void stats1_tile(const PairArgs& a, int n0, int row0,
         for (int i = 2; i < 32; i += 2) m0 = fmaxf(m0, f[i]), m1 = fmaxf(m1, f[i + 1]);
         const float nm = fmaxf(fmaxf(m0, m1), m);
         const float z = nm > -INFINITY ? nm : 0.f;  // (a NaN still reaches the sum)
-        const float b = lift(nm, a.c);
-        float t[4] = {};
-#pragma unroll
-        for (int i = 0; i < 32; ++i) t[i & 3] += ex2(fmaf(f[i], a.c, b));
-        s = s * ex2((m - z) * a.c) + ((t[0] + t[1]) + (t[2] + t[3]));
+        s = s * ex2((m - z) * a.c) + masses(f, z, a.c);
         m = nm;
     }
     if (row < n_rows) a.tab[(int64_t)(n0 / kHalfN) * a.rpad + row] = make_float2(m, s);
 }
 
+// The row's G = cs 2^{(x - z) c} - cf p, with z the row's largest logit and cs = cf / S
+// (by difference here too: 2^{x c - lse} would round the log-partition).
 __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& maps, int n0,
                                           int row0, int lane, int n_rows, uint32_t taddr,
-                                          const RowList& list, float cf, float l, Stage& out) {
+                                          const RowList& list, float cf, float cs, float z,
+                                          Stage& out) {
     const int row = row0 + lane;
     const bool on = row < n_rows;
+    const uint64_t z2 = f2(z, z), c2 = f2(a.c, a.c), cs2 = f2(cs, cs);
     const int lo = a.v0 + n0;
     int k = list.k;
     // rows up to the next K block of d_weight are written (zero past the last)
@@ -560,9 +563,9 @@ __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& map
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float lo_ = on ? cf * ex2(fmaf(f[2 * i], a.c, -l)) : 0.f;
-                const float hi_ = on ? cf * ex2(fmaf(f[2 * i + 1], a.c, -l)) : 0.f;
-                w[i] = tc::pack_bf16(__float_as_uint(lo_), __float_as_uint(hi_));
+                float e0, e1;
+                f2split(f2mul(f2_mass(f2(f[2 * i], f[2 * i + 1]), z2, c2), cs2), e0, e1);
+                w[i] = on ? tc::pack_bf16(__float_as_uint(e0), __float_as_uint(e1)) : 0u;
             }
 #pragma unroll
             for (int v = 0; v < 4; ++v)
@@ -577,7 +580,7 @@ __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& map
             float p = __ldg(list.p + k++);
             while (k < list.n && __ldg(list.id + k) == base + col) p += __ldg(list.p + k++);
             reinterpret_cast<bf16*>(chunk_at(box, lane, col >> 3))[col & 7] =
-                __float2bfloat16_rn(cf * (ex2(fmaf(x, a.c, -l)) - p));
+                __float2bfloat16_rn(fmaf(cs, ex2((x - z) * a.c), -(cf * p)));
         }
         out.store(&maps.o, n0 + 64 * g, row0, inside);
     }
@@ -983,9 +986,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
                 const int row = row0 + lane;
                 const bool on = row < n_rows;
                 const RowList list(a, row, on, a.v0 + n0);
-                const float cf = on ? __ldg(a.coef + row) : 0.f, l = on ? __ldg(a.lse2 + row) : 0.f;
+                const float cf = on ? __ldg(a.coef + row) : 0.f;
+                const float cs = on ? __ldg(a.coefs + row) : 0.f, z = on ? __ldg(a.top + row) : 0.f;
                 if (!ready()) break;
-                grad_tile(a, maps, n0, row0, lane, n_rows, acc_addr(h0), list, cf, l, out);
+                grad_tile(a, maps, n0, row0, lane, n_rows, acc_addr(h0), list, cf, cs, z, out);
                 release();
             } else {
                 if (!ready()) break;
@@ -1027,9 +1031,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
 // in block order by the last block to finish.
 constexpr int kRowsOf = 8;
 __global__ void __launch_bounds__(256)
-    k_rows(const float2* tab, int ntab, int64_t stride, Targets tg, int K, float c, float T,
-           const float* xk, float* lse2, float* coef, float* row_loss, float* logz, double* part,
-           float* loss) {
+    k_rows(const float2* tab, int ntab, int64_t stride, Targets tg, int K, float c, double invT,
+           const float* xk, float* top, float* coef, float* coefs, float* row_loss, float* logz,
+           double* part, float* loss) {
     constexpr int RB = kRowsOf;
     constexpr int P = 256 / RB;
     __shared__ float2 ms[8][RB];
@@ -1067,8 +1071,12 @@ __global__ void __launch_bounds__(256)
                                             : make_float2(-INFINITY, 0.f);
                 join(e, 8);
             }
+        // sum p x as ref + sum p (x - ref) with the first entry's logit ref: the
+        // probabilities add up to 1 only to a float's rounding, which x would multiply
+        const float x0 = on ? xk[(size_t)i * K] : 0.f;
+        const double ref = x0 > -INFINITY ? (double)x0 : 0.0;
         for (int k = pt; k < n; k += P)
-            dot += (double)tg.p[(size_t)r * K + k] * (double)xk[(size_t)i * K + k];
+            dot += (double)tg.p[(size_t)r * K + k] * ((double)xk[(size_t)i * K + k] - ref);
 #pragma unroll
         for (int o = RB; o < 32; o <<= 1) {
             const float2 e = make_float2(__shfl_xor_sync(0xffffffffu, m, o),
@@ -1085,13 +1093,16 @@ __global__ void __launch_bounds__(256)
 #pragma unroll
                 for (int u = 1; u < 8; ++u) e[u - 1] = ms[u][q], dot += dots[u][q];
                 join(e, 7);
-                const double lz = (double)m / (double)T + (double)logf(s);
+                const double l = (double)logf(s), lz = (double)m * invT + l;
                 if (!isfinite(lz)) atomicOr(tg.status, VSD_STATUS_BAD_ROW);
-                const float rl = (float)((double)plogp + lz - dot / (double)T);
+                const float rl =
+                    (float)((double)plogp + l + (((double)m - ref) - dot) * invT);
                 logz[r] = (float)lz;
                 row_loss[r] = rl;
-                lse2[i] = (float)(lz * kLog2e);
-                coef[i] = wm > 0.f ? kTopMantissa * (w / wm) : 0.f;
+                const float cf = wm > 0.f ? kTopMantissa * (w / wm) : 0.f;
+                top[i] = m;
+                coef[i] = cf;
+                coefs[i] = cf / s;
                 if (w != 0.f) wloss = (double)w * (double)rl;
             }
             wloss = warp_sum(wloss);
@@ -1193,8 +1204,9 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     float* X = at<float>(ws, w.X);
     bf16* G = at<bf16>(ws, w.G);
     float2* tab = at<float2>(ws, w.tab);
-    float *xk = at<float>(ws, w.xk), *lse2 = at<float>(ws, w.lse2), *coef = at<float>(ws, w.coef),
-          *kappa = at<float>(ws, w.kappa), *dh = at<float>(ws, w.dh);
+    float *xk = at<float>(ws, w.xk), *top = at<float>(ws, w.top), *coef = at<float>(ws, w.coef),
+          *coefs = at<float>(ws, w.coefs), *kappa = at<float>(ws, w.kappa),
+          *dh = at<float>(ws, w.dh);
     const float c = (float)(kLog2e / (double)T);
     const int64_t hrows = w.hrows;
     PairMaps maps;
@@ -1234,8 +1246,9 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     a.c = c;
     a.tab = tab;
     a.xk = xk;
-    a.lse2 = lse2;
+    a.top = top;
     a.coef = coef;
+    a.coefs = coefs;
     a.kappa = kappa;
     a.split = w.split;
     a.want_dh = s.dh;
@@ -1271,16 +1284,14 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         ra.K = K;
         ra.ldx = ra.ldg = w.piece;
         ra.gcols = w.piece;
-        ra.c = c;
-        ra.invT = 1.f / T;
         ra.row_loss = out.row_loss;
         ra.logz = out.logz;
         ra.same_align = true;
-        e = launch_row_loss<float, bf16, true>(X, G, ra, kTopMantissa, resident_clusters, st);
+        e = launch_row_loss<float, bf16, true>(X, G, ra, T, kTopMantissa, resident_clusters, st);
     } else {
         e = launch_dep(true, k_rows, dim3((unsigned)((R + kRowsOf - 1) / kRowsOf)), 256, 0, 1, st,
-                       tab, (int)(2 * units), (int64_t)w.rpad, tg, K, c, T, xk, lse2, coef,
-                       out.row_loss, out.logz, at<double>(ws, w.part), grads ? nullptr : out.loss);
+                       tab, (int)(2 * units), (int64_t)w.rpad, tg, K, c, 1.0 / (double)T, xk, top, coef,
+                       coefs, out.row_loss, out.logz, at<double>(ws, w.part), grads ? nullptr : out.loss);
     }
     if (e != cudaSuccess || !grads) return e;
     for (int q = 0; q < w.npiece; ++q) {

@@ -18,6 +18,7 @@
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <stdint.h>
 
 #include <type_traits>
@@ -44,7 +45,8 @@ struct RowArgs {
     bool by4;            // rounds of four vectors
     int64_t ldx, ldg;    // row pitches in elements
     int gcols;           // columns of a gradient row that are written (zero from V on)
-    float c, invT;
+    float c;
+    float invT, invT_lo; // 1 / T and what its rounding left
     float *row_loss, *logz;
     bool same_align;     // gradient rows start where logits rows do, modulo 16 bytes
 };
@@ -363,7 +365,8 @@ __global__ void __launch_bounds__(kRowThreads)
             for (int k = lane; k < cnt_n; k += 32) dot = fmaf(ps[par][k], xs[par][k] - M, dot);
             dot = warp_sum(dot);
             if (lane == 0) {
-                const float l = logf(S), lz = fmaf(M, a.invT, l);
+                const float l = logf(S);
+                const float lz = fmaf(M, a.invT, fmaf(fmaxf(M, -FLT_MAX), a.invT_lo, l));
                 if (!isfinite(lz)) atomicOr(a.tg.status, VSD_STATUS_BAD_ROW);
                 a.logz[row] = lz;
                 a.row_loss[row] = row_plogp + (l - dot * a.invT);
@@ -412,14 +415,18 @@ __global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const flo
     }
 }
 
-// Launches a.rows rows (a.vper, a.by4 and a.rounds are set here).
+// Launches a.rows rows at temperature T (a.c, a.invT, a.vper, a.by4 and a.rounds are
+// set here).
 // resident: clusters of a kernel's blocks of so many threads and bytes that can
 // be resident at once.
 template <typename TI, typename TO, bool LM>
-cudaError_t launch_row_loss(const TI* logits, TO* grad, RowArgs a, float top,
+cudaError_t launch_row_loss(const TI* logits, TO* grad, RowArgs a, float T, float top,
                             int (*resident)(const void*, int, size_t, int),
                             cudaStream_t st) {
     constexpr int PV = Traits<TI>::kPerVec;
+    a.c = (float)(kLog2e / (double)T);
+    a.invT = 1.f / T;
+    a.invT_lo = (float)(1.0 / (double)T - (double)a.invT);
     const int64_t need = ((int64_t)a.V + 2 * PV - 2) / PV;  // vectors, whatever the offset
     int64_t C = 1;
     while (C < kMaxCluster && C * kSegBytes < 16 * need) C *= 2;

@@ -84,8 +84,6 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     a.K = in.K;
     a.ldx = a.ldg = in.V;
     a.gcols = in.V;
-    a.c = (float)(kLog2e / (double)T);
-    a.invT = 1.f / T;
     a.row_loss = out.row_loss;
     a.logz = out.logz;
     a.same_align = (((uintptr_t)logits ^ (uintptr_t)out.grad) & 15) == 0;
@@ -95,10 +93,10 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
     if (bf16)
         e = launch_row_loss<__nv_bfloat16, __nv_bfloat16, false>(
             static_cast<const __nv_bfloat16*>(logits), static_cast<__nv_bfloat16*>(out.grad), a,
-            1.f, resident_clusters, st);
+            T, 1.f, resident_clusters, st);
     else
         e = launch_row_loss<float, float, false>(static_cast<const float*>(logits),
-                                                 static_cast<float*>(out.grad), a, 1.f,
+                                                 static_cast<float*>(out.grad), a, T, 1.f,
                                                  resident_clusters, st);
     if (e != cudaSuccess) return e;
     return launch_dep(true, k_mean_loss, dim3(1), 1024, 0, 1, st, a.tg, in.R, out.row_loss,

@@ -663,3 +663,79 @@ def test_lanes_that_differ(vsd, R, V, H, K, piece):
     x = H64 @ W64.T
     ref = plain(x, i64, p, counted, torch.ones(R).double(), 1.0)
     check(got, ref, x, logit_bound(H64, W64), 1.0, torch.bfloat16, H64, W64, i64, p)
+
+
+@pytest.mark.parametrize("H", [64, 1024])
+@pytest.mark.parametrize("grads,piece", [(False, 0), (True, 0), (True, 256)])
+@pytest.mark.parametrize("T,K", [(1.0, 1), (0.7, 1), (0.7, 2)])
+def test_exponents_by_difference(vsd, H, grads, piece, T, K):
+    """Logits far from zero, exact (one product each): one or two tokens hold a
+    row's mass, so its loss does not depend on how large they are.  The errors left
+    are those of logf (an ulp), of one rounding of m / T in logz, and with two
+    entries of their probabilities (expf and a division: 2^-20 in all)."""
+    R, V = 200, 700
+    g = torch.Generator(device="cuda").manual_seed(31)
+    m = (100.0 + 4000.0 * torch.rand(H, generator=g, device="cuda") ** 2).bfloat16()
+    pair = torch.rand(V, H, generator=g, device="cuda").topk(2, dim=0).indices  # two tokens a column
+    two = torch.arange(H, device="cuda") % 2 == 1
+    w = torch.zeros(V, H, dtype=torch.bfloat16, device="cuda")
+    w.scatter_(0, pair[:1], m[None])
+    w.scatter_(0, pair[1:], torch.where(two, m, torch.zeros_like(m))[None])
+    col = torch.arange(R, device="cuda") % H
+    h = torch.zeros(R, H, dtype=torch.bfloat16, device="cuda")
+    h[torch.arange(R, device="cuda"), col] = 1.0
+    ids = pair[:, col].T.to(torch.int32)
+    ids[:, 1].masked_fill_(~two[col], -1)
+    ids = ids[:, :K].contiguous()
+    t = torch.randn(R, K, generator=g, device="cuda")
+    got = vsd.lmhead_distill(h, w, ids, t, T=T, d_hidden=grads, d_weight=grads, piece=piece)
+    T = float(np.float32(T))  # (the temperature that the call takes)
+    _, p, counted = teacher_target(ids, t, T, V)
+    assert counted.all()
+    two, m = two[col].cpu(), f64(m[col])
+    ls = torch.where(two, np.log(2.0), 0.0).double()
+    want = torch.where(p > 0, p * torch.log(p.clamp(min=1e-300)), 0.0).sum(1) + ls
+    assert ((f64(got["row_loss"]) - want).abs() <= 2.0 ** -23 + (K - 1) * 2.0 ** -20).all()
+    lz = m / T + ls
+    assert ((f64(got["logz"]) - lz).abs() <= 2.0 ** -24 * lz + 2.0 ** -23).all()
+    if grads:
+        share = 1.0 / (R * T)
+        dw, size = torch.zeros(2, V, H, dtype=torch.float64)
+        for r in range(R):
+            c = int(col[r])
+            for k in range(2):
+                q = 0.5 if two[r] else 1.0 - k
+                term = share * (q - (float(p[r, k]) if k < K else 0.0))
+                dw[int(pair[k, c]), c] += term
+                size[int(pair[k, c]), c] += abs(term)
+        # each term's rounding in G, the output's, and the probabilities' error
+        err = (f64(got["d_weight"]) - dw).abs()
+        bound = 2.0 ** -8 * (size + dw.abs()) + (K - 1) * 4 * share * 2.0 ** -20 + 1e-30
+        assert (err <= bound).all()
+
+
+@pytest.mark.parametrize("H", [64, 1024])
+@pytest.mark.parametrize("grads,piece", [(False, 0), (True, 0), (True, 256)])
+def test_rows_at_the_lowest_value(vsd, H, grads, piece):
+    """Rows whose logits are all bfloat16's lowest value are uniform."""
+    R, V = 70, 512
+    h = torch.zeros(R, H, dtype=torch.bfloat16, device="cuda")
+    h[:, 0] = 1
+    w = torch.zeros(V, H, dtype=torch.bfloat16, device="cuda")
+    w[:, 0] = torch.finfo(torch.bfloat16).min
+    labels = (torch.arange(R, device="cuda") * 7 % V).to(torch.int32)
+    ws = torch.empty(vsd.lmhead_loss_workspace_bytes(R, V, H, 1, grads, piece), dtype=torch.uint8,
+                     device="cuda")
+    got = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False, d_weight=grads, piece=piece,
+                                   workspace=ws)
+    assert vsd.device_status(ws) == (0, 0)
+    assert (got["logz"] == torch.finfo(torch.bfloat16).min).all()  # log V is below its last bit
+    # logf's ulp at 6.2 and the result's rounding
+    assert ((f64(got["row_loss"]) - np.log(V)).abs() <= 2.0 ** -20).all()
+    if grads:
+        q = torch.full((V,), 1.0 / V, dtype=torch.float64)
+        q -= torch.bincount(labels.cpu().long(), minlength=V) / R
+        # G's entries, R of 1 / V and the label's, and the output: 2^-8 each
+        label = torch.bincount(labels.cpu().long(), minlength=V) / R
+        bound = 2.0 ** -8 * (2.0 / V + label + q.abs())
+        assert ((f64(got["d_weight"])[:, 0] - q).abs() <= bound).all()
