@@ -43,7 +43,16 @@ constexpr int kPieceUnit = 256;  // a piece's columns are a multiple of this
 // x 4096: 2.44 ms with pieces of 8192 columns, 2.45 with one of 32000).
 constexpr int64_t kPieceBytes = 128ll << 20;
 constexpr int64_t kKeepBytes = 64ll << 20;
-constexpr int64_t kPairs = 76;  // pairs of SMs
+// Pairs of SMs, of the part these kernels are built for: the plan and the workspace's
+// size go by it on any device, and no launch has more.
+constexpr int64_t kPairs = 76;
+// The tensor cores' running sum truncates: up to 1e-7 of it a step of 16 where the
+// terms have one sign (5.2 % after 2^19 steps).  Longer sums than these, in K blocks,
+// are cut into parts that are added up in fp32: the gradient's logits at 8192 hidden
+// elements (5e-5 of a logit), products at 65536 rows or columns (4e-4, a fifth of
+// their rounding to bf16).
+constexpr int kLongLogits = 128, kLongProd = 1024;
+constexpr int64_t kCarry = 8 * 32 * 128;  // a CTA's sums so far: the epilogue's part of a tile
 constexpr int kStoreCost = 5;    // K blocks of time that storing a d_weight tile takes at least
 // The operand G is scaled so that the largest weight sits at the top of a
 // binade (1.984 ..), where bf16's relative rounding error is least: a row's
@@ -56,9 +65,10 @@ int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct LmWs {
     size_t status, done, zero_end, nrows, wsum, wmax, kappa, unit, share, n, id, p, plogp, w,
-        rowmap, rowinv, top, coef, coefs, xk, tab, part, hid, X, G, dh, total;
+        rowmap, rowinv, top, coef, coefs, xk, tab, part, hid, X, G, dh, carry, total;
     int rpad, hrows, piece, npiece, split;  // rows padded to a tile, to a K block
     bool keep;  // the logits are kept (one piece)
+    bool cut_grad, cut_prod;  // long sums are cut into parts
 };
 
 LmWs lm_ws(const LmLossShape& s) {
@@ -136,6 +146,10 @@ LmWs lm_ws(const LmLossShape& s) {
     w.X = take(w.keep ? 4 * (size_t)w.hrows * w.piece : 0);
     w.G = take(grads ? 2 * (size_t)w.hrows * w.piece : 0);
     w.dh = take(s.dh ? 4 * (size_t)w.rpad * s.H * w.split : 0);
+    w.cut_grad = grads && !w.keep && (s.H + BK - 1) / BK > kLongLogits;
+    w.cut_prod = (s.dw && w.hrows / BK > kLongProd) ||
+                 (s.dh && (w.piece / BK + w.split - 1) / w.split > kLongProd);
+    w.carry = take(w.cut_grad || w.cut_prod ? 4 * kCarry * 2 * kPairs : 0);
     w.total = o;
     return w;
 }
@@ -182,13 +196,17 @@ __global__ void __launch_bounds__(256)
 //              product is for:
 //     logits   A = hidden rows, B = weight rows, both K-major.  kStats: per row
 //              and half tile (max, sum 2^{(x - max) c}) and the target logits
-//              in it.  kKeep: the logits themselves, fp32.  kGrad: G, rounded to
-//              bf16.  The tensor cores' running sum truncates, an error that
-//              grows with the number of K steps, so K is summed in parts of 512
-//              that are added up here in fp32 (round to nearest).
+//              in it.  kKeep: the logits themselves, fp32.  Both sum K in parts
+//              of 512 that are added up in the epilogue's registers (round to
+//              nearest: the tensor cores' truncation grows with the steps).
+//              kGrad: G, rounded to bf16.  Its epilogue has no registers for
+//              that; its sums are cut at kLongLogits.
 //     d_hidden A = G (K-major), B = weight (MN-major, as it lies): fp32 sums,
 //              added up over the pieces of the vocabulary by TMA.
 //     d_weight A = G (MN-major), B = hidden (MN-major): one rounding to bf16.
+//              Both products' sums are cut at kLongProd.
+// A cut sum is carried from part to part in the workspace, 16 KB a warp (CUT: an
+// instance of its own; the registers it takes cost 48 x 128256 x 4096 546 to 558 us).
 // What is stored goes through 4 KB of swizzled shared memory per warp and a TMA
 // store.  Every wait is bounded: one that runs out sets VSD_STATUS_TIMEOUT, and
 // the pair winds down, waits for its copies and MMAs in flight and frees its
@@ -211,6 +229,7 @@ constexpr int kMaxStages = 9;
 constexpr uint32_t kTmemAll = 2 * BT;
 constexpr uint64_t kWaitNs = 2000000000ull;
 constexpr int kGroupM = 16;                    // M tiles that share B tiles in L2
+static_assert(kCarry == kTileWarps * 32 * kHalfN, "a CTA's accumulator");
 
 struct PairBars {
     uint64_t full[kMaxStages];    // leader: both CTAs' bytes landed
@@ -260,7 +279,8 @@ struct PairArgs {
     Targets tg;
     int R, K;              // rows of the call, entries of a target list
     int H, V, v0, cols;    // this piece: columns v0 .. v0 + cols - 1
-    int nkh, part;         // K blocks of the hidden size, of a partial sum of the logits
+    int nkh, part;         // K blocks of the hidden size, of an uncut sum
+    float* carry;
     int64_t rpad;
     float c;
     float2* tab;
@@ -391,10 +411,27 @@ struct RowList {
     }
 };
 
-// 32 accumulators as floats, -inf from column `lim` on.
-__device__ __forceinline__ void read32(uint32_t taddr, int lim, float (&f)[32]) {
-    uint32_t u[32];
+// 32 accumulators of a lane, with the sum of the parts before, if any (element i of
+// carry at 32 i; kCarryStep on from one 32 columns to the next).
+constexpr int kCarryStep = 32 * 32;
+__device__ __forceinline__ void sum32(uint32_t taddr, const float* carry, uint32_t (&u)[32]) {
+    __syncwarp();  // (tensor memory is read by whole warps)
     tc::tmem_ld32(taddr, u);
+    if (carry) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            u[i] = __float_as_uint(__uint_as_float(u[i]) + carry[32 * i]);
+    }
+}
+__device__ __forceinline__ const float* carried(const float* carry, int g) {
+    return carry ? carry + g * kCarryStep : nullptr;
+}
+
+// 32 accumulators as floats, -inf from column `lim` on.
+__device__ __forceinline__ void read32(uint32_t taddr, const float* carry, int lim,
+                                       float (&f)[32]) {
+    uint32_t u[32];
+    sum32(taddr, carry, u);
 #pragma unroll
     for (int i = 0; i < 32; ++i) f[i] = i < lim ? __uint_as_float(u[i]) : -INFINITY;
 }
@@ -510,7 +547,7 @@ __device__ __forceinline__ void stats1_tile(const PairArgs& a, int n0, int row0,
 #pragma unroll 1
     for (int g = 0; g < kHalfN / 32; ++g) {
         float f[32];
-        read32(taddr + 32u * g, lim - 32 * g, f);
+        read32(taddr + 32u * g, nullptr, lim - 32 * g, f);
         if (g == kHalfN / 32 - 1) release();
         const int end = min(lo + 32 * (g + 1), hi);
         if (__any_sync(0xffffffffu, id < end)) {
@@ -527,7 +564,6 @@ __device__ __forceinline__ void stats1_tile(const PairArgs& a, int n0, int row0,
                 ++k;
                 id = k < list.n ? __ldg(list.id + k) : hi;
             }
-            __syncwarp();  // (the lanes' entries differ; tensor memory is read by whole warps)
         }
         float m0 = f[0], m1 = f[1];
 #pragma unroll
@@ -544,8 +580,8 @@ __device__ __forceinline__ void stats1_tile(const PairArgs& a, int n0, int row0,
 // (by difference here too: 2^{x c - lse} would round the log-partition).
 __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& maps, int n0,
                                           int row0, int lane, int n_rows, uint32_t taddr,
-                                          const RowList& list, float cf, float cs, float z,
-                                          Stage& out) {
+                                          const float* carry, const RowList& list, float cf,
+                                          float cs, float z, Stage& out) {
     const int row = row0 + lane;
     const bool on = row < n_rows;
     const uint64_t z2 = f2(z, z), c2 = f2(a.c, a.c), cs2 = f2(cs, cs);
@@ -559,7 +595,8 @@ __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& map
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float f[32];
-            read32(taddr + 64u * g + 32u * h, a.cols - n0 - 64 * g - 32 * h, f);
+            read32(taddr + 64u * g + 32u * h, carried(carry, 2 * g + h),
+                   a.cols - n0 - 64 * g - 32 * h, f);
             uint32_t w[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -589,7 +626,7 @@ __device__ __forceinline__ void grad_tile(const PairArgs& a, const PairMaps& map
 // d_hidden in one part and the last piece: the earlier pieces' sums are added
 // here, rounded once and stored in the caller's row.
 __device__ __forceinline__ void dh_last_tile(const PairArgs& a, bool none, int n0, int row,
-                                             int n_rows, uint32_t taddr) {
+                                             int n_rows, uint32_t taddr, const float* carry) {
     const bool on = row < n_rows;
     const float s = none ? 0.f : __ldg(a.kappa);
     const float* part = a.dh + (size_t)row * a.H;
@@ -597,8 +634,7 @@ __device__ __forceinline__ void dh_last_tile(const PairArgs& a, bool none, int n
 #pragma unroll 1
     for (int g = 0; g < kHalfN / 32; ++g) {
         uint32_t u[32];
-        __syncwarp();  // (rows past the last leave the rest out)
-        tc::tmem_ld32(taddr + 32u * g, u);
+        sum32(taddr + 32u * g, carried(carry, g), u);
         const int x = n0 + 32 * g;
         if (!on) continue;
 #pragma unroll
@@ -625,10 +661,10 @@ __device__ __forceinline__ void dh_last_tile(const PairArgs& a, bool none, int n
 
 __device__ __forceinline__ void dh_tile(const PairArgs& a, const PairMaps& maps, const Job& j,
                                         int n0, int row0, int lane, int n_rows, uint32_t taddr,
-                                        Stage& out) {
+                                        const float* carry, Stage& out) {
     const bool none = j.kb0 == j.kb1;
     if (a.last && a.split == 1) {
-        dh_last_tile(a, none, n0, row0 + lane, n_rows, taddr);
+        dh_last_tile(a, none, n0, row0 + lane, n_rows, taddr, carry);
         return;
     }
     if (none && !a.first) return;  // nothing to add
@@ -636,7 +672,7 @@ __device__ __forceinline__ void dh_tile(const PairArgs& a, const PairMaps& maps,
     for (int g = 0; g < kHalfN / 32; ++g) {
         unsigned char* box = out.acquire();
         uint32_t u[32];
-        tc::tmem_ld32(taddr + 32u * g, u);
+        sum32(taddr + 32u * g, carried(carry, g), u);
 #pragma unroll
         for (int v = 0; v < 8; ++v)
             *chunk_at(box, lane, v) =
@@ -656,10 +692,9 @@ __device__ __forceinline__ void few_keep_tile(const PairArgs& a, int col, int i0
         if (i0 + c < n_rows) a.X[(size_t)(i0 + c) * a.ldx + col] = u[c];
 }
 __device__ __forceinline__ void few_dh_tile(const PairArgs& a, const Job& j, int col, int i0,
-                                            int n_rows, uint32_t taddr) {
+                                            int n_rows, uint32_t taddr, const float* carry) {
     uint32_t u[32];
-    __syncwarp();  // (columns past the last leave the rest out)
-    tc::tmem_ld32(taddr, u);
+    sum32(taddr, carry, u);
     if (col >= a.H) return;
     if (a.split == 1) {
         const float s = __ldg(a.kappa);
@@ -681,15 +716,15 @@ __device__ __forceinline__ void few_dh_tile(const PairArgs& a, const Job& j, int
 // while this one is stored: an SM's stores leave at 32 bytes a cycle at most.
 template <typename Release>
 __device__ __forceinline__ void dw_tile(const PairArgs& a, const Job& j, int n0, int row0,
-                                        int lane, uint32_t taddr, unsigned char* box,
-                                        Release release) {
+                                        int lane, uint32_t taddr, const float* carry,
+                                        unsigned char* box, Release release) {
     const bool none = j.kb0 == j.kb1;
     const float s = none ? 0.f : __ldg(a.kappa);
     uint32_t w[kHalfN / 2];
 #pragma unroll
     for (int g = 0; g < kHalfN / 32; ++g) {
         uint32_t u[32];
-        tc::tmem_ld32(taddr + 32u * g, u);
+        sum32(taddr + 32u * g, carried(carry, g), u);
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             w[16 * g + i] = none ? 0u
@@ -740,7 +775,7 @@ template <bool kSplit> __device__ __forceinline__ void give_registers() {
     if (kSplit) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(kRegsFew));
 }
 
-template <int MODE, int NF>
+template <int MODE, int NF, bool CUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::kThreads, 1)
     k_pair(const __grid_constant__ PairMaps maps, const PairArgs a) {
     using Cfg = PairCfg<MODE, NF>;
@@ -776,7 +811,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
     dep_wait();
     const int n_rows = *(const volatile int*)a.tg.nrows;
     const bool all = n_rows == a.R;  // hidden as it is
-    // K blocks summed at a time: the logits' parts, or all of a product's
+    // sums cut for the epilogue's registers
     constexpr bool kParts = MODE == kStats || MODE == kKeep;
     constexpr bool kSplitRegs = kParts && !kFew;
     Jobs<MODE, kFew> jobs(a, n_rows);
@@ -867,7 +902,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
                 const int kb1 = MODE == kProd ? j.kb1 : a.nkh;
                 int kb = j.kb0;
                 do {  // (a job without K blocks hands on its accumulator unread)
-                    const int end = kParts ? min(kb1, kb + a.part) : kb1;
+                    const int end = kParts || CUT ? min(kb1, kb + a.part) : kb1;
                     const int buf = lt & 1;
                     const uint32_t use = (uint32_t)lt >> 1;
                     if (use > 0 && !wait_pair(&sb->acc_empty[buf], (use - 1) & 1u, sb, status)) {
@@ -931,11 +966,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
         };
         const int f0 = ((warp - 4) >> 2 & 1) * (NF / 2);  // its rows of a turned tile
         while (jobs.next(j)) {
-            if (Cfg::kSets == 2 && (lt & 1) != set) {
+            if (Cfg::kSets == 2 && CUT) {  // (one set takes all parts: its phases in a row)
+                if (set) break;
+            } else if (Cfg::kSets == 2 && (lt & 1) != set) {
                 ++lt;
                 continue;
             }
             const int row0 = j.m0 + 128 * rank + 32 * q, n0 = j.n0 + h0;
+            const float* carry = nullptr;
+            if constexpr (CUT) {  // all parts but a sum's last
+                const bool turned = kFew && j.kind == 1;
+                const int len = MODE == kGrad ? a.nkh : j.kb1 - j.kb0;
+                float* mine = a.carry + (int64_t)(blockIdx.x * kTileWarps + warp - 4) *
+                                            (kHalfN * 32) + lane;
+                bool ok = true;
+                for (int kb = a.part; kb < len; kb += a.part) {
+                    if (!(ok = ready())) break;
+#pragma unroll 1
+                    for (int g = 0; g < (turned ? NF / 64 : kHalfN / 32); ++g) {
+                        uint32_t u[32];
+                        sum32(acc_addr((turned ? f0 : h0) + 32 * g), carried(carry, g), u);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            mine[g * kCarryStep + 32 * i] = __uint_as_float(u[i]);
+                    }
+                    carry = mine;
+                    release();
+                }
+                if (!ok) break;
+            }
             if (MODE == kKeep && kFew) {
                 float x[kFew ? NF / 2 : 1];
                 bool ok = true;
@@ -989,7 +1048,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
                 const float cf = on ? __ldg(a.coef + row) : 0.f;
                 const float cs = on ? __ldg(a.coefs + row) : 0.f, z = on ? __ldg(a.top + row) : 0.f;
                 if (!ready()) break;
-                grad_tile(a, maps, n0, row0, lane, n_rows, acc_addr(h0), list, cf, cs, z, out);
+                grad_tile(a, maps, n0, row0, lane, n_rows, acc_addr(h0), carry, list, cf, cs, z,
+                          out);
                 release();
             } else {
                 if (!ready()) break;
@@ -997,15 +1057,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
                 if (kFew && j.kind == 1) {
 #pragma unroll
                     for (int g = 0; g < NF / 64; ++g)
-                        few_dh_tile(a, j, row0 + lane, f0 + 32 * g, n_rows, acc_addr(f0 + 32 * g));
+                        few_dh_tile(a, j, row0 + lane, f0 + 32 * g, n_rows, acc_addr(f0 + 32 * g),
+                                    carried(carry, g));
                 } else if (n0 >= a.H) {
                     // no column of the output
                 } else if (j.kind == 1) {
-                    dh_tile(a, maps, j, n0, row0, lane, n_rows, t, out);
+                    dh_tile(a, maps, j, n0, row0, lane, n_rows, t, carry, out);
                 } else {
                     // (a TMA store may still read the box)
                     if (!kFew && a.want_dh) out.acquire();
-                    dw_tile(a, j, n0, row0, lane, t, out.buf, release);
+                    dw_tile(a, j, n0, row0, lane, t, carry, out.buf, release);
                     continue;
                 }
                 release();
@@ -1178,14 +1239,15 @@ size_t lmloss_workspace_bytes(const LmLossShape& s) {
     return lmloss_shape_ok(s) ? lm_ws(s).total : 0;
 }
 
-template <int MODE, int NF = 0>
+template <int MODE, int NF = 0, bool CUT = false>
 static cudaError_t launch_pair(const PairMaps& maps, const PairArgs& a, int64_t jobs,
                                cudaStream_t st) {
     constexpr size_t smem = PairCfg<MODE, NF>::kSmem;
-    cudaError_t e = ensure_dyn_smem((const void*)k_pair<MODE, NF>, smem);
+    cudaError_t e = ensure_dyn_smem((const void*)k_pair<MODE, NF, CUT>, smem);
     if (e != cudaSuccess) return e;
-    const int64_t pairs = std::max<int64_t>(1, std::min<int64_t>(jobs, device_sm_count() / 2));
-    return launch_dep(true, k_pair<MODE, NF>, dim3((unsigned)(2 * pairs)),
+    const int64_t most = std::min<int64_t>(kPairs, device_sm_count() / 2);
+    const int64_t pairs = std::max<int64_t>(1, std::min(jobs, most));
+    return launch_dep(true, k_pair<MODE, NF, CUT>, dim3((unsigned)(2 * pairs)),
                       PairCfg<MODE, NF>::kThreads, smem, 1, st, maps, a);
 }
 
@@ -1255,6 +1317,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     a.want_dw = s.dw;
     a.dh = dh;
     a.row_loss = out.row_loss;
+    a.carry = at<float>(ws, w.carry);
     a.X = X;
     a.ldx = w.piece;
     a.d_hidden = static_cast<bf16*>(out.d_hidden);
@@ -1301,11 +1364,22 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         a.last = q == w.npiece - 1;
         a.loss = q == 0 ? out.loss : nullptr;
         const int64_t nu = (a.cols + kPieceUnit - 1) / kPieceUnit;
-        if (!w.keep && (e = launch_pair<kGrad>(maps, a, mt * nu, st)) != cudaSuccess) return e;
+        a.part = kLongLogits;
+        if (!w.keep) {
+            e = w.cut_grad ? launch_pair<kGrad, 0, true>(maps, a, mt * nu, st)
+                           : launch_pair<kGrad>(maps, a, mt * nu, st);
+            if (e != cudaSuccess) return e;
+        }
+        a.part = kLongProd;
         const int64_t jobs = (s.dh ? mt * ht * w.split : 0) + (s.dw ? nu * ht : 0);
-        e = nf == 64    ? launch_pair<kProd, 64>(maps, a, jobs, st)
-            : nf == 128 ? launch_pair<kProd, 128>(maps, a, jobs, st)
-                        : launch_pair<kProd>(maps, a, jobs, st);
+        if (w.cut_prod)
+            e = nf == 64    ? launch_pair<kProd, 64, true>(maps, a, jobs, st)
+                : nf == 128 ? launch_pair<kProd, 128, true>(maps, a, jobs, st)
+                            : launch_pair<kProd, 0, true>(maps, a, jobs, st);
+        else
+            e = nf == 64    ? launch_pair<kProd, 64>(maps, a, jobs, st)
+                : nf == 128 ? launch_pair<kProd, 128>(maps, a, jobs, st)
+                            : launch_pair<kProd>(maps, a, jobs, st);
         if (e != cudaSuccess) return e;
     }
     if (s.dh && w.split > 1) {

@@ -739,3 +739,87 @@ def test_rows_at_the_lowest_value(vsd, H, grads, piece):
         label = torch.bincount(labels.cpu().long(), minlength=V) / R
         bound = 2.0 ** -8 * (2.0 / V + label + q.abs())
         assert ((f64(got["d_weight"])[:, 0] - q).abs() <= bound).all()
+
+
+def test_d_weight_of_many_rows(vsd):
+    """Eight million rows whose terms all have one sign: G is exact (q = 1/2), so
+    what is left is the sum's error and the rounding to bfloat16.  An uncut part of
+    the sum has 4096 steps, each truncated by an ulp at most."""
+    R, V, H = 1 << 23, 2, 8
+    g = torch.Generator(device="cuda").manual_seed(1)
+    h = (1.0 + torch.rand(R, H, generator=g, device="cuda")).bfloat16()
+    w = torch.zeros(V, H, dtype=torch.bfloat16, device="cuda")
+    labels = torch.zeros(R, dtype=torch.int32, device="cuda")
+    got = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False)
+    want = 0.5 * f64(h.double().mean(0))
+    err = torch.maximum((f64(got["d_weight"][0]) + want).abs(),
+                        (f64(got["d_weight"][1]) - want).abs()) / want
+    assert (err <= 2.0 ** -8 + 4096 * 2.0 ** -23).all(), err
+
+
+def test_gradient_at_a_long_hidden_size(vsd):
+    """A hidden size whose sums take 32768 steps: the gradient's logits are as near
+    as parts of 512 steps make them, each step truncated by an ulp at most."""
+    R, V, H = 1, 512, 1 << 19
+    g = torch.Generator(device="cuda").manual_seed(2)
+    h = (1.0 + torch.rand(R, H, generator=g, device="cuda")).bfloat16()
+    top = 12.0 + 4.0 * torch.rand(V, 1, generator=g, device="cuda")
+    w = (top / (1.5 * H) * (0.5 + torch.rand(V, H, generator=g, device="cuda"))).bfloat16()
+    labels = torch.zeros(R, dtype=torch.int32, device="cuda")
+    got = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False, piece=256)
+    x = torch.cat([h.double() @ w[v:v + 64].double().T for v in range(0, V, 64)], 1)[0]
+    q = torch.softmax(x, 0)
+    have = torch.cat([(got["d_weight"][v:v + 64].double() / h.double()).mean(1)
+                      for v in range(0, V, 64)])
+    rel = ((have - q) / q)[1:].cpu()  # (the label's q - 1 is rounded at 1)
+    # G's rounding (the outputs' own averages out over H: 1e-4), and the parts of the
+    # logits and of the log-partition
+    assert (rel.abs() <= 2.0 ** -8 + 2 * 512 * 2.0 ** -23 * float(x.max()) + 1e-4).all()
+
+
+@pytest.mark.parametrize("R,V,H,K,piece", [(300, 700, 16456, 5, 256), (66000, 300, 72, 1, 256),
+                                           (40, 66000, 64, 3, 0)])
+def test_sums_in_parts(vsd, R, V, H, K, piece):
+    """Hidden sizes, rows and vocabularies at which sums are cut, or just are not."""
+    h, w, g = head(R, V, H, 900 + R, gain=1.0 / H ** 0.5)
+    ids = torch.randint(0, V, (R, K), generator=g, device="cuda").to(torch.int32)
+    t = torch.randn(R, K, generator=g, device="cuda")
+    ids[1::7] = -1
+    got = vsd.lmhead_distill(h, w, ids, t, piece=piece)
+    i64, p, counted = teacher_target(ids, t, 1.0, V)
+    H64, W64 = f64(h), f64(w)
+    x = H64 @ W64.T
+    ref = plain(x, i64, p, counted, torch.ones(R).double(), 1.0)
+    check(got, ref, x, logit_bound(H64, W64), 1.0, torch.bfloat16, H64, W64, i64, p)
+
+
+@pytest.mark.parametrize("R,V,H,dw", [(40, 65800, 38912, False), (100, 65800, 38912, False),
+                                      (2048, 131072, 6144, True)])
+def test_d_hidden_of_long_sums(vsd, R, V, H, dw):
+    """d_hidden over more columns than an uncut sum has, in one part (many tiles), for
+    turned tiles and others: some rows and columns against float64."""
+    g = torch.Generator(device="cuda").manual_seed(R)
+    h = torch.randn(R, H, generator=g, device="cuda").bfloat16()
+    w = torch.empty(V, H, dtype=torch.bfloat16, device="cuda")
+    for v in range(0, V, 1 << 14):
+        n = min(V, v + (1 << 14)) - v
+        w[v:v + n] = 2.0 / H ** 0.5 * torch.randn(n, H, generator=g, device="cuda")
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda").to(torch.int32)
+    got = vsd.lmhead_cross_entropy(h, w, labels, d_weight=dw)
+    rows = torch.arange(0, R, max(1, R // 13), device="cuda")
+    cols = torch.arange(0, H, 97, device="cuda")
+    x = torch.cat([(h[rows].double() @ w[v:v + 8192].double().T) for v in range(0, V, 8192)], 1)
+    size = torch.cat([(h[rows].double().abs() @ w[v:v + 8192].double().abs().T).amax(1, keepdim=True)
+                      for v in range(0, V, 8192)], 1).amax(1)
+    lab = labels[rows].long()[:, None]
+    G = torch.softmax(x, 1)
+    assert ((torch.logsumexp(x, 1) - x.gather(1, lab)[:, 0] - got["row_loss"][rows].double()).abs()
+            <= 2 * H * U * size + 2.0 ** -18).all()
+    G.scatter_add_(1, lab, -torch.ones_like(lab, dtype=torch.float64))
+    G /= R
+    W64 = w[:, cols].double()
+    want, mass = G @ W64, G.abs() @ W64.abs()
+    # a logit's error in q, G's rounding, the cut sums' truncation (4096 steps a part),
+    # the output's rounding
+    bound = mass * (2 * H * U * size[:, None] + 2.0 ** -8 + 4096 * 2.0 ** -23) + 2.0 ** -8 * want.abs()
+    assert ((got["d_hidden"][rows][:, cols].double() - want).abs() <= bound).all()
