@@ -383,35 +383,63 @@ __global__ void __launch_bounds__(kRowThreads)
     }
 }
 
-// The weighted mean of the rows' losses, in row order, by one block.
+// A sum in two floats: what the additions to hi round off is exact and goes to lo, so
+// that it holds some 2^-45 of its terms.  (Where hi is not finite, lo is NaN.)
+struct Sum2 {
+    float hi = 0.f, lo = 0.f;
+    __device__ __forceinline__ void add(float x, float rest) {
+        const float s = hi + x, b = s - hi;
+        lo += ((hi - (s - b)) + (x - b)) + rest;
+        hi = s;
+    }
+    __device__ __forceinline__ void warp() {
+#pragma unroll
+        for (int o = 16; o; o >>= 1)
+            add(__shfl_xor_sync(0xffffffffu, hi, o), __shfl_xor_sync(0xffffffffu, lo, o));
+    }
+};
+
+// The weighted mean of the rows' losses, in row order, by one block, rounded once.  (With
+// sums in 64 bits a call on 32 x 1024 logits takes 16.2 us as a graph, 14.9 so; on 768 x
+// 32000 35.6 and 31.7.)
 __global__ void __launch_bounds__(1024) k_mean_loss(Targets tg, int R, const float* row_loss,
                                                     float* loss) {
-    __shared__ float part[32];
+    __shared__ float2 part[32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     dep_launch();
     dep_wait();
     const float unit = *tg.unit;
-    double sum = 0.0;
+    Sum2 sum;
     for (int64_t b = threadIdx.x; b < R; b += 1024 * 4) {
         float w[4], l[4];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             const int64_t r = min(b + u * 1024, (int64_t)R - 1);
             const bool on = ld_cg(tg.n + r) >= 0 && b + u * 1024 < R;
-            w[u] = on ? ld_cg(tg.w + r) : 0.f;
+            w[u] = on ? ld_cg(tg.w + r) * unit : 0.f;
             l[u] = ld_cg(row_loss + r);
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-            if (w[u] != 0.f) sum += (double)(w[u] * unit) * (double)l[u];
+            if (w[u] != 0.f) {
+                const float x = w[u] * l[u];
+                sum.add(x, fmaf(w[u], l[u], -x));
+            }
     }
-    // (a thread's sum in 64 bits, the tree over threads in 32: no long chain)
-    const float t = warp_sum((float)sum);
-    if (lane == 0) part[warp] = t;
+    sum.warp();
+    if (lane == 0) part[warp] = make_float2(sum.hi, sum.lo);
     __syncthreads();
     if (warp == 0) {
-        const float all = warp_sum(part[lane]);
-        if (lane == 0) *loss = all / (float)(*tg.wsum * (double)unit);
+        const double all = *tg.wsum * (double)unit;  // 1 .. 2, or a power of two beyond
+        const float d = (float)all, d_lo = (float)(all - (double)d);
+        sum.hi = part[lane].x;
+        sum.lo = part[lane].y;
+        sum.warp();
+        if (lane == 0) {
+            // (hi + lo) / (d + d_lo): the quotient of the first parts, and the rest's
+            const float q = sum.hi / d, rest = (fmaf(-q, d, sum.hi) + sum.lo - q * d_lo) / d;
+            *loss = isfinite(rest) ? q + rest : q;
+        }
     }
 }
 

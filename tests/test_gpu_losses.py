@@ -823,3 +823,19 @@ def test_d_hidden_of_long_sums(vsd, R, V, H, dw):
     # the output's rounding
     bound = mass * (2 * H * U * size[:, None] + 2.0 ** -8 + 4096 * 2.0 ** -23) + 2.0 ** -8 * want.abs()
     assert ((got["d_hidden"][rows][:, cols].double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+def test_mean_of_the_losses(vsd, weighted):
+    """The mean of the rows' losses is taken in 64 bits and rounded once."""
+    for seed in range(8):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        R, V = 3001, 50
+        x = 3.0 * torch.randn(R, V, generator=g, device="cuda")
+        ids = torch.randint(0, V, (R, 2), generator=g, device="cuda").to(torch.int32)
+        t = torch.randn(R, 2, generator=g, device="cuda")
+        rw = torch.rand(R, generator=g, device="cuda") if weighted else None
+        got = vsd.topk_distill(x, ids, t, row_weight=rw, grad=False)
+        w64 = f64(rw) if weighted else torch.ones(R).double()
+        want = float((w64 * f64(got["row_loss"])).sum() / w64.sum())
+        assert abs(float(got["loss"]) - want) <= 2.0 ** -24 * (1 + 1e-6) * want, (seed, want)
