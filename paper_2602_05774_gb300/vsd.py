@@ -555,6 +555,17 @@ def _grad_tensor(want, like, name):
     return want
 
 
+def _loss_call(name, device, *args):
+    """A loss's entry point on the current stream of its tensors' device, which has to
+    be the current one while kernels are launched."""
+    entry = getattr(_lib(), name)
+    if device.index == torch.cuda.current_device():
+        _check(entry(*args, _stream(device.index)), name)
+        return
+    with torch.cuda.device(device):
+        _check(entry(*args, _stream(device.index)), name)
+
+
 def _loss_outputs(R, device):
     f = dict(dtype=torch.float32, device=device)
     return dict(loss=torch.empty(1, **f), row_loss=torch.empty(R, **f), logz=torch.empty(R, **f))
@@ -621,12 +632,9 @@ def lmhead_cross_entropy(hidden, weight, labels, ignore_index=-100, row_weight=N
     _check_row_weight(row_weight, R)
     out, st, ws, R, V, H = _lmhead_loss(hidden, weight, 1, d_hidden, d_weight, piece, workspace,
                                         (labels, row_weight))
-    _check(_lib().vsd_lmhead_cross_entropy(hidden.data_ptr(), weight.data_ptr(), R, V, H,
-                                           labels.data_ptr(), int(ignore_index),
-                                           _data_ptr(row_weight), float(grad_scale), int(piece),
-                                           C.byref(st), ws.data_ptr(), ws.nbytes,
-                                           _stream(hidden.device.index)),
-           "vsd_lmhead_cross_entropy")
+    _loss_call("vsd_lmhead_cross_entropy", hidden.device, hidden.data_ptr(), weight.data_ptr(), R,
+               V, H, labels.data_ptr(), int(ignore_index), _data_ptr(row_weight),
+               float(grad_scale), int(piece), C.byref(st), ws.data_ptr(), ws.nbytes)
     return out
 
 
@@ -640,12 +648,10 @@ def lmhead_distill(hidden, weight, teacher_ids, teacher_logits, T=1.0, row_weigh
     K = _check_teacher(teacher_ids, teacher_logits, row_weight, R)
     out, st, ws, R, V, H = _lmhead_loss(hidden, weight, K, d_hidden, d_weight, piece, workspace,
                                         (teacher_ids, teacher_logits, row_weight))
-    _check(_lib().vsd_lmhead_distill(hidden.data_ptr(), weight.data_ptr(), R, V, H,
-                                     teacher_ids.data_ptr(), teacher_logits.data_ptr(),
-                                     _dtype_code(teacher_logits), K, float(T),
-                                     _data_ptr(row_weight), float(grad_scale), int(piece),
-                                     C.byref(st), ws.data_ptr(), ws.nbytes,
-                                     _stream(hidden.device.index)), "vsd_lmhead_distill")
+    _loss_call("vsd_lmhead_distill", hidden.device, hidden.data_ptr(), weight.data_ptr(), R, V, H,
+               teacher_ids.data_ptr(), teacher_logits.data_ptr(), _dtype_code(teacher_logits), K,
+               float(T), _data_ptr(row_weight), float(grad_scale), int(piece), C.byref(st),
+               ws.data_ptr(), ws.nbytes)
     return out
 
 
@@ -673,12 +679,10 @@ def topk_distill(logits, teacher_ids, teacher_logits, T=1.0, row_weight=None, gr
     ws = _loss_workspace(_topk_bytes(R, V, K), workspace, dev)
     st = LossOutputs(out["loss"].data_ptr(), out["row_loss"].data_ptr(), out["logz"].data_ptr(),
                      None, None, None if g is None else g.data_ptr())
-    _check(_lib().vsd_topk_distill(logits.data_ptr(), _dtype_code(logits), R, V,
-                                   teacher_ids.data_ptr(), teacher_logits.data_ptr(),
-                                   _dtype_code(teacher_logits), K, float(T),
-                                   _data_ptr(row_weight), float(grad_scale), C.byref(st),
-                                   ws.data_ptr(), ws.nbytes, _stream(dev.index)),
-           "vsd_topk_distill")
+    _loss_call("vsd_topk_distill", dev, logits.data_ptr(), _dtype_code(logits), R, V,
+               teacher_ids.data_ptr(), teacher_logits.data_ptr(), _dtype_code(teacher_logits), K,
+               float(T), _data_ptr(row_weight), float(grad_scale), C.byref(st), ws.data_ptr(),
+               ws.nbytes)
     return out
 
 

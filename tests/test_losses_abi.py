@@ -91,3 +91,32 @@ def test_binding_refuses_cpu_tensors(vsd):
         vsd.lmhead_distill(h, w, i, t)
     with pytest.raises(ValueError):
         vsd.topk_distill(torch.zeros(4, 100), i, t)
+
+
+def test_losses_launch_on_their_tensors_device(vsd, monkeypatch):
+    """The device of the tensors is the current one when the library is called."""
+    now = [0]
+
+    class On:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.device.index
+
+        def __exit__(self, *a):
+            now[0] = self.before
+
+    class Lib:
+        def entry(self, *args):
+            calls.append((now[0], args))
+            return 0
+
+    calls = []
+    monkeypatch.setattr(vsd, "_lib", lambda: Lib())
+    monkeypatch.setattr(vsd, "_stream", lambda i: "stream of %d" % i)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", On)
+    vsd._loss_call("entry", torch.device("cuda", 1), 7)
+    vsd._loss_call("entry", torch.device("cuda", 0), 8)
+    assert calls == [(1, (7, "stream of 1")), (0, (8, "stream of 0"))] and now == [0]
