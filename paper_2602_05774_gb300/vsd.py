@@ -549,6 +549,7 @@ def _grad_tensor(want, like, name):
     if want is False or want is None:
         return None
     _need_cuda(want)
+    _same_device(like, want)
     if want.dtype != like.dtype or want.shape != like.shape:
         raise ValueError("%s must have the type and shape of the tensor it is the gradient of"
                          % name)

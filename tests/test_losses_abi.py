@@ -93,6 +93,33 @@ def test_binding_refuses_cpu_tensors(vsd):
         vsd.topk_distill(torch.zeros(4, 100), i, t)
 
 
+def _on_host(vsd, monkeypatch):
+    """CPU tensors pass as CUDA ones; tensors on the meta device stand for those of
+    another GPU; no call reaches the library."""
+    monkeypatch.setattr(vsd, "_need_cuda", lambda *ts: None)
+
+    def no_call(*a):
+        raise AssertionError("the library was called")
+    monkeypatch.setattr(vsd, "_loss_call", no_call)
+
+
+def test_gradients_on_another_device_are_refused(vsd, monkeypatch):
+    _on_host(vsd, monkeypatch)
+    h = torch.zeros(4, 64, dtype=torch.bfloat16)
+    w = torch.zeros(100, 64, dtype=torch.bfloat16)
+    x = torch.zeros(4, 100)
+    i = torch.zeros(4, 2, dtype=torch.int32)
+    t = torch.zeros(4, 2)
+    far = dict(dtype=torch.bfloat16, device="meta")
+    for bad in (lambda: vsd.lmhead_cross_entropy(h, w, i[:, 0], d_hidden=torch.empty(4, 64, **far)),
+                lambda: vsd.lmhead_cross_entropy(h, w, i[:, 0], d_weight=torch.empty(100, 64, **far)),
+                lambda: vsd.lmhead_distill(h, w, i, t, d_hidden=torch.empty(4, 64, **far)),
+                lambda: vsd.lmhead_distill(h, w, i, t, d_weight=torch.empty(100, 64, **far)),
+                lambda: vsd.topk_distill(x, i, t, grad=torch.empty(4, 100, device="meta"))):
+        with pytest.raises(ValueError, match="one device"):
+            bad()
+
+
 def test_losses_launch_on_their_tensors_device(vsd, monkeypatch):
     """The device of the tensors is the current one when the library is called."""
     now = [0]
