@@ -388,8 +388,11 @@ vsd_status vsd_lmhead_backward(const void* hidden, const void* weight, int32_t H
  * A counted row whose log-partition is not finite (NaN or +inf logits, or all
  * -inf) sets VSD_STATUS_BAD_ROW; NaN then spreads as in the formulas.
  * Sums are in fp32 or wider and in a fixed order: a call repeated on the same
- * inputs gives the same bits.  Outputs may not overlap inputs (but for
- * vsd_topk_distill's gradient, see there).  The kernels' waits for copies, matrix
+ * inputs gives the same bits.  Outputs may not overlap inputs or one another, but
+ * vsd_topk_distill's gradient may be the logits, and of the LM-head calls' gradients
+ * one asked for alone may be the tensor it is the gradient of; another overlap of a
+ * gradient with hidden, weight, logits or the other gradient is refused
+ * (VSD_ERR_INVALID_ARG).  The kernels' waits for copies, matrix
  * instructions and the other blocks of a cluster end after 2 s at most; one that
  * runs out sets VSD_STATUS_TIMEOUT.
  * ------------------------------------------------------------------------ */

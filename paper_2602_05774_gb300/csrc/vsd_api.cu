@@ -711,6 +711,12 @@ static vsd_status check_loss_call(const vsd_loss_outputs* out, const TargetIn& i
     return VSD_OK;
 }
 
+// Whether two arrays (either may be NULL) share a byte.
+static bool overlap(const void* a, size_t an, const void* b, size_t bn) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && x < y + bn && y < x + an;
+}
+
 static vsd_status lmhead_loss_call(const void* hidden, const void* weight, int32_t H,
                                    const TargetIn& in, float T, float grad_scale, int32_t piece,
                                    const vsd_loss_outputs* out, void* ws, size_t ws_bytes,
@@ -725,6 +731,14 @@ static vsd_status lmhead_loss_call(const void* hidden, const void* weight, int32
         return VSD_ERR_INVALID_ARG;
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < lmloss_workspace_bytes(s))
         return VSD_ERR_WORKSPACE;
+    // hidden is read beside d_weight's stores and the weight beside d_hidden's; alone, a
+    // gradient is stored after its tensor's last read (d_weight's rows after theirs)
+    const void *dh = out->d_hidden, *dw = out->d_weight;
+    const size_t hb = 2 * (size_t)in.R * H, wb = 2 * (size_t)in.V * H;
+    if (overlap(dh, hb, weight, wb) || overlap(dw, wb, hidden, hb) || overlap(dh, hb, dw, wb) ||
+        (overlap(dh, hb, hidden, hb) && (dw || dh != hidden)) ||
+        (overlap(dw, wb, weight, wb) && (dh || dw != weight)))
+        return VSD_ERR_INVALID_ARG;
     return from_cuda(lmloss(s, hidden, weight, in, T, grad_scale, *out, ws,
                             static_cast<cudaStream_t>(stream)));
 }
@@ -784,6 +798,9 @@ vsd_status vsd_topk_distill(const void* logits, vsd_dtype dtype, int32_t R, int3
         return VSD_ERR_INVALID_ARG;
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < topk_workspace_bytes(R, V, K))
         return VSD_ERR_WORKSPACE;
+    const size_t bytes = (size_t)R * V * (dtype == VSD_BF16 ? 2 : 4);
+    if (out->grad != logits && overlap(out->grad, bytes, logits, bytes))
+        return VSD_ERR_INVALID_ARG;  // (rows ahead are read while a row's gradient is stored)
     return from_cuda(topk_distill(logits, dtype == VSD_BF16, in, T, grad_scale, *out, ws,
                                   static_cast<cudaStream_t>(stream)));
 }

@@ -839,3 +839,32 @@ def test_mean_of_the_losses(vsd, weighted):
         w64 = f64(rw) if weighted else torch.ones(R).double()
         want = float((w64 * f64(got["row_loss"])).sum() / w64.sum())
         assert abs(float(got["loss"]) - want) <= 2.0 ** -24 * (1 + 1e-6) * want, (seed, want)
+
+
+@pytest.mark.parametrize("R,V,H,piece", [(40, 3000, 264, 0), (100, 700, 72, 0), (300, 2000, 136, 256),
+                                         (300, 2000, 136, 0)])
+def test_a_gradient_alone_in_its_tensors_place(vsd, R, V, H, piece):
+    """One gradient alone may be written over the tensor it is the gradient of; with
+    both that is refused, and so is any other overlap."""
+    h, w, g = head(R, V, H, 40 + R)
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda").to(torch.int32)
+    for skip in (False, True):
+        if skip:
+            labels[::3] = -100
+        kw = dict(piece=piece)
+        want_h = vsd.lmhead_cross_entropy(h, w, labels, d_weight=False, **kw)["d_hidden"]
+        want_w = vsd.lmhead_cross_entropy(h, w, labels, d_hidden=False, **kw)["d_weight"]
+        h2, w2 = h.clone(), w.clone()
+        vsd.lmhead_cross_entropy(h2, w, labels, d_hidden=h2, d_weight=False, **kw)
+        vsd.lmhead_cross_entropy(h, w2, labels, d_hidden=False, d_weight=w2, **kw)
+        assert torch.equal(h2, want_h) and torch.equal(w2, want_w)
+    x = torch.zeros(R * 50 + 8, device="cuda")
+    ids, t = teacher(R, 50, 2, g)
+    for bad in (lambda: vsd.lmhead_cross_entropy(h, w, labels, d_hidden=h),
+                lambda: vsd.lmhead_cross_entropy(h, w, labels, d_weight=w),
+                lambda: vsd.lmhead_cross_entropy(h, w[:R], labels, d_hidden=w[:R], d_weight=False),
+                lambda: vsd.topk_distill(x[:R * 50].view(R, 50), ids, t,
+                                         grad=x[8:].view(R, 50))):
+        with pytest.raises(vsd.VsdError) as e:
+            bad()
+        assert e.value.code == 1

@@ -147,3 +147,30 @@ def test_losses_launch_on_their_tensors_device(vsd, monkeypatch):
     vsd._loss_call("entry", torch.device("cuda", 1), 7)
     vsd._loss_call("entry", torch.device("cuda", 0), 8)
     assert calls == [(1, (7, "stream of 1")), (0, (8, "stream of 0"))] and now == [0]
+
+
+@host_only
+def test_overlapping_gradients_are_refused(vsd):
+    lib = vsd.load()
+    h, w, x, y, z = (0x1000000 * i for i in range(1, 6))  # never dereferenced
+    R, V, H, big = 4, 100, 64, 1 << 40
+    hb, wb = 2 * R * H, 2 * V * H
+
+    def code(dh, dw):
+        o = vsd.LossOutputs(z, z, z, dh, dw, None)
+        a = lib.vsd_lmhead_cross_entropy(h, w, R, V, H, z, -100, None, 1.0, 0, C.byref(o), z, big,
+                                         None)
+        b = lib.vsd_lmhead_distill(h, w, R, V, H, z, z, 0, 4, 1.0, None, 1.0, 0, C.byref(o), z, big,
+                                   None)
+        return a, b
+
+    for dh, dw in ((h, x), (x, w), (h, w), (w, None), (None, h), (x, x), (x, x + hb - 16),
+                   (x + wb - 16, x), (h + 16, None), (None, w + 16), (None, w - wb + 16),
+                   (w + wb - 16, None)):
+        assert code(dh, dw) == (1, 1), (hex(dh or 0), hex(dw or 0))
+    for dt, size in ((0, 4), (1, 2)):
+        n = R * V * size
+        for grad in (x + size, x - size, x + n - size, x - n + size):
+            o = vsd.LossOutputs(z, z, z, None, None, grad)
+            assert lib.vsd_topk_distill(x, dt, R, V, z, z, 0, 4, 1.0, None, 1.0, C.byref(o), z, big,
+                                        None) == 1
