@@ -868,3 +868,84 @@ def test_a_gradient_alone_in_its_tensors_place(vsd, R, V, H, piece):
         with pytest.raises(vsd.VsdError) as e:
             bad()
         assert e.value.code == 1
+
+
+KEPT = [  # R, V, H, K: more than 128 rows whose logits are kept, in one part of K or several
+    (129, 1000, 64, 1), (257, 3000, 264, 4), (300, 3000, 520, 1), (513, 1500, 1032, 33),
+    (300, 33000, 40, 3), (1000, 2000, 136, 128)]
+
+
+@pytest.mark.parametrize("R,V,H,K", KEPT)
+@pytest.mark.parametrize("ignored", [False, True])
+def test_kept_logits(vsd, R, V, H, K, ignored):
+    """The library's choice for some hundred rows, with every row counted and not."""
+    h, w, g = head(R, V, H, 1100 + R, gain=1.0 / H ** 0.5)
+    ids, t = teacher(R, V, K, g)
+    if ignored:
+        ids[torch.randperm(R, generator=g, device="cuda")[: R // 3]] = -1
+    rw = torch.rand(R, generator=g, device="cuda")
+    got = vsd.lmhead_distill(h, w, ids, t, T=2.0, row_weight=rw)
+    i64, p, counted = teacher_target(ids, t, 2.0, V)
+    H64, W64 = f64(h), f64(w)
+    x = H64 @ W64.T
+    ref = plain(x, i64, p, counted, f64(rw), 2.0)
+    check(got, ref, x, logit_bound(H64, W64), 2.0, torch.bfloat16, H64, W64, i64, p)
+
+
+def test_several_pieces_by_the_librarys_choice(vsd):
+    """4096 rows whose G passes a piece: all gradients against float64."""
+    R, V, H = 4096, 20000, 72
+    h, w, g = head(R, V, H, 17, gain=0.1)
+    labels = torch.randint(0, V, (R,), generator=g, device="cuda").to(torch.int32)
+    labels[::5] = -100
+    n = vsd.lmhead_loss_workspace_bytes
+    assert n(R, V, H) < n(R, V, H, piece=V)  # (more than one piece)
+    got = vsd.lmhead_cross_entropy(h, w, labels)
+    counted = labels != -100
+    H64, W64, lab = h.double(), w.double(), labels.clamp(min=0).long()[:, None]
+    x = H64 @ W64.T
+    size = (H64.abs() @ W64.abs().T).amax(1)
+    G = torch.softmax(x, 1)
+    row = torch.where(counted, torch.logsumexp(x, 1) - x.gather(1, lab)[:, 0], 0.0)
+    tol = 2 * H * U * size + 16 * U * x.abs().amax(1) + 2.0 ** -20
+    assert ((got["row_loss"].double() - row).abs() <= tol).all()
+    G.scatter_add_(1, lab, -torch.ones_like(lab, dtype=torch.float64))
+    G *= (counted / counted.sum())[:, None]
+    # q's error by its logits', G's rounding, fp32 sums, the output's rounding
+    rel = 2.0 ** -8 + 2 * float(tol.max())
+    for name, a, b in (("d_hidden", G, W64), ("d_weight", G.T, H64)):
+        want = a @ b
+        bound = (rel + a.shape[1] * U) * (a.abs() @ b.abs()) + 2.0 ** -8 * want.abs()
+        assert ((got[name].double() - want).abs() <= bound).all(), name
+
+
+@pytest.mark.parametrize("R,V,H,K", [(40, 3000, 264, 5), (300, 1537, 1032, 64), (700, 5000, 72, 1)])
+def test_distill_without_gradients(vsd, R, V, H, K):
+    h, w, g = head(R, V, H, 1300 + R, gain=1.0 / H ** 0.5)
+    ids, t = teacher(R, V, K, g, torch.bfloat16)
+    ids[1::9] = -1
+    rw = torch.rand(R, generator=g, device="cuda")
+    got = vsd.lmhead_distill(h, w, ids, t, T=2.0, row_weight=rw, d_hidden=False, d_weight=False)
+    assert set(got) == {"loss", "row_loss", "logz"}
+    i64, p, counted = teacher_target(ids, t, 2.0, V)
+    H64, W64 = f64(h), f64(w)
+    x = H64 @ W64.T
+    ref = plain(x, i64, p, counted, f64(rw), 2.0)
+    check(got, ref, x, logit_bound(H64, W64), 2.0, torch.bfloat16, H64, W64, i64, p)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("R,V,K", [(1, 1, 1), (9, 1031, 128), (700, 2000, 6), (40, 128256, 10)])
+def test_topk_without_gradient(vsd, R, V, K, dt):
+    g = torch.Generator(device="cuda").manual_seed(1500 + R)
+    x = (4.0 * torch.randn(R, V, generator=g, device="cuda")).to(dt)
+    ids, t = teacher(R, V, K, g)
+    if R > 4:
+        ids[3] = -1
+        x[3] = NAN
+    x64 = f64(x)
+    got = vsd.topk_distill(x, ids, t, T=0.75, grad=False)
+    assert set(got) == {"loss", "row_loss", "logz"}
+    i64, p, counted = teacher_target(ids, t, 0.75, V)
+    ref = plain(x64, i64, p, counted, torch.ones(R).double(), 0.75)
+    check(got, ref, x64, torch.zeros(()).expand(R, 1).double(), 0.75, dt, ids=i64, p=p)
