@@ -40,7 +40,8 @@ constexpr int kRowPad = 256;     // the workspace's rows are a multiple of this
 constexpr int BK = 64;           // K block of the products
 constexpr int kPieceUnit = 256;  // a piece's columns are a multiple of this
 // Bytes of a piece's G: about the L2.  The time hardly depends on it (4096 x 32000
-// x 4096: 2.44 ms with pieces of 8192 columns, 2.45 with one of 32000).
+// x 4096 with pieces of 8192, 16128 and 32000 columns: within the 5 % that the power
+// limit moves them).
 constexpr int64_t kPieceBytes = 128ll << 20;
 constexpr int64_t kKeepBytes = 64ll << 20;
 // Pairs of SMs, of the part these kernels are built for: the plan and the workspace's
@@ -60,7 +61,6 @@ constexpr int kStoreCost = 5;    // K blocks of time that storing a d_weight til
 // dominate the products.  The outputs take the factor back in fp32 (kappa).
 constexpr float kTopMantissa = 1.984375f;
 
-size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 struct LmWs {
@@ -80,8 +80,8 @@ LmWs lm_ws(const LmLossShape& s) {
     const int64_t vpad = round_up(s.V, kPieceUnit);
     const int64_t most = std::max<int64_t>(1, kPieceBytes / (2 * (int64_t)w.hrows * kPieceUnit));
     // few rows: the whole vocabulary's logits (4 bytes) and G (2) fit the space
-    // of the weight, or are small; they are made once (48 x 128256 x 4096: 555 us,
-    // 747 with two sweeps; 1000 x 32000 x 4096: 535 and 641)
+    // of the weight, or are small; they are made once (48 x 128256 x 4096: 540 us,
+    // 714 with two sweeps; 1000 x 32000 x 4096: 528 and 637)
     const int64_t whole = 6 * (int64_t)w.hrows * vpad;
     w.keep = grads && (s.piece ? s.piece >= s.V : true) && w.rpad <= 65280 &&  // (a grid's rows)
              whole <= std::max<int64_t>(2 * (int64_t)s.V * s.H, kKeepBytes);
@@ -98,7 +98,10 @@ LmWs lm_ws(const LmLossShape& s) {
     // time by 0.3 us a K block (its own rounds, or where d_weight's jobs fill in
     // the pairs' share of all and part of a job), 6 us for the launch that adds
     // parts up and, for a part, 0.1 us and its bytes' way out and back at 6 TB/s;
-    // each part of 8 K blocks at least
+    // each part of 8 K blocks at least.  (d_hidden alone, and with the best of nine
+    // other numbers of parts: 48 x 128256 x 4096 353 us and 348, 300 x 32000 x 4096 201
+    // and 201, 777 x 32003 x 2056 306 and 306, 40 x 60000 x 264 47 and 48, 1000 x 128256
+    // x 1024 531 and 527; in one part 696, 256, 358, 270 and 913)
     const int64_t ht = (s.H + kRowPad - 1) / kRowPad, tiles = (int64_t)(w.rpad / kRowPad) * ht;
     w.split = 1;
     if (tiles < 2 * kPairs) {
@@ -152,10 +155,6 @@ LmWs lm_ws(const LmLossShape& s) {
     w.carry = take(w.cut_grad || w.cut_prod ? 4 * kCarry * 2 * kPairs : 0);
     w.total = o;
     return w;
-}
-
-template <typename U> U* at(void* ws, size_t off) {
-    return reinterpret_cast<U*>(static_cast<char*>(ws) + off);
 }
 
 // ------------------------------------------------------------ rows
@@ -241,7 +240,7 @@ struct PairBars {
     int err;
 };
 // kStats1: kStats where one partial sum spans the hidden size (1715 x 105611 x
-// 104: 390 us a step, 416 with kStats)
+// 104: 371 us a step, 393 with kStats)
 enum { kStats = 0, kKeep = 1, kGrad = 2, kProd = 3, kStats1 = 4 };
 
 // Few rows (NF = 64 or 128 at most): the products with the rows' side are turned
@@ -254,9 +253,9 @@ template <int MODE, int NF> struct PairCfg {
     static constexpr bool kFew = NF > 0;
     // Epilogues that exponentiate take as long as some ten K blocks: two sets of
     // warps, one for each accumulator, for the gradient and for kStats1 (1715 x
-    // 105611 x 104: 387 us, 418 with one).  kStats and kKeep have no registers
-    // for it; the products gain more from the stage it costs (300 x 32000 x
-    // 4096: 258 us with one set, 266 with two).
+    // 105611 x 104: 371 us; 400 with one set for the gradient, 399 for kStats1).
+    // kStats and kKeep have no registers for it; the products gain more from the
+    // stage it costs (3 % of a step of 300 x 32000 x 4096).
     static constexpr int kSets = MODE == kGrad || MODE == kStats1 ? 2 : 1;
     static constexpr int kThreads = 32 * (4 + kSets * kTileWarps);
     static constexpr int kFewB = NF / 2 * BK * 2;  // the rows' half of a turned stage
@@ -1257,25 +1256,26 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     const LmWs w = lm_ws(s);
     const int R = s.R, V = s.V, H = s.H, K = s.K;
     const bool grads = s.dh || s.dw;
-    Targets tg{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
-               at<float>(ws, w.plogp), at<float>(ws, w.w), nullptr, at<int32_t>(ws, w.rowmap),
-               at<int32_t>(ws, w.rowinv), at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum),
-               at<float>(ws, w.wmax), at<float>(ws, w.kappa), at<float>(ws, w.unit),
-               at<float>(ws, w.share), at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
-    bf16* hid = at<bf16>(ws, w.hid);
-    float* X = at<float>(ws, w.X);
-    bf16* G = at<bf16>(ws, w.G);
-    float2* tab = at<float2>(ws, w.tab);
-    float *xk = at<float>(ws, w.xk), *top = at<float>(ws, w.top), *coef = at<float>(ws, w.coef),
-          *coefs = at<float>(ws, w.coefs), *kappa = at<float>(ws, w.kappa),
-          *dh = at<float>(ws, w.dh);
+    Targets tg{ws_at<int32_t>(ws, w.n), ws_at<int32_t>(ws, w.id), ws_at<float>(ws, w.p),
+               ws_at<float>(ws, w.plogp), ws_at<float>(ws, w.w), nullptr,
+               ws_at<int32_t>(ws, w.rowmap), ws_at<int32_t>(ws, w.rowinv),
+               ws_at<int32_t>(ws, w.nrows), ws_at<double>(ws, w.wsum), ws_at<float>(ws, w.wmax),
+               ws_at<float>(ws, w.kappa), ws_at<float>(ws, w.unit), ws_at<float>(ws, w.share),
+               ws_at<int32_t>(ws, w.done), ws_at<int32_t>(ws, w.status)};
+    bf16* hid = ws_at<bf16>(ws, w.hid);
+    float* X = ws_at<float>(ws, w.X);
+    bf16* G = ws_at<bf16>(ws, w.G);
+    float2* tab = ws_at<float2>(ws, w.tab);
+    float *xk = ws_at<float>(ws, w.xk), *top = ws_at<float>(ws, w.top),
+          *coef = ws_at<float>(ws, w.coef), *coefs = ws_at<float>(ws, w.coefs),
+          *kappa = ws_at<float>(ws, w.kappa), *dh = ws_at<float>(ws, w.dh);
     const float c = (float)(kLog2e / (double)T);
     const int64_t hrows = w.hrows;
     PairMaps maps;
     memset(&maps, 0, sizeof(maps));
     using vsd_lm::make_map_sw128;
-    // few rows: turned products (128256 x 4096: 555 us at 48 rows, 580 not turned;
-    // 596 and 617 at 100)
+    // few rows: turned products (128256 x 4096: 540 us at 48 rows, 549 not turned;
+    // 589 and 600 at 100)
     const int nf = !w.keep ? 0 : R <= 64 ? 64 : R <= 128 ? 128 : 0;
     const int rbox = nf ? nf / 2 : 128;                              // rows of a K-major half tile
     bool ok = make_map_sw128(&maps.a, hid, false, hrows, H, H, rbox) &&
@@ -1317,7 +1317,7 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
     a.want_dw = s.dw;
     a.dh = dh;
     a.row_loss = out.row_loss;
-    a.carry = at<float>(ws, w.carry);
+    a.carry = ws_at<float>(ws, w.carry);
     a.X = X;
     a.ldx = w.piece;
     a.d_hidden = static_cast<bf16*>(out.d_hidden);
@@ -1353,8 +1353,9 @@ cudaError_t lmloss(const LmLossShape& s, const void* hidden, const void* weight,
         e = launch_row_loss<float, bf16, true>(X, G, ra, T, kTopMantissa, resident_clusters, st);
     } else {
         e = launch_dep(true, k_rows, dim3((unsigned)((R + kRowsOf - 1) / kRowsOf)), 256, 0, 1, st,
-                       tab, (int)(2 * units), (int64_t)w.rpad, tg, K, c, 1.0 / (double)T, xk, top, coef,
-                       coefs, out.row_loss, out.logz, at<double>(ws, w.part), grads ? nullptr : out.loss);
+                       tab, (int)(2 * units), (int64_t)w.rpad, tg, K, c, 1.0 / (double)T, xk, top,
+                       coef, coefs, out.row_loss, out.logz, ws_at<double>(ws, w.part),
+                       grads ? nullptr : out.loss);
     }
     if (e != cudaSuccess || !grads) return e;
     for (int q = 0; q < w.npiece; ++q) {

@@ -3,11 +3,18 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <stddef.h>
 
 #include "vsd.h"
 #include "vsd_target.cuh"
 
 namespace vsd {
+
+// Workspaces: arrays at multiples of 256 bytes.
+inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+template <typename U> U* ws_at(void* ws, size_t off) {
+    return reinterpret_cast<U*>(static_cast<char*>(ws) + off);
+}
 
 // Sizes of an LM-head loss call.
 struct LmLossShape {

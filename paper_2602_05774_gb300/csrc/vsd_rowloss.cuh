@@ -459,8 +459,8 @@ cudaError_t launch_row_loss(const TI* logits, TO* grad, RowArgs a, float T, floa
     int64_t C = 1;
     while (C < kMaxCluster && C * kSegBytes < 16 * need) C *= 2;
     int64_t vper = std::min<int64_t>((need + C - 1) / C, kSegMax / 16);
-    // four vectors a thread at a time (4096 x 128256 bf16, the loss alone: 202 us,
-    // 218 with one), one where a segment has no more than two
+    // four vectors a thread at a time (4096 x 128256 bf16, the loss alone: 7 % less
+    // time than with one), one where a segment has no more than two
     a.by4 = vper > 2 * kRowThreads;
     const int64_t unit = kRowThreads * (a.by4 ? 4 : 1);
     vper = (vper + unit - 1) / unit * unit;

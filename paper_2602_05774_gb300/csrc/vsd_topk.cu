@@ -20,8 +20,6 @@
 namespace vsd {
 namespace {
 
-size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 struct TopkWs {
     size_t status, done, zero_end, nrows, wsum, wmax, kappa, unit, share, n, id, p, plogp, w, part,
         total;
@@ -55,10 +53,6 @@ TopkWs topk_ws(int R, int K) {
     return w;
 }
 
-template <typename U> U* at(void* ws, size_t off) {
-    return reinterpret_cast<U*>(static_cast<char*>(ws) + off);
-}
-
 }  // namespace
 
 bool topk_shape_ok(int R, int V, int K) {
@@ -74,11 +68,12 @@ cudaError_t topk_distill(const void* logits, bool bf16, const TargetIn& in, floa
                          cudaStream_t st) {
     const TopkWs w = topk_ws(in.R, in.K);
     RowArgs a{};
-    a.tg = Targets{at<int32_t>(ws, w.n), at<int32_t>(ws, w.id), at<float>(ws, w.p),
-                   at<float>(ws, w.plogp), at<float>(ws, w.w), at<double>(ws, w.part), nullptr,
-                   nullptr, at<int32_t>(ws, w.nrows), at<double>(ws, w.wsum),
-                   at<float>(ws, w.wmax), at<float>(ws, w.kappa), at<float>(ws, w.unit),
-                   at<float>(ws, w.share), at<int32_t>(ws, w.done), at<int32_t>(ws, w.status)};
+    a.tg = Targets{ws_at<int32_t>(ws, w.n), ws_at<int32_t>(ws, w.id), ws_at<float>(ws, w.p),
+                   ws_at<float>(ws, w.plogp), ws_at<float>(ws, w.w), ws_at<double>(ws, w.part),
+                   nullptr, nullptr, ws_at<int32_t>(ws, w.nrows), ws_at<double>(ws, w.wsum),
+                   ws_at<float>(ws, w.wmax), ws_at<float>(ws, w.kappa), ws_at<float>(ws, w.unit),
+                   ws_at<float>(ws, w.share), ws_at<int32_t>(ws, w.done),
+                   ws_at<int32_t>(ws, w.status)};
     a.rows = in.R;
     a.V = in.V;
     a.K = in.K;
