@@ -371,10 +371,13 @@ vsd_status vsd_lmhead_backward(const void* hidden, const void* weight, int32_t H
  *
  * The target p is the label's one-hot (cross entropy, T = 1), or the teacher's
  * top logits renormalised over the row's valid entries,
- * p_rk = softmax_k(teacher_rk / T) (Eq. klv's distribution, from supplied
- * logits).  A row is counted unless its label is ignore_index, or none of its
- * teacher entries is valid; rows not counted have loss, logz and gradient 0,
- * whatever their hidden states or logits hold (NaN included).
+ * p_rk = softmax_k(teacher_rk / T).  q is over the whole vocabulary; the top-K
+ * term of the E/M step (kl_weight) is another objective: it renormalises the
+ * draft over the K tokens too and has no gradient outside them.
+ *
+ * A row is counted unless its label is ignore_index, or none of its teacher
+ * entries is valid; rows not counted have loss, logz and gradient 0, whatever
+ * their hidden states or logits hold (NaN included).
  *   labels         [R]; a label outside [0, V) other than ignore_index sets
  *                  VSD_STATUS_BAD_TOKEN and its row is not counted.
  *   teacher_ids    [R][K]; a negative id is no entry (its logit is not looked
@@ -413,9 +416,11 @@ typedef struct {
  * K: entries of a teacher row (1 for labels); grads: whether a gradient is
  * asked for; piece: vocabulary columns worked on at a time, 0 = the library's
  * choice.  The logits are never kept whole when R is large: the workspace holds
- * the gradient of one piece (bf16).  Where a piece spans the vocabulary and its
- * logits are no larger than the weight (few rows), they are kept and made
- * once.  A larger piece uses more workspace and fewer launches. */
+ * the gradient of one piece (bf16), statistics of 16 bytes a row and 256 columns,
+ * the rows' packed hidden states and d_hidden's sums in fp32 (of several parts of
+ * the vocabulary where its tiles are few).  Where a piece spans the vocabulary
+ * and its logits are no larger than the weight (few rows), they are kept and
+ * made once.  A larger piece uses more workspace and fewer launches. */
 size_t vsd_lmhead_loss_workspace_bytes(int32_t R, int32_t V, int32_t H, int32_t K, int32_t grads,
                                        int32_t piece);
 
@@ -426,9 +431,11 @@ size_t vsd_lmhead_loss_workspace_bytes(int32_t R, int32_t V, int32_t H, int32_t 
  *   (VSD_ERR_INVALID_ARG); 1 <= V <= 1048576, 1 <= R <= 16777216.
  * Logits are sums of exact products in fp32, never rounded to bf16; their
  * gradient is rounded to bf16 once, as the operand of the two products that
- * carry it, and those are summed in fp32 and rounded once to bf16.  ws as for
- * the other calls (256-byte aligned, its first word the status word, cleared
- * here). */
+ * carry it, and those are summed in fp32 and rounded once to bf16.  The tensor
+ * cores truncate as they sum, so longer sums are made of parts added to nearest:
+ * of 512 elements for the losses, 8192 for logits made again for the gradient,
+ * 65536 for the products.  ws as for the other calls (256-byte aligned, its
+ * first word the status word, cleared here). */
 vsd_status vsd_lmhead_cross_entropy(const void* hidden, const void* weight, int32_t R, int32_t V,
                                     int32_t H, const int32_t* labels, int32_t ignore_index,
                                     const float* row_weight, float grad_scale, int32_t piece,
