@@ -13,7 +13,7 @@
 // kept and made once.
 //
 // Bound by the tensor cores for many rows (4096 x 32000 x 4096 with gradients:
-// 2.51 to 2.56 ms from GPU to GPU for 4.29 TFLOP, 1.68 to 1.71 PFLOP/s, where
+// 2.51 to 2.57 ms from GPU to GPU for 4.29 TFLOP, 1.67 to 1.71 PFLOP/s, where
 // cuBLAS sustains 1.69), by memory for few (48 x 128256 x 4096: 0.54 ms for the
 // weight read twice and its gradient written, 3.15 GB).
 #include <cuda_bf16.h>
@@ -1086,8 +1086,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairCfg<MODE, NF>::k
 // kRowsOf counted rows per block, 256 / kRowsOf threads each: log-partition,
 // loss and gradient coefficient.  A thread takes every (256 / kRowsOf)-th part
 // and list entry of its row (consecutive threads: consecutive rows, so a read
-// fills its 32-byte sectors).  Latency bounds it: 8 us at 4096 rows x 250 parts,
-// 17 with 32 rows to a block.  With `loss` the blocks' weighted losses are added
+// fills its 32-byte sectors).  Latency bounds it: 9 us at 4096 rows x 250 parts, about
+// half of what 32 rows to a block take.  With `loss` the blocks' weighted losses are added
 // in block order by the last block to finish.
 constexpr int kRowsOf = 8;
 __global__ void __launch_bounds__(256)
