@@ -28,6 +28,11 @@ SYMBOLS = ("vsd_workspace_bytes", "vsd_sample_paths", "vsd_verify_paths",
            "vsd_reference_logkappa", "vsd_tree_estep_mstep", "vsd_lmhead_backward",
            "vsd_lmhead_loss_workspace_bytes", "vsd_lmhead_cross_entropy", "vsd_lmhead_distill",
            "vsd_topk_distill_workspace_bytes", "vsd_topk_distill")
+# include/vsd_decode.h
+DECODE_SYMBOLS = ("vsd_quantize_fp8", "vsd_lmhead_logits_fp8",
+                  "vsd_sample_filtered_workspace_bytes", "vsd_sample_filtered")
+STATUS_BAD_PARAM = 16
+FP8_BLOCK = 128
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
 
@@ -59,6 +64,7 @@ LINEAR_FIELDS = ("tokens", "logq_tok", "alpha", "accept", "accept_len", "corr_to
                  "kl_loss")
 TREE_FIELDS = ("alpha", "accept", "path_accept", "logkappa", "corr_tokens", "deepest",
                "accept_len", "bonus", "row_stats")
+FILTERED_FIELDS = ("tokens", "logq_tok", "kept", "filtered")
 LOSS_FIELDS = ("loss", "row_loss", "logz", "d_hidden", "d_weight", "grad")
 TREE_EM_FIELDS = ("corr_tokens", "logq_tok", "logq_corr", "logkappa", "logkappa_corr",
                   "logkappa_ref", "weights", "loss", "grad")
@@ -78,6 +84,16 @@ class TreeEmOutputs(C.Structure):
 
 class LossOutputs(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in LOSS_FIELDS]
+
+
+class Policy(C.Structure):
+    _fields_ = [("T", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float),
+                ("min_p", C.c_float), ("row_T", C.c_void_p), ("row_top_k", C.c_void_p),
+                ("row_top_p", C.c_void_p), ("row_min_p", C.c_void_p)]
+
+
+class FilteredOutputs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in FILTERED_FIELDS]
 
 
 _LIB = None
@@ -136,6 +152,13 @@ def _lib():
         lib.vsd_topk_distill_workspace_bytes.restype = C.c_size_t
         lib.vsd_topk_distill.argtypes = [vp, C.c_int, i32, i32, vp, vp, C.c_int, i32, f32, vp,
                                          f32, C.POINTER(LossOutputs), vp, C.c_size_t, vp]
+        lib.vsd_quantize_fp8.argtypes = [vp, C.c_int, i32, i32, i32, vp, vp, vp]
+        lib.vsd_lmhead_logits_fp8.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, C.c_size_t,
+                                              vp]
+        lib.vsd_sample_filtered_workspace_bytes.argtypes = [i32] * 2
+        lib.vsd_sample_filtered_workspace_bytes.restype = C.c_size_t
+        lib.vsd_sample_filtered.argtypes = [vp, C.c_int, i32, i32, C.POINTER(Policy), vp,
+                                            C.POINTER(FilteredOutputs), vp, C.c_size_t, vp]
         lib.vsd_status_string.argtypes = [C.c_int]
         lib.vsd_status_string.restype = C.c_char_p
         lib.vsd_version.restype = C.c_char_p
@@ -144,7 +167,8 @@ def _lib():
                      "vsd_noalloc_device_status", "vsd_reference_logkappa",
                      "vsd_tree_estep_mstep",
                      "vsd_lmhead_logits", "vsd_lmhead_estep_mstep", "vsd_lmhead_backward",
-                     "vsd_lmhead_cross_entropy", "vsd_lmhead_distill", "vsd_topk_distill"):
+                     "vsd_lmhead_cross_entropy", "vsd_lmhead_distill", "vsd_topk_distill",
+                     "vsd_quantize_fp8", "vsd_lmhead_logits_fp8", "vsd_sample_filtered"):
             getattr(lib, name).restype = C.c_int
         _LIB = lib
     return _LIB
@@ -685,6 +709,127 @@ def topk_distill(logits, teacher_ids, teacher_logits, T=1.0, row_weight=None, gr
                float(T), _data_ptr(row_weight), float(grad_scale), C.byref(st), ws.data_ptr(),
                ws.nbytes)
     return out
+
+
+def quantize_fp8(x, block_rows=1, q=None, scale=None):
+    """(q, scale): x [R][H] (float32 or bf16, H a multiple of 16) in e4m3 with a power
+    of two as scale for each block of block_rows (1: hidden states, 128: the weight)
+    rows and 128 columns.  q and scale may be given to write into."""
+    _need_cuda(x, q, scale)
+    _same_device(x, q, scale)
+    if x.dim() != 2:
+        raise ValueError("x must be [R, H]")
+    if block_rows not in (1, FP8_BLOCK):
+        raise ValueError("block_rows must be 1 or %d" % FP8_BLOCK)
+    R, H = x.shape
+    shape = _scale_shape(R, H, block_rows)
+    if q is None:
+        q = torch.empty(R, H, dtype=torch.float8_e4m3fn, device=x.device)
+    if scale is None:
+        scale = torch.empty(shape, dtype=torch.float32, device=x.device)
+    _check_fp8(q, scale, block_rows, "q", "scale")
+    if q.shape != x.shape:
+        raise ValueError("q must have the shape of x")
+    _loss_call("vsd_quantize_fp8", x.device, x.data_ptr(), _dtype_code(x), R, H, int(block_rows),
+               q.data_ptr(), scale.data_ptr())
+    return q, scale
+
+
+def _scale_shape(R, H, block_rows):
+    return (-(-R // block_rows), -(-H // FP8_BLOCK))
+
+
+def _check_fp8(q, scale, block_rows, name, scale_name):
+    if q.dtype != torch.float8_e4m3fn or q.dim() != 2:
+        raise ValueError("%s must be a float8_e4m3fn matrix" % name)
+    if scale.dtype != torch.float32 or tuple(scale.shape) != _scale_shape(*q.shape, block_rows):
+        raise ValueError("%s must be float32 of shape %s"
+                         % (scale_name, _scale_shape(*q.shape, block_rows)))
+
+
+def lmhead_logits_fp8(hidden, hidden_scale, weight, weight_scale, out=None, workspace=None):
+    """Draft logits [R][V] (bf16) = hidden [R][H] . weight [V][H]^T of e4m3 matrices:
+    hidden with a scale for each row and 128 columns, weight with one for each 128 x 128
+    block, as quantize_fp8(hidden) and quantize_fp8(weight, block_rows=128) give them."""
+    _need_cuda(hidden, hidden_scale, weight, weight_scale, out, workspace)
+    _same_device(hidden, hidden_scale, weight, weight_scale, out, workspace)
+    _check_fp8(hidden, hidden_scale, 1, "hidden", "hidden_scale")
+    _check_fp8(weight, weight_scale, FP8_BLOCK, "weight", "weight_scale")
+    (R, H), V = hidden.shape, weight.shape[0]
+    if weight.shape[1] != H:
+        raise ValueError("hidden and weight disagree on the hidden size")
+    dev = hidden.device
+    if out is None:
+        out = torch.empty(R, V, dtype=torch.bfloat16, device=dev)
+    elif out.dtype != torch.bfloat16 or tuple(out.shape) != (R, V):
+        raise ValueError("out must be bfloat16 of shape (%d, %d)" % (R, V))
+    ws = workspace if workspace is not None else torch.empty(256, dtype=torch.uint8, device=dev)
+    _loss_call("vsd_lmhead_logits_fp8", dev, hidden.data_ptr(), hidden_scale.data_ptr(),
+               weight.data_ptr(), weight_scale.data_ptr(), R, V, H, out.data_ptr(), ws.data_ptr(),
+               ws.nbytes)
+    return out
+
+
+def _policy(R, logits, T, top_k, top_p, min_p):
+    """The struct, and the tensors in it."""
+    values, rows = [], []
+    for name, v, dtype, off in (("T", T, torch.float32, 1.0), ("top_k", top_k, torch.int32, 0),
+                                ("top_p", top_p, torch.float32, 1.0),
+                                ("min_p", min_p, torch.float32, 0.0)):
+        if torch.is_tensor(v):
+            _need_cuda(v)
+            _same_device(logits, v)
+            if v.dtype != dtype or tuple(v.shape) != (R,):
+                raise ValueError("%s must be a number or %s of shape (%d,)" % (name, dtype, R))
+            values.append(off)
+            rows.append(v.data_ptr())
+        else:
+            values.append(max(0, min(int(v), 2 ** 31 - 1)) if dtype == torch.int32 else float(v))
+            rows.append(None)
+    return Policy(*values, *rows)
+
+
+def _filtered_call(logits, u, T, top_k, top_p, min_p, filtered, workspace):
+    _need_cuda(logits, u, workspace)
+    _same_device(logits, u, workspace)
+    V = logits.shape[-1]
+    R = _rows(logits, V)
+    dev = logits.device
+    out = {}
+    if u is not None:
+        if u.dtype != torch.float32 or u.numel() != R:
+            raise ValueError("u must be float32, one for each of the %d rows" % R)
+        out["tokens"] = torch.empty(R, dtype=torch.int32, device=dev)
+        out["logq_tok"] = torch.empty(R, dtype=torch.float32, device=dev)
+    out["kept"] = torch.empty(R, dtype=torch.int32, device=dev)
+    filt = _grad_tensor(filtered, logits, "filtered")
+    if filt is not None:
+        out["filtered"] = filt
+    policy = _policy(R, logits, T, top_k, top_p, min_p)
+    ws = _loss_workspace(_lib().vsd_sample_filtered_workspace_bytes(R, V), workspace, dev)
+    st = FilteredOutputs(*[_data_ptr(out.get(n)) for n in FILTERED_FIELDS])
+    _loss_call("vsd_sample_filtered", dev, logits.data_ptr(), _dtype_code(logits), R, V,
+               C.byref(policy), _data_ptr(u), C.byref(st), ws.data_ptr(), ws.nbytes)
+    return out
+
+
+def sample_filtered(logits, u, T=1.0, top_k=0, top_p=1.0, min_p=0.0, filtered=False,
+                    workspace=None):
+    """One token a row of logits [R][V] by the uniforms u [R], from what temperature,
+    top-k, top-p and min-p leave: {"tokens": [R], "logq_tok": [R] its log probability
+    among the kept, "kept": [R] how many are}.  Each parameter is a number or a tensor
+    [R] (float32; top_k int32); T = 0 is greedy, top_k <= 0, top_p >= 1 and min_p <= 0
+    are off.  filtered=True adds "filtered", the logits with the other tokens at -inf,
+    for the verification of the drawn tokens at the same T; a tensor is written into,
+    the logits themselves among them."""
+    return _filtered_call(logits, u, T, top_k, top_p, min_p, filtered, workspace)
+
+
+def filter_logits(logits, T=1.0, top_k=0, top_p=1.0, min_p=0.0, out=True, workspace=None):
+    """The logits [R][V] with the tokens at -inf that sample_filtered() would not keep:
+    {"filtered": [R][V], "kept": [R]}.  `out`: a tensor to write into, the logits
+    themselves among them."""
+    return _filtered_call(logits, None, T, top_k, top_p, min_p, out, workspace)
 
 
 def estep_mstep_noalloc(draft, target, u_draft, u_accept, u_correct, K, D, T,
