@@ -84,7 +84,8 @@ def _code_only(text):
 # Sources of the supervised losses and of the 8-bit head's drafting alone: no workload
 # here runs their kernels.
 LOSS_SOURCES = ("vsd_lmloss.cu", "vsd_loss.h", "vsd_pair.cuh", "vsd_rowloss.cuh",
-                "vsd_target.cuh", "vsd_topk.cu", "vsd_fixed.cuh", "vsd_fp8.cu", "vsd_sample.cu")
+                "vsd_target.cuh", "vsd_topk.cu", "vsd_dep.cuh", "vsd_fixed.cuh", "vsd_fp8.cu",
+                "vsd_sample.cu")
 
 
 def kernel_source_hash():
