@@ -68,15 +68,6 @@ __host__ __device__ __forceinline__ int exp_shift(int V) {
     while (s < 30 && (1 << s) < V) ++s;
     return s < 12 ? 12 : s;
 }
-__host__ __device__ __forceinline__ ExpScale exp_scale(float T, int shift) {
-    const double c = 1.4426950408889634073599246810019 / (double)T;
-    ExpScale s;
-    s.c = (float)c;
-    s.c_lo = (float)(c - (double)s.c);
-    s.shift = shift;
-    return s;
-}
-
 #ifdef __CUDA_ARCH__
 #define VSD_ADD(a, b) __fadd_rn(a, b)
 #define VSD_MUL(a, b) __fmul_rn(a, b)
@@ -87,12 +78,30 @@ __host__ __device__ __forceinline__ ExpScale exp_scale(float T, int shift) {
 #define VSD_FMA(a, b, c) fmaf(a, b, c)
 #endif
 
+// n / T in two floats, n given in two.
+__host__ __device__ __forceinline__ void over(float n, float n_lo, float T, float& hi, float& lo) {
+    hi = n / T;
+    lo = VSD_FMA(-hi, T, n);
+    lo = VSD_ADD(lo, n_lo) / T;
+}
+__host__ __device__ __forceinline__ ExpScale exp_scale(float T, int shift) {
+    ExpScale s;
+    over(1.44269502162933349609375f, 1.92596299e-8f, T, s.c, s.c_lo);  // log2(e)
+    s.shift = shift;
+    return s;
+}
+// m - x in two floats.
+__host__ __device__ __forceinline__ float gap(float x, float m, float& lo) {
+    const float d = VSD_ADD(m, -x), b = VSD_ADD(d, -m);
+    lo = VSD_ADD(VSD_ADD(m, -VSD_ADD(d, -b)), -VSD_ADD(x, b));
+    return d;
+}
+
 // exp((x - m) / T) in units of 2^-(62 - shift), to the nearest; x <= m.
 __host__ __device__ __forceinline__ uint64_t exp_fixed(float x, float m, const ExpScale& s,
                                                        const uint64_t* tab) {
-    // d + e = m - x
-    const float d = VSD_ADD(m, -x), b = VSD_ADD(d, -m);
-    const float e = VSD_ADD(VSD_ADD(m, -VSD_ADD(d, -b)), -VSD_ADD(x, b));
+    float e;
+    const float d = gap(x, m, e);
     const float y = VSD_MUL(d, s.c);
     if (!(y < 63.f)) return 0;  // (and where m - x is past a float's range)
     const float yl = VSD_FMA(e, s.c, VSD_FMA(d, s.c_lo, VSD_FMA(d, s.c, -y)));
@@ -121,6 +130,32 @@ __host__ __device__ __forceinline__ uint64_t exp_fixed(float x, float m, const E
     const uint64_t v = w - (uint64_t)((int64_t)wh * z >> 11);
     const int sh = s.shift + (at >> 11);
     return sh < 64 ? (v + (1ull << (sh - 1))) >> sh : 0;
+}
+
+// ln(e / w) for e, w in such units, e = exp((x - m) / T) and w a sum of such with e
+// among them: -(m - x) / T - ln(w), rounded once but for some 2^-8 of a step.  ln(w)
+// is the float l = logf(w) and what w exp(-l) is off 1.
+__host__ __device__ __forceinline__ float log_share(float x, float m, float T, uint64_t w, int shift,
+                                                    const uint64_t* tab) {
+    float inv, inv_lo, e;
+    over(1.f, 0.f, T, inv, inv_lo);
+    const float d = gap(x, m, e), y = VSD_MUL(d, inv);
+    const float yl = VSD_FMA(e, inv, VSD_FMA(d, inv_lo, VSD_FMA(d, inv, -y)));
+    const float one = ldexpf(1.f, shift - 62);
+    const float l = logf((float)w * one);
+    // w exp(-l), about 1
+    const uint64_t back = exp_fixed(-l, 0.f, exp_scale(1.f, 12), tab);
+#ifdef __CUDA_ARCH__
+    const uint64_t hi = __umul64hi(w, back), lo = w * back;
+#else
+    const unsigned __int128 p = (unsigned __int128)w * back;
+    const uint64_t hi = (uint64_t)(p >> 64), lo = (uint64_t)p;
+#endif
+    const uint64_t q = hi << (shift + 2) | lo >> (62 - shift);  // in units of 2^-50
+    const float t = (float)((int64_t)(q - (1ull << 50))) * 0x1p-50f;
+    const float s = VSD_ADD(y, l), b = VSD_ADD(s, -y);
+    const float sl = VSD_ADD(VSD_ADD(y, -VSD_ADD(s, -b)), VSD_ADD(l, -b));
+    return -VSD_ADD(s, VSD_ADD(VSD_ADD(sl, yl), t));
 }
 
 #undef VSD_ADD

@@ -2,274 +2,1068 @@
 // leave of a distribution, and the logits these leave (include/vsd_decode.h).
 //
 // Every filter keeps a first part of the tokens in the order (logit falling, id
-// rising), so what is kept is one place in that order: a logit, and how many of the
-// tokens that equal it.  Masses are whole numbers (vsd_fixed.cuh).
+// rising), so what is kept is one place in that order: a logit, and the last id kept
+// among those that equal it.  Masses that a decision hangs on are whole numbers
+// (vsd_fixed.cuh): sums of them are exact, in whatever order threads add them.
 //
-// One block a row; a filter's place is found by bisection of the logits' ordered
-// bits, each step one pass over the row.
+// A block works on a row, two blocks to an SM.  Bound by memory where the filters leave
+// few tokens: the row comes from memory once, and from L2 for the passes after the
+// first.  A row takes as few of these steps as decide it:
+//
+//   top      the maximum, and a bound `lo` that enough tokens reach: the n-th largest
+//            of each warp's 32 lane maxima, the least over the warps.
+//   list     the tokens from `lo` on, sorted; a prefix sum of their masses gives every
+//            filter's place and the draw.  A nucleus also needs the mass of all others,
+//            a sum of approximate exponentials (2^-16 off at most): where that leaves
+//            the place open, it is summed again exactly.
+//   bracket  a nucleus past the list: a histogram of approximate masses over 1024
+//            steps of the logit brackets its place, the tokens in the bracket are
+//            listed, and the mass above it is summed exactly.
+//   search   whatever these leave open (a list that overflows, by large k or equal
+//            logits): bisection of the logits' ordered bits, exact counts and masses
+//            each step.
+//
+// Where the kept tokens are not all in the list, the exact sums are also kept by region
+// of the row; the draw finds the region, then the token in it.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <float.h>
+#include <limits.h>
 #include <math.h>
 #include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
 
 #include "vsd_common.cuh"
 #include "vsd_decode.h"
 #include "vsd_fixed.cuh"
+#include "vsd_launch.h"
 
 namespace vsd {
 namespace {
 
 constexpr int kSampleThreads = 512;
 constexpr int kSampleWarps = kSampleThreads / 32;
+constexpr int kList = 4096;
+constexpr int kPlaceBits = 12;           // of a place in it
+constexpr int kBins = 1024;
+constexpr int kWant = 128;               // a list's least length, where top-k does not say
+constexpr int kDeep = 8;                 // vectors a lane has in flight
+constexpr int kRegions = (1 << 18) / (32 * kDeep) + 1;
 constexpr float kMinT = 0x1p-64f, kMaxT = 0x1p64f;
+static_assert(kList == 1 << kPlaceBits && kList % kSampleThreads == 0 && kBins % kSampleThreads == 0, "whole rounds");
 
 struct SampleArgs {
     vsd_policy policy;
     const float* u;
     vsd_filtered_outputs out;
-    int V, shift;
+    int R, V, shift;
+    bool same_align;     // filtered rows start where logits rows do, modulo 16 bytes
     int* status;
 };
 
 __constant__ ExpParts kExpParts = make_exp_parts();
 
-__device__ __forceinline__ float value_of(float x) { return x + 0.f; }  // (-0 is 0)
-__device__ __forceinline__ float value_of(__nv_bfloat16 x) { return __bfloat162float(x) + 0.f; }
-__device__ __forceinline__ void put_none(float* x) { *x = -INFINITY; }
-__device__ __forceinline__ void put_none(__nv_bfloat16* x) {
-    *reinterpret_cast<unsigned short*>(x) = 0xFF80u;
+__device__ __forceinline__ float float_of(float x) { return x; }
+__device__ __forceinline__ float float_of(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T none_of();
+template <> __device__ __forceinline__ float none_of<float>() { return -INFINITY; }
+template <> __device__ __forceinline__ __nv_bfloat16 none_of<__nv_bfloat16>() {
+    return __ushort_as_bfloat16(0xFF80u);
 }
-// Bits whose order is the logits'.
+// Bits whose order is the logits' (-0 as 0).
 __device__ __forceinline__ uint32_t key_of(float x) {
-    const uint32_t b = __float_as_uint(x);
+    const uint32_t b = __float_as_uint(x + 0.f);
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float of_key(uint32_t k) {
     return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k);
 }
-constexpr uint32_t kKeyNegInf = 0x007FFFFFu;
+constexpr uint32_t kKeyNone = 0x007FFFFFu;  // of -inf
 
-template <typename U> __device__ __forceinline__ U block_sum(U v, U* part) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
-    __syncthreads();
-    U s = 0;
-    for (int i = 0; i < kSampleWarps; ++i) s += part[i];
-    return s;
+// The largest element of a vector, NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+template <typename T> __device__ __forceinline__ float vec_max_nan(const uint4& v);
+template <> __device__ __forceinline__ float vec_max_nan<float>(const uint4& v) {
+    return max_nan(max_nan(__uint_as_float(v.x), __uint_as_float(v.y)),
+                   max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
+}
+template <> __device__ __forceinline__ float vec_max_nan<__nv_bfloat16>(const uint4& v) {
+    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+    const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(p[0], p[1]), __hmax2_nan(p[2], p[3]));
+    return max_nan(__low2float(m), __high2float(m));
 }
 
-// floor(f w) for 0 <= f < 1
-__device__ __forceinline__ uint64_t share_of(uint64_t w, float f) {
+// Element e of a vector.
+template <typename T> __device__ __forceinline__ float element(const uint4& q, int e);
+template <> __device__ __forceinline__ float element<float>(const uint4& q, int e) {
+    return __uint_as_float(e & 2 ? (e & 1 ? q.w : q.z) : (e & 1 ? q.y : q.x));
+}
+template <> __device__ __forceinline__ float element<__nv_bfloat16>(const uint4& q, int e) {
+    const uint32_t w = e & 4 ? (e & 2 ? q.w : q.z) : (e & 2 ? q.y : q.x);
+    return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
+}
+
+// f w in whole numbers for 0 <= f < 1: rounded down, or up.
+__device__ __forceinline__ uint64_t share_of(uint64_t w, float f, bool up) {
     if (!(f > 0.f)) return 0;
     int e;
-    const float m = frexpf(f, &e);  // f = m 2^e
-    const uint64_t k = (uint64_t)(m * 16777216.f);
-    const int sh = 24 - e;          // f = k 2^-sh, sh >= 24
+    const uint64_t k = (uint64_t)(frexpf(f, &e) * 16777216.f);  // f = k 2^-sh
+    const int sh = 24 - e;                                       // 24 at least
     const uint64_t hi = __umul64hi(w, k), lo = w * k;
-    if (sh >= 128) return 0;
-    return sh >= 64 ? hi >> (sh - 64) : hi << (64 - sh) | lo >> sh;
+    uint64_t q, rest;
+    if (sh >= 128) q = 0, rest = hi | lo;
+    else if (sh > 64) q = hi >> (sh - 64), rest = lo | hi << (128 - sh);
+    else if (sh == 64) q = hi, rest = lo;
+    else q = hi << (64 - sh) | lo >> sh, rest = lo << (64 - sh);
+    return q + (up && rest ? 1 : 0);
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kSampleThreads) k_sample(const T* logits, SampleArgs a) {
-    __shared__ uint64_t tab[kExpTab];
-    __shared__ uint64_t part[kSampleThreads];
-    __shared__ int chosen, limit;
-    const int tid = threadIdx.x, V = a.V;
-    const int64_t r = blockIdx.x;
-    const T* x = logits + r * V;
-    for (int j = tid; j < kExpTab; j += kSampleThreads) tab[j] = exp_entry(kExpParts, j);
-    auto row = [&](const float* p, float v) { return p ? p[r] : v; };
-    const float Tr = row(a.policy.row_T, a.policy.T), top_p = row(a.policy.row_top_p, a.policy.top_p),
-                min_p = row(a.policy.row_min_p, a.policy.min_p);
-    const int top_k = a.policy.row_top_k ? a.policy.row_top_k[r] : a.policy.top_k;
-    const bool ok_par = (Tr == 0.f || (Tr >= kMinT && Tr <= kMaxT)) && top_p == top_p && min_p == min_p;
-    // the maximum, the live tokens
-    uint32_t top = 0;
-    int live = 0;
-    bool bad = false;
-    for (int v = tid; v < V; v += kSampleThreads) {
-        const float f = value_of(x[v]);
-        bad |= !(f < INFINITY);
-        live += f > -INFINITY;
-        top = max(top, key_of(f));
+__device__ __forceinline__ uint64_t warp_sum_u64(uint64_t v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ uint64_t warp_scan_u64(uint64_t v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint64_t n = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += n;
     }
-    live = (int)block_sum((uint64_t)live, part);
-    bad = __syncthreads_or(bad);
-    top = __reduce_max_sync(0xffffffffu, top);
-    if ((tid & 31) == 0) part[tid >> 5] = top;
-    __syncthreads();
-    for (int i = 0; i < kSampleWarps; ++i) top = max(top, (uint32_t)part[i]);
-    T* filt = a.out.filtered ? static_cast<T*>(a.out.filtered) + r * V : nullptr;
-    if (bad || live == 0 || !ok_par) {
-        if (tid == 0) {
-            atomicOr(a.status, (bad || live == 0 ? VSD_STATUS_BAD_ROW : 0) |
-                                   (ok_par ? 0 : VSD_STATUS_BAD_PARAM));
-            if (a.out.tokens) a.out.tokens[r] = -1;
-            if (a.out.logq_tok) a.out.logq_tok[r] = NAN;
-            if (a.out.kept) a.out.kept[r] = 0;
-        }
-        if (filt)
-            for (int v = tid; v < V; v += kSampleThreads) put_none(filt + v);
-        return;
+    return v;
+}
+
+// What is decided about a row.
+enum { kDone = 0, kExactTail = 1, kBracket = 2, kSearch = 3, kOverflow = 4, kAbove = 5 };
+struct Decision {
+    int what;
+    float cut;       // tokens above it are kept, and those at it up to id `limit`
+    int limit, kept;
+    int token;       // the token drawn, or -1
+    uint64_t all;    // the kept tokens' mass
+    int bin0, bin1;    // of the bracket
+};
+
+
+// 128 bits of a logits row (which may be written later, by this block alone).
+__device__ __forceinline__ uint4 ld_row(const void* p) {
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+
+// U: vectors of a lane at a time.  A region is 32 U vectors of a warp, one after
+// another in the row; warps take regions in turn.
+template <typename T, int U> struct Sampler {
+    static constexpr int PV = Traits<T>::kPerVec;
+    static constexpr int kRegion = 32 * U;
+
+    struct Shared {
+        uint64_t tab[kExpTab];
+        uint64_t list[kList];      // (key, ~id)
+        uint64_t mass[kList];      // of the sorted list
+        uint32_t order[kList];     // ids and places in the list; a histogram
+        uint64_t region[U == kDeep ? kRegions : kSampleThreads * kDeep / 64 + 2];
+        uint64_t part[kSampleWarps], value;
+        Decision dec;
+        int count, token;
+    };
+
+    const SampleArgs& a;
+    Shared& s;
+    int tid, lane, warp;
+    // of the row
+    const T* x;
+    int off, nvec;  // elements before x in its first vector; vectors
+    float m, T_, c;
+    ExpScale sc;
+
+    __device__ Sampler(const SampleArgs& args, Shared& sh) : a(args), s(sh) {
+        tid = threadIdx.x;
+        lane = tid & 31;
+        warp = tid >> 5;
     }
-    const float m = of_key(top);
-    const ExpScale sc = exp_scale(Tr > 0.f ? Tr : 1.f, a.shift);
-    auto mass_of = [&](uint32_t k) { return exp_fixed(of_key(k), m, sc, tab); };
-    auto count_from = [&](uint32_t k) {
-        int n = 0;
-        for (int v = tid; v < V; v += kSampleThreads) n += key_of(value_of(x[v])) >= k;
-        return (int)block_sum((uint64_t)n, part);
-    };
-    auto mass_from = [&](uint32_t k) {
-        uint64_t s = 0;
-        for (int v = tid; v < V; v += kSampleThreads) {
-            const uint32_t q = key_of(value_of(x[v]));
-            if (q >= k) s += mass_of(q);
+
+    __device__ uint64_t block_sum(uint64_t v) {
+        v = warp_sum_u64(v);
+        __syncthreads();
+        if (lane == 0) s.part[warp] = v;
+        __syncthreads();
+        uint64_t t = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleWarps; ++i) t += s.part[i];
+        return t;
+    }
+    // The sum of v over the threads before this one, and over all.
+    __device__ uint64_t block_scan(uint64_t v, uint64_t& all) {
+        const uint64_t incl = warp_scan_u64(v, lane);
+        __syncthreads();
+        if (lane == 31) s.part[warp] = incl;
+        __syncthreads();
+        uint64_t before = incl - v;
+        all = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleWarps; ++i) {
+            if (i < warp) before += s.part[i];
+            all += s.part[i];
         }
-        return block_sum(s, part);
+        return before;
+    }
+
+    // ------------------------------------------------------------ the row
+    __device__ void open(const T* row) {
+        x = row;
+        off = (int)(((uintptr_t)x / sizeof(T)) % PV);
+        nvec = (a.V + off + PV - 1) / PV;
+    }
+    // Vector j of the row, -inf where it reaches past it.
+    __device__ uint4 vec(int j) const {
+        const int first = id_of(j);
+        if (first >= 0 && first + PV <= a.V) return ld_row(x + first);
+        T e[PV];
+#pragma unroll
+        for (int i = 0; i < PV; ++i)
+            e[i] = first + i >= 0 && first + i < a.V ? x[first + i] : none_of<T>();
+        uint4 q;
+        memcpy(&q, e, 16);
+        return q;
+    }
+    // The id of element 0 of vector j.
+    __device__ int id_of(int j) const { return j * PV - off; }
+    __device__ uint64_t mass_of(float v) const { return exp_fixed(v, m, sc, s.tab); }
+    __device__ float approx(float v) const { return ex2((v - m) * c); }
+    // f(vector, j) for this thread's vectors of the row, end(region) after a region's.
+    template <typename F, typename E> __device__ void each(F f, E end) const {
+        const uint4 none = make_uint4(Traits<T>::kNegInf, Traits<T>::kNegInf, Traits<T>::kNegInf,
+                                      Traits<T>::kNegInf);
+        for (int j0 = warp * kRegion; j0 < nvec; j0 += kSampleWarps * kRegion) {
+            uint4 q[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const int j = j0 + 32 * i + lane;
+                q[i] = j < nvec ? vec(j) : none;
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) f(q[i], j0 + 32 * i + lane);
+            end(j0 / kRegion);
+        }
+    }
+    template <typename F> __device__ void each(F f) const {
+        each(f, [](int) {});
+    }
+
+    // ------------------------------------------------------------ the list
+    // What a listing leaves beside the list: the exact mass and the number of the tokens
+    // above, and the mass, approximate or exact, of the rest.
+    struct Found {
+        uint64_t above, tail;
+        int n_above;
+        bool below;  // whether there is a rest
     };
-    // The place of the kept tokens' last: all above `cut` and `ties` of those at it.
-    uint32_t cut = kKeyNegInf + 1;
-    int ties = V;
-    int kept = live;
-    // the n-th token's place
-    auto place = [&](int n) {
-        uint32_t lo = kKeyNegInf + 1, hi = top;
+    // A sum of approximate masses.
+    struct Sum {
+        float hi = 0.f, lo = 0.f;
+        __device__ __forceinline__ void add(float v) {
+            const float t = hi + v;
+            lo += v - (t - hi);
+            hi = t;
+        }
+    };
+    __device__ __forceinline__ void list(float v, int id) {
+        const int at = atomicAdd(&s.count, 1);
+        if (at < kList) s.list[at] = (uint64_t)key_of(v) << 32 | (uint32_t)~id;
+    }
+    // One vector: its tokens from `lo` on are listed, the others' masses relative to `ref`
+    // added up.
+    template <bool TAIL>
+    __device__ __forceinline__ void list_vec(uint4 q, int j, float lo, float ref, Sum& sum,
+                                             bool& below) {
+        const float top = vec_max<T>(q);
+        uint32_t hits = 0;
+        if (top >= lo) {
+            float v[PV];
+            unpack<T>(q, v);
+#pragma unroll
+            for (int e = 0; e < PV; ++e) {
+                hits |= v[e] >= lo ? 1u << e : 0u;
+                below |= v[e] < lo && v[e] > -INFINITY;
+            }
+            for (uint32_t h = hits; h; h &= h - 1) {
+                const int e = __ffs(h) - 1;
+                list(element<T>(q, e), id_of(j) + e);
+            }
+            if (TAIL) {
+#pragma unroll
+                for (int e = 0; e < PV; ++e)
+                    if (hits >> e & 1) v[e] = -INFINITY;
+                float t = 0.f;
+#pragma unroll
+                for (int e = 0; e < PV; ++e) t += ex2((v[e] - ref) * c);
+                sum.add(t);
+            }
+            return;
+        }
+        below |= top > -INFINITY;
+        if (TAIL) {
+            uint64_t p[PV / 2];
+            vec_pairs<T>(q, p);
+            const uint64_t m2 = f2(ref, ref), c2 = f2(c, c);
+            uint64_t acc = f2_mass(p[0], m2, c2);
+#pragma unroll
+            for (int e = 1; e < PV / 2; ++e) acc = f2add(acc, f2_mass(p[e], m2, c2));
+            float p0, p1;
+            f2split(acc, p0, p1);
+            sum.add(p0 + p1);
+        }
+    }
+    __device__ uint64_t fixed_of(float v) const {
+        return __float2ull_rn(v * ldexpf(1.f, 62 - sc.shift));
+    }
+    // Lists the tokens from `lo` on; the rest's mass exactly, or not at all.
+    template <bool TAIL> __device__ Found collect(float lo, bool exact) {
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        Found f{0, 0, 0, false};
+        Sum sum;
+        each([&](const uint4& q, int j) {
+            if (TAIL && exact) {
+                list_vec<false>(q, j, lo, m, sum, f.below);
+                float v[PV];
+                unpack<T>(q, v);
+#pragma unroll
+                for (int e = 0; e < PV; ++e)
+                    if (v[e] < lo) f.tail += mass_of(v[e]);
+            } else {
+                list_vec<TAIL>(q, j, lo, m, sum, f.below);
+            }
+        });
+        if (TAIL && !exact) f.tail = fixed_of(sum.hi + sum.lo);
+        f.below = __syncthreads_or(f.below);
+        f.tail = TAIL ? block_sum(f.tail) : 0;
+        return f;
+    }
+    // The same by bins of the logit: tokens in bins before bin0 are above, those of bins
+    // bin0 .. bin1 are listed; the mass above is left by region too.
+    __device__ int bin_of(float v, float per) const {
+        return (int)fminf((m - v) * per, (float)kBins);
+    }
+    template <bool TAIL>
+    __device__ Found collect_bins(float per, int bin0, int bin1, bool exact) {
+        if (tid == 0) s.count = 0;
+        __syncthreads();
+        Found f{0, 0, 0, false};
+        Sum sum;
+        uint64_t above = 0;
+        each(
+            [&](const uint4& q, int j) {
+                float v[PV];
+                unpack<T>(q, v);
+                if (bin_of(vec_max<T>(q), per) > bin1 && !(TAIL && exact)) {
+                    f.below |= vec_max<T>(q) > -INFINITY;
+                    if (TAIL) {
+                        float t = 0.f;
+#pragma unroll
+                        for (int e = 0; e < PV; ++e) t += approx(v[e]);
+                        sum.add(t);
+                    }
+                    return;
+                }
+                uint32_t over = 0, in = 0;
+                float t = 0.f;
+#pragma unroll
+                for (int e = 0; e < PV; ++e) {
+                    const int bin = bin_of(v[e], per);
+                    const bool rest = bin > bin1;
+                    over |= bin < bin0 ? 1u << e : 0u;
+                    in |= bin >= bin0 && !rest && v[e] > -INFINITY ? 1u << e : 0u;
+                    f.below |= rest && v[e] > -INFINITY;
+                    if (TAIL && !exact) t += rest ? approx(v[e]) : 0.f;
+                    else if (TAIL && rest) f.tail += mass_of(v[e]);
+                }
+                if (TAIL) sum.add(t);
+                f.n_above += __popc(over);
+                for (uint32_t h = over; h; h &= h - 1) above += mass_of(element<T>(q, __ffs(h) - 1));
+                for (uint32_t h = in; h; h &= h - 1) {
+                    const int e = __ffs(h) - 1;
+                    list(element<T>(q, e), id_of(j) + e);
+                }
+            },
+            [&](int region) {
+                const uint64_t w = warp_sum_u64(above);
+                if (lane == 0) s.region[region] = w;
+                f.above += above;
+                above = 0;
+            });
+        if (TAIL && !exact) f.tail = fixed_of(sum.hi + sum.lo);
+        f.below = __syncthreads_or(f.below);
+        f.above = block_sum(f.above);
+        f.n_above = (int)block_sum((uint64_t)f.n_above);
+        f.tail = TAIL ? block_sum(f.tail) : 0;
+        return f;
+    }
+
+    // Sorts n entries (the array holds them up to the next power of two).
+    template <typename E, bool FALLING> __device__ void sort(E* v, int n) {
+        int size = 2;
+        while (size < n) size *= 2;
+        for (int i = n + tid; i < size; i += kSampleThreads) v[i] = FALLING ? (E)0 : ~(E)0;
+        for (int k = 2; k <= size; k *= 2)
+            for (int j = k / 2; j > 0; j /= 2) {
+                __syncthreads();
+                for (int i = tid; i < size / 2; i += kSampleThreads) {
+                    const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
+                    const E p = v[lo], q = v[hi];
+                    const bool down = ((lo & k) == 0) == FALLING;
+                    if (down ? p < q : p > q) v[lo] = q, v[hi] = p;
+                }
+            }
+        __syncthreads();
+    }
+
+    // From the list of n: every filter's place, the kept tokens and, where they are all
+    // listed, the draw.  f: what is before and behind the list (`open`: its tail is known
+    // to 2^-16 only); `floor`: no token behind it has `least`; `known`: the mass of the
+    // first top_k, whose place is not looked for again.
+    __device__ void decide(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
+                           float top_p, uint64_t least, bool draw, float u) {
+        sort<uint64_t, true>(s.list, n);
+        // masses and their prefix sums, Q entries a thread
+        constexpr int Q = kList / kSampleThreads;
+        uint64_t e[Q], own = 0;
+        int big = 0;
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const int p = tid * Q + i;
+            e[i] = p < n ? mass_of(of_key((uint32_t)(s.list[p] >> 32))) : 0;
+            if (p < n) s.mass[p] = e[i];
+            own += e[i];
+            big += p < n && e[i] >= least;
+        }
+        uint64_t listed;
+        const uint64_t before = f.above + block_scan(own, listed);
+        listed += f.above;
+        const int A = f.n_above + n, kNone = INT_MAX;
+        const int big_n = (int)block_sum((uint64_t)big);
+        const int pos_k = known ? kNone : top_k > 0 && top_k <= A ? top_k : f.below ? kNone : A;
+        const int pos_m = least == 0 || (big_n == n && f.below && !floor) ? kNone : f.n_above + big_n;
+        int kept = min(pos_k, pos_m), what = kDone;
+        // (known: those behind the first top_k are not kept; here they are behind the place)
+        if (pos_k <= f.n_above || (least != 0 && big_n == 0 && f.n_above > 0)) {
+            what = kSearch;  // a place is among those above
+        } else if (top_p < 1.f) {
+            uint64_t w0, w1;  // the mass that top_p is a share of, at least and at most
+            if (known) {
+                w0 = w1 = known;
+            } else if (pos_k != kNone) {
+                const int last = pos_k - f.n_above - 1;
+                if (last / Q == tid) {
+                    uint64_t w = before;
+#pragma unroll
+                    for (int i = 0; i < Q; ++i)
+                        if (i <= last % Q) w += e[i];
+                    s.value = w;
+                }
+                __syncthreads();
+                w0 = w1 = s.value;
+                if (tid == 0) s.dec.all = w0;
+            } else {
+                // (and 2^-28 of the first token, for terms of large exponents)
+                const uint64_t slack = open ? (f.tail >> 16) + (1ull << (62 - sc.shift) >> 28) + 1 : 0;
+                w0 = listed + (f.tail > slack ? f.tail - slack : 0);
+                w1 = listed + f.tail + slack;
+            }
+            const uint64_t g0 = max(share_of(w0, top_p, true), (uint64_t)1);
+            const uint64_t g1 = max(share_of(w1, top_p, true), (uint64_t)1);
+            // how many prefix sums stay below either goal
+            uint64_t cum = before;
+            int n0 = 0, n1 = 0;
+#pragma unroll
+            for (int i = 0; i < Q; ++i) {
+                cum += e[i];
+                if (tid * Q + i < n) n0 += cum < g0, n1 += cum < g1;
+            }
+            const uint64_t both = block_sum((uint64_t)n0 << 32 | (uint32_t)n1);
+            const int p0 = min(kept, f.n_above + (int)(both >> 32) + 1);
+            const int p1 = min(kept, f.n_above + (int)(uint32_t)both + 1);
+            if (top_k > 0 && pos_k == kNone && !known) what = kSearch;
+            else if (f.n_above > 0 && f.above >= g0) what = top_k > 0 && !known ? kAbove : kSearch;
+            else if (p1 > A) what = kBracket;
+            else if (p0 != p1) what = kExactTail;
+            kept = p0;
+        } else if (kept == kNone) {
+            what = kSearch;
+        }
+        if (what == kDone) {
+            const int here = kept - f.n_above;  // kept entries of the list
+            uint64_t w = 0;
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+                if (tid * Q + i < here) w += e[i];
+            const uint64_t all = f.above + block_sum(w);
+            if (draw && f.n_above == 0) {
+                // the kept tokens by id, and the first whose prefix sum passes the goal
+                const uint64_t goal = share_of(all, u < 1.f ? u : 0.f, false);
+                if (tid == 0) s.token = u >= 1.f ? here - 1 : 0;
+                for (int i = tid; i < here; i += kSampleThreads)
+                    s.order[i] = ~(uint32_t)s.list[i] << kPlaceBits | (uint32_t)i;
+                sort<uint32_t, false>(s.order, here);
+                uint64_t o[Q], sum = 0, every;
+#pragma unroll
+                for (int i = 0; i < Q; ++i) {
+                    const int p = tid * Q + i;
+                    o[i] = p < here ? s.mass[s.order[p] & (kList - 1)] : 0;
+                    sum += o[i];
+                }
+                uint64_t at = block_scan(sum, every);
+                if (u >= 0.f && u < 1.f && at <= goal && goal < at + sum) {
+                    int hit = 0;
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) {
+                        at += o[i];
+                        hit += at <= goal;
+                    }
+                    s.token = tid * Q + hit;
+                }
+                __syncthreads();
+            }
+            if (tid == 0) {
+                const uint64_t entry = s.list[here - 1];
+                s.dec.cut = of_key((uint32_t)(entry >> 32));
+                s.dec.limit = (int)~(uint32_t)entry;
+                s.dec.kept = kept;
+                s.dec.all = all;
+                s.dec.token = draw && f.n_above == 0 ? (int)(s.order[s.token] >> kPlaceBits) : -1;
+            }
+            if (draw && f.n_above > 0)  // the list's part of the regions' masses
+                for (int i = tid; i < here; i += kSampleThreads)
+                    atomicAdd(reinterpret_cast<unsigned long long*>(
+                                  &s.region[((int)~(uint32_t)s.list[i] + off) / PV / kRegion]),
+                              (unsigned long long)s.mass[i]);
+        } else if (tid == 0 && what == kBracket) {
+            s.dec.all = listed + f.tail;
+        }
+        if (tid == 0) s.dec.what = what;
+        __syncthreads();
+    }
+
+    // Decides by a list that is there, with the rest's mass made exact where that is needed.
+    __device__ int settle(Found f, float lo, bool floor, int top_k, float top_p, uint64_t least,
+                          bool draw, float u) {
+        const bool tail = top_p < 1.f && top_k <= 0;
+        for (bool exact = false;; exact = true) {
+            if (exact) f = collect<true>(lo, true);
+            const int n = s.count;
+            if (n > kList || n == 0) return kOverflow;
+            decide(n, f, tail && !exact, floor, 0, top_k, top_p, least, draw, u);
+            if (s.dec.what != kExactTail) return s.dec.what;
+        }
+    }
+    // Lists by bins, and decides.
+    __device__ int settle_bins(float per, int bin0, int bin1, bool floor, uint64_t known, int top_k,
+                               float top_p, uint64_t least, bool draw, float u) {
+        const bool tail = top_p < 1.f && top_k <= 0;
+        for (bool exact = false;; exact = true) {
+            __syncthreads();
+            const Found f = tail ? collect_bins<true>(per, bin0, bin1, exact)
+                                 : collect_bins<false>(per, bin0, bin1, false);
+            const int n = s.count;
+            if (n > kList || n == 0) return kSearch;
+            decide(n, f, tail && !exact, floor, known, top_k, top_p, least, draw, u);
+            if (s.dec.what != kExactTail) return s.dec.what;
+        }
+    }
+
+    // ------------------------------------------------------------ the bracket
+    // A histogram over bins of the logit, each token weighing one (COUNT) or its
+    // approximate mass in units; leaves the bins that hold the place where the weights
+    // pass `goal`, known to `slack`.
+    template <bool COUNT> __device__ void histogram(float per, float unit, uint64_t goal, uint64_t slack) {
+        for (int i = tid; i < kBins; i += kSampleThreads) s.order[i] = 0;
+        if (tid == 0) s.dec.bin0 = 0, s.dec.bin1 = kBins - 1;
+        __syncthreads();
+        each([&](const uint4& q, int) {
+            if (bin_of(vec_max<T>(q), per) >= kBins) return;
+            float v[PV];
+            unpack<T>(q, v);
+#pragma unroll
+            for (int e = 0; e < PV; ++e) {
+                const int b = bin_of(v[e], per);
+                if (b < kBins) atomicAdd(&s.order[b], COUNT ? 1u : __float2uint_rn(approx(v[e]) * unit));
+            }
+        });
+        __syncthreads();
+        constexpr int Q = kBins / kSampleThreads;
+        uint64_t w[Q], sum = 0, all;
+#pragma unroll
+        for (int i = 0; i < Q; ++i) sum += w[i] = s.order[tid * Q + i];
+        uint64_t cum = block_scan(sum, all);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const uint64_t next = cum + w[i];
+            if (cum + slack < goal && next + slack >= goal) s.dec.bin0 = tid * Q + i;
+            if (cum < goal + slack && next >= goal + slack) s.dec.bin1 = tid * Q + i;
+            cum = next;
+        }
+        __syncthreads();
+    }
+    // For a nucleus, of which `whole` is all: bins from m down to the least logit that it
+    // can reach.  Returns bins per unit of the logit.
+    __device__ float bracket(float top_p, uint64_t whole) {
+        // tokens whose logit leaves them less than (1 - top_p) / V of the mass are out
+        const float z = (float)whole * ldexpf(1.f, sc.shift - 62);
+        const float reach = T_ * (logf((float)a.V / ((1.f - top_p) * z)) + 0.01f);
+        const float per = (float)kBins / reach;
+        // in units of 2^-30 of the mass: half a unit a token, and 2^-15
+        histogram<false>(per, 1073741824.f / z, (uint64_t)(top_p * 1073741824.f),
+                         (uint64_t)a.V / 2 + (1 << 15) + 2);
+        return per;
+    }
+
+    // ------------------------------------------------------------ the search
+    // The tokens from a key on: how many, their mass, and the least key among them; and the
+    // largest key below.
+    struct From {
+        int n;
+        uint64_t mass;
+        uint32_t least, under;
+    };
+    template <bool MASS> __device__ From from_key(uint32_t k) {
+        From f{0, 0, ~0u, 0};
+        each([&](const uint4& q, int) {
+            uint32_t in = 0;
+#pragma unroll
+            for (int e = 0; e < PV; ++e) {
+                const uint32_t y = key_of(element<T>(q, e));
+                if (y >= k) {
+                    in |= 1u << e;
+                    f.least = min(f.least, y);
+                } else {
+                    f.under = max(f.under, y);
+                }
+            }
+            f.n += __popc(in);
+            if (MASS)
+                for (; in; in &= in - 1) f.mass += mass_of(element<T>(q, __ffs(in) - 1));
+        });
+        f.n = (int)block_sum((uint64_t)f.n);
+        if (MASS) f.mass = block_sum(f.mass);
+        const uint64_t ends = (uint64_t)__reduce_min_sync(0xffffffffu, f.least) << 32 |
+                              (uint32_t)~__reduce_max_sync(0xffffffffu, f.under);
+        __syncthreads();
+        if (lane == 0) s.part[warp] = ends;
+        __syncthreads();
+        f.least = ~0u;
+        f.under = 0;
+        for (int i = 0; i < kSampleWarps; ++i) {
+            f.least = min(f.least, (uint32_t)(s.part[i] >> 32));
+            f.under = max(f.under, ~(uint32_t)s.part[i]);
+        }
+        return f;
+    }
+    __device__ int count_from(uint32_t k) { return from_key<false>(k).n; }
+    // The largest key in lo .. hi from which on the tokens are `goal`, in number or mass
+    // (from lo on they are): bisection, each time to a key that is there.
+    template <bool MASS> __device__ uint32_t last_key(uint32_t lo, uint32_t hi, uint64_t goal) {
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo + 1) / 2;
-            if (count_from(mid) >= n) lo = mid;
-            else hi = mid - 1;
+            const From f = from_key<MASS>(mid);
+            if ((MASS ? f.mass : (uint64_t)f.n) >= goal) lo = f.least;
+            else hi = max(lo, f.under);
         }
-        cut = lo;
-        ties = n - (lo == 0xFFFFFFFFu ? 0 : count_from(lo + 1));
-        kept = n;
+        return lo;
+    }
+    // The place of the n-th token.
+    struct Place {
+        uint32_t key;
+        int ties, n;  // of those at the key
     };
-    if (Tr == 0.f) {
-        place(1);
-    } else {
-        if (top_k > 0 && top_k < live) place(top_k);
-        int n = kept;
+    __device__ Place place(uint32_t top, int n) {
+        const uint32_t k = last_key<false>(kKeyNone + 1, top, (uint64_t)n);
+        return Place{k, n - count_from(k + 1), n};
+    }
+    // Every filter's place by bisection; leaves cut, limit and kept.
+    __device__ void search(uint32_t top, int top_k, float top_p, uint64_t least) {
+        const uint32_t bottom = kKeyNone + 1;
+        const int live = count_from(bottom);
+        Place at{bottom, live, live};
+        if (top_k > 0 && top_k < live) at = place(top, top_k);
+        else at.ties = live - count_from(bottom + 1);
+        int n = at.n;
         if (top_p < 1.f) {
-            const uint64_t above = mass_from(cut + 1), at = mass_of(cut);
-            const uint64_t all = kept == live ? mass_from(cut) : above + at * (uint64_t)ties;
-            // C >= p W, a whole number C
-            uint64_t goal = share_of(all, top_p);
-            if (share_of(all, top_p) == 0) goal = 1;
-            else {
-                // rounded up unless exact
-                int e;
-                const uint64_t kk = (uint64_t)(frexpf(top_p, &e) * 16777216.f);
-                const int sh = 24 - e;
-                const uint64_t back_hi = __umul64hi(all, kk), back_lo = all * kk;
-                const bool whole = sh >= 64 ? (back_lo == 0 && (sh == 64 || (back_hi << (128 - sh)) == 0))
-                                            : (back_lo << (64 - sh)) == 0;
-                if (!whole) ++goal;
-            }
-            uint32_t lo = cut, hi = top;
-            auto mass_in = [&](uint32_t k) { return k == cut ? all : mass_from(k); };
-            while (lo < hi) {
-                const uint32_t mid = lo + (hi - lo + 1) / 2;
-                if (mass_in(mid) >= goal) lo = mid;
-                else hi = mid - 1;
-            }
-            const uint64_t before = mass_from(lo + 1), each = mass_of(lo);
-            const int count_before = count_from(lo + 1);
-            const uint64_t t = (goal - before + each - 1) / each;
-            n = count_before + (int)t;
+            const uint64_t all = from_key<true>(at.key + 1).mass + mass_of(of_key(at.key)) * (uint64_t)at.ties;
+            const uint64_t goal = max(share_of(all, top_p, true), (uint64_t)1);
+            const uint32_t lo = last_key<true>(at.key, top, goal);
+            const From f = from_key<true>(lo + 1);
+            const uint64_t one = max(mass_of(of_key(lo)), (uint64_t)1);
+            n = (int)min((uint64_t)n, (uint64_t)f.n + (goal - f.mass + one - 1) / one);
         }
-        if (min_p > 0.f) {
-            const double thr = (double)m + (double)Tr * log((double)fminf(min_p, 1.f));
-            const uint32_t k = key_of(value_of(__double2float_ru(thr)));
-            n = min(n, count_from(max(k, kKeyNegInf + 1)));
+        if (least != 0) {
+            uint32_t lo = bottom, hi = top;
+            while (lo < hi) {  // the lowest logit whose mass suffices
+                const uint32_t mid = lo + (hi - lo) / 2;
+                if (mass_of(of_key(mid)) >= least) hi = mid;
+                else lo = mid + 1;
+            }
+            n = min(n, count_from(lo));
         }
-        if (n < kept) place(n);
+        if (n < at.n) at = place(top, n);
+        if (tid == 0) {
+            s.dec.cut = of_key(at.key);
+            s.dec.kept = at.n;
+            s.dec.limit = INT_MAX;
+        }
+        __syncthreads();
+        if (at.ties < count_from(at.key) - (at.n - at.ties)) tie_limit(at.key, at.ties);
     }
-    // ids up to `limit` among those at the cut
-    if (tid == 0) limit = V;
-    __syncthreads();
-    const int seg = (V + kSampleThreads - 1) / kSampleThreads;
-    const int v0 = min(V, tid * seg), v1 = min(V, v0 + seg);
-    {
+    // The id of the ties-th token at the key.
+    __device__ void tie_limit(uint32_t key, int ties) {
+        auto equal = [&](const uint4& q) {
+            float v[PV];
+            unpack<T>(q, v);
+            int n = 0;
+#pragma unroll
+            for (int e = 0; e < PV; ++e) n += key_of(v[e]) == key;
+            return n;
+        };
         int n = 0;
-        for (int v = v0; v < v1; ++v) n += key_of(value_of(x[v])) == cut;
-        part[tid] = n;
-        __syncthreads();
-        uint64_t before = 0;
-        for (int i = 0; i < tid; ++i) before += part[i];
-        if ((int64_t)before < ties && (int64_t)(before + n) >= ties) {
-            int left = ties - (int)before;
-            for (int v = v0; v < v1; ++v)
-                if (key_of(value_of(x[v])) == cut && --left == 0) limit = v;
+        each([&](const uint4& q, int) { n += equal(q); },
+             [&](int region) {
+                 const uint64_t w = warp_sum_u64((uint64_t)n);
+                 if (lane == 0) s.region[region] = w;
+                 n = 0;
+             });
+        uint64_t goal = (uint64_t)ties - 1;
+        const int region = pick_region(goal);
+        const int j = region * kRegion + tid;
+        const uint4 q = tid < kRegion && j < nvec ? vec(j) : uint4();
+        const int mine = tid < kRegion && j < nvec ? equal(q) : 0;
+        uint64_t all;
+        uint64_t before = block_scan((uint64_t)mine, all);
+        if (before <= goal && goal < before + mine) {
+            float v[PV];
+            unpack<T>(q, v);
+#pragma unroll
+            for (int e = 0; e < PV; ++e)
+                if (key_of(v[e]) == key && before++ == goal) s.dec.limit = id_of(j) + e;
         }
         __syncthreads();
     }
-    const int lim = limit;
-    auto is_kept = [&](uint32_t k, int v) { return k > cut || (k == cut && v <= lim); };
-    if (a.u) {
-        const float u = a.u[r];
-        uint64_t s = 0;
-        int last = -1, first = V;
-        for (int v = v0; v < v1; ++v) {
-            const uint32_t k = key_of(value_of(x[v]));
-            if (is_kept(k, v)) {
-                s += mass_of(k);
-                last = v;
-                first = min(first, v);
+    // The region whose sum, added to those before, passes the goal; less what is before.
+    __device__ int pick_region(uint64_t& goal) {
+        const int n = (nvec + kRegion - 1) / kRegion;
+        constexpr int Q = (kRegions + kSampleThreads - 1) / kSampleThreads;
+        __syncthreads();
+        if (tid == 0) s.token = n - 1, s.value = 0;
+        uint64_t w[Q], sum = 0, all;
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            w[i] = tid * Q + i < n ? s.region[tid * Q + i] : 0;
+            sum += w[i];
+        }
+        uint64_t at = block_scan(sum, all);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            if (at <= goal && goal < at + w[i]) s.token = tid * Q + i, s.value = at;
+            at += w[i];
+        }
+        __syncthreads();
+        goal -= s.value;
+        return s.token;
+    }
+
+    // ------------------------------------------------------------ the draw
+    __device__ bool is_kept(float v, int id) const {
+        return v > s.dec.cut || (v == s.dec.cut && id <= s.dec.limit);
+    }
+    // The kept tokens' number, and their masses by region.
+    __device__ void weigh(bool draw) {
+        uint64_t w = 0, all = 0;
+        int n = 0;
+        each(
+            [&](const uint4& q, int j) {
+                float v[PV];
+                unpack<T>(q, v);
+                if (!draw) {
+#pragma unroll
+                    for (int e = 0; e < PV; ++e) n += is_kept(v[e], id_of(j) + e);
+                    return;
+                }
+#pragma unroll
+                for (int e = 0; e < PV; ++e)
+                    if (is_kept(v[e], id_of(j) + e)) ++n, w += mass_of(v[e]);
+            },
+            [&](int region) {
+                if (!draw) return;
+                const uint64_t r = warp_sum_u64(w);
+                if (lane == 0) s.region[region] = r;
+                all += w;
+                w = 0;
+            });
+        n = (int)block_sum((uint64_t)n);
+        all = block_sum(all);
+        if (tid == 0) s.dec.kept = n, s.dec.all = all;
+        __syncthreads();
+    }
+    // The token of u, from the kept masses by region.
+    __device__ int find(float u) {
+        if (!(u >= 0.f && u < 1.f)) {  // the last kept, or the first
+            __syncthreads();
+            if (tid == 0) s.token = u >= 1.f ? -1 : INT_MAX;
+            __syncthreads();
+            each([&](const uint4& q, int j) {
+                float v[PV];
+                unpack<T>(q, v);
+#pragma unroll
+                for (int e = 0; e < PV; ++e)
+                    if (is_kept(v[e], id_of(j) + e)) {
+                        if (u >= 1.f) atomicMax(&s.token, id_of(j) + e);
+                        else atomicMin(&s.token, id_of(j) + e);
+                    }
+            });
+            __syncthreads();
+            return s.token;
+        }
+        uint64_t goal = share_of(s.dec.all, u, false);
+        const int j = pick_region(goal) * kRegion + tid;
+        const bool in = tid < kRegion && j < nvec;
+        float v[PV];
+        uint64_t w = 0, all;
+        if (in) {
+            unpack<T>(vec(j), v);
+#pragma unroll
+            for (int e = 0; e < PV; ++e)
+                if (is_kept(v[e], id_of(j) + e)) w += mass_of(v[e]);
+        }
+        uint64_t at = block_scan(w, all);
+        if (in && at <= goal && goal < at + w) {
+#pragma unroll
+            for (int e = 0; e < PV; ++e)
+                if (is_kept(v[e], id_of(j) + e)) {
+                    const uint64_t next = at + mass_of(v[e]);
+                    if (at <= goal && goal < next) s.token = id_of(j) + e;
+                    at = next;
+                }
+        }
+        __syncthreads();
+        return s.token;
+    }
+
+    // ------------------------------------------------------------ a row
+    __device__ void write_filtered(int64_t r, bool none) {
+        T* o = static_cast<T*>(a.out.filtered) + r * a.V;
+        each([&](const uint4& q, int j) {
+            const int id = id_of(j);
+            float v[PV];
+            unpack<T>(q, v);
+            T e[PV];
+            memcpy(e, &q, 16);
+#pragma unroll
+            for (int i = 0; i < PV; ++i)
+                if (none || !is_kept(v[i], id + i)) e[i] = none_of<T>();
+            if (a.same_align && id >= 0 && id + PV <= a.V) {
+                uint4 p;
+                memcpy(&p, e, 16);
+                *reinterpret_cast<uint4*>(o + id) = p;
+            } else {
+#pragma unroll
+                for (int i = 0; i < PV; ++i)
+                    if (id + i >= 0 && id + i < a.V) o[id + i] = e[i];
+            }
+        });
+    }
+
+    __device__ void row(int64_t r) {
+        const vsd_policy& p = a.policy;
+        T_ = p.row_T ? p.row_T[r] : p.T;
+        float top_p = p.row_top_p ? p.row_top_p[r] : p.top_p;
+        float min_p = p.row_min_p ? p.row_min_p[r] : p.min_p;
+        int top_k = p.row_top_k ? p.row_top_k[r] : p.top_k;
+        const float u = a.u ? a.u[r] : 0.f;
+        const bool ok = (T_ == 0.f || (T_ >= kMinT && T_ <= kMaxT)) && top_p == top_p && min_p == min_p;
+        const bool draw = a.u != nullptr;
+        if (T_ == 0.f) top_k = 1, top_p = 1.f, min_p = 0.f, T_ = 1.f;  // the first token alone
+        if (top_p <= 0.f) top_k = 1, top_p = 1.f;
+        sc = exp_scale(T_, a.shift);
+        c = sc.c;
+        // min_p as a mass
+        const uint64_t one = 1ull << (62 - sc.shift);
+        const uint64_t least = !(min_p > 0.f) ? 0
+                               : min_p >= 1.f ? one
+                                              : max(share_of(one, min_p, true), (uint64_t)1);
+        const bool filters = top_k > 0 || top_p < 1.f || least != 0;
+        const bool tail = top_p < 1.f && top_k <= 0;
+        // how far below the maximum min_p reaches, and what rounding may make of it
+        const float span = least != 0 && least < one ? -T_ * logf(min_p) : 0.f;
+        auto rounding = [&](float top) { return (span + fabsf(top) + T_) * 1e-5f; };
+
+        // one pass: the maximum, the list and the rest's mass.  After the first round of
+        // vectors a bound `lo` that `want` of the lanes' maxima reach, and a reference for
+        // the masses: the maximum so far.
+        const int want = top_k > 0 ? top_k : kWant;
+        float mx = -INFINITY, lo = -FLT_MAX, ref = 0.f;
+        bool floor = false;
+        Found f{0, 0, 0, false};
+        Sum sum;
+        if (tid == 0) s.count = 0;
+        const uint4 none = make_uint4(Traits<T>::kNegInf, Traits<T>::kNegInf, Traits<T>::kNegInf,
+                                      Traits<T>::kNegInf);
+        for (int j1 = 0; j1 < nvec; j1 += kSampleWarps * kRegion) {
+            const int j0 = j1 + warp * kRegion + lane;
+            uint4 q[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) q[i] = j0 + 32 * i < nvec ? vec(j0 + 32 * i) : none;
+#pragma unroll
+            for (int i = 0; i < U; ++i) mx = max_nan(mx, vec_max_nan<T>(q[i]));
+            if (!filters) continue;
+            if (j1 == 0) {
+                const uint32_t key = key_of(mx), high = key >> 16;
+                const uint32_t w = __reduce_max_sync(0xffffffffu, key);
+                if (lane == 0) s.part[warp] = w;
+                uint32_t t = 0;
+                if (top_k != 1)
+                    for (uint32_t bit = 0x8000u; bit; bit >>= 1)
+                        if (__syncthreads_count(high >= (t | bit)) >= want) t |= bit;
+                __syncthreads();
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < kSampleWarps; ++i) top = max(top, (uint32_t)s.part[i]);
+                const uint32_t lo_key = top_k == 1 ? top : t << 16;
+                ref = of_key(top);
+                lo = lo_key <= kKeyNone ? -FLT_MAX : of_key(lo_key);
+                if (least != 0 && top_p >= 1.f) {
+                    // no token below max + T ln(min_p) is kept, and the maximum may grow
+                    const float under = ref - span - rounding(ref);
+                    floor = top_k <= 0 || under > lo;
+                    if (floor) lo = under;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                if (tail) list_vec<true>(q[i], j0 + 32 * i, lo, ref, sum, f.below);
+                else list_vec<false>(q[i], j0 + 32 * i, lo, ref, sum, f.below);
             }
         }
+        const bool bad = __syncthreads_or(!(mx < INFINITY));
+        const uint32_t w = __reduce_max_sync(0xffffffffu, key_of(mx));
+        if (lane == 0) s.part[warp] = w;
         __syncthreads();
-        part[tid] = s;
-        if (tid == 0) chosen = -1;
-        __syncthreads();
-        uint64_t before = 0, all = 0;
-        for (int i = 0; i < kSampleThreads; ++i) {
-            if (i == tid) before = all;
-            all += part[i];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleWarps; ++i) top = max(top, (uint32_t)s.part[i]);
+        const bool dead = bad || top <= kKeyNone;
+        if (dead || !ok) {
+            if (tid == 0) {
+                atomicOr(a.status, (dead ? VSD_STATUS_BAD_ROW : 0) | (ok ? 0 : VSD_STATUS_BAD_PARAM));
+                if (a.out.tokens) a.out.tokens[r] = -1;
+                if (a.out.logq_tok) a.out.logq_tok[r] = NAN;
+                if (a.out.kept) a.out.kept[r] = 0;
+            }
+            if (a.out.filtered) write_filtered(r, true);
+            return;
         }
-        if (u >= 1.f) {
-            if (last >= 0) atomicMax(&chosen, last);
-        } else if (!(u >= 0.f)) {
-            if (tid == 0) chosen = V;
-            __syncthreads();
-            if (first < V) atomicMin(&chosen, first);
-        } else {
-            const uint64_t goal = share_of(all, u);
-            if (before <= goal && goal < before + s) {
-                uint64_t c = before;
-                for (int v = v0; v < v1; ++v) {
-                    const uint32_t k = key_of(value_of(x[v]));
-                    if (!is_kept(k, v)) continue;
-                    c += mass_of(k);
-                    if (c > goal) {
-                        chosen = v;
-                        break;
+        m = of_key(top);
+        if (tid == 0) s.dec.token = -1;
+        int what = kDone;
+        if (filters) {
+            if (tail) {
+                // (where the reference was too far below: once more, relative to m)
+                const float t = (sum.hi + sum.lo) * ex2((ref - m) * c);
+                f.tail = fixed_of(t);
+                if (__syncthreads_or(!(t < 2e6f) || !(sum.hi < 1e30f) || !(ref > -INFINITY)))
+                    f = collect<true>(lo, false);
+                else
+                    f.tail = block_sum(f.tail);
+            }
+            f.below = __syncthreads_or(f.below);
+            what = settle(f, lo, floor, top_k, top_p, least, draw, u);
+            if (what == kOverflow) {
+                if (tail) {
+                    what = kBracket;
+                    // (the list's part of the mass, from all of it)
+                    f = collect<true>(FLT_MAX, false);
+                    if (tid == 0) s.dec.all = f.tail;
+                    __syncthreads();
+                } else {
+                    // the place of the k-th token, or of min_p
+                    const float per = ((float)kBins - 0.1f) / (m - lo);
+                    if (per > 0.f && per < INFINITY) {
+                        int bin0, bin1;
+                        if (floor) {
+                            bin0 = bin_of(m - span + rounding(m), per);
+                            bin1 = bin_of(m - span - rounding(m), per);
+                        } else {
+                            histogram<true>(per, 0.f, (uint64_t)top_k, 0);
+                            bin0 = s.dec.bin0;
+                            bin1 = s.dec.bin1;
+                        }
+                        what = settle_bins(per, bin0, bin1, floor, 0, top_k, top_p, least, draw, u);
                     }
                 }
             }
+            if (what == kBracket || what == kAbove) {
+                const uint64_t whole = s.dec.all;
+                const float per = bracket(top_p, whole);
+                what = settle_bins(per, s.dec.bin0, s.dec.bin1, false, what == kAbove ? whole : 0, top_k,
+                                   top_p, least, draw, u);
+            }
+            if (what != kDone) {
+                search(top, top_k, top_p, least);
+                weigh(draw);
+                if (tid == 0) s.dec.token = -1;
+            }
+        } else {
+            if (tid == 0) s.dec.cut = -FLT_MAX, s.dec.limit = INT_MAX;
+            __syncthreads();
+            weigh(draw);
         }
         __syncthreads();
-        if (tid == 0) {
-            if (a.out.tokens) a.out.tokens[r] = chosen;
-            if (a.out.logq_tok) {
-                const float f = value_of(x[chosen]);
-                a.out.logq_tok[r] = Tr == 0.f ? 0.f
-                    : (float)(((double)f - (double)m) / (double)Tr -
-                              log((double)all * exp2((double)(a.shift - 62))));
+        if (draw) {
+            const int id = s.dec.token >= 0 ? s.dec.token : find(u);
+            if (tid == 0) {
+                if (a.out.tokens) a.out.tokens[r] = id;
+                if (a.out.logq_tok)
+                    a.out.logq_tok[r] = log_share(float_of(x[id]), m, T_, s.dec.all, sc.shift, s.tab);
             }
         }
+        if (tid == 0 && a.out.kept) a.out.kept[r] = s.dec.kept;
+        if (a.out.filtered) write_filtered(r, false);
     }
-    if (tid == 0 && a.out.kept) a.out.kept[r] = kept;
-    if (filt) {
+};
+
+template <typename T, int U>
+__global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const T* logits, const SampleArgs a) {
+    using S = Sampler<T, U>;
+    extern __shared__ __align__(128) unsigned char sample_smem[];
+    typename S::Shared& s = *reinterpret_cast<typename S::Shared*>(sample_smem);
+    S w(a, s);
+    for (int j = threadIdx.x; j < kExpTab; j += kSampleThreads) s.tab[j] = exp_entry(kExpParts, j);
+    for (int64_t r = blockIdx.x; r < a.R; r += gridDim.x) {
         __syncthreads();
-        for (int v = tid; v < V; v += kSampleThreads) {
-            const T raw = x[v];
-            if (is_kept(key_of(value_of(raw)), v)) filt[v] = raw;
-            else put_none(filt + v);
-        }
+        w.open(logits + r * a.V);
+        w.row(r);
     }
+}
+
+template <typename T, int U>
+cudaError_t launch_sample(const void* logits, const SampleArgs& a, cudaStream_t st) {
+    auto k = k_sample<T, U>;
+    constexpr size_t smem = sizeof(typename Sampler<T, U>::Shared);
+    const int blocks = blocks_per_sm((const void*)k, kSampleThreads, smem) * device_sm_count();
+    if (blocks < 1) return cudaErrorInvalidConfiguration;
+    k<<<std::min(blocks, a.R), kSampleThreads, smem, st>>>(static_cast<const T*>(logits), a);
+    return cudaGetLastError();
+}
+// (short rows: a vector a lane, so that all warps have some)
+template <typename T>
+cudaError_t sample(const void* logits, const SampleArgs& a, cudaStream_t st) {
+    return a.V <= kSampleThreads * kDeep / 2 * Traits<T>::kPerVec ? launch_sample<T, 1>(logits, a, st)
+                                                                  : launch_sample<T, kDeep>(logits, a, st);
 }
 
 bool share_bytes(const void* a, size_t an, const void* b, size_t bn) {
@@ -324,12 +1118,11 @@ vsd_status vsd_sample_filtered(const void* logits, vsd_dtype dtype, int32_t R, i
     if (!u && !out->kept && !out->filtered) return VSD_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (cudaMemsetAsync(ws, 0, 256, st) != cudaSuccess) return VSD_ERR_CUDA;
-    const SampleArgs a{p, u, *out, V, exp_shift(V), static_cast<int*>(ws)};
-    if (dtype == VSD_BF16)
-        k_sample<<<R, kSampleThreads, 0, st>>>(static_cast<const __nv_bfloat16*>(logits), a);
-    else
-        k_sample<<<R, kSampleThreads, 0, st>>>(static_cast<const float*>(logits), a);
-    return cudaGetLastError() == cudaSuccess ? VSD_OK : VSD_ERR_CUDA;
+    const bool same = (((uintptr_t)logits ^ (uintptr_t)out->filtered) & 15) == 0;
+    const SampleArgs a{p, u, *out, R, V, exp_shift(V), same, static_cast<int*>(ws)};
+    const cudaError_t e = dtype == VSD_BF16 ? sample<__nv_bfloat16>(logits, a, st)
+                                            : sample<float>(logits, a, st);
+    return e == cudaSuccess ? VSD_OK : VSD_ERR_CUDA;
 }
 
 }  // extern "C"
