@@ -14,7 +14,7 @@
 //            of each warp's 32 lane maxima, the least over the warps.
 //   list     the tokens from `lo` on, sorted; a prefix sum of their masses gives every
 //            filter's place and the draw.  A nucleus also needs the mass of all others,
-//            a sum of approximate exponentials (2^-16 off at most): where that leaves
+//            a sum of approximate exponentials (2^-20 off, or so): where that leaves
 //            the place open, it is summed again exactly.
 //   bracket  a nucleus past the list: a histogram of approximate masses over 1024
 //            steps of the logit brackets its place, the tokens in the bracket are
@@ -109,6 +109,51 @@ template <> __device__ __forceinline__ float element<__nv_bfloat16>(const uint4&
     return __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
 }
 
+// For each element of q whether it is from `lo` on: all bits of its place set, or none.
+// (lo: a value of the type)
+template <typename T> __device__ __forceinline__ uint4 mask_from(const uint4& q, float lo);
+template <> __device__ __forceinline__ uint4 mask_from<float>(const uint4& q, float lo) {
+    auto one = [&](uint32_t w) { return __uint_as_float(w) >= lo ? ~0u : 0u; };
+    return make_uint4(one(q.x), one(q.y), one(q.z), one(q.w));
+}
+template <> __device__ __forceinline__ uint4 mask_from<__nv_bfloat16>(const uint4& q, float lo) {
+    const __nv_bfloat162 l = __float2bfloat162_rn(lo);
+    auto two = [&](uint32_t w) { return __hge2_mask(*reinterpret_cast<const __nv_bfloat162*>(&w), l); };
+    return make_uint4(two(q.x), two(q.y), two(q.z), two(q.w));
+}
+// q with -inf where the mask is set.
+template <typename T> __device__ __forceinline__ uint4 cleared(const uint4& q, const uint4& m) {
+    constexpr uint32_t n = Traits<T>::kNegInf;
+    return make_uint4((q.x & ~m.x) | (n & m.x), (q.y & ~m.y) | (n & m.y), (q.z & ~m.z) | (n & m.z),
+                      (q.w & ~m.w) | (n & m.w));
+}
+// The mask's elements as bits.
+template <typename T> __device__ __forceinline__ uint32_t bits_of(const uint4& m);
+template <> __device__ __forceinline__ uint32_t bits_of<float>(const uint4& m) {
+    return (m.x & 1u) | (m.y & 2u) | (m.z & 4u) | (m.w & 8u);
+}
+template <> __device__ __forceinline__ uint32_t bits_of<__nv_bfloat16>(const uint4& m) {
+    auto two = [](uint32_t w, uint32_t b) { return (w & b) | (w >> 16 & b << 1); };
+    return two(m.x, 1u) | two(m.y, 4u) | two(m.z, 16u) | two(m.w, 64u);
+}
+// The lowest finite value of the type.
+template <typename T> __device__ __forceinline__ float lowest_of();
+template <> __device__ __forceinline__ float lowest_of<float>() { return -FLT_MAX; }
+template <> __device__ __forceinline__ float lowest_of<__nv_bfloat16>() {
+    return __uint_as_float(0xFF7F0000u);
+}
+// The nearest value of the type at or below, or above.
+template <typename T> __device__ __forceinline__ float down_to(float v);
+template <> __device__ __forceinline__ float down_to<float>(float v) { return v; }
+template <> __device__ __forceinline__ float down_to<__nv_bfloat16>(float v) {
+    return __bfloat162float(__float2bfloat16_rd(v));
+}
+template <typename T> __device__ __forceinline__ float up_to(float v);
+template <> __device__ __forceinline__ float up_to<float>(float v) { return v; }
+template <> __device__ __forceinline__ float up_to<__nv_bfloat16>(float v) {
+    return __bfloat162float(__float2bfloat16_ru(v));
+}
+
 // f w in whole numbers for 0 <= f < 1: rounded down, or up.
 __device__ __forceinline__ uint64_t share_of(uint64_t w, float f, bool up) {
     if (!(f > 0.f)) return 0;
@@ -149,6 +194,13 @@ struct Decision {
     int bin0, bin1;    // of the bracket
 };
 
+
+__device__ __forceinline__ uint64_t f2fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t f2neg(uint64_t a) { return a ^ 0x8000000080000000ull; }
 
 // 128 bits of a logits row (which may be written later, by this block alone).
 __device__ __forceinline__ uint4 ld_row(const void* p) {
@@ -216,6 +268,21 @@ template <typename T, int U> struct Sampler {
         return before;
     }
 
+    // The same by the first warp alone (G = 32).
+    template <int G> __device__ void sync() {
+        if (G == 32) __syncwarp();
+        else __syncthreads();
+    }
+    template <int G> __device__ uint64_t group_sum(uint64_t v) {
+        return G == 32 ? warp_sum_u64(v) : block_sum(v);
+    }
+    template <int G> __device__ uint64_t group_scan(uint64_t v, uint64_t& all) {
+        if (G != 32) return block_scan(v, all);
+        const uint64_t incl = warp_scan_u64(v, lane);
+        all = __shfl_sync(0xffffffffu, incl, 31);
+        return incl - v;
+    }
+
     // ------------------------------------------------------------ the row
     __device__ void open(const T* row) {
         x = row;
@@ -279,122 +346,82 @@ template <typename T, int U> struct Sampler {
         const int at = atomicAdd(&s.count, 1);
         if (at < kList) s.list[at] = (uint64_t)key_of(v) << 32 | (uint32_t)~id;
     }
+    // The sum of a vector's masses relative to `ref`, each 2^-20 off at most (up to an
+    // exponent of 40): ex2's 2^-22, and what rounding takes from v - ref.  (The product
+    // with c is made in two floats.)
+    __device__ __forceinline__ float approx_sum(const uint4& q, float ref) const {
+        uint64_t p[PV / 2];
+        vec_pairs<T>(q, p);
+        const uint64_t m2 = f2(ref, ref), c2 = f2(c, c), cl2 = f2(sc.c_lo, sc.c_lo);
+        const uint64_t l2 = f2(0.6931472f, 0.6931472f);
+        uint64_t acc = f2(0.f, 0.f);
+#pragma unroll
+        for (int e = 0; e < PV / 2; ++e) {
+            const uint64_t d = f2sub(p[e], m2), y = f2mul(d, c2);
+            const uint64_t r = f2fma(d, cl2, f2fma(d, c2, f2neg(y)));
+            float y0, y1, r0, r1;
+            f2split(y, y0, y1);
+            f2split(f2mul(r, l2), r0, r1);
+            // (of -inf there is no remainder)
+            const uint64_t x2 = f2(ex2(y0), ex2(y1));
+            acc = f2add(acc, f2fma(x2, f2(y0 > -200.f ? r0 : 0.f, y1 > -200.f ? r1 : 0.f), x2));
+        }
+        float s0, s1;
+        f2split(acc, s0, s1);
+        return s0 + s1;
+    }
     // One vector: its tokens from `lo` on are listed, the others' masses relative to `ref`
     // added up.
     template <bool TAIL>
-    __device__ __forceinline__ void list_vec(uint4 q, int j, float lo, float ref, Sum& sum,
+    __device__ __forceinline__ void list_vec(const uint4& q, int j, float lo, float ref, Sum& sum,
                                              bool& below) {
-        const float top = vec_max<T>(q);
-        uint32_t hits = 0;
-        if (top >= lo) {
-            float v[PV];
-            unpack<T>(q, v);
-#pragma unroll
-            for (int e = 0; e < PV; ++e) {
-                hits |= v[e] >= lo ? 1u << e : 0u;
-                below |= v[e] < lo && v[e] > -INFINITY;
-            }
-            for (uint32_t h = hits; h; h &= h - 1) {
+        uint4 rest = q;
+        if (vec_max<T>(q) >= lo) {
+            const uint4 in = mask_from<T>(q, lo);
+            for (uint32_t h = bits_of<T>(in); h; h &= h - 1) {
                 const int e = __ffs(h) - 1;
                 list(element<T>(q, e), id_of(j) + e);
             }
-            if (TAIL) {
-#pragma unroll
-                for (int e = 0; e < PV; ++e)
-                    if (hits >> e & 1) v[e] = -INFINITY;
-                float t = 0.f;
-#pragma unroll
-                for (int e = 0; e < PV; ++e) t += ex2((v[e] - ref) * c);
-                sum.add(t);
-            }
-            return;
+            rest = cleared<T>(q, in);
         }
-        below |= top > -INFINITY;
-        if (TAIL) {
-            uint64_t p[PV / 2];
-            vec_pairs<T>(q, p);
-            const uint64_t m2 = f2(ref, ref), c2 = f2(c, c);
-            uint64_t acc = f2_mass(p[0], m2, c2);
-#pragma unroll
-            for (int e = 1; e < PV / 2; ++e) acc = f2add(acc, f2_mass(p[e], m2, c2));
-            float p0, p1;
-            f2split(acc, p0, p1);
-            sum.add(p0 + p1);
-        }
+        below |= vec_max<T>(rest) > -INFINITY;
+        if (TAIL) sum.add(approx_sum(rest, ref));
     }
     __device__ uint64_t fixed_of(float v) const {
         return __float2ull_rn(v * ldexpf(1.f, 62 - sc.shift));
     }
-    // Lists the tokens from `lo` on; the rest's mass exactly, or not at all.
-    template <bool TAIL> __device__ Found collect(float lo, bool exact) {
-        if (tid == 0) s.count = 0;
-        __syncthreads();
-        Found f{0, 0, 0, false};
-        Sum sum;
-        each([&](const uint4& q, int j) {
-            if (TAIL && exact) {
-                list_vec<false>(q, j, lo, m, sum, f.below);
-                float v[PV];
-                unpack<T>(q, v);
-#pragma unroll
-                for (int e = 0; e < PV; ++e)
-                    if (v[e] < lo) f.tail += mass_of(v[e]);
-            } else {
-                list_vec<TAIL>(q, j, lo, m, sum, f.below);
-            }
-        });
-        if (TAIL && !exact) f.tail = fixed_of(sum.hi + sum.lo);
-        f.below = __syncthreads_or(f.below);
-        f.tail = TAIL ? block_sum(f.tail) : 0;
-        return f;
-    }
-    // The same by bins of the logit: tokens in bins before bin0 are above, those of bins
-    // bin0 .. bin1 are listed; the mass above is left by region too.
-    __device__ int bin_of(float v, float per) const {
-        return (int)fminf((m - v) * per, (float)kBins);
-    }
-    template <bool TAIL>
-    __device__ Found collect_bins(float per, int bin0, int bin1, bool exact) {
+    // Tokens from `hi` on are above, those from `lo` on are listed.  Left is the mass
+    // above, by region too; of the rest it is approximate, exact, or not summed at all.
+    template <bool TAIL> __device__ Found collect(float hi, float lo, bool exact) {
         if (tid == 0) s.count = 0;
         __syncthreads();
         Found f{0, 0, 0, false};
         Sum sum;
         uint64_t above = 0;
+        const bool over = hi < INFINITY;
         each(
             [&](const uint4& q, int j) {
-                float v[PV];
-                unpack<T>(q, v);
-                if (bin_of(vec_max<T>(q), per) > bin1 && !(TAIL && exact)) {
-                    f.below |= vec_max<T>(q) > -INFINITY;
-                    if (TAIL) {
-                        float t = 0.f;
-#pragma unroll
-                        for (int e = 0; e < PV; ++e) t += approx(v[e]);
-                        sum.add(t);
-                    }
-                    return;
+                uint4 left = q;
+                if (over && vec_max<T>(q) >= hi) {
+                    const uint4 in = mask_from<T>(q, hi);
+                    const uint32_t b = bits_of<T>(in);
+                    f.n_above += __popc(b);
+                    for (uint32_t h = b; h; h &= h - 1) above += mass_of(element<T>(q, __ffs(h) - 1));
+                    left = cleared<T>(q, in);
                 }
-                uint32_t over = 0, in = 0;
-                float t = 0.f;
+                if (TAIL && exact) {
+                    list_vec<false>(left, j, lo, m, sum, f.below);
+                    const uint4 rest = cleared<T>(left, mask_from<T>(left, lo));
+                    float v[PV];
+                    unpack<T>(rest, v);
 #pragma unroll
-                for (int e = 0; e < PV; ++e) {
-                    const int bin = bin_of(v[e], per);
-                    const bool rest = bin > bin1;
-                    over |= bin < bin0 ? 1u << e : 0u;
-                    in |= bin >= bin0 && !rest && v[e] > -INFINITY ? 1u << e : 0u;
-                    f.below |= rest && v[e] > -INFINITY;
-                    if (TAIL && !exact) t += rest ? approx(v[e]) : 0.f;
-                    else if (TAIL && rest) f.tail += mass_of(v[e]);
-                }
-                if (TAIL) sum.add(t);
-                f.n_above += __popc(over);
-                for (uint32_t h = over; h; h &= h - 1) above += mass_of(element<T>(q, __ffs(h) - 1));
-                for (uint32_t h = in; h; h &= h - 1) {
-                    const int e = __ffs(h) - 1;
-                    list(element<T>(q, e), id_of(j) + e);
+                    for (int e = 0; e < PV; ++e) f.tail += mass_of(v[e]);
+                } else {
+                    list_vec<TAIL>(left, j, lo, m, sum, f.below);
                 }
             },
             [&](int region) {
+                if (!over) return;
                 const uint64_t w = warp_sum_u64(above);
                 if (lane == 0) s.region[region] = w;
                 f.above += above;
@@ -402,39 +429,42 @@ template <typename T, int U> struct Sampler {
             });
         if (TAIL && !exact) f.tail = fixed_of(sum.hi + sum.lo);
         f.below = __syncthreads_or(f.below);
-        f.above = block_sum(f.above);
-        f.n_above = (int)block_sum((uint64_t)f.n_above);
+        f.above = over ? block_sum(f.above) : 0;
+        f.n_above = over ? (int)block_sum((uint64_t)f.n_above) : 0;
         f.tail = TAIL ? block_sum(f.tail) : 0;
         return f;
     }
+    __device__ int bin_of(float v, float per) const {
+        return (int)fminf((m - v) * per, (float)kBins);
+    }
 
     // Sorts n entries (the array holds them up to the next power of two).
-    template <typename E, bool FALLING> __device__ void sort(E* v, int n) {
+    template <int G, typename E, bool FALLING> __device__ void sort(E* v, int n) {
         int size = 2;
         while (size < n) size *= 2;
-        for (int i = n + tid; i < size; i += kSampleThreads) v[i] = FALLING ? (E)0 : ~(E)0;
+        for (int i = n + tid; i < size; i += G) v[i] = FALLING ? (E)0 : ~(E)0;
         for (int k = 2; k <= size; k *= 2)
             for (int j = k / 2; j > 0; j /= 2) {
-                __syncthreads();
-                for (int i = tid; i < size / 2; i += kSampleThreads) {
+                sync<G>();
+                for (int i = tid; i < size / 2; i += G) {
                     const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
                     const E p = v[lo], q = v[hi];
                     const bool down = ((lo & k) == 0) == FALLING;
                     if (down ? p < q : p > q) v[lo] = q, v[hi] = p;
                 }
             }
-        __syncthreads();
+        sync<G>();
     }
 
     // From the list of n: every filter's place, the kept tokens and, where they are all
-    // listed, the draw.  f: what is before and behind the list (`open`: its tail is known
-    // to 2^-16 only); `floor`: no token behind it has `least`; `known`: the mass of the
+    // listed, the draw.  By G threads, Q entries each.  f: what is before and behind the list (`open`: its tail is known
+    // to 2^-19 only); `floor`: no token behind it has `least`; `known`: the mass of the
     // first top_k, whose place is not looked for again.
+    template <int G, int Q>
     __device__ void decide(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
                            float top_p, uint64_t least, bool draw, float u) {
-        sort<uint64_t, true>(s.list, n);
+        sort<G, uint64_t, true>(s.list, n);
         // masses and their prefix sums, Q entries a thread
-        constexpr int Q = kList / kSampleThreads;
         uint64_t e[Q], own = 0;
         int big = 0;
 #pragma unroll
@@ -446,10 +476,10 @@ template <typename T, int U> struct Sampler {
             big += p < n && e[i] >= least;
         }
         uint64_t listed;
-        const uint64_t before = f.above + block_scan(own, listed);
+        const uint64_t before = f.above + group_scan<G>(own, listed);
         listed += f.above;
         const int A = f.n_above + n, kNone = INT_MAX;
-        const int big_n = (int)block_sum((uint64_t)big);
+        const int big_n = (int)group_sum<G>((uint64_t)big);
         const int pos_k = known ? kNone : top_k > 0 && top_k <= A ? top_k : f.below ? kNone : A;
         const int pos_m = least == 0 || (big_n == n && f.below && !floor) ? kNone : f.n_above + big_n;
         int kept = min(pos_k, pos_m), what = kDone;
@@ -469,12 +499,12 @@ template <typename T, int U> struct Sampler {
                         if (i <= last % Q) w += e[i];
                     s.value = w;
                 }
-                __syncthreads();
+                sync<G>();
                 w0 = w1 = s.value;
                 if (tid == 0) s.dec.all = w0;
             } else {
                 // (and 2^-28 of the first token, for terms of large exponents)
-                const uint64_t slack = open ? (f.tail >> 16) + (1ull << (62 - sc.shift) >> 28) + 1 : 0;
+                const uint64_t slack = open ? (f.tail >> 19) + (1ull << (62 - sc.shift) >> 28) + 1 : 0;
                 w0 = listed + (f.tail > slack ? f.tail - slack : 0);
                 w1 = listed + f.tail + slack;
             }
@@ -488,7 +518,7 @@ template <typename T, int U> struct Sampler {
                 cum += e[i];
                 if (tid * Q + i < n) n0 += cum < g0, n1 += cum < g1;
             }
-            const uint64_t both = block_sum((uint64_t)n0 << 32 | (uint32_t)n1);
+            const uint64_t both = group_sum<G>((uint64_t)n0 << 32 | (uint32_t)n1);
             const int p0 = min(kept, f.n_above + (int)(both >> 32) + 1);
             const int p1 = min(kept, f.n_above + (int)(uint32_t)both + 1);
             if (top_k > 0 && pos_k == kNone && !known) what = kSearch;
@@ -505,14 +535,14 @@ template <typename T, int U> struct Sampler {
 #pragma unroll
             for (int i = 0; i < Q; ++i)
                 if (tid * Q + i < here) w += e[i];
-            const uint64_t all = f.above + block_sum(w);
+            const uint64_t all = f.above + group_sum<G>(w);
             if (draw && f.n_above == 0) {
                 // the kept tokens by id, and the first whose prefix sum passes the goal
                 const uint64_t goal = share_of(all, u < 1.f ? u : 0.f, false);
                 if (tid == 0) s.token = u >= 1.f ? here - 1 : 0;
-                for (int i = tid; i < here; i += kSampleThreads)
+                for (int i = tid; i < here; i += G)
                     s.order[i] = ~(uint32_t)s.list[i] << kPlaceBits | (uint32_t)i;
-                sort<uint32_t, false>(s.order, here);
+                sort<G, uint32_t, false>(s.order, here);
                 uint64_t o[Q], sum = 0, every;
 #pragma unroll
                 for (int i = 0; i < Q; ++i) {
@@ -520,7 +550,7 @@ template <typename T, int U> struct Sampler {
                     o[i] = p < here ? s.mass[s.order[p] & (kList - 1)] : 0;
                     sum += o[i];
                 }
-                uint64_t at = block_scan(sum, every);
+                uint64_t at = group_scan<G>(sum, every);
                 if (u >= 0.f && u < 1.f && at <= goal && goal < at + sum) {
                     int hit = 0;
 #pragma unroll
@@ -530,7 +560,7 @@ template <typename T, int U> struct Sampler {
                     }
                     s.token = tid * Q + hit;
                 }
-                __syncthreads();
+                sync<G>();
             }
             if (tid == 0) {
                 const uint64_t entry = s.list[here - 1];
@@ -541,7 +571,7 @@ template <typename T, int U> struct Sampler {
                 s.dec.token = draw && f.n_above == 0 ? (int)(s.order[s.token] >> kPlaceBits) : -1;
             }
             if (draw && f.n_above > 0)  // the list's part of the regions' masses
-                for (int i = tid; i < here; i += kSampleThreads)
+                for (int i = tid; i < here; i += G)
                     atomicAdd(reinterpret_cast<unsigned long long*>(
                                   &s.region[((int)~(uint32_t)s.list[i] + off) / PV / kRegion]),
                               (unsigned long long)s.mass[i]);
@@ -549,32 +579,37 @@ template <typename T, int U> struct Sampler {
             s.dec.all = listed + f.tail;
         }
         if (tid == 0) s.dec.what = what;
+    }
+    // The same by as few threads as the list needs: a warp up to 128 entries (by all
+    // threads, most of whose work would be waiting, a list of 20 takes 9 us; so 2).
+    __device__ void decide_by(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
+                              float top_p, uint64_t least, bool draw, float u) {
+        __syncthreads();
+        if (n <= 128) {
+            if (warp == 0) decide<32, 4>(n, f, open, floor, known, top_k, top_p, least, draw, u);
+        } else if (n <= kSampleThreads) {
+            decide<kSampleThreads, 1>(n, f, open, floor, known, top_k, top_p, least, draw, u);
+        } else {
+            decide<kSampleThreads, kList / kSampleThreads>(n, f, open, floor, known, top_k, top_p, least,
+                                                           draw, u);
+        }
         __syncthreads();
     }
 
-    // Decides by a list that is there, with the rest's mass made exact where that is needed.
-    __device__ int settle(Found f, float lo, bool floor, int top_k, float top_p, uint64_t least,
-                          bool draw, float u) {
-        const bool tail = top_p < 1.f && top_k <= 0;
-        for (bool exact = false;; exact = true) {
-            if (exact) f = collect<true>(lo, true);
-            const int n = s.count;
-            if (n > kList || n == 0) return kOverflow;
-            decide(n, f, tail && !exact, floor, 0, top_k, top_p, least, draw, u);
-            if (s.dec.what != kExactTail) return s.dec.what;
-        }
-    }
-    // Lists by bins, and decides.
-    __device__ int settle_bins(float per, int bin0, int bin1, bool floor, uint64_t known, int top_k,
-                               float top_p, uint64_t least, bool draw, float u) {
+    // Decides by a list of the tokens from `lo` on, behind those from `hi` on, with the
+    // rest's mass made exact where that is needed.  (f: of a list that is there; else it is
+    // made.)
+    __device__ int settle(const Found* made, float hi, float lo, bool floor, uint64_t known,
+                          int top_k, float top_p, uint64_t least, bool draw, float u) {
         const bool tail = top_p < 1.f && top_k <= 0;
         for (bool exact = false;; exact = true) {
             __syncthreads();
-            const Found f = tail ? collect_bins<true>(per, bin0, bin1, exact)
-                                 : collect_bins<false>(per, bin0, bin1, false);
+            const Found f = made && !exact ? *made
+                            : tail         ? collect<true>(hi, lo, exact)
+                                           : collect<false>(hi, lo, false);
             const int n = s.count;
-            if (n > kList || n == 0) return kSearch;
-            decide(n, f, tail && !exact, floor, known, top_k, top_p, least, draw, u);
+            if (n > kList || n == 0) return kOverflow;
+            decide_by(n, f, tail && !exact, floor, known, top_k, top_p, least, draw, u);
             if (s.dec.what != kExactTail) return s.dec.what;
         }
     }
@@ -611,6 +646,13 @@ template <typename T, int U> struct Sampler {
             cum = next;
         }
         __syncthreads();
+    }
+    // The logits that the bracket's bins end at, and a step beyond.
+    __device__ void edges(float per, float& hi, float& lo) const {
+        const float step = 0.01f / per + fabsf(m) * 1e-6f;
+        const float top = m - (float)s.dec.bin0 / per + step, end = m - (float)(s.dec.bin1 + 1) / per - step;
+        hi = s.dec.bin0 == 0 ? INFINITY : up_to<T>(top);
+        lo = down_to<T>(end);
     }
     // For a nucleus, of which `whole` is all: bins from m down to the least logit that it
     // can reach.  Returns bins per unit of the logit.
@@ -906,7 +948,7 @@ template <typename T, int U> struct Sampler {
         // vectors a bound `lo` that `want` of the lanes' maxima reach, and a reference for
         // the masses: the maximum so far.
         const int want = top_k > 0 ? top_k : kWant;
-        float mx = -INFINITY, lo = -FLT_MAX, ref = 0.f;
+        float mx = -INFINITY, lo = lowest_of<T>(), ref = 0.f;
         bool floor = false;
         Found f{0, 0, 0, false};
         Sum sum;
@@ -933,14 +975,16 @@ template <typename T, int U> struct Sampler {
                 uint32_t top = 0;
 #pragma unroll
                 for (int i = 0; i < kSampleWarps; ++i) top = max(top, (uint32_t)s.part[i]);
-                const uint32_t lo_key = top_k == 1 ? top : t << 16;
+                // (a value of the type: the halved keys of negative bf16 end in ones)
+                const uint32_t ones = sizeof(T) == 2 && !(t & 0x8000u) ? 0xFFFFu : 0u;
+                const uint32_t lo_key = top_k == 1 ? top : t << 16 | ones;
                 ref = of_key(top);
-                lo = lo_key <= kKeyNone ? -FLT_MAX : of_key(lo_key);
+                lo = lo_key <= (kKeyNone | 0xFFFFu) ? lowest_of<T>() : of_key(lo_key);
                 if (least != 0 && top_p >= 1.f) {
                     // no token below max + T ln(min_p) is kept, and the maximum may grow
                     const float under = ref - span - rounding(ref);
                     floor = top_k <= 0 || under > lo;
-                    if (floor) lo = under;
+                    if (floor) lo = down_to<T>(under);
                 }
             }
 #pragma unroll
@@ -976,41 +1020,38 @@ template <typename T, int U> struct Sampler {
                 const float t = (sum.hi + sum.lo) * ex2((ref - m) * c);
                 f.tail = fixed_of(t);
                 if (__syncthreads_or(!(t < 2e6f) || !(sum.hi < 1e30f) || !(ref > -INFINITY)))
-                    f = collect<true>(lo, false);
+                    f = collect<true>(INFINITY, lo, false);
                 else
                     f.tail = block_sum(f.tail);
             }
             f.below = __syncthreads_or(f.below);
-            what = settle(f, lo, floor, top_k, top_p, least, draw, u);
+            what = settle(&f, INFINITY, lo, floor, 0, top_k, top_p, least, draw, u);
             if (what == kOverflow) {
                 if (tail) {
                     what = kBracket;
                     // (the list's part of the mass, from all of it)
-                    f = collect<true>(FLT_MAX, false);
+                    f = collect<true>(INFINITY, INFINITY, false);
                     if (tid == 0) s.dec.all = f.tail;
                     __syncthreads();
                 } else {
                     // the place of the k-th token, or of min_p
                     const float per = ((float)kBins - 0.1f) / (m - lo);
                     if (per > 0.f && per < INFINITY) {
-                        int bin0, bin1;
-                        if (floor) {
-                            bin0 = bin_of(m - span + rounding(m), per);
-                            bin1 = bin_of(m - span - rounding(m), per);
-                        } else {
+                        float high = up_to<T>(m - span + rounding(m)), low = down_to<T>(m - span - rounding(m));
+                        if (!floor) {
                             histogram<true>(per, 0.f, (uint64_t)top_k, 0);
-                            bin0 = s.dec.bin0;
-                            bin1 = s.dec.bin1;
+                            edges(per, high, low);
                         }
-                        what = settle_bins(per, bin0, bin1, floor, 0, top_k, top_p, least, draw, u);
+                        what = settle(nullptr, high, low, floor, 0, top_k, top_p, least, draw, u);
                     }
                 }
             }
             if (what == kBracket || what == kAbove) {
                 const uint64_t whole = s.dec.all;
-                const float per = bracket(top_p, whole);
-                what = settle_bins(per, s.dec.bin0, s.dec.bin1, false, what == kAbove ? whole : 0, top_k,
-                                   top_p, least, draw, u);
+                float high, low;
+                edges(bracket(top_p, whole), high, low);
+                what = settle(nullptr, high, low, false, what == kAbove ? whole : 0, top_k, top_p, least,
+                              draw, u);
             }
             if (what != kDone) {
                 search(top, top_k, top_p, least);
