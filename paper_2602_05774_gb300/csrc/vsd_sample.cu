@@ -49,7 +49,7 @@ constexpr int kList = 4096;
 constexpr int kPlaceBits = 12;           // of a place in it
 constexpr int kBins = 1024;
 constexpr int kWant = 128;               // a list's least length, where top-k does not say
-constexpr int kDeep = 8;                 // vectors a lane has in flight
+constexpr int kDeep = 8;                 // vectors of a lane in a long row's regions
 constexpr int kRegions = (1 << 18) / (32 * kDeep) + 1;
 constexpr float kMinT = 0x1p-64f, kMaxT = 0x1p64f;
 static_assert(kList == 1 << kPlaceBits && kList % kSampleThreads == 0 && kBins % kSampleThreads == 0, "whole rounds");
@@ -190,7 +190,7 @@ struct Decision {
     float cut;       // tokens above it are kept, and those at it up to id `limit`
     int limit, kept;
     int token;       // the token drawn, or -1
-    uint64_t all;    // the kept tokens' mass
+    uint64_t all, listed;  // the kept tokens' mass; for a bracket, the whole and the list's
     int bin0, bin1;    // of the bracket
 };
 
@@ -215,6 +215,7 @@ __device__ __forceinline__ uint4 ld_row(const void* p) {
 template <typename T, int U> struct Sampler {
     static constexpr int PV = Traits<T>::kPerVec;
     static constexpr int kRegion = 32 * U;
+    static constexpr int kLoad = U < 4 ? U : 4;  // vectors of a lane in flight
 
     struct Shared {
         uint64_t tab[kExpTab];
@@ -233,7 +234,7 @@ template <typename T, int U> struct Sampler {
     // of the row
     const T* x;
     int off, nvec;  // elements before x in its first vector; vectors
-    float m, T_, c;
+    float m, T_, c, base;  // (base: where a histogram's bins begin)
     ExpScale sc;
 
     __device__ Sampler(const SampleArgs& args, Shared& sh) : a(args), s(sh) {
@@ -242,7 +243,7 @@ template <typename T, int U> struct Sampler {
         warp = tid >> 5;
     }
 
-    __device__ uint64_t block_sum(uint64_t v) {
+    __device__ __forceinline__ uint64_t block_sum(uint64_t v) {
         v = warp_sum_u64(v);
         __syncthreads();
         if (lane == 0) s.part[warp] = v;
@@ -253,7 +254,7 @@ template <typename T, int U> struct Sampler {
         return t;
     }
     // The sum of v over the threads before this one, and over all.
-    __device__ uint64_t block_scan(uint64_t v, uint64_t& all) {
+    __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t& all) {
         const uint64_t incl = warp_scan_u64(v, lane);
         __syncthreads();
         if (lane == 31) s.part[warp] = incl;
@@ -269,14 +270,14 @@ template <typename T, int U> struct Sampler {
     }
 
     // The same by the first warp alone (G = 32).
-    template <int G> __device__ void sync() {
+    template <int G> __device__ __forceinline__ void sync() {
         if (G == 32) __syncwarp();
         else __syncthreads();
     }
-    template <int G> __device__ uint64_t group_sum(uint64_t v) {
+    template <int G> __device__ __forceinline__ uint64_t group_sum(uint64_t v) {
         return G == 32 ? warp_sum_u64(v) : block_sum(v);
     }
-    template <int G> __device__ uint64_t group_scan(uint64_t v, uint64_t& all) {
+    template <int G> __device__ __forceinline__ uint64_t group_scan(uint64_t v, uint64_t& all) {
         if (G != 32) return block_scan(v, all);
         const uint64_t incl = warp_scan_u64(v, lane);
         all = __shfl_sync(0xffffffffu, incl, 31);
@@ -284,13 +285,13 @@ template <typename T, int U> struct Sampler {
     }
 
     // ------------------------------------------------------------ the row
-    __device__ void open(const T* row) {
+    __device__ __forceinline__ void open(const T* row) {
         x = row;
         off = (int)(((uintptr_t)x / sizeof(T)) % PV);
         nvec = (a.V + off + PV - 1) / PV;
     }
     // Vector j of the row, -inf where it reaches past it.
-    __device__ uint4 vec(int j) const {
+    __device__ __forceinline__ uint4 vec(int j) const {
         const int first = id_of(j);
         if (first >= 0 && first + PV <= a.V) return ld_row(x + first);
         T e[PV];
@@ -302,26 +303,29 @@ template <typename T, int U> struct Sampler {
         return q;
     }
     // The id of element 0 of vector j.
-    __device__ int id_of(int j) const { return j * PV - off; }
-    __device__ uint64_t mass_of(float v) const { return exp_fixed(v, m, sc, s.tab); }
-    __device__ float approx(float v) const { return ex2((v - m) * c); }
+    __device__ __forceinline__ int id_of(int j) const { return j * PV - off; }
+    __device__ __forceinline__ uint64_t mass_of(float v) const { return exp_fixed(v, m, sc, s.tab); }
+    __device__ __forceinline__ float approx(float v) const { return ex2((v - m) * c); }
     // f(vector, j) for this thread's vectors of the row, end(region) after a region's.
-    template <typename F, typename E> __device__ void each(F f, E end) const {
+    template <typename F, typename E> __device__ __forceinline__ void each(F f, E end) const {
         const uint4 none = make_uint4(Traits<T>::kNegInf, Traits<T>::kNegInf, Traits<T>::kNegInf,
                                       Traits<T>::kNegInf);
         for (int j0 = warp * kRegion; j0 < nvec; j0 += kSampleWarps * kRegion) {
-            uint4 q[U];
+#pragma unroll 1
+            for (int h = 0; h < U; h += kLoad) {
+                uint4 q[kLoad];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int j = j0 + 32 * i + lane;
-                q[i] = j < nvec ? vec(j) : none;
+                for (int i = 0; i < kLoad; ++i) {
+                    const int j = j0 + 32 * (h + i) + lane;
+                    q[i] = j < nvec ? vec(j) : none;
+                }
+#pragma unroll
+                for (int i = 0; i < kLoad; ++i) f(q[i], j0 + 32 * (h + i) + lane);
             }
-#pragma unroll
-            for (int i = 0; i < U; ++i) f(q[i], j0 + 32 * i + lane);
             end(j0 / kRegion);
         }
     }
-    template <typename F> __device__ void each(F f) const {
+    template <typename F> __device__ __forceinline__ void each(F f) const {
         each(f, [](int) {});
     }
 
@@ -387,12 +391,12 @@ template <typename T, int U> struct Sampler {
         below |= vec_max<T>(rest) > -INFINITY;
         if (TAIL) sum.add(approx_sum(rest, ref));
     }
-    __device__ uint64_t fixed_of(float v) const {
+    __device__ __forceinline__ uint64_t fixed_of(float v) const {
         return __float2ull_rn(v * ldexpf(1.f, 62 - sc.shift));
     }
     // Tokens from `hi` on are above, those from `lo` on are listed.  Left is the mass
     // above, by region too; of the rest it is approximate, exact, or not summed at all.
-    template <bool TAIL> __device__ Found collect(float hi, float lo, bool exact) {
+    template <bool TAIL> __device__ __forceinline__ Found collect(float hi, float lo, bool exact) {
         if (tid == 0) s.count = 0;
         __syncthreads();
         Found f{0, 0, 0, false};
@@ -434,12 +438,12 @@ template <typename T, int U> struct Sampler {
         f.tail = TAIL ? block_sum(f.tail) : 0;
         return f;
     }
-    __device__ int bin_of(float v, float per) const {
-        return (int)fminf((m - v) * per, (float)kBins);
+    __device__ __forceinline__ int bin_of(float v, float per) const {
+        return (int)fmaxf(fminf((base - v) * per, (float)kBins), -1.f);
     }
 
     // Sorts n entries (the array holds them up to the next power of two).
-    template <int G, typename E, bool FALLING> __device__ void sort(E* v, int n) {
+    template <int G, typename E, bool FALLING> __device__ __forceinline__ void sort(E* v, int n) {
         int size = 2;
         while (size < n) size *= 2;
         for (int i = n + tid; i < size; i += G) v[i] = FALLING ? (E)0 : ~(E)0;
@@ -456,14 +460,28 @@ template <typename T, int U> struct Sampler {
         sync<G>();
     }
 
+    // Sorts the list by counting, for each entry, the larger ones: two threads an entry, n
+    // at most kSampleThreads / 2.  (A list of 256: 2 us less than by sort().)
+    __device__ __forceinline__ void sort_by_rank(int n) {
+        const int i = tid >> 1;
+        const uint64_t mine = i < n ? s.list[i] : 0;
+        int rank = 0;
+        if (i < n)
+            for (int k = tid & 1; k < n; k += 2) rank += s.list[k] > mine;
+        rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+        __syncthreads();
+        if (i < n && !(tid & 1)) s.list[rank] = mine;
+        __syncthreads();
+    }
+
     // From the list of n: every filter's place, the kept tokens and, where they are all
     // listed, the draw.  By G threads, Q entries each.  f: what is before and behind the list (`open`: its tail is known
     // to 2^-19 only); `floor`: no token behind it has `least`; `known`: the mass of the
     // first top_k, whose place is not looked for again.
     template <int G, int Q>
-    __device__ void decide(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
+    __device__ __forceinline__ void decide(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
                            float top_p, uint64_t least, bool draw, float u) {
-        sort<G, uint64_t, true>(s.list, n);
+        if (Q > 1 && G > 32) sort<G, uint64_t, true>(s.list, n);  // (else it is sorted)
         // masses and their prefix sums, Q entries a thread
         uint64_t e[Q], own = 0;
         int big = 0;
@@ -501,7 +519,7 @@ template <typename T, int U> struct Sampler {
                 }
                 sync<G>();
                 w0 = w1 = s.value;
-                if (tid == 0) s.dec.all = w0;
+                if (tid == 0) s.dec.all = w0, s.dec.listed = 0;
             } else {
                 // (and 2^-28 of the first token, for terms of large exponents)
                 const uint64_t slack = open ? (f.tail >> 19) + (1ull << (62 - sc.shift) >> 28) + 1 : 0;
@@ -540,25 +558,37 @@ template <typename T, int U> struct Sampler {
                 // the kept tokens by id, and the first whose prefix sum passes the goal
                 const uint64_t goal = share_of(all, u < 1.f ? u : 0.f, false);
                 if (tid == 0) s.token = u >= 1.f ? here - 1 : 0;
-                for (int i = tid; i < here; i += G)
-                    s.order[i] = ~(uint32_t)s.list[i] << kPlaceBits | (uint32_t)i;
-                sort<G, uint32_t, false>(s.order, here);
-                uint64_t o[Q], sum = 0, every;
-#pragma unroll
-                for (int i = 0; i < Q; ++i) {
-                    const int p = tid * Q + i;
-                    o[i] = p < here ? s.mass[s.order[p] & (kList - 1)] : 0;
-                    sum += o[i];
-                }
-                uint64_t at = group_scan<G>(sum, every);
-                if (u >= 0.f && u < 1.f && at <= goal && goal < at + sum) {
-                    int hit = 0;
+                sync<G>();
+                if (here <= 128 && u >= 0.f && u < 1.f) {
+                    // each entry's mass before it, straight
+                    for (int i = tid; i < here; i += G) {
+                        const uint32_t id = ~(uint32_t)s.list[i];
+                        uint64_t at = 0;
+                        for (int k = 0; k < here; ++k)
+                            if (~(uint32_t)s.list[k] < id) at += s.mass[k];
+                        if (at <= goal && goal < at + s.mass[i]) s.order[0] = id << kPlaceBits, s.token = 0;
+                    }
+                } else {
+                    for (int i = tid; i < here; i += G)
+                        s.order[i] = ~(uint32_t)s.list[i] << kPlaceBits | (uint32_t)i;
+                    sort<G, uint32_t, false>(s.order, here);
+                    uint64_t o[Q], sum = 0, every;
 #pragma unroll
                     for (int i = 0; i < Q; ++i) {
-                        at += o[i];
-                        hit += at <= goal;
+                        const int p = tid * Q + i;
+                        o[i] = p < here ? s.mass[s.order[p] & (kList - 1)] : 0;
+                        sum += o[i];
                     }
-                    s.token = tid * Q + hit;
+                    uint64_t at = group_scan<G>(sum, every);
+                    if (u >= 0.f && u < 1.f && at <= goal && goal < at + sum) {
+                        int hit = 0;
+#pragma unroll
+                        for (int i = 0; i < Q; ++i) {
+                            at += o[i];
+                            hit += at <= goal;
+                        }
+                        s.token = tid * Q + hit;
+                    }
                 }
                 sync<G>();
             }
@@ -577,14 +607,17 @@ template <typename T, int U> struct Sampler {
                               (unsigned long long)s.mass[i]);
         } else if (tid == 0 && what == kBracket) {
             s.dec.all = listed + f.tail;
+            s.dec.listed = f.n_above == 0 ? listed : 0;
         }
         if (tid == 0) s.dec.what = what;
     }
     // The same by as few threads as the list needs: a warp up to 128 entries (by all
     // threads, most of whose work would be waiting, a list of 20 takes 9 us; so 2).
-    __device__ void decide_by(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
+    __device__ __forceinline__ void decide_by(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
                               float top_p, uint64_t least, bool draw, float u) {
         __syncthreads();
+        if (n <= kSampleThreads / 2) sort_by_rank(n);
+        else if (n <= kSampleThreads) sort<kSampleThreads, uint64_t, true>(s.list, n);
         if (n <= 128) {
             if (warp == 0) decide<32, 4>(n, f, open, floor, known, top_k, top_p, least, draw, u);
         } else if (n <= kSampleThreads) {
@@ -596,10 +629,31 @@ template <typename T, int U> struct Sampler {
         __syncthreads();
     }
 
+    // The first token alone: the largest entry of the list.
+    __device__ __forceinline__ int first_alone() {
+        uint64_t best = 0;
+        for (int i = tid; i < s.count; i += kSampleThreads) best = max(best, s.list[i]);
+        const uint32_t key = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
+        const uint32_t id = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == key ? (uint32_t)best : 0u);
+        __syncthreads();
+        if (lane == 0) s.part[warp] = (uint64_t)key << 32 | id;
+        __syncthreads();
+        if (tid == 0) {
+#pragma unroll
+            for (int i = 0; i < kSampleWarps; ++i) best = max(best, s.part[i]);
+            s.dec.cut = m;
+            s.dec.limit = s.dec.token = (int)~(uint32_t)best;
+            s.dec.kept = 1;
+            s.dec.all = 1ull << (62 - sc.shift);
+        }
+        __syncthreads();
+        return kDone;
+    }
+
     // Decides by a list of the tokens from `lo` on, behind those from `hi` on, with the
     // rest's mass made exact where that is needed.  (f: of a list that is there; else it is
     // made.)
-    __device__ int settle(const Found* made, float hi, float lo, bool floor, uint64_t known,
+    __device__ __forceinline__ int settle(const Found* made, float hi, float lo, bool floor, uint64_t known,
                           int top_k, float top_p, uint64_t least, bool draw, float u) {
         const bool tail = top_p < 1.f && top_k <= 0;
         for (bool exact = false;; exact = true) {
@@ -615,56 +669,88 @@ template <typename T, int U> struct Sampler {
     }
 
     // ------------------------------------------------------------ the bracket
-    // A histogram over bins of the logit, each token weighing one (COUNT) or its
-    // approximate mass in units; leaves the bins that hold the place where the weights
-    // pass `goal`, known to `slack`.
-    template <bool COUNT> __device__ void histogram(float per, float unit, uint64_t goal, uint64_t slack) {
+    // A histogram over bins of the logit from `base` down, each token in them weighing one
+    // (COUNT) or its approximate mass in units; `sample`: of an eighth of the row.  goal_of
+    // gives, for the whole weight, the goal and how far it may be off; left are the bins
+    // that hold the place where the weights pass it.
+    template <bool COUNT, typename Goal>
+    __device__ __forceinline__ void histogram(float per, float unit, bool sample, Goal goal_of) {
         for (int i = tid; i < kBins; i += kSampleThreads) s.order[i] = 0;
         if (tid == 0) s.dec.bin0 = 0, s.dec.bin1 = kBins - 1;
         __syncthreads();
-        each([&](const uint4& q, int) {
+        auto count = [&](const uint4& q, int) {
             if (bin_of(vec_max<T>(q), per) >= kBins) return;
             float v[PV];
             unpack<T>(q, v);
 #pragma unroll
             for (int e = 0; e < PV; ++e) {
                 const int b = bin_of(v[e], per);
-                if (b < kBins) atomicAdd(&s.order[b], COUNT ? 1u : __float2uint_rn(approx(v[e]) * unit));
+                if (b >= 0 && b < kBins)
+                    atomicAdd(&s.order[b], COUNT ? 1u : __float2uint_rn(approx(v[e]) * unit));
             }
-        });
+        };
+        if (sample) {
+            for (int j0 = warp * kRegion; j0 < nvec; j0 += kSampleWarps * kRegion)
+                if (j0 + lane < nvec) count(vec(j0 + lane), 0);
+        } else {
+            each(count);
+        }
         __syncthreads();
         constexpr int Q = kBins / kSampleThreads;
-        uint64_t w[Q], sum = 0, all;
+        uint64_t w[Q], sum = 0, all, goal, slack;
 #pragma unroll
         for (int i = 0; i < Q; ++i) sum += w[i] = s.order[tid * Q + i];
         uint64_t cum = block_scan(sum, all);
+        goal_of(all, goal, slack);
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
-            const uint64_t next = cum + w[i];
-            if (cum + slack < goal && next + slack >= goal) s.dec.bin0 = tid * Q + i;
-            if (cum < goal + slack && next >= goal + slack) s.dec.bin1 = tid * Q + i;
-            cum = next;
+            const uint64_t after = cum + w[i];
+            if (cum + slack < goal && after + slack >= goal) s.dec.bin0 = tid * Q + i;
+            if (cum < goal + slack && after >= goal + slack) s.dec.bin1 = tid * Q + i;
+            cum = after;
         }
         __syncthreads();
     }
-    // The logits that the bracket's bins end at, and a step beyond.
-    __device__ void edges(float per, float& hi, float& lo) const {
-        const float step = 0.01f / per + fabsf(m) * 1e-6f;
-        const float top = m - (float)s.dec.bin0 / per + step, end = m - (float)(s.dec.bin1 + 1) / per - step;
-        hi = s.dec.bin0 == 0 ? INFINITY : up_to<T>(top);
-        lo = down_to<T>(end);
-    }
-    // For a nucleus, of which `whole` is all: bins from m down to the least logit that it
-    // can reach.  Returns bins per unit of the logit.
-    __device__ float bracket(float top_p, uint64_t whole) {
+    // For a nucleus, of which `whole` is all: bins down to the least logit that it can
+    // reach.  Returns bins per unit of the logit.
+    __device__ __forceinline__ float bracket(float top_p, uint64_t whole) {
         // tokens whose logit leaves them less than (1 - top_p) / V of the mass are out
         const float z = (float)whole * ldexpf(1.f, sc.shift - 62);
         const float reach = T_ * (logf((float)a.V / ((1.f - top_p) * z)) + 0.01f);
         const float per = (float)kBins / reach;
+        base = m;
         // in units of 2^-30 of the mass: half a unit a token, and 2^-15
-        histogram<false>(per, 1073741824.f / z, (uint64_t)(top_p * 1073741824.f),
-                         (uint64_t)a.V / 2 + (1 << 15) + 2);
+        histogram<false>(per, 1073741824.f / z, false, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
+            goal = (uint64_t)(top_p * 1073741824.f);
+            slack = (uint64_t)a.V / 2 + (1 << 15) + 2;
+        });
         return per;
+    }
+    // The same behind a list of the tokens from `lo` on, of mass `listed`, by an eighth of
+    // the rest: the place may be off by some deviations of the sample's weight up to it,
+    // whose square is at most that weight times the largest token's.  0 if there are none.
+    __device__ __forceinline__ float bracket_rest(float top_p, uint64_t whole, uint64_t listed, float lo) {
+        const float one = ldexpf(1.f, sc.shift - 62), z = (float)whole * one;
+        const float rest = (float)(whole - listed) * one, need = top_p * z - (float)listed * one;
+        const float reach = T_ * (logf((float)a.V / ((1.f - top_p) * z)) + 0.01f) - (m - lo);
+        if (!(reach > 0.f) || !(need > 0.f) || !(need < rest)) return 0.f;
+        const float per = (float)kBins / reach, unit = 1073741824.f / rest;
+        base = lo;
+        histogram<false>(per, unit, true, [&](uint64_t all, uint64_t& goal, uint64_t& slack) {
+            const float g = (float)all * (need / rest), top = approx(lo) * unit;
+            goal = (uint64_t)g;
+            slack = (uint64_t)(3.f * sqrtf(g * top) + 4.f * top) + (uint64_t)a.V / 16 + 2;
+        });
+        return per;
+    }
+
+    // The logits that the bracket's bins end at, and a step beyond.
+    __device__ __forceinline__ void edges(float per, float& hi, float& lo) const {
+        const float step = 0.01f / per + (fabsf(m) + fabsf(base)) * 1e-6f;
+        const float top = base - (float)s.dec.bin0 / per + step;
+        const float end = base - (float)(s.dec.bin1 + 1) / per - step;
+        hi = s.dec.bin0 == 0 && base == m ? INFINITY : up_to<T>(top);
+        lo = down_to<T>(end);
     }
 
     // ------------------------------------------------------------ the search
@@ -675,7 +761,7 @@ template <typename T, int U> struct Sampler {
         uint64_t mass;
         uint32_t least, under;
     };
-    template <bool MASS> __device__ From from_key(uint32_t k) {
+    template <bool MASS> __device__ __forceinline__ From from_key(uint32_t k) {
         From f{0, 0, ~0u, 0};
         each([&](const uint4& q, int) {
             uint32_t in = 0;
@@ -708,10 +794,10 @@ template <typename T, int U> struct Sampler {
         }
         return f;
     }
-    __device__ int count_from(uint32_t k) { return from_key<false>(k).n; }
+    __device__ __forceinline__ int count_from(uint32_t k) { return from_key<false>(k).n; }
     // The largest key in lo .. hi from which on the tokens are `goal`, in number or mass
     // (from lo on they are): bisection, each time to a key that is there.
-    template <bool MASS> __device__ uint32_t last_key(uint32_t lo, uint32_t hi, uint64_t goal) {
+    template <bool MASS> __device__ __forceinline__ uint32_t last_key(uint32_t lo, uint32_t hi, uint64_t goal) {
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo + 1) / 2;
             const From f = from_key<MASS>(mid);
@@ -725,12 +811,12 @@ template <typename T, int U> struct Sampler {
         uint32_t key;
         int ties, n;  // of those at the key
     };
-    __device__ Place place(uint32_t top, int n) {
+    __device__ __forceinline__ Place place(uint32_t top, int n) {
         const uint32_t k = last_key<false>(kKeyNone + 1, top, (uint64_t)n);
         return Place{k, n - count_from(k + 1), n};
     }
     // Every filter's place by bisection; leaves cut, limit and kept.
-    __device__ void search(uint32_t top, int top_k, float top_p, uint64_t least) {
+    __device__ __forceinline__ void search(uint32_t top, int top_k, float top_p, uint64_t least) {
         const uint32_t bottom = kKeyNone + 1;
         const int live = count_from(bottom);
         Place at{bottom, live, live};
@@ -764,7 +850,7 @@ template <typename T, int U> struct Sampler {
         if (at.ties < count_from(at.key) - (at.n - at.ties)) tie_limit(at.key, at.ties);
     }
     // The id of the ties-th token at the key.
-    __device__ void tie_limit(uint32_t key, int ties) {
+    __device__ __forceinline__ void tie_limit(uint32_t key, int ties) {
         auto equal = [&](const uint4& q) {
             float v[PV];
             unpack<T>(q, v);
@@ -797,7 +883,7 @@ template <typename T, int U> struct Sampler {
         __syncthreads();
     }
     // The region whose sum, added to those before, passes the goal; less what is before.
-    __device__ int pick_region(uint64_t& goal) {
+    __device__ __forceinline__ int pick_region(uint64_t& goal) {
         const int n = (nvec + kRegion - 1) / kRegion;
         constexpr int Q = (kRegions + kSampleThreads - 1) / kSampleThreads;
         __syncthreads();
@@ -820,11 +906,11 @@ template <typename T, int U> struct Sampler {
     }
 
     // ------------------------------------------------------------ the draw
-    __device__ bool is_kept(float v, int id) const {
+    __device__ __forceinline__ bool is_kept(float v, int id) const {
         return v > s.dec.cut || (v == s.dec.cut && id <= s.dec.limit);
     }
     // The kept tokens' number, and their masses by region.
-    __device__ void weigh(bool draw) {
+    __device__ __forceinline__ void weigh(bool draw) {
         uint64_t w = 0, all = 0;
         int n = 0;
         each(
@@ -853,7 +939,7 @@ template <typename T, int U> struct Sampler {
         __syncthreads();
     }
     // The token of u, from the kept masses by region.
-    __device__ int find(float u) {
+    __device__ __forceinline__ int find(float u) {
         if (!(u >= 0.f && u < 1.f)) {  // the last kept, or the first
             __syncthreads();
             if (tid == 0) s.token = u >= 1.f ? -1 : INT_MAX;
@@ -897,7 +983,7 @@ template <typename T, int U> struct Sampler {
     }
 
     // ------------------------------------------------------------ a row
-    __device__ void write_filtered(int64_t r, bool none) {
+    __device__ __forceinline__ void write_filtered(int64_t r, bool none) {
         T* o = static_cast<T*>(a.out.filtered) + r * a.V;
         each([&](const uint4& q, int j) {
             const int id = id_of(j);
@@ -920,7 +1006,7 @@ template <typename T, int U> struct Sampler {
         });
     }
 
-    __device__ void row(int64_t r) {
+    __device__ __forceinline__ void row(int64_t r, const T* next) {
         const vsd_policy& p = a.policy;
         T_ = p.row_T ? p.row_T[r] : p.T;
         float top_p = p.row_top_p ? p.row_top_p[r] : p.top_p;
@@ -955,13 +1041,14 @@ template <typename T, int U> struct Sampler {
         if (tid == 0) s.count = 0;
         const uint4 none = make_uint4(Traits<T>::kNegInf, Traits<T>::kNegInf, Traits<T>::kNegInf,
                                       Traits<T>::kNegInf);
-        for (int j1 = 0; j1 < nvec; j1 += kSampleWarps * kRegion) {
-            const int j0 = j1 + warp * kRegion + lane;
-            uint4 q[U];
+        constexpr int kRound = kSampleWarps * 32 * kLoad;
+        for (int j1 = 0; j1 < nvec; j1 += kRound) {
+            const int j0 = j1 + warp * (32 * kLoad) + lane;
+            uint4 q[kLoad];
 #pragma unroll
-            for (int i = 0; i < U; ++i) q[i] = j0 + 32 * i < nvec ? vec(j0 + 32 * i) : none;
+            for (int i = 0; i < kLoad; ++i) q[i] = j0 + 32 * i < nvec ? vec(j0 + 32 * i) : none;
 #pragma unroll
-            for (int i = 0; i < U; ++i) mx = max_nan(mx, vec_max_nan<T>(q[i]));
+            for (int i = 0; i < kLoad; ++i) mx = max_nan(mx, vec_max_nan<T>(q[i]));
             if (!filters) continue;
             if (j1 == 0) {
                 const uint32_t key = key_of(mx), high = key >> 16;
@@ -988,11 +1075,15 @@ template <typename T, int U> struct Sampler {
                 }
             }
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
+            for (int i = 0; i < kLoad; ++i) {
                 if (tail) list_vec<true>(q[i], j0 + 32 * i, lo, ref, sum, f.below);
                 else list_vec<false>(q[i], j0 + 32 * i, lo, ref, sum, f.below);
             }
         }
+        if (next)  // (into L2, while this row is decided)
+            for (int64_t i = (int64_t)tid * 128; i < (int64_t)a.V * (int64_t)sizeof(T);
+                 i += kSampleThreads * 128)
+                asm volatile("prefetch.global.L2 [%0];" :: "l"(reinterpret_cast<const char*>(next) + i));
         const bool bad = __syncthreads_or(!(mx < INFINITY));
         const uint32_t w = __reduce_max_sync(0xffffffffu, key_of(mx));
         if (lane == 0) s.part[warp] = w;
@@ -1012,57 +1103,69 @@ template <typename T, int U> struct Sampler {
             return;
         }
         m = of_key(top);
-        if (tid == 0) s.dec.token = -1;
-        int what = kDone;
+        if (tid == 0) s.dec.token = -1, s.dec.cut = -FLT_MAX, s.dec.limit = INT_MAX;
+        bool sums = !filters;  // whether the kept tokens' masses are still to be summed
         if (filters) {
+            bool made = true;
+            uint64_t whole = 0, listed = 0;
             if (tail) {
                 // (where the reference was too far below: once more, relative to m)
                 const float t = (sum.hi + sum.lo) * ex2((ref - m) * c);
                 f.tail = fixed_of(t);
-                if (__syncthreads_or(!(t < 2e6f) || !(sum.hi < 1e30f) || !(ref > -INFINITY)))
-                    f = collect<true>(INFINITY, lo, false);
-                else
-                    f.tail = block_sum(f.tail);
+                made = !__syncthreads_or(!(t < 2e6f) || !(sum.hi < 1e30f) || !(ref > -INFINITY));
+                f.tail = block_sum(f.tail);
             }
             f.below = __syncthreads_or(f.below);
-            what = settle(&f, INFINITY, lo, floor, 0, top_k, top_p, least, draw, u);
-            if (what == kOverflow) {
-                if (tail) {
-                    what = kBracket;
-                    // (the list's part of the mass, from all of it)
-                    f = collect<true>(INFINITY, INFINITY, false);
-                    if (tid == 0) s.dec.all = f.tail;
-                    __syncthreads();
+            // a list from `low` on behind what is from `high` on, until one decides: the
+            // first; where a long top-k or min_p overflows it, one around its place; for a
+            // nucleus past it one around its place by a sample, then by all of the row
+            float high = INFINITY, low = lo;
+            uint64_t known = 0;
+            int what;
+            for (int step = 0;; made = false) {
+                what = step == 0 && top_k == 1 && s.count <= kList
+                           ? first_alone()
+                           : settle(made ? &f : nullptr, high, low, floor, known, top_k, top_p, least,
+                                    draw, u);
+                if (what == kDone || step == 4) break;
+                float per = 0.f;
+                if (step == 0 && what == kOverflow && !tail) {
+                    step = 1;
+                    high = up_to<T>(m - span + rounding(m));
+                    low = down_to<T>(m - span - rounding(m));
+                    if (floor) continue;
+                    per = ((float)kBins - 0.1f) / (m - lo);
+                    base = m;
+                    if (!(per > 0.f && per < INFINITY)) break;
+                    histogram<true>(per, 0.f, false, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
+                        goal = (uint64_t)top_k;
+                        slack = 0;
+                    });
                 } else {
-                    // the place of the k-th token, or of min_p
-                    const float per = ((float)kBins - 0.1f) / (m - lo);
-                    if (per > 0.f && per < INFINITY) {
-                        float high = up_to<T>(m - span + rounding(m)), low = down_to<T>(m - span - rounding(m));
-                        if (!floor) {
-                            histogram<true>(per, 0.f, (uint64_t)top_k, 0);
-                            edges(per, high, low);
-                        }
-                        what = settle(nullptr, high, low, floor, 0, top_k, top_p, least, draw, u);
+                    if (step < 2) {
+                        if (what != kBracket && what != kAbove) break;
+                        floor = false;
+                        if (what == kAbove) known = s.dec.all;
+                        step = what == kAbove ? 3 : 2;
+                        whole = s.dec.all;
+                        listed = s.dec.listed;
+                        if (step == 2) per = bracket_rest(top_p, whole, listed, lo);
+                    }
+                    if (per == 0.f) {
+                        step = 4;
+                        per = bracket(top_p, whole);
                     }
                 }
-            }
-            if (what == kBracket || what == kAbove) {
-                const uint64_t whole = s.dec.all;
-                float high, low;
-                edges(bracket(top_p, whole), high, low);
-                what = settle(nullptr, high, low, false, what == kAbove ? whole : 0, top_k, top_p, least,
-                              draw, u);
+                edges(per, high, low);
             }
             if (what != kDone) {
                 search(top, top_k, top_p, least);
-                weigh(draw);
                 if (tid == 0) s.dec.token = -1;
+                sums = true;
             }
-        } else {
-            if (tid == 0) s.dec.cut = -FLT_MAX, s.dec.limit = INT_MAX;
-            __syncthreads();
-            weigh(draw);
         }
+        __syncthreads();
+        if (sums) weigh(draw);
         __syncthreads();
         if (draw) {
             const int id = s.dec.token >= 0 ? s.dec.token : find(u);
@@ -1087,7 +1190,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const T* logits, c
     for (int64_t r = blockIdx.x; r < a.R; r += gridDim.x) {
         __syncthreads();
         w.open(logits + r * a.V);
-        w.row(r);
+        w.row(r, r + gridDim.x < a.R ? logits + (r + gridDim.x) * a.V : nullptr);
     }
 }
 
