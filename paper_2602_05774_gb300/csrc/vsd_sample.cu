@@ -243,45 +243,45 @@ template <typename T, int U> struct Sampler {
         warp = tid >> 5;
     }
 
-    __device__ __forceinline__ uint64_t block_sum(uint64_t v) {
-        v = warp_sum_u64(v);
-        __syncthreads();
-        if (lane == 0) s.part[warp] = v;
-        __syncthreads();
-        uint64_t t = 0;
-#pragma unroll
-        for (int i = 0; i < kSampleWarps; ++i) t += s.part[i];
-        return t;
-    }
+    __device__ __forceinline__ uint64_t block_sum(uint64_t v) { return group_sum<kSampleThreads>(v); }
     // The sum of v over the threads before this one, and over all.
     __device__ __forceinline__ uint64_t block_scan(uint64_t v, uint64_t& all) {
+        return group_scan<kSampleThreads>(v, all);
+    }
+    // The same by the first G threads.
+    template <int G> __device__ __forceinline__ void sync() {
+        if (G == 32) __syncwarp();
+        else if (G < kSampleThreads) asm volatile("bar.sync 1, %0;" :: "n"(G) : "memory");
+        else __syncthreads();
+    }
+    template <int G> __device__ __forceinline__ uint64_t group_scan(uint64_t v, uint64_t& all) {
         const uint64_t incl = warp_scan_u64(v, lane);
-        __syncthreads();
+        if (G == 32) {
+            all = __shfl_sync(0xffffffffu, incl, 31);
+            return incl - v;
+        }
+        sync<G>();
         if (lane == 31) s.part[warp] = incl;
-        __syncthreads();
+        sync<G>();
         uint64_t before = incl - v;
         all = 0;
 #pragma unroll
-        for (int i = 0; i < kSampleWarps; ++i) {
+        for (int i = 0; i < G / 32; ++i) {
             if (i < warp) before += s.part[i];
             all += s.part[i];
         }
         return before;
     }
-
-    // The same by the first warp alone (G = 32).
-    template <int G> __device__ __forceinline__ void sync() {
-        if (G == 32) __syncwarp();
-        else __syncthreads();
-    }
     template <int G> __device__ __forceinline__ uint64_t group_sum(uint64_t v) {
-        return G == 32 ? warp_sum_u64(v) : block_sum(v);
-    }
-    template <int G> __device__ __forceinline__ uint64_t group_scan(uint64_t v, uint64_t& all) {
-        if (G != 32) return block_scan(v, all);
-        const uint64_t incl = warp_scan_u64(v, lane);
-        all = __shfl_sync(0xffffffffu, incl, 31);
-        return incl - v;
+        v = warp_sum_u64(v);
+        if (G == 32) return v;
+        sync<G>();
+        if (lane == 0) s.part[warp] = v;
+        sync<G>();
+        uint64_t t = 0;
+#pragma unroll
+        for (int i = 0; i < G / 32; ++i) t += s.part[i];
+        return t;
     }
 
     // ------------------------------------------------------------ the row
@@ -289,6 +289,11 @@ template <typename T, int U> struct Sampler {
         x = row;
         off = (int)(((uintptr_t)x / sizeof(T)) % PV);
         nvec = (a.V + off + PV - 1) / PV;
+    }
+    // Brings a row into L2.
+    __device__ __forceinline__ void bring(const T* row) const {
+        for (int64_t i = (int64_t)tid * 128; i < (int64_t)a.V * (int64_t)sizeof(T); i += kSampleThreads * 128)
+            asm volatile("prefetch.global.L2 [%0];" :: "l"(reinterpret_cast<const char*>(row) + i));
     }
     // Vector j of the row, -inf where it reaches past it.
     __device__ __forceinline__ uint4 vec(int j) const {
@@ -521,8 +526,7 @@ template <typename T, int U> struct Sampler {
                 w0 = w1 = s.value;
                 if (tid == 0) s.dec.all = w0, s.dec.listed = 0;
             } else {
-                // (and 2^-28 of the first token, for terms of large exponents)
-                const uint64_t slack = open ? (f.tail >> 19) + (1ull << (62 - sc.shift) >> 28) + 1 : 0;
+                const uint64_t slack = open ? tail_slack(f.tail) : 0;
                 w0 = listed + (f.tail > slack ? f.tail - slack : 0);
                 w1 = listed + f.tail + slack;
             }
@@ -611,15 +615,17 @@ template <typename T, int U> struct Sampler {
         }
         if (tid == 0) s.dec.what = what;
     }
-    // The same by as few threads as the list needs: a warp up to 128 entries (by all
-    // threads, most of whose work would be waiting, a list of 20 takes 9 us; so 2).
+    // The same by as few threads as the list needs (what the others would do takes issue
+    // slots from the SM's other block).
     __device__ __forceinline__ void decide_by(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
                               float top_p, uint64_t least, bool draw, float u) {
         __syncthreads();
         if (n <= kSampleThreads / 2) sort_by_rank(n);
         else if (n <= kSampleThreads) sort<kSampleThreads, uint64_t, true>(s.list, n);
-        if (n <= 128) {
-            if (warp == 0) decide<32, 4>(n, f, open, floor, known, top_k, top_p, least, draw, u);
+        if (n <= 32) {
+            if (warp == 0) decide<32, 1>(n, f, open, floor, known, top_k, top_p, least, draw, u);
+        } else if (n <= 128) {
+            if (warp < 4) decide<128, 1>(n, f, open, floor, known, top_k, top_p, least, draw, u);
         } else if (n <= kSampleThreads) {
             decide<kSampleThreads, 1>(n, f, open, floor, known, top_k, top_p, least, draw, u);
         } else {
@@ -650,6 +656,47 @@ template <typename T, int U> struct Sampler {
         return kDone;
     }
 
+    // Leaves of a list of n, an entry a thread, the largest k and what equals the k-th.
+    __device__ __forceinline__ int prune(int n, int k, Found& f) {
+        const uint64_t mine = tid < n ? s.list[tid] : 0;
+        const uint32_t key = (uint32_t)(mine >> 32);
+        uint32_t t = 0;
+        // (of bf16 the lower halves are alike)
+        for (uint32_t bit = 1u << 31; bit >= (sizeof(T) == 2 ? 1u << 16 : 1u); bit >>= 1)
+            if (__syncthreads_count(key >= (t | bit)) >= k) t |= bit;
+        const bool in = key >= t && tid < n;
+        const uint32_t w = __ballot_sync(0xffffffffu, in);
+        if (lane == 0) s.part[warp] = __popc(w);
+        __syncthreads();
+        int at = __popc(w & ((1u << lane) - 1)), all = 0;
+#pragma unroll
+        for (int i = 0; i < kSampleWarps; ++i) {
+            at += i < warp ? (int)s.part[i] : 0;
+            all += (int)s.part[i];
+        }
+        if (in) s.list[at] = mine;
+        f.below |= all < n;
+        __syncthreads();
+        return all;
+    }
+    // Whether a nucleus is certain to reach past the list.
+    __device__ __forceinline__ bool past(int n, const Found& f, float top_p) {
+        uint64_t w = 0;
+#pragma unroll 1
+        for (int i = tid; i < n; i += kSampleThreads) w += mass_of(of_key((uint32_t)(s.list[i] >> 32)));
+        w = block_sum(w);
+        const uint64_t slack = tail_slack(f.tail);
+        if (w >= share_of(w + (f.tail > slack ? f.tail - slack : 0), top_p, true)) return false;
+        if (tid == 0) s.dec.all = w + f.tail, s.dec.listed = w;
+        __syncthreads();
+        return true;
+    }
+    // How far an approximate sum may be off (and 2^-28 of the first token, for terms of
+    // large exponents).
+    __device__ __forceinline__ uint64_t tail_slack(uint64_t tail) const {
+        return (tail >> 19) + (1ull << (62 - sc.shift) >> 28) + 1;
+    }
+
     // Decides by a list of the tokens from `lo` on, behind those from `hi` on, with the
     // rest's mass made exact where that is needed.  (f: of a list that is there; else it is
     // made.)
@@ -661,9 +708,12 @@ template <typename T, int U> struct Sampler {
             const Found f = made && !exact ? *made
                             : tail         ? collect<true>(hi, lo, exact)
                                            : collect<false>(hi, lo, false);
-            const int n = s.count;
+            int n = s.count;
             if (n > kList || n == 0) return kOverflow;
-            decide_by(n, f, tail && !exact, floor, known, top_k, top_p, least, draw, u);
+            Found g = f;
+            if (made && top_k > 0 && n > top_k && n > 64 && n <= kSampleThreads) n = prune(n, top_k, g);
+            if (made && tail && n > kSampleThreads / 4 && least == 0 && past(n, f, top_p)) return kBracket;
+            decide_by(n, g, tail && !exact, floor, known, top_k, top_p, least, draw, u);
             if (s.dec.what != kExactTail) return s.dec.what;
         }
     }
@@ -1080,10 +1130,7 @@ template <typename T, int U> struct Sampler {
                 else list_vec<false>(q[i], j0 + 32 * i, lo, ref, sum, f.below);
             }
         }
-        if (next)  // (into L2, while this row is decided)
-            for (int64_t i = (int64_t)tid * 128; i < (int64_t)a.V * (int64_t)sizeof(T);
-                 i += kSampleThreads * 128)
-                asm volatile("prefetch.global.L2 [%0];" :: "l"(reinterpret_cast<const char*>(next) + i));
+        if (next) bring(next);  // (while this row is decided)
         const bool bad = __syncthreads_or(!(mx < INFINITY));
         const uint32_t w = __reduce_max_sync(0xffffffffu, key_of(mx));
         if (lane == 0) s.part[warp] = w;
@@ -1186,6 +1233,7 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const T* logits, c
     extern __shared__ __align__(128) unsigned char sample_smem[];
     typename S::Shared& s = *reinterpret_cast<typename S::Shared*>(sample_smem);
     S w(a, s);
+    w.bring(logits + (int64_t)blockIdx.x * a.V);
     for (int j = threadIdx.x; j < kExpTab; j += kSampleThreads) s.tab[j] = exp_entry(kExpParts, j);
     for (int64_t r = blockIdx.x; r < a.R; r += gridDim.x) {
         __syncthreads();
