@@ -307,23 +307,30 @@ template <typename T, int U> struct Sampler {
         memcpy(&q, e, 16);
         return q;
     }
+    // Vectors j0, j0 + 32, ... of this lane (j0 - lane is the warp's).
+    __device__ __forceinline__ void load(int j0, uint4 (&q)[kLoad]) const {
+        if (id_of(j0 - lane) >= 0 && id_of(j0 - lane + 32 * kLoad) <= a.V) {  // (all inside)
+            const T* p = x + id_of(j0);
+#pragma unroll
+            for (int i = 0; i < kLoad; ++i) q[i] = ld_row(p + 32 * PV * i);
+        } else {
+            const uint4 none = make_uint4(Traits<T>::kNegInf, Traits<T>::kNegInf, Traits<T>::kNegInf,
+                                          Traits<T>::kNegInf);
+#pragma unroll
+            for (int i = 0; i < kLoad; ++i) q[i] = j0 + 32 * i < nvec ? vec(j0 + 32 * i) : none;
+        }
+    }
     // The id of element 0 of vector j.
     __device__ __forceinline__ int id_of(int j) const { return j * PV - off; }
     __device__ __forceinline__ uint64_t mass_of(float v) const { return exp_fixed(v, m, sc, s.tab); }
     __device__ __forceinline__ float approx(float v) const { return ex2((v - m) * c); }
     // f(vector, j) for this thread's vectors of the row, end(region) after a region's.
     template <typename F, typename E> __device__ __forceinline__ void each(F f, E end) const {
-        const uint4 none = make_uint4(Traits<T>::kNegInf, Traits<T>::kNegInf, Traits<T>::kNegInf,
-                                      Traits<T>::kNegInf);
         for (int j0 = warp * kRegion; j0 < nvec; j0 += kSampleWarps * kRegion) {
 #pragma unroll 1
             for (int h = 0; h < U; h += kLoad) {
                 uint4 q[kLoad];
-#pragma unroll
-                for (int i = 0; i < kLoad; ++i) {
-                    const int j = j0 + 32 * (h + i) + lane;
-                    q[i] = j < nvec ? vec(j) : none;
-                }
+                load(j0 + 32 * h + lane, q);
 #pragma unroll
                 for (int i = 0; i < kLoad; ++i) f(q[i], j0 + 32 * (h + i) + lane);
             }
@@ -1089,14 +1096,11 @@ template <typename T, int U> struct Sampler {
         Found f{0, 0, 0, false};
         Sum sum;
         if (tid == 0) s.count = 0;
-        const uint4 none = make_uint4(Traits<T>::kNegInf, Traits<T>::kNegInf, Traits<T>::kNegInf,
-                                      Traits<T>::kNegInf);
         constexpr int kRound = kSampleWarps * 32 * kLoad;
         for (int j1 = 0; j1 < nvec; j1 += kRound) {
             const int j0 = j1 + warp * (32 * kLoad) + lane;
             uint4 q[kLoad];
-#pragma unroll
-            for (int i = 0; i < kLoad; ++i) q[i] = j0 + 32 * i < nvec ? vec(j0 + 32 * i) : none;
+            load(j0, q);
 #pragma unroll
             for (int i = 0; i < kLoad; ++i) mx = max_nan(mx, vec_max_nan<T>(q[i]));
             if (!filters) continue;
@@ -1190,12 +1194,23 @@ template <typename T, int U> struct Sampler {
                     });
                 } else {
                     if (step < 2) {
+                        if (step == 0 && what == kBracket && least != 0) {
+                            // (the place of min_p may come before)
+                            step = 1;
+                            floor = true;
+                            whole = s.dec.all;
+                            listed = s.dec.listed;
+                            high = up_to<T>(m - span + rounding(m));
+                            low = down_to<T>(m - span - rounding(m));
+                            continue;
+                        }
+                        const bool again = floor && whole;  // (after a look at the place of min_p)
+                        if (again) what = kBracket;
                         if (what != kBracket && what != kAbove) break;
                         floor = false;
                         if (what == kAbove) known = s.dec.all;
                         step = what == kAbove ? 3 : 2;
-                        whole = s.dec.all;
-                        listed = s.dec.listed;
+                        if (!again) whole = s.dec.all, listed = s.dec.listed;
                         if (step == 2) per = bracket_rest(top_p, whole, listed, lo);
                     }
                     if (per == 0.f) {
