@@ -14,7 +14,7 @@
 //            of each warp's 32 lane maxima, the least over the warps.
 //   list     the tokens from `lo` on, sorted; a prefix sum of their masses gives every
 //            filter's place and the draw.  A nucleus also needs the mass of all others,
-//            a sum of approximate exponentials (2^-20 off, or so): where that leaves
+//            a sum of approximate exponentials (2^-17 off at most): where that leaves
 //            the place open, it is summed again exactly.
 //   bracket  a nucleus past the list: a histogram of approximate masses over 1024
 //            steps of the logit brackets its place, the tokens in the bracket are
@@ -200,7 +200,6 @@ __device__ __forceinline__ uint64_t f2fma(uint64_t a, uint64_t b, uint64_t c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
-__device__ __forceinline__ uint64_t f2neg(uint64_t a) { return a ^ 0x8000000080000000ull; }
 
 // 128 bits of a logits row (which may be written later, by this block alone).
 __device__ __forceinline__ uint4 ld_row(const void* p) {
@@ -225,7 +224,7 @@ template <typename T, int U> struct Sampler {
         uint64_t region[U == kDeep ? kRegions : kSampleThreads * kDeep / 64 + 2];
         uint64_t part[kSampleWarps], value;
         Decision dec;
-        int count, token;
+        int count, token, next;
     };
 
     const SampleArgs& a;
@@ -235,6 +234,7 @@ template <typename T, int U> struct Sampler {
     const T* x;
     int off, nvec;  // elements before x in its first vector; vectors
     float m, T_, c, base;  // (base: where a histogram's bins begin)
+    float above_from;      // of the list at hand
     ExpScale sc;
 
     __device__ Sampler(const SampleArgs& args, Shared& sh) : a(args), s(sh) {
@@ -345,7 +345,7 @@ template <typename T, int U> struct Sampler {
     // What a listing leaves beside the list: the exact mass and the number of the tokens
     // above, and the mass, approximate or exact, of the rest.
     struct Found {
-        uint64_t above, tail;
+        uint64_t above, tail, slack;  // (how far the tail may be off)
         int n_above;
         bool below;  // whether there is a rest
     };
@@ -362,46 +362,58 @@ template <typename T, int U> struct Sampler {
         const int at = atomicAdd(&s.count, 1);
         if (at < kList) s.list[at] = (uint64_t)key_of(v) << 32 | (uint32_t)~id;
     }
-    // The sum of a vector's masses relative to `ref`, each 2^-20 off at most (up to an
-    // exponent of 40): ex2's 2^-22, and what rounding takes from v - ref.  (The product
-    // with c is made in two floats.)
+    // The sum of a vector's masses relative to `ref`, where exponents are 40 at most off by
+    // 2^-17 of itself at most: ex2's 2^-22, and what v - ref, c and their product are
+    // rounded by.  FINE: by 2^-19, the product with c in two floats.  (The first pass over a
+    // row does without, as it would take half as long again; behind a bracket it spares
+    // four of five exact sums.)
+    template <bool FINE>
     __device__ __forceinline__ float approx_sum(const uint4& q, float ref) const {
         uint64_t p[PV / 2];
         vec_pairs<T>(q, p);
-        const uint64_t m2 = f2(ref, ref), c2 = f2(c, c), cl2 = f2(sc.c_lo, sc.c_lo);
-        const uint64_t l2 = f2(0.6931472f, 0.6931472f);
+        const uint64_t m2 = f2(ref, ref), c2 = f2(c, c);
         uint64_t acc = f2(0.f, 0.f);
 #pragma unroll
         for (int e = 0; e < PV / 2; ++e) {
-            const uint64_t d = f2sub(p[e], m2), y = f2mul(d, c2);
-            const uint64_t r = f2fma(d, cl2, f2fma(d, c2, f2neg(y)));
-            float y0, y1, r0, r1;
-            f2split(y, y0, y1);
-            f2split(f2mul(r, l2), r0, r1);
-            // (of -inf there is no remainder)
-            const uint64_t x2 = f2(ex2(y0), ex2(y1));
-            acc = f2add(acc, f2fma(x2, f2(y0 > -200.f ? r0 : 0.f, y1 > -200.f ? r1 : 0.f), x2));
+            if (FINE) {
+                const uint64_t d = f2sub(p[e], m2), y = f2mul(d, c2);
+                float y0, y1, r0, r1;
+                f2split(y, y0, y1);
+                f2split(f2mul(f2fma(d, f2(sc.c_lo, sc.c_lo), f2fma(d, c2, f2(-y0, -y1))),
+                              f2(0.6931472f, 0.6931472f)), r0, r1);
+                const uint64_t x2 = f2(ex2(y0), ex2(y1));
+                // (of -inf there is no remainder)
+                acc = f2add(acc, f2fma(x2, f2(y0 > -200.f ? r0 : 0.f, y1 > -200.f ? r1 : 0.f), x2));
+            } else {
+                acc = f2add(acc, f2_mass(p[e], m2, c2));
+            }
         }
         float s0, s1;
         f2split(acc, s0, s1);
         return s0 + s1;
     }
-    // One vector: its tokens from `lo` on are listed, the others' masses relative to `ref`
-    // added up.
-    template <bool TAIL>
-    __device__ __forceinline__ void list_vec(const uint4& q, int j, float lo, float ref, Sum& sum,
-                                             bool& below) {
-        uint4 rest = q;
-        if (vec_max<T>(q) >= lo) {
-            const uint4 in = mask_from<T>(q, lo);
+    // One vector, its largest element `top`: its tokens from `lo` on are listed, the others'
+    // masses relative to `ref` added up, and the largest of them kept.
+    template <bool TAIL, bool FINE>
+    __device__ __forceinline__ void list_vec(const uint4& q, float top, int j, float lo, float ref,
+                                             Sum& sum, float& under) {
+        if (top >= lo) {
+            const uint4 in = mask_from<T>(q, lo), rest = cleared<T>(q, in);
             for (uint32_t h = bits_of<T>(in); h; h &= h - 1) {
                 const int e = __ffs(h) - 1;
                 list(element<T>(q, e), id_of(j) + e);
             }
-            rest = cleared<T>(q, in);
+            under = fmaxf(under, vec_max<T>(rest));
+            if (TAIL) sum.add(approx_sum<FINE>(rest, ref));
+            return;
         }
-        below |= vec_max<T>(rest) > -INFINITY;
-        if (TAIL) sum.add(approx_sum(rest, ref));
+        under = fmaxf(under, top);
+        if (TAIL) sum.add(approx_sum<FINE>(q, ref));
+    }
+    // How far an approximate sum may be off (and 2^-28 of the first token, for terms of
+    // large exponents).
+    __device__ __forceinline__ uint64_t tail_slack(uint64_t tail, int bits) const {
+        return (tail >> bits) + (1ull << (62 - sc.shift) >> 28) + 1;
     }
     __device__ __forceinline__ uint64_t fixed_of(float v) const {
         return __float2ull_rn(v * ldexpf(1.f, 62 - sc.shift));
@@ -411,29 +423,32 @@ template <typename T, int U> struct Sampler {
     template <bool TAIL> __device__ __forceinline__ Found collect(float hi, float lo, bool exact) {
         if (tid == 0) s.count = 0;
         __syncthreads();
-        Found f{0, 0, 0, false};
+        Found f{0, 0, 0, 0, false};
         Sum sum;
         uint64_t above = 0;
+        float under = -INFINITY;
         const bool over = hi < INFINITY;
         each(
             [&](const uint4& q, int j) {
                 uint4 left = q;
-                if (over && vec_max<T>(q) >= hi) {
+                float top = vec_max<T>(q);
+                if (over && top >= hi) {
                     const uint4 in = mask_from<T>(q, hi);
                     const uint32_t b = bits_of<T>(in);
                     f.n_above += __popc(b);
                     for (uint32_t h = b; h; h &= h - 1) above += mass_of(element<T>(q, __ffs(h) - 1));
                     left = cleared<T>(q, in);
+                    top = vec_max<T>(left);
                 }
                 if (TAIL && exact) {
-                    list_vec<false>(left, j, lo, m, sum, f.below);
+                    list_vec<false, false>(left, top, j, lo, m, sum, under);
                     const uint4 rest = cleared<T>(left, mask_from<T>(left, lo));
                     float v[PV];
                     unpack<T>(rest, v);
 #pragma unroll
                     for (int e = 0; e < PV; ++e) f.tail += mass_of(v[e]);
                 } else {
-                    list_vec<TAIL>(left, j, lo, m, sum, f.below);
+                    list_vec<TAIL, true>(left, top, j, lo, m, sum, under);
                 }
             },
             [&](int region) {
@@ -444,10 +459,11 @@ template <typename T, int U> struct Sampler {
                 above = 0;
             });
         if (TAIL && !exact) f.tail = fixed_of(sum.hi + sum.lo);
-        f.below = __syncthreads_or(f.below);
+        f.below = __syncthreads_or(under > -INFINITY);
         f.above = over ? block_sum(f.above) : 0;
         f.n_above = over ? (int)block_sum((uint64_t)f.n_above) : 0;
         f.tail = TAIL ? block_sum(f.tail) : 0;
+        f.slack = TAIL && !exact ? tail_slack(f.tail, 19) : 0;
         return f;
     }
     __device__ __forceinline__ int bin_of(float v, float per) const {
@@ -487,11 +503,10 @@ template <typename T, int U> struct Sampler {
     }
 
     // From the list of n: every filter's place, the kept tokens and, where they are all
-    // listed, the draw.  By G threads, Q entries each.  f: what is before and behind the list (`open`: its tail is known
-    // to 2^-19 only); `floor`: no token behind it has `least`; `known`: the mass of the
+    // listed, the draw.  By G threads, Q entries each.  f: what is before and behind the list; `floor`: no token behind it has `least`; `known`: the mass of the
     // first top_k, whose place is not looked for again.
     template <int G, int Q>
-    __device__ __forceinline__ void decide(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
+    __device__ __forceinline__ void decide(int n, const Found& f, bool floor, uint64_t known, int top_k,
                            float top_p, uint64_t least, bool draw, float u) {
         if (Q > 1 && G > 32) sort<G, uint64_t, true>(s.list, n);  // (else it is sorted)
         // masses and their prefix sums, Q entries a thread
@@ -514,7 +529,7 @@ template <typename T, int U> struct Sampler {
         const int pos_m = least == 0 || (big_n == n && f.below && !floor) ? kNone : f.n_above + big_n;
         int kept = min(pos_k, pos_m), what = kDone;
         // (known: those behind the first top_k are not kept; here they are behind the place)
-        if (pos_k <= f.n_above || (least != 0 && big_n == 0 && f.n_above > 0)) {
+        if (pos_k <= f.n_above || (least != 0 && big_n == 0 && f.n_above > 0 && !floor)) {
             what = kSearch;  // a place is among those above
         } else if (top_p < 1.f) {
             uint64_t w0, w1;  // the mass that top_p is a share of, at least and at most
@@ -533,9 +548,8 @@ template <typename T, int U> struct Sampler {
                 w0 = w1 = s.value;
                 if (tid == 0) s.dec.all = w0, s.dec.listed = 0;
             } else {
-                const uint64_t slack = open ? tail_slack(f.tail) : 0;
-                w0 = listed + (f.tail > slack ? f.tail - slack : 0);
-                w1 = listed + f.tail + slack;
+                w0 = listed + (f.tail > f.slack ? f.tail - f.slack : 0);
+                w1 = listed + f.tail + f.slack;
             }
             const uint64_t g0 = max(share_of(w0, top_p, true), (uint64_t)1);
             const uint64_t g1 = max(share_of(w1, top_p, true), (uint64_t)1);
@@ -604,9 +618,9 @@ template <typename T, int U> struct Sampler {
                 sync<G>();
             }
             if (tid == 0) {
-                const uint64_t entry = s.list[here - 1];
-                s.dec.cut = of_key((uint32_t)(entry >> 32));
-                s.dec.limit = (int)~(uint32_t)entry;
+                const uint64_t entry = here ? s.list[here - 1] : 0;
+                s.dec.cut = here ? of_key((uint32_t)(entry >> 32)) : above_from;
+                s.dec.limit = here ? (int)~(uint32_t)entry : INT_MAX;
                 s.dec.kept = kept;
                 s.dec.all = all;
                 s.dec.token = draw && f.n_above == 0 ? (int)(s.order[s.token] >> kPlaceBits) : -1;
@@ -624,19 +638,21 @@ template <typename T, int U> struct Sampler {
     }
     // The same by as few threads as the list needs (what the others would do takes issue
     // slots from the SM's other block).
-    __device__ __forceinline__ void decide_by(int n, const Found& f, bool open, bool floor, uint64_t known, int top_k,
+    __device__ __forceinline__ void decide_by(int n, const Found& f, bool floor, uint64_t known, int top_k,
                               float top_p, uint64_t least, bool draw, float u) {
         __syncthreads();
         if (n <= kSampleThreads / 2) sort_by_rank(n);
         else if (n <= kSampleThreads) sort<kSampleThreads, uint64_t, true>(s.list, n);
         if (n <= 32) {
-            if (warp == 0) decide<32, 1>(n, f, open, floor, known, top_k, top_p, least, draw, u);
+            if (warp == 0) decide<32, 1>(n, f, floor, known, top_k, top_p, least, draw, u);
         } else if (n <= 128) {
-            if (warp < 4) decide<128, 1>(n, f, open, floor, known, top_k, top_p, least, draw, u);
+            if (warp < 4) decide<128, 1>(n, f, floor, known, top_k, top_p, least, draw, u);
         } else if (n <= kSampleThreads) {
-            decide<kSampleThreads, 1>(n, f, open, floor, known, top_k, top_p, least, draw, u);
+            decide<kSampleThreads, 1>(n, f, floor, known, top_k, top_p, least, draw, u);
+        } else if (n <= 2 * kSampleThreads) {
+            decide<kSampleThreads, 2>(n, f, floor, known, top_k, top_p, least, draw, u);
         } else {
-            decide<kSampleThreads, kList / kSampleThreads>(n, f, open, floor, known, top_k, top_p, least,
+            decide<kSampleThreads, kList / kSampleThreads>(n, f, floor, known, top_k, top_p, least,
                                                            draw, u);
         }
         __syncthreads();
@@ -692,18 +708,11 @@ template <typename T, int U> struct Sampler {
 #pragma unroll 1
         for (int i = tid; i < n; i += kSampleThreads) w += mass_of(of_key((uint32_t)(s.list[i] >> 32)));
         w = block_sum(w);
-        const uint64_t slack = tail_slack(f.tail);
-        if (w >= share_of(w + (f.tail > slack ? f.tail - slack : 0), top_p, true)) return false;
+        if (w >= share_of(w + (f.tail > f.slack ? f.tail - f.slack : 0), top_p, true)) return false;
         if (tid == 0) s.dec.all = w + f.tail, s.dec.listed = w;
         __syncthreads();
         return true;
     }
-    // How far an approximate sum may be off (and 2^-28 of the first token, for terms of
-    // large exponents).
-    __device__ __forceinline__ uint64_t tail_slack(uint64_t tail) const {
-        return (tail >> 19) + (1ull << (62 - sc.shift) >> 28) + 1;
-    }
-
     // Decides by a list of the tokens from `lo` on, behind those from `hi` on, with the
     // rest's mass made exact where that is needed.  (f: of a list that is there; else it is
     // made.)
@@ -716,11 +725,12 @@ template <typename T, int U> struct Sampler {
                             : tail         ? collect<true>(hi, lo, exact)
                                            : collect<false>(hi, lo, false);
             int n = s.count;
-            if (n > kList || n == 0) return kOverflow;
+            above_from = hi;
+            if (n > kList || (n == 0 && !(floor && f.n_above > 0))) return kOverflow;
             Found g = f;
             if (made && top_k > 0 && n > top_k && n > 64 && n <= kSampleThreads) n = prune(n, top_k, g);
             if (made && tail && n > kSampleThreads / 4 && least == 0 && past(n, f, top_p)) return kBracket;
-            decide_by(n, g, tail && !exact, floor, known, top_k, top_p, least, draw, u);
+            decide_by(n, g, floor, known, top_k, top_p, least, draw, u);
             if (s.dec.what != kExactTail) return s.dec.what;
         }
     }
@@ -1063,7 +1073,8 @@ template <typename T, int U> struct Sampler {
         });
     }
 
-    __device__ __forceinline__ void row(int64_t r, const T* next) {
+    // Row r; the first thread has the next one's number, all get it back.
+    __device__ __forceinline__ int row(int64_t r, int ticket, const T* logits) {
         const vsd_policy& p = a.policy;
         T_ = p.row_T ? p.row_T[r] : p.T;
         float top_p = p.row_top_p ? p.row_top_p[r] : p.top_p;
@@ -1087,24 +1098,28 @@ template <typename T, int U> struct Sampler {
         const float span = least != 0 && least < one ? -T_ * logf(min_p) : 0.f;
         auto rounding = [&](float top) { return (span + fabsf(top) + T_) * 1e-5f; };
 
+        constexpr int kRound = kSampleWarps * 32 * kLoad;
         // one pass: the maximum, the list and the rest's mass.  After the first round of
         // vectors a bound `lo` that `want` of the lanes' maxima reach, and a reference for
         // the masses: the maximum so far.
-        const int want = top_k > 0 ? top_k : kWant;
+        // (for a long row's k a share of it and some more; were they too few, a histogram
+        // finds the place)
+        const int rounds = (nvec + kRound - 1) / kRound;
+        const int want = top_k <= 0 ? kWant : rounds == 1 ? top_k : min(top_k, (3 * min(top_k, 1 << 16)) / (2 * rounds) + 24);
         float mx = -INFINITY, lo = lowest_of<T>(), ref = 0.f;
+        float under = -INFINITY;
         bool floor = false;
-        Found f{0, 0, 0, false};
+        Found f{0, 0, 0, 0, false};
         Sum sum;
         if (tid == 0) s.count = 0;
-        constexpr int kRound = kSampleWarps * 32 * kLoad;
         for (int j1 = 0; j1 < nvec; j1 += kRound) {
             const int j0 = j1 + warp * (32 * kLoad) + lane;
             uint4 q[kLoad];
             load(j0, q);
+            if (j1 == 0 || !filters) {
 #pragma unroll
-            for (int i = 0; i < kLoad; ++i) mx = max_nan(mx, vec_max_nan<T>(q[i]));
-            if (!filters) continue;
-            if (j1 == 0) {
+                for (int i = 0; i < kLoad; ++i) mx = max_nan(mx, vec_max_nan<T>(q[i]));
+                if (!filters) continue;
                 const uint32_t key = key_of(mx), high = key >> 16;
                 const uint32_t w = __reduce_max_sync(0xffffffffu, key);
                 if (lane == 0) s.part[warp] = w;
@@ -1123,19 +1138,23 @@ template <typename T, int U> struct Sampler {
                 lo = lo_key <= (kKeyNone | 0xFFFFu) ? lowest_of<T>() : of_key(lo_key);
                 if (least != 0 && top_p >= 1.f) {
                     // no token below max + T ln(min_p) is kept, and the maximum may grow
-                    const float under = ref - span - rounding(ref);
-                    floor = top_k <= 0 || under > lo;
-                    if (floor) lo = down_to<T>(under);
+                    const float bound = ref - span - rounding(ref);
+                    floor = top_k <= 0 || bound > lo;
+                    if (floor) lo = down_to<T>(bound);
                 }
             }
 #pragma unroll
             for (int i = 0; i < kLoad; ++i) {
-                if (tail) list_vec<true>(q[i], j0 + 32 * i, lo, ref, sum, f.below);
-                else list_vec<false>(q[i], j0 + 32 * i, lo, ref, sum, f.below);
+                const float most = vec_max_nan<T>(q[i]);
+                mx = max_nan(mx, most);
+                if (tail) list_vec<true, false>(q[i], most, j0 + 32 * i, lo, ref, sum, under);
+                else list_vec<false, false>(q[i], most, j0 + 32 * i, lo, ref, sum, under);
             }
         }
-        if (next) bring(next);  // (while this row is decided)
+        if (tid == 0) s.next = ticket;
         const bool bad = __syncthreads_or(!(mx < INFINITY));
+        const int next = s.next;
+        if (next < a.R) bring(logits + (int64_t)next * a.V);  // (while this row is decided)
         const uint32_t w = __reduce_max_sync(0xffffffffu, key_of(mx));
         if (lane == 0) s.part[warp] = w;
         __syncthreads();
@@ -1151,7 +1170,7 @@ template <typename T, int U> struct Sampler {
                 if (a.out.kept) a.out.kept[r] = 0;
             }
             if (a.out.filtered) write_filtered(r, true);
-            return;
+            return next;
         }
         m = of_key(top);
         if (tid == 0) s.dec.token = -1, s.dec.cut = -FLT_MAX, s.dec.limit = INT_MAX;
@@ -1165,8 +1184,9 @@ template <typename T, int U> struct Sampler {
                 f.tail = fixed_of(t);
                 made = !__syncthreads_or(!(t < 2e6f) || !(sum.hi < 1e30f) || !(ref > -INFINITY));
                 f.tail = block_sum(f.tail);
+                f.slack = tail_slack(f.tail, 17);
             }
-            f.below = __syncthreads_or(f.below);
+            f.below = __syncthreads_or(under > -INFINITY);
             // a list from `low` on behind what is from `high` on, until one decides: the
             // first; where a long top-k or min_p overflows it, one around its place; for a
             // nucleus past it one around its place by a sample, then by all of the row
@@ -1180,12 +1200,12 @@ template <typename T, int U> struct Sampler {
                                     draw, u);
                 if (what == kDone || step == 4) break;
                 float per = 0.f;
-                if (step == 0 && what == kOverflow && !tail) {
+                if (step == 0 && !tail && (what == kOverflow || (what == kSearch && top_k > 0 && !floor))) {
                     step = 1;
                     high = up_to<T>(m - span + rounding(m));
                     low = down_to<T>(m - span - rounding(m));
                     if (floor) continue;
-                    per = ((float)kBins - 0.1f) / (m - lo);
+                    per = ((float)kBins - 0.1f) / ((m - lo) * (what == kOverflow ? 1.f : 3.f));
                     base = m;
                     if (!(per > 0.f && per < INFINITY)) break;
                     histogram<true>(per, 0.f, false, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
@@ -1239,6 +1259,7 @@ template <typename T, int U> struct Sampler {
         }
         if (tid == 0 && a.out.kept) a.out.kept[r] = s.dec.kept;
         if (a.out.filtered) write_filtered(r, false);
+        return next;
     }
 };
 
@@ -1250,10 +1271,15 @@ __global__ void __launch_bounds__(kSampleThreads, 2) k_sample(const T* logits, c
     S w(a, s);
     w.bring(logits + (int64_t)blockIdx.x * a.V);
     for (int j = threadIdx.x; j < kExpTab; j += kSampleThreads) s.tab[j] = exp_entry(kExpParts, j);
-    for (int64_t r = blockIdx.x; r < a.R; r += gridDim.x) {
+    // rows as blocks come to them: they take unlike times (4096 x 128256 by top_p, dealt
+    // round instead: 5 % more)
+    for (int64_t r = blockIdx.x; r < a.R;) {
         __syncthreads();
         w.open(logits + r * a.V);
-        w.row(r, r + gridDim.x < a.R ? logits + (r + gridDim.x) * a.V : nullptr);
+        // (asked for here, looked at when the row has been read)
+        int next = a.R;
+        if (threadIdx.x == 0 && a.R > gridDim.x) next = (int)gridDim.x + atomicAdd(a.status + 1, 1);
+        r = w.row(r, next, logits);
     }
 }
 
