@@ -85,7 +85,8 @@ def _code_only(text):
 # here runs their kernels.
 LOSS_SOURCES = ("vsd_lmloss.cu", "vsd_loss.h", "vsd_pair.cuh", "vsd_rowloss.cuh",
                 "vsd_target.cuh", "vsd_topk.cu", "vsd_dep.cuh", "vsd_fixed.cuh", "vsd_fp8.cu",
-                "vsd_sample.cu")
+                "vsd_sample.cu", "vsd_sample.cuh", "vsd_sample.h", "vsd_sample_f32.cu",
+                "vsd_sample_bf16.cu")
 
 
 def kernel_source_hash():

@@ -17,7 +17,7 @@ OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libvsd.so")
 SOURCES = ["vsd_api.cu", "vsd_kernels_f32.cu", "vsd_kernels_bf16.cu", "vsd_noalloc.cu",
            "vsd_lmhead.cu", "vsd_lmhead_bwd.cu", "vsd_lmloss.cu", "vsd_topk.cu",
-           "vsd_fp8.cu", "vsd_sample.cu"]
+           "vsd_fp8.cu", "vsd_sample.cu", "vsd_sample_f32.cu", "vsd_sample_bf16.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-I" + INCLUDE, "-I" + CSRC]
 
