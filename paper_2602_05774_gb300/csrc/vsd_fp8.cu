@@ -20,37 +20,139 @@ namespace {
 
 constexpr int kBlock = 128;  // columns of a scale
 
-__device__ __forceinline__ float f32_of(float x) { return x; }
-__device__ __forceinline__ float f32_of(__nv_bfloat16 x) { return __bfloat162float(x); }
+// ------------------------------------------------------------ quantizing
+// s = 2^ceil(log2(amax / 448)), q = x / s, an exact product with 2^-log2(s) rounded once.
+// Bound by memory: one read, one write of half or a quarter of it.
 
-// The least power of two s with amax / s <= 448 = 1.75 2^8.
-__device__ __forceinline__ float scale_of(float amax) {
-    if (!(amax < INFINITY)) return NAN;
-    if (amax == 0.f) return 1.f;
-    const uint32_t b = __float_as_uint(amax);
-    int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7FFFFFu) > 0x600000u);
-    return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
+// The least power of two s with amax / s <= 448 = 1.75 2^8, and its reciprocal; amax by
+// its bits (NaN is above infinity).
+__device__ __forceinline__ float scale_of(uint32_t amax, float& inv) {
+    if (amax >= 0x7F800000u) return inv = NAN;
+    if (amax == 0) return inv = 1.f;
+    const int e = max((int)(amax >> 23) - 127 - 8 + ((amax & 0x7FFFFFu) > 0x600000u), -126);
+    inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    return __uint_as_float((uint32_t)(127 + e) << 23);
+}
+// The largest magnitude of a vector, by its bits.
+template <typename T> __device__ __forceinline__ uint32_t vec_amax(const uint4& q);
+template <> __device__ __forceinline__ uint32_t vec_amax<float>(const uint4& q) {
+    constexpr uint32_t m = 0x7FFFFFFFu;
+    return max(max(q.x & m, q.y & m), max(q.z & m, q.w & m));
+}
+template <> __device__ __forceinline__ uint32_t vec_amax<__nv_bfloat16>(const uint4& q) {
+    constexpr uint32_t m = 0x7FFF0000u;
+    const uint32_t hi = max(max(q.x & m, q.y & m), max(q.z & m, q.w & m));
+    const uint32_t lo = max(max(q.x << 16 & m, q.y << 16 & m), max(q.z << 16 & m, q.w << 16 & m));
+    return max(hi, lo);
+}
+__device__ __forceinline__ uint32_t e4m3x4(float a, float b, float c, float d) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+    return lo | hi << 16;
+}
+// A vector of x to 4 or 8 bytes of q.
+__device__ __forceinline__ void put_vec(__nv_fp8_e4m3* q, const uint4& v, float inv, float) {
+    float f[4];
+    unpack<float>(v, f);
+    *reinterpret_cast<uint32_t*>(q) = e4m3x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+}
+__device__ __forceinline__ void put_vec(__nv_fp8_e4m3* q, const uint4& v, float inv, __nv_bfloat16) {
+    float f[8];
+    unpack<__nv_bfloat16>(v, f);
+    *reinterpret_cast<uint2*>(q) = make_uint2(e4m3x4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv),
+                                              e4m3x4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv));
+}
+
+constexpr int kQuantThreads = 256;
+
+// A scale for each row and 128 columns: kGroup lanes hold a block, kMany blocks each.
+template <typename T>
+__global__ void __launch_bounds__(kQuantThreads)
+    k_quantize_rows(const T* x, int64_t R, int H, __nv_fp8_e4m3* q, float* scale) {
+    constexpr int PV = Traits<T>::kPerVec, kGroup = kBlock / PV, kMany = 4;
+    const int nk = (H + kBlock - 1) / kBlock, lane = threadIdx.x % kGroup;
+    const int64_t units = R * nk, groups = (int64_t)gridDim.x * (kQuantThreads / kGroup);
+    // (whole warps go round together: w is the unit of a warp's first group)
+    const int sub = threadIdx.x % 32 / kGroup;
+    for (int64_t w = (int64_t)blockIdx.x * (kQuantThreads / kGroup) + threadIdx.x / kGroup - sub; w < units;
+         w += groups * kMany) {
+        const int64_t u0 = w + sub;
+        uint4 v[kMany];
+        int64_t at[kMany];
+#pragma unroll
+        for (int i = 0; i < kMany; ++i) {
+            const int64_t u = u0 + i * groups, r = u / nk;
+            const int col = (int)(u - r * nk) * kBlock + lane * PV;
+            at[i] = u < units && col < H ? r * H + col : -1;
+            v[i] = at[i] >= 0 ? *reinterpret_cast<const uint4*>(x + at[i]) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < kMany; ++i) {
+            uint32_t m = vec_amax<T>(v[i]);
+            // (a group is a warp or half of one; all its lanes come here)
+#pragma unroll
+            for (int o = kGroup / 2; o; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+            float inv;
+            const float s = scale_of(m, inv);
+            const int64_t u = u0 + i * groups;
+            if (at[i] >= 0) put_vec(q + at[i], v[i], inv, T());
+            if (lane == 0 && u < units) scale[u] = s;
+        }
+    }
+}
+
+// A scale for 128 x 128: a block of threads holds it in registers.
+template <typename T>
+__global__ void __launch_bounds__(kQuantThreads, 3)
+    k_quantize_blocks(const T* x, int64_t R, int H, __nv_fp8_e4m3* q, float* scale) {
+    constexpr int PV = Traits<T>::kPerVec, kGroup = kBlock / PV;        // lanes of a row
+    constexpr int kStep = kQuantThreads / kGroup, kMany = kBlock / kStep;  // rows at a time
+    __shared__ uint32_t part[kQuantThreads / 32];
+    const int64_t r0 = (int64_t)blockIdx.y * kBlock + threadIdx.x / kGroup;
+    const int col = blockIdx.x * kBlock + threadIdx.x % kGroup * PV;
+    uint4 v[kMany];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < kMany; ++i) {
+        const int64_t r = r0 + i * kStep;
+        v[i] = r < R && col < H ? *reinterpret_cast<const uint4*>(x + r * H + col) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < kMany; ++i) m = max(m, vec_amax<T>(v[i]));
+    m = __reduce_max_sync(0xffffffffu, m);
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kQuantThreads / 32; ++i) m = max(m, part[i]);
+    float inv;
+    const float s = scale_of(m, inv);
+    if (threadIdx.x == 0) scale[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
+#pragma unroll
+    for (int i = 0; i < kMany; ++i) {
+        const int64_t r = r0 + i * kStep;
+        if (r < R && col < H) put_vec(q + r * H + col, v[i], inv, T());
+    }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256)
-    k_quantize(const T* x, int R, int H, int rows, __nv_fp8_e4m3* q, float* scale) {
-    __shared__ uint32_t amax;
-    const int64_t r0 = (int64_t)blockIdx.y * rows;
-    const int h0 = blockIdx.x * kBlock, nr = (int)min((int64_t)rows, R - r0), nh = min(kBlock, H - h0);
-    if (threadIdx.x == 0) amax = 0;
-    __syncthreads();
-    uint32_t m = 0;
-    for (int i = threadIdx.x; i < nr * nh; i += blockDim.x)
-        m = max(m, __float_as_uint(f32_of(x[(r0 + i / nh) * H + h0 + i % nh])) & 0x7FFFFFFFu);
-    atomicMax(&amax, m);
-    __syncthreads();
-    const float s = scale_of(__uint_as_float(amax));
-    if (threadIdx.x == 0) scale[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
-    for (int i = threadIdx.x; i < nr * nh; i += blockDim.x) {
-        const int64_t at = (r0 + i / nh) * H + h0 + i % nh;
-        q[at] = __nv_fp8_e4m3(f32_of(x[at]) / s);
+cudaError_t quantize(const T* x, int R, int H, int block_rows, __nv_fp8_e4m3* q, float* scale,
+                     cudaStream_t st) {
+    const int nk = (H + kBlock - 1) / kBlock;
+    if (block_rows == 1) {
+        constexpr int kPer = 4 * kQuantThreads * Traits<T>::kPerVec / kBlock;  // a block's at a time
+        const int64_t blocks = ((int64_t)R * nk + kPer - 1) / kPer;
+        k_quantize_rows<T><<<(int)std::min<int64_t>(blocks, 16 * device_sm_count()), kQuantThreads, 0, st>>>(
+            x, R, H, q, scale);
+        return cudaGetLastError();
     }
+    // (a grid's second dimension ends at 65535)
+    constexpr int kMost = 65535;
+    for (int64_t b = 0; b * kBlock < R; b += kMost) {
+        const int64_t rows = std::min<int64_t>(R - b * kBlock, (int64_t)kMost * kBlock);
+        k_quantize_blocks<T><<<dim3(nk, (int)((rows + kBlock - 1) / kBlock)), kQuantThreads, 0, st>>>(
+            x + b * kBlock * H, rows, H, q + b * kBlock * H, scale + b * nk);
+    }
+    return cudaGetLastError();
 }
 
 // ------------------------------------------------------------ the head
@@ -616,13 +718,12 @@ vsd_status vsd_quantize_fp8(const void* x, vsd_dtype dtype, int32_t R, int32_t H
     if (share_bytes(x, xb, q, n) || share_bytes(x, xb, scale, sb) || share_bytes(q, n, scale, sb))
         return VSD_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const dim3 grid(nh, nr);
     __nv_fp8_e4m3* out = static_cast<__nv_fp8_e4m3*>(q);
-    if (dtype == VSD_BF16)
-        k_quantize<<<grid, 256, 0, st>>>(static_cast<const __nv_bfloat16*>(x), R, H, block_rows, out, scale);
-    else
-        k_quantize<<<grid, 256, 0, st>>>(static_cast<const float*>(x), R, H, block_rows, out, scale);
-    return cudaGetLastError() == cudaSuccess ? VSD_OK : VSD_ERR_CUDA;
+    const cudaError_t e =
+        dtype == VSD_BF16
+            ? quantize(static_cast<const __nv_bfloat16*>(x), R, H, block_rows, out, scale, st)
+            : quantize(static_cast<const float*>(x), R, H, block_rows, out, scale, st);
+    return e == cudaSuccess ? VSD_OK : VSD_ERR_CUDA;
 }
 
 vsd_status vsd_lmhead_logits_fp8(const void* hidden, const float* hidden_scale,

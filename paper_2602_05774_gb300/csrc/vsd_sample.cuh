@@ -441,7 +441,7 @@ template <typename T> struct Sampler {
                 if (TAIL && exact) {
                     list_vec<false, false>(left, top, j, lo, m, sum, under);
                     const uint4 rest = cleared<T>(left, mask_from<T>(left, lo));
-#pragma unroll 1
+#pragma unroll 4
                     for (int e = 0; e < PV; ++e) f.tail += mass_of(element<T>(rest, e));
                 } else {
                     list_vec<TAIL, true>(left, top, j, lo, m, sum, under);
@@ -1008,13 +1008,14 @@ template <typename T> struct Sampler {
         int n = 0;
         each(
             [&](const uint4& q, int j) {
-#pragma unroll 2
-                for (int e = 0; e < PV; ++e) {
-                    const float v = element<T>(q, e);
-                    if (!is_kept(v, id_of(j) + e)) continue;
-                    ++n;
-                    if (draw) w += mass_of(v);
-                }
+                float v[PV];
+                unpack<T>(q, v);
+#pragma unroll
+                for (int e = 0; e < PV; ++e) n += is_kept(v[e], id_of(j) + e);
+                if (!draw) return;
+#pragma unroll
+                for (int e = 0; e < PV; ++e)
+                    if (is_kept(v[e], id_of(j) + e)) w += mass_of(v[e]);
             },
             [&](int region) {
                 if (!draw) return;

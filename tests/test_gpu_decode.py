@@ -120,6 +120,19 @@ def test_quantize_spreads_what_is_not_finite(vsd, rows, dtype):
     assert torch.equal(s[~bad], clean[1][~bad])
 
 
+@pytest.mark.parametrize("shape,rows", [((70001, 144), 1), ((8388608 + 200, 16), 128), ((140000, 16400), 1)])
+def test_quantize_many_rows(vsd, shape, rows):
+    """More blocks than a grid's second dimension, and more than 2^31 elements."""
+    x = torch.randn(shape[0], shape[1], generator=gen(5), device="cuda", dtype=torch.bfloat16)
+    q, s = vsd.quantize_fp8(x, block_rows=rows)
+    for lo in (0, shape[0] // 256 * 128, (shape[0] - 140) // 128 * 128):
+        part = slice(lo, min(lo + 140, shape[0]))
+        rq, rs = plain_quantize(x[part].float().cpu(), rows)
+        n = rs.shape[0] - (1 if part.stop < shape[0] and rows > 1 else 0)  # (whole blocks)
+        assert torch.equal(s[lo // rows:lo // rows + n].cpu(), rs[:n])
+        assert torch.equal(q[part].float().cpu()[:n * rows], rq[:n * rows])
+
+
 def test_quantize_into_given_tensors(vsd):
     x = torch.randn(129, 144, generator=gen(4), device="cuda")
     q0, s0 = vsd.quantize_fp8(x, block_rows=128)
