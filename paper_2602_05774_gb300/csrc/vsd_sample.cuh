@@ -188,12 +188,6 @@ struct Decision {
 };
 
 
-__device__ __forceinline__ uint64_t f2fma(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-
 // 128 bits of a logits row (which may be written later, by this block alone).
 __device__ __forceinline__ uint4 ld_row(const void* p) {
     uint4 r;
@@ -208,6 +202,8 @@ template <typename T> struct Sampler {
     static constexpr int PV = Traits<T>::kPerVec;
     static constexpr int NT = kSampleThreads, kWarps = NT / 32;
     static constexpr int kLoad = 4;  // vectors of a lane in flight
+    static constexpr int kQueue = 32 + 32 * PV;  // tokens of a warp that wait for their masses
+    static_assert(kWarps * kQueue * sizeof(float) <= kList * sizeof(uint64_t), "in the masses' place");
 
     struct Shared {
         uint64_t tab[kExpTab];
@@ -360,39 +356,24 @@ template <typename T> struct Sampler {
         const int at = atomicAdd(&s.count, 1);
         if (at < kList) s.list[at] = (uint64_t)key_of(v) << 32 | (uint32_t)~id;
     }
-    // The sum of a vector's masses relative to `ref`, where exponents are 40 at most off by
-    // 2^-17 of itself at most: ex2's 2^-22, and what v - ref, c and their product are
-    // rounded by.  FINE: by 2^-19, the product with c in two floats.  (The first pass over a
-    // row does without, as it would take half as long again; behind a bracket it spares
-    // four of five exact sums.)
-    template <bool FINE>
+    // The sum of a vector's masses relative to `ref`, off by 2^-17 of itself at most, where
+    // exponents are 40 at most: ex2's 2^-22, and what v - ref, c and their product are
+    // rounded by.  (A product in two floats is off by 2^-19, takes twice the instructions,
+    // and spares but one nucleus in twenty its exact sum.)
     __device__ __forceinline__ float approx_sum(const uint4& q, float ref) const {
         uint64_t p[PV / 2];
         vec_pairs<T>(q, p);
         const uint64_t m2 = f2(ref, ref), c2 = f2(c, c);
-        uint64_t acc = f2(0.f, 0.f);
+        uint64_t acc = f2_mass(p[0], m2, c2);
 #pragma unroll
-        for (int e = 0; e < PV / 2; ++e) {
-            if (FINE) {
-                const uint64_t d = f2sub(p[e], m2), y = f2mul(d, c2);
-                float y0, y1, r0, r1;
-                f2split(y, y0, y1);
-                f2split(f2mul(f2fma(d, f2(sc.c_lo, sc.c_lo), f2fma(d, c2, f2(-y0, -y1))),
-                              f2(0.6931472f, 0.6931472f)), r0, r1);
-                const uint64_t x2 = f2(ex2(y0), ex2(y1));
-                // (of -inf there is no remainder)
-                acc = f2add(acc, f2fma(x2, f2(y0 > -200.f ? r0 : 0.f, y1 > -200.f ? r1 : 0.f), x2));
-            } else {
-                acc = f2add(acc, f2_mass(p[e], m2, c2));
-            }
-        }
+        for (int e = 1; e < PV / 2; ++e) acc = f2add(acc, f2_mass(p[e], m2, c2));
         float s0, s1;
         f2split(acc, s0, s1);
         return s0 + s1;
     }
     // One vector, its largest element `top`: its tokens from `lo` on are listed, the others'
     // masses relative to `ref` added up, and the largest of them kept.
-    template <bool TAIL, bool FINE>
+    template <bool TAIL>
     __device__ __forceinline__ void list_vec(const uint4& q, float top, int j, float lo, float ref,
                                              Sum& sum, float& under) {
         if (top >= lo) {
@@ -402,16 +383,16 @@ template <typename T> struct Sampler {
                 list(element<T>(q, e), id_of(j) + e);
             }
             under = fmaxf(under, vec_max<T>(rest));
-            if (TAIL) sum.add(approx_sum<FINE>(rest, ref));
+            if (TAIL) sum.add(approx_sum(rest, ref));
             return;
         }
         under = fmaxf(under, top);
-        if (TAIL) sum.add(approx_sum<FINE>(q, ref));
+        if (TAIL) sum.add(approx_sum(q, ref));
     }
     // How far an approximate sum may be off (and 2^-28 of the first token, for terms of
     // large exponents).
-    __device__ __forceinline__ uint64_t tail_slack(uint64_t tail, int bits) const {
-        return (tail >> bits) + (1ull << (62 - sc.shift) >> 28) + 1;
+    __device__ __forceinline__ uint64_t tail_slack(uint64_t tail) const {
+        return (tail >> 17) + (1ull << (62 - sc.shift) >> 28) + 1;
     }
     __device__ __forceinline__ uint64_t fixed_of(float v) const {
         return __float2ull_rn(v * ldexpf(1.f, 62 - sc.shift));
@@ -426,29 +407,49 @@ template <typename T> struct Sampler {
         uint64_t above = 0;
         float under = -INFINITY;
         const bool over = hi < INFINITY;
+        // Tokens above wait until a warp has 32, so that its lanes are all of use: 3 in 100
+        // tokens are above where a nucleus is wide.
+        float* const queue = reinterpret_cast<float*>(s.mass) + warp * kQueue;
+        int waiting = 0;
         each(
             [&](const uint4& q, int j) {
                 uint4 left = q;
                 float top = vec_max<T>(q);
-                if (over && top >= hi) {
+                if (over && __any_sync(0xffffffffu, top >= hi)) {
                     const uint4 in = mask_from<T>(q, hi);
                     const uint32_t b = bits_of<T>(in);
-                    f.n_above += __popc(b);
-                    for (uint32_t h = b; h; h &= h - 1) above += mass_of(element<T>(q, __ffs(h) - 1));
+                    const int mine = __popc(b);
+                    int at = mine;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const int v = __shfl_up_sync(0xffffffffu, at, o);
+                        if (lane >= o) at += v;
+                    }
+                    const int n = __shfl_sync(0xffffffffu, at, 31);
+                    at += waiting - mine;
+                    for (uint32_t h = b; h; h &= h - 1) queue[at++] = element<T>(q, __ffs(h) - 1);
+                    f.n_above += mine;
+                    waiting += n;
+                    __syncwarp();
+                    for (; waiting >= 32; waiting -= 32) above += mass_of(queue[waiting - 32 + lane]);
+                    __syncwarp();
                     left = cleared<T>(q, in);
                     top = vec_max<T>(left);
                 }
                 if (TAIL && exact) {
-                    list_vec<false, false>(left, top, j, lo, m, sum, under);
+                    list_vec<false>(left, top, j, lo, m, sum, under);
                     const uint4 rest = cleared<T>(left, mask_from<T>(left, lo));
 #pragma unroll 4
                     for (int e = 0; e < PV; ++e) f.tail += mass_of(element<T>(rest, e));
                 } else {
-                    list_vec<TAIL, true>(left, top, j, lo, m, sum, under);
+                    list_vec<TAIL>(left, top, j, lo, m, sum, under);
                 }
             },
             [&](int region) {
                 if (!over) return;
+                if (lane < waiting) above += mass_of(queue[lane]);
+                waiting = 0;
+                __syncwarp();
                 const uint64_t w = warp_sum_u64(above);
                 if (lane == 0) s.region[region] = w;
                 f.above += above;
@@ -459,7 +460,7 @@ template <typename T> struct Sampler {
         f.above = over ? block_sum(f.above) : 0;
         f.n_above = over ? (int)block_sum((uint64_t)f.n_above) : 0;
         f.tail = TAIL ? block_sum(f.tail) : 0;
-        f.slack = TAIL && !exact ? tail_slack(f.tail, 19) : 0;
+        f.slack = TAIL && !exact ? tail_slack(f.tail) : 0;
         return f;
     }
     __device__ __forceinline__ int bin_of(float v, float per) const {
@@ -643,6 +644,8 @@ template <typename T> struct Sampler {
             if (warp == 0) decide<32, 1>(n, f, floor, known, top_k, top_p, least, draw, u);
         } else if (n <= NT) {
             decide<NT, 1>(n, f, floor, known, top_k, top_p, least, draw, u);
+        } else if (n <= 2 * NT) {
+            decide<NT, 2>(n, f, floor, known, top_k, top_p, least, draw, u);
         } else {
             decide<NT, kList / NT>(n, f, floor, known, top_k, top_p, least, draw, u);
         }
@@ -1168,8 +1171,8 @@ template <typename T> struct Sampler {
             for (int i = 0; i < kLoad; ++i) {
                 const float most = vec_max_nan<T>(q[i]);
                 mx = max_nan(mx, most);
-                if (tail) list_vec<true, false>(q[i], most, j0 + NT * i, lo, ref, sum, under);
-                else list_vec<false, false>(q[i], most, j0 + NT * i, lo, ref, sum, under);
+                if (tail) list_vec<true>(q[i], most, j0 + NT * i, lo, ref, sum, under);
+                else list_vec<false>(q[i], most, j0 + NT * i, lo, ref, sum, under);
             }
         }
         if (tid == 0) s.next = ticket;
@@ -1205,7 +1208,7 @@ template <typename T> struct Sampler {
                 f.tail = fixed_of(t);
                 made = !__syncthreads_or(!(t < 2e6f) || !(sum.hi < 1e30f) || !(ref > -INFINITY));
                 f.tail = block_sum(f.tail);
-                f.slack = tail_slack(f.tail, 17);
+                f.slack = tail_slack(f.tail);
             }
             f.below = __syncthreads_or(under > -INFINITY);
             // a list from `low` on behind what is from `high` on, until one decides: the
