@@ -203,7 +203,10 @@ template <typename T> struct Sampler {
     static constexpr int NT = kSampleThreads, kWarps = NT / 32;
     static constexpr int kLoad = 4;  // vectors of a lane in flight
     static constexpr int kQueue = 32 + 32 * PV;  // tokens of a warp that wait for their masses
-    static_assert(kWarps * kQueue * sizeof(float) <= kList * sizeof(uint64_t), "in the masses' place");
+    static_assert(kWarps * kQueue * sizeof(float) <= kList * sizeof(uint64_t) &&
+                      kWarps * kQueue * sizeof(uint16_t) <= kList * sizeof(uint32_t) &&
+                      32 * kDeep * PV <= 65536,
+                  "in the masses' place, and the orders'");
 
     struct Shared {
         uint64_t tab[kExpTab];
@@ -399,6 +402,8 @@ template <typename T> struct Sampler {
     }
     // Tokens from `hi` on are above, those from `lo` on are listed.  Left is the mass
     // above, by region too; of the rest it is approximate, exact, or not summed at all.
+    // (Tokens from `lo` on wait in a warp's queue until there are 32, so that all its lanes
+    // are of use: a few in 100 tokens are above where a nucleus is wide.)
     template <bool TAIL> __device__ __forceinline__ Found collect(float hi, float lo, bool exact) {
         if (tid == 0) s.count = 0;
         __syncthreads();
@@ -406,59 +411,76 @@ template <typename T> struct Sampler {
         Sum sum;
         uint64_t above = 0;
         float under = -INFINITY;
-        const bool over = hi < INFINITY;
-        // Tokens above wait until a warp has 32, so that its lanes are all of use: 3 in 100
-        // tokens are above where a nucleus is wide.
-        float* const queue = reinterpret_cast<float*>(s.mass) + warp * kQueue;
+        float* const value = reinterpret_cast<float*>(s.mass) + warp * kQueue;
+        uint16_t* const place = reinterpret_cast<uint16_t*>(s.order) + warp * kQueue;
         int waiting = 0;
-        each(
-            [&](const uint4& q, int j) {
-                uint4 left = q;
-                float top = vec_max<T>(q);
-                if (over && __any_sync(0xffffffffu, top >= hi)) {
-                    const uint4 in = mask_from<T>(q, hi);
-                    const uint32_t b = bits_of<T>(in);
-                    const int mine = __popc(b);
-                    int at = mine;
+        // the last n that wait, of the region that begins at vector j0
+        auto drain = [&](int n, int j0) {
+            __syncwarp();
+            waiting -= n;
+            const bool on = lane < n;
+            const float v = on ? value[waiting + lane] : 0.f;
+            const int id = on ? id_of(j0) + place[waiting + lane] : 0;
+            const bool over = on && v >= hi, in = on && !over;
+            if (over) above += mass_of(v), ++f.n_above;
+            const uint32_t w = __ballot_sync(0xffffffffu, in);
+            if (w) {
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&s.count, __popc(w));
+                at = __shfl_sync(0xffffffffu, at, 0) + __popc(w & ((1u << lane) - 1));
+                if (in && at < kList) s.list[at] = (uint64_t)key_of(v) << 32 | (uint32_t)~id;
+            }
+            __syncwarp();
+        };
+        for (int j0 = warp * depth; j0 < nvec; j0 += kWarps * depth) {
+            const int stop = min(nvec, j0 + depth);
+#pragma unroll 1
+            for (int h = j0; h < stop; h += 32 * kLoad) {
+                uint4 q4[kLoad];
+                load<32>(h + lane, stop, q4);
+#pragma unroll 1
+                for (int i = 0; i < kLoad && h + 32 * i < stop; ++i) {
+                    const uint4 q = i == 0 ? q4[0] : i == 1 ? q4[1] : i == 2 ? q4[2] : q4[3];
+                    uint4 rest = q;
+                    if (__any_sync(0xffffffffu, vec_max<T>(q) >= lo)) {
+                        const uint4 in = mask_from<T>(q, lo);
+                        const uint32_t b = bits_of<T>(in);
+                        const int rel = (h - j0 + 32 * i + lane) * PV;
+                        rest = cleared<T>(q, in);
+                        float v[PV];
+                        unpack<T>(q, v);
 #pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) {
-                        const int v = __shfl_up_sync(0xffffffffu, at, o);
-                        if (lane >= o) at += v;
+                        for (int e = 0; e < PV; ++e) {
+                            const bool on = b >> e & 1;
+                            const uint32_t w = __ballot_sync(0xffffffffu, on);
+                            if (on) {
+                                const int at = waiting + __popc(w & ((1u << lane) - 1));
+                                value[at] = v[e];
+                                place[at] = (uint16_t)(rel + e);
+                            }
+                            waiting += __popc(w);
+                        }
+                        while (waiting >= 32) drain(32, j0);
                     }
-                    const int n = __shfl_sync(0xffffffffu, at, 31);
-                    at += waiting - mine;
-                    for (uint32_t h = b; h; h &= h - 1) queue[at++] = element<T>(q, __ffs(h) - 1);
-                    f.n_above += mine;
-                    waiting += n;
-                    __syncwarp();
-                    for (; waiting >= 32; waiting -= 32) above += mass_of(queue[waiting - 32 + lane]);
-                    __syncwarp();
-                    left = cleared<T>(q, in);
-                    top = vec_max<T>(left);
-                }
-                if (TAIL && exact) {
-                    list_vec<false>(left, top, j, lo, m, sum, under);
-                    const uint4 rest = cleared<T>(left, mask_from<T>(left, lo));
+                    under = fmaxf(under, vec_max<T>(rest));
+                    if (TAIL && exact) {
 #pragma unroll 4
-                    for (int e = 0; e < PV; ++e) f.tail += mass_of(element<T>(rest, e));
-                } else {
-                    list_vec<TAIL>(left, top, j, lo, m, sum, under);
+                        for (int e = 0; e < PV; ++e) f.tail += mass_of(element<T>(rest, e));
+                    } else if (TAIL) {
+                        sum.add(approx_sum(rest, m));
+                    }
                 }
-            },
-            [&](int region) {
-                if (!over) return;
-                if (lane < waiting) above += mass_of(queue[lane]);
-                waiting = 0;
-                __syncwarp();
-                const uint64_t w = warp_sum_u64(above);
-                if (lane == 0) s.region[region] = w;
-                f.above += above;
-                above = 0;
-            });
+            }
+            if (waiting) drain(waiting, j0);
+            const uint64_t w = warp_sum_u64(above);
+            if (lane == 0) s.region[j0 / depth] = w;
+            f.above += above;
+            above = 0;
+        }
         if (TAIL && !exact) f.tail = fixed_of(sum.hi + sum.lo);
         f.below = __syncthreads_or(under > -INFINITY);
-        f.above = over ? block_sum(f.above) : 0;
-        f.n_above = over ? (int)block_sum((uint64_t)f.n_above) : 0;
+        f.above = block_sum(f.above);
+        f.n_above = (int)block_sum((uint64_t)f.n_above);
         f.tail = TAIL ? block_sum(f.tail) : 0;
         f.slack = TAIL && !exact ? tail_slack(f.tail) : 0;
         return f;
@@ -746,7 +768,7 @@ template <typename T> struct Sampler {
 
     // ------------------------------------------------------------ the bracket
     // A histogram over bins of the logit from `base` down, each token in them weighing one
-    // (COUNT) or its approximate mass in units; `sample`: of an eighth of the row.  goal_of
+    // (COUNT) or its approximate mass in units; `sample`: of a quarter of the row.  goal_of
     // gives, for the whole weight, the goal and how far it may be off; left are the bins
     // that hold the place where the weights pass it.
     template <bool COUNT, typename Goal>
@@ -769,7 +791,7 @@ template <typename T> struct Sampler {
         };
         if (sample) {
             for (int j0 = warp * depth; j0 < nvec; j0 += kWarps * depth)
-                if (j0 + lane < nvec) count(vec(j0 + lane), 0);
+                for (int j = j0 + lane; j < min(nvec, j0 + 64); j += 32) count(vec(j), 0);
         } else {
             each(count);
         }
@@ -780,6 +802,20 @@ template <typename T> struct Sampler {
         for (int i = 0; i < Q; ++i) sum += w[i] = s.order[tid * Q + i];
         uint64_t cum = block_scan(sum, all);
         goal_of(all, goal, slack);
+        if (sample) {
+            // and some deviations of the sampled weight up to the goal: the root of the sum of
+            // its tokens' squares
+            uint64_t squares = 0, every;
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+                squares += w[i] * (uint64_t)(approx(base - ((float)(tid * Q + i) + 0.5f) / per) * unit);
+            const uint64_t before = block_scan(squares, every);
+            if (tid == 0) s.value = 0;
+            __syncthreads();
+            if (cum < goal && cum + sum >= goal) s.value = before + squares;
+            __syncthreads();
+            slack += (uint64_t)(2.5f * sqrtf((float)s.value));
+        }
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
             const uint64_t after = cum + w[i];
@@ -787,6 +823,7 @@ template <typename T> struct Sampler {
             if (cum < goal + slack && after >= goal + slack) s.dec.bin1 = tid * Q + i;
             cum = after;
         }
+        if (tid == 0 && goal > all + slack) s.dec.bin0 = kBins;  // (past them all)
         __syncthreads();
     }
     // For a nucleus, of which `whole` is all: bins down to the least logit that it can
@@ -804,9 +841,8 @@ template <typename T> struct Sampler {
         });
         return per;
     }
-    // The same behind a list of the tokens from `lo` on, of mass `listed`, by an eighth of
-    // the rest: the place may be off by some deviations of the sample's weight up to it,
-    // whose square is at most that weight times the largest token's.  0 if there are none.
+    // The same behind a list of the tokens from `lo` on, of mass `listed`, by a quarter of
+    // the rest.  0 if there are none.
     __device__ __forceinline__ float bracket_rest(float top_p, uint64_t whole, uint64_t listed, float lo) {
         const float one = ldexpf(1.f, sc.shift - 62), z = (float)whole * one;
         const float rest = (float)(whole - listed) * one, need = top_p * z - (float)listed * one;
@@ -814,10 +850,9 @@ template <typename T> struct Sampler {
         if (!(reach > 0.f) || !(need > 0.f) || !(need < rest)) return 0.f;
         const float per = (float)kBins / reach, unit = 1073741824.f / rest;
         base = lo;
-        histogram<false>(per, unit, true, [&](uint64_t all, uint64_t& goal, uint64_t& slack) {
-            const float g = (float)all * (need / rest), top = approx(lo) * unit;
-            goal = (uint64_t)g;
-            slack = (uint64_t)(3.f * sqrtf(g * top) + 4.f * top) + (uint64_t)a.V / 16 + 2;
+        histogram<false>(per, unit, true, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
+            goal = (uint64_t)(need * unit * (depth > 64 ? 64.f / (float)depth : 1.f));
+            slack = (uint64_t)a.V / 8 + 2;
         });
         return per;
     }
@@ -1201,7 +1236,7 @@ template <typename T> struct Sampler {
         bool sums = !filters;  // whether the kept tokens' masses are still to be summed
         if (filters) {
             bool made = true;
-            uint64_t whole = 0, listed = 0;
+            uint64_t whole = 0, listed = 0;  // of a nucleus past the first list
             if (tail) {
                 // (where the reference was too far below: once more, relative to m)
                 const float t = (sum.hi + sum.lo) * ex2((ref - m) * c);
@@ -1211,76 +1246,76 @@ template <typename T> struct Sampler {
                 f.slack = tail_slack(f.tail);
             }
             f.below = __syncthreads_or(under > -INFINITY);
-            // a list from `low` on behind what is from `high` on, until one decides: the
-            // first; where a long top-k or min_p overflows it, one around its place; for a
-            // nucleus past it one around its place by a sample, then by all of the row
-            float high = INFINITY, low = lo;
+            // A list from `low` on, behind what is from `high` on, until one decides.  First the
+            // one at hand (kFirst); where k or min_p overflows it, or min_p may come before a
+            // nucleus past it, one around their place (kNear); for a nucleus past it one around
+            // its place by a sample, then by all of the row (kRest, kRow), and within one that
+            // overflows a narrower one.
+            enum { kFirst, kNear, kRest, kRow };
+            float high = INFINITY, low = lo, per;
             uint64_t known = 0;
-            int what, tries = 0;
-            for (int step = 0;; made = false) {
-                what = step == 0 && top_k == 1 && s.count <= kList
+            int what, step = kFirst, tries = 0;
+            for (;; made = false) {
+                what = step == kFirst && top_k == 1 && s.count <= kList
                            ? first_alone()
                            : settle(made ? &f : nullptr, high, low, floor, known, top_k, top_p, least,
                                     draw, u);
-                if (what == kDone || step >= 7) break;
-                float per = 0.f;
-                if (step >= 2 && what == kOverflow && s.count > kList) {
-                    // too many in the bracket: again, within it
-                    step = max(step + 1, 5);
-                    per = bracket_within(top_p, whole, s.dec.listed, s.dec.all, fminf(high, m), low);
-                    if (!(per > 0.f)) break;
-                    const float was_high = high, was_low = low;
-                    edges(per, high, low);
-                    high = fminf(high, was_high);
-                    low = fmaxf(low, was_low);
+                if (what == kDone) break;
+                if (step == kFirst && what == kOverflow && tail) {
+                    // (a bound that a quarter of the entries at hand reach)
+                    const float raised = higher(kList / 4);
+                    if (tries++ == 2 || !(raised > lo)) break;
+                    low = lo = raised;
                     continue;
                 }
-                if (step >= 4) break;
-                if (step == 0 && !tail && (what == kOverflow || (what == kSearch && top_k > 0 && !floor))) {
-                    step = 1;
+                if (step == kFirst && (what == kBracket ? least != 0
+                                                        : what != kAbove && (floor || top_k > 0))) {
+                    step = kNear;
+                    whole = what == kBracket ? s.dec.all : 0;
+                    listed = s.dec.listed;
                     high = up_to<T>(m - span + rounding(m));
                     low = down_to<T>(m - span - rounding(m));
+                    floor = floor || what == kBracket;
                     if (floor) continue;
+                    // the k-th token: among those at hand, or past them
                     per = ((float)kBins - 0.1f) / ((m - lo) * (what == kOverflow ? 1.f : 3.f));
-                    base = m;
                     if (!(per > 0.f && per < INFINITY)) break;
+                    base = m;
                     histogram<true>(per, 0.f, false, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
                         goal = (uint64_t)top_k;
                         slack = 0;
                     });
-                } else {
-                    if (step < 2) {
-                        if (step == 0 && what == kOverflow && tail && tries++ < 2) {
-                            // (a bound that a quarter of the entries at hand reach)
-                            const float raised = higher(kList / 4);
-                            if (!(raised > lo)) break;
-                            low = lo = raised;
-                            continue;
-                        }
-                        if (step == 0 && what == kBracket && least != 0) {
-                            // (the place of min_p may come before)
-                            step = 1;
-                            floor = true;
-                            whole = s.dec.all;
-                            listed = s.dec.listed;
-                            high = up_to<T>(m - span + rounding(m));
-                            low = down_to<T>(m - span - rounding(m));
-                            continue;
-                        }
-                        const bool again = floor && whole;  // (after a look at the place of min_p)
-                        if (again) what = kBracket;
-                        if (what != kBracket && what != kAbove) break;
-                        floor = false;
-                        if (what == kAbove) known = s.dec.all;
-                        step = what == kAbove ? 3 : 2;
-                        if (!again) whole = s.dec.all, listed = s.dec.listed;
-                        if (step == 2) per = bracket_rest(top_p, whole, listed, lo);
+                    if (s.dec.bin0 >= kBins) break;
+                    edges(per, high, low);
+                    continue;
+                }
+                if (step < kRest) {
+                    if (what == kBracket || what == kAbove) whole = s.dec.all, listed = s.dec.listed;
+                    if (!whole) break;
+                    floor = false;
+                    known = what == kAbove ? whole : 0;
+                    step = kRest;
+                    tries = 0;
+                    per = listed && !known ? bracket_rest(top_p, whole, listed, lo) : 0.f;
+                    if (per > 0.f && s.dec.bin0 < kBins) {
+                        edges(per, high, low);
+                        continue;
                     }
-                    if (per == 0.f) {
-                        step = 4;
-                        per = bracket(top_p, whole);
+                } else if (what == kOverflow && s.count > kList && tries++ < 3) {
+                    per = bracket_within(top_p, whole, s.dec.listed, s.dec.all, fminf(high, m), low);
+                    if (per > 0.f && s.dec.bin0 < kBins) {
+                        const float was_high = high, was_low = low;
+                        edges(per, high, low);
+                        high = fminf(high, was_high);
+                        low = fmaxf(low, was_low);
+                        continue;
                     }
                 }
+                if (step == kRow) break;
+                step = kRow;
+                tries = 0;
+                per = bracket(top_p, whole);
+                if (s.dec.bin0 >= kBins) break;
                 edges(per, high, low);
             }
             if (what != kDone) {
