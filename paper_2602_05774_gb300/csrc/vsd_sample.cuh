@@ -489,22 +489,75 @@ template <typename T> struct Sampler {
         return (int)fminf((base - v) * per, (float)kBins);
     }
 
-    // Sorts n entries (the array holds them up to the next power of two).
-    template <int G, typename E, bool FALLING> __device__ __forceinline__ void sort(E* v, int n) {
+    // Sorts n <= NT Q entries (the array holds as many): Q a thread in its registers, a
+    // comparison's other side in them too, or another lane's, or (32 Q and more entries
+    // away) in shared memory.  A list of 2048: 24 us with all of them in shared memory.
+    template <int Q, typename E, bool FALLING> __device__ __forceinline__ void sort(E* v, int n) {
+        E e[Q];
+#pragma unroll
+        for (int i = 0; i < Q; ++i)
+            e[i] = tid * Q + i < n ? v[tid * Q + i] : FALLING ? (E)0 : ~(E)0;
         int size = 2;
         while (size < n) size *= 2;
-        for (int i = n + tid; i < size; i += G) v[i] = FALLING ? (E)0 : ~(E)0;
-        for (int k = 2; k <= size; k *= 2)
-            for (int j = k / 2; j > 0; j /= 2) {
-                sync<G>();
-                for (int i = tid; i < size / 2; i += G) {
-                    const int lo = 2 * i - (i & (j - 1)), hi = lo + j;
-                    const E p = v[lo], q = v[hi];
-                    const bool down = ((lo & k) == 0) == FALLING;
-                    if (down ? p < q : p > q) v[lo] = q, v[hi] = p;
-                }
+        const bool in = warp * 32 * Q < size;
+#pragma unroll 1
+        for (int k = 2; k <= size; k *= 2) {
+            // entry i takes the larger or the smaller of itself and the one `j` away
+            auto take = [&](int i, int j, E other) {
+                const int p = tid * Q + i;
+                const bool larger = (((p & k) == 0) == FALLING) == ((p & j) == 0);
+                if ((e[i] > other) != larger) e[i] = other;
+            };
+            int j = k / 2;
+#pragma unroll 1
+            for (; j >= 32 * Q; j /= 2) {
+                __syncthreads();
+                if (in)
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) v[i * NT + tid] = e[i];
+                __syncthreads();
+                if (in)
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) take(i, j, v[i * NT + (tid ^ (j / Q))]);
             }
-        sync<G>();
+            if (in) {
+#pragma unroll 1
+                for (; j >= Q; j /= 2)
+#pragma unroll
+                    for (int i = 0; i < Q; ++i) take(i, j, __shfl_xor_sync(0xffffffffu, e[i], j / Q));
+#pragma unroll
+                for (int h = Q / 2; h >= 1; h /= 2)
+                    if (h < k)
+#pragma unroll
+                        for (int i = 0; i < Q; ++i)
+                            if (!(i & h)) {
+                                const E a = e[i], b = e[i | h];
+                                take(i, h, b);
+                                take(i | h, h, a);
+                            }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < Q; ++i)
+            if (tid * Q + i < n) v[tid * Q + i] = e[i];
+        __syncthreads();
+    }
+
+    // Sorts the orders by id: of more than 32, or of a warp's list.
+    template <int G, int Q> __device__ __forceinline__ void sort_ids(int n) {
+        if constexpr (G > 32) {
+            __syncthreads();
+            sort<Q, uint32_t, false>(s.order, n);
+        } else {
+            __syncwarp();
+            const uint32_t mine = lane < n ? s.order[lane] : ~0u;
+            int rank = 0;
+            for (int k = 0; k < n; ++k) rank += s.order[k] < mine;
+            __syncwarp();
+            if (lane < n) s.order[rank] = mine;
+            __syncwarp();
+        }
     }
 
     // Sorts the list by counting, for each entry, the larger ones: two threads an entry, n
@@ -527,7 +580,7 @@ template <typename T> struct Sampler {
     template <int G, int Q>
     __device__ __forceinline__ void decide(int n, const Found& f, bool floor, uint64_t known, int top_k,
                            float top_p, uint64_t least, bool draw, float u) {
-        if (Q > 1 && G > 32) sort<G, uint64_t, true>(s.list, n);  // (else it is sorted)
+        if constexpr (Q > 1) sort<Q, uint64_t, true>(s.list, n);  // (else it is sorted)
         // masses and their prefix sums, Q entries a thread
         uint64_t e[Q], own = 0;
         int big = 0;
@@ -615,7 +668,7 @@ template <typename T> struct Sampler {
                 } else {
                     for (int i = tid; i < here; i += G)
                         s.order[i] = ~(uint32_t)s.list[i] << kPlaceBits | (uint32_t)i;
-                    sort<G, uint32_t, false>(s.order, here);
+                    sort_ids<G, Q>(here);
                     uint64_t o[Q], sum = 0, every;
 #pragma unroll
                     for (int i = 0; i < Q; ++i) {
@@ -661,7 +714,7 @@ template <typename T> struct Sampler {
                               float top_p, uint64_t least, bool draw, float u) {
         __syncthreads();
         if (n <= NT / 2) sort_by_rank(n);
-        else if (n <= NT) sort<NT, uint64_t, true>(s.list, n);
+        else if (n <= NT) sort<1, uint64_t, true>(s.list, n);
         if (n <= 32) {
             if (warp == 0) decide<32, 1>(n, f, floor, known, top_k, top_p, least, draw, u);
         } else if (n <= NT) {
