@@ -449,17 +449,22 @@ template <typename T> struct Sampler {
                         rest = cleared<T>(q, in);
                         float v[PV];
                         unpack<T>(q, v);
+                        // where this lane's go: behind those of the lanes before, whose
+                        // numbers (PV at most) are added bit by bit
+                        const int n = __popc(b);
+                        int at = waiting;
 #pragma unroll
-                        for (int e = 0; e < PV; ++e) {
-                            const bool on = b >> e & 1;
-                            const uint32_t w = __ballot_sync(0xffffffffu, on);
-                            if (on) {
-                                const int at = waiting + __popc(w & ((1u << lane) - 1));
-                                value[at] = v[e];
-                                place[at] = (uint16_t)(rel + e);
-                            }
-                            waiting += __popc(w);
+                        for (int i = 0; 1 << i <= PV; ++i) {
+                            const uint32_t w = __ballot_sync(0xffffffffu, n >> i & 1);
+                            at += __popc(w & ((1u << lane) - 1)) << i;
+                            waiting += __popc(w) << i;
                         }
+#pragma unroll
+                        for (int e = 0; e < PV; ++e)
+                            if (b >> e & 1) {
+                                value[at] = v[e];
+                                place[at++] = (uint16_t)(rel + e);
+                            }
                         while (waiting >= 32) drain(32, j0);
                     }
                     under = fmaxf(under, vec_max<T>(rest));
