@@ -826,18 +826,27 @@ template <typename T> struct Sampler {
 
     // ------------------------------------------------------------ the bracket
     // A histogram over bins of the logit from `base` down, each token in them weighing one
-    // (COUNT) or its approximate mass in units; `sample`: of a quarter of the row.  goal_of
-    // gives, for the whole weight, the goal and how far it may be off; left are the bins
-    // that hold the place where the weights pass it.
-    template <bool COUNT, typename Goal>
-    __device__ __forceinline__ void histogram(float per, float unit, bool sample, Goal goal_of) {
+    // (COUNT) or its approximate mass in units.  Left are the bins that hold the place where
+    // the weights pass the goal, which may be off by `slack`.  SAMPLE: of a quarter of the
+    // row; the place is also where the weight from below, what is past the bins with it,
+    // passes `tail`, and the better known of the two is taken.  (A nucleus of 0.95 that
+    // is 12000 tokens of 128256: a bracket of 500 tokens from below, 7300 from above.)
+    struct Aim {
+        uint64_t goal, slack, tail;
+    };
+    template <bool COUNT, bool SAMPLE>
+    __device__ __forceinline__ void histogram(float per, float unit, const Aim& aim) {
         for (int i = tid; i < kBins; i += NT) s.order[i] = 0;
         if (tid == 0) s.dec.bin0 = 0, s.dec.bin1 = kBins - 1;
         __syncthreads();
         // (from a list's or bracket's edge down: those at it are before)
         const float edge = base < m ? base : INFINITY;
+        Sum past;
         auto count = [&](const uint4& q, int) {
-            if (bin_of(vec_max<T>(q), per) >= kBins) return;
+            if (bin_of(vec_max<T>(q), per) >= kBins) {
+                if (SAMPLE) past.add(approx_sum(q, m));
+                return;
+            }
             float v[PV];
             unpack<T>(q, v);
 #pragma unroll
@@ -845,34 +854,41 @@ template <typename T> struct Sampler {
                 const int b = bin_of(v[e], per);
                 if (b < kBins && v[e] < edge)
                     atomicAdd(&s.order[b], COUNT ? 1u : __float2uint_rn(approx(v[e]) * unit));
+                else if (SAMPLE && b >= kBins)
+                    past.add(approx(v[e]));
             }
         };
-        if (sample) {
+        if (SAMPLE) {
             for (int j0 = warp * depth; j0 < nvec; j0 += kWarps * depth)
-                for (int j = j0 + lane; j < min(nvec, j0 + 64); j += 32) count(vec(j), 0);
+                for (int j = j0 + lane; j < min(nvec, j0 + sampled()); j += 32) count(vec(j), 0);
         } else {
             each(count);
         }
         __syncthreads();
         constexpr int Q = kBins / NT;
-        uint64_t w[Q], sum = 0, all, goal, slack;
+        uint64_t w[Q], sum = 0, all, goal = aim.goal, slack = aim.slack;
 #pragma unroll
         for (int i = 0; i < Q; ++i) sum += w[i] = s.order[tid * Q + i];
         uint64_t cum = block_scan(sum, all);
-        goal_of(all, goal, slack);
-        if (sample) {
-            // and some deviations of the sampled weight up to the goal: the root of the sum of
-            // its tokens' squares
+        if (SAMPLE) {
+            // some deviations of the sampled weight up to the place, or from it on: the root
+            // of the sum of its tokens' squares
             uint64_t squares = 0, every;
 #pragma unroll
             for (int i = 0; i < Q; ++i)
                 squares += w[i] * (uint64_t)(approx(base - ((float)(tid * Q + i) + 0.5f) / per) * unit);
             const uint64_t before = block_scan(squares, every);
-            if (tid == 0) s.value = 0;
+            const uint64_t beyond = block_sum(__float2ull_rn((past.hi + past.lo) * unit));
+            const uint64_t from = all + beyond > aim.tail ? all + beyond - aim.tail : 0;
+            if (tid == 0) s.region[0] = every, s.region[1] = 0;
             __syncthreads();
-            if (cum < goal && cum + sum >= goal) s.value = before + squares;
+            if (cum < goal && cum + sum >= goal) s.region[0] = before + squares;
+            if (cum < from && cum + sum >= from) s.region[1] = before;
             __syncthreads();
-            slack += (uint64_t)(2.5f * sqrtf((float)s.value));
+            const uint64_t last = (uint64_t)(approx(base - (float)kBins / per) * unit);
+            const uint64_t above = s.region[0], below = every - s.region[1] + beyond * last;
+            if (below < above) goal = from;
+            slack += (uint64_t)(2.5f * sqrtf((float)min(above, below)));
         }
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
@@ -884,6 +900,8 @@ template <typename T> struct Sampler {
         if (tid == 0 && goal > all + slack) s.dec.bin0 = kBins;  // (past them all)
         __syncthreads();
     }
+    // Vectors of a region that are a sample.
+    __device__ __forceinline__ int sampled() const { return min(depth, 64); }
     // For a nucleus, of which `whole` is all: bins down to the least logit that it can
     // reach.  Returns bins per unit of the logit.
     __device__ __forceinline__ float bracket(float top_p, uint64_t whole) {
@@ -893,10 +911,8 @@ template <typename T> struct Sampler {
         const float per = (float)kBins / reach;
         base = m;
         // in units of 2^-30 of the mass: half a unit a token, and 2^-15
-        histogram<false>(per, 1073741824.f / z, false, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
-            goal = (uint64_t)(top_p * 1073741824.f);
-            slack = (uint64_t)a.V / 2 + (1 << 15) + 2;
-        });
+        histogram<false, false>(per, 1073741824.f / z,
+                                Aim{(uint64_t)(top_p * 1073741824.f), (uint64_t)a.V / 2 + (1 << 15) + 2, 0});
         return per;
     }
     // The same behind a list of the tokens from `lo` on, of mass `listed`, by a quarter of
@@ -908,10 +924,10 @@ template <typename T> struct Sampler {
         if (!(reach > 0.f) || !(need > 0.f) || !(need < rest)) return 0.f;
         const float per = (float)kBins / reach, unit = 1073741824.f / rest;
         base = lo;
-        histogram<false>(per, unit, true, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
-            goal = (uint64_t)(need * unit * (depth > 64 ? 64.f / (float)depth : 1.f));
-            slack = (uint64_t)a.V / 8 + 2;
-        });
+        const int n = nvec / depth * sampled() + min(nvec % depth, sampled());
+        const float part = unit * (float)n / (float)nvec;
+        histogram<false, true>(per, unit, Aim{(uint64_t)(need * part), (uint64_t)a.V / 8 + 2,
+                                              (uint64_t)((rest - need) * part)});
         return per;
     }
 
@@ -926,11 +942,10 @@ template <typename T> struct Sampler {
         if (!(here > 0.f) || !(per > 0.f) || !(per < INFINITY)) return 0.f;
         const float unit = 1073741824.f / here;
         base = hi;
-        histogram<false>(per, unit, false, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
-            goal = need > 0.f ? (uint64_t)(need * unit) : 0;
-            // (what `whole` may be off by, in these units, and half a unit a token)
-            slack = (uint64_t)a.V / 2 + (1 << 14) + (uint64_t)((float)whole * one * 0x1p-16f * unit);
-        });
+        // (off: what `whole` may be, in these units, and half a unit a token)
+        const uint64_t off = (uint64_t)((float)whole * one * 0x1p-16f * unit);
+        histogram<false, false>(per, unit, Aim{need > 0.f ? (uint64_t)(need * unit) : 0,
+                                               (uint64_t)a.V / 2 + (1 << 14) + off, 0});
         return per;
     }
     // The logits that the bracket's bins end at, and a step beyond.
@@ -1339,10 +1354,7 @@ template <typename T> struct Sampler {
                     per = ((float)kBins - 0.1f) / ((m - lo) * (what == kOverflow ? 1.f : 3.f));
                     if (!(per > 0.f && per < INFINITY)) break;
                     base = m;
-                    histogram<true>(per, 0.f, false, [&](uint64_t, uint64_t& goal, uint64_t& slack) {
-                        goal = (uint64_t)top_k;
-                        slack = 0;
-                    });
+                    histogram<true, false>(per, 0.f, Aim{(uint64_t)top_k, 0, 0});
                     if (s.dec.bin0 >= kBins) break;
                     edges(per, high, low);
                     continue;
