@@ -401,10 +401,10 @@ template <typename T> struct Sampler {
         return __float2ull_rn(v * ldexpf(1.f, 62 - sc.shift));
     }
     // Tokens from `hi` on are above, those from `lo` on are listed.  Left is the mass
-    // above, by region too; of the rest it is approximate, exact, or not summed at all.
+    // above, by region too; of the rest it is approximate, or not summed at all.
     // (Tokens from `lo` on wait in a warp's queue until there are 32, so that all its lanes
     // are of use: a few in 100 tokens are above where a nucleus is wide.)
-    template <bool TAIL> __device__ __forceinline__ Found collect(float hi, float lo, bool exact) {
+    template <bool TAIL> __device__ __forceinline__ Found collect(float hi, float lo) {
         if (tid == 0) s.count = 0;
         __syncthreads();
         Found f{0, 0, 0, 0, false};
@@ -468,12 +468,7 @@ template <typename T> struct Sampler {
                         while (waiting >= 32) drain(32, j0);
                     }
                     under = fmaxf(under, vec_max<T>(rest));
-                    if (TAIL && exact) {
-#pragma unroll 4
-                        for (int e = 0; e < PV; ++e) f.tail += mass_of(element<T>(rest, e));
-                    } else if (TAIL) {
-                        sum.add(approx_sum(rest, m));
-                    }
+                    if (TAIL) sum.add(approx_sum(rest, m));
                 }
             }
             if (waiting) drain(waiting, j0);
@@ -482,13 +477,46 @@ template <typename T> struct Sampler {
             f.above += above;
             above = 0;
         }
-        if (TAIL && !exact) f.tail = fixed_of(sum.hi + sum.lo);
+        if (TAIL) f.tail = fixed_of(sum.hi + sum.lo);
         f.below = __syncthreads_or(under > -INFINITY);
         f.above = block_sum(f.above);
         f.n_above = (int)block_sum((uint64_t)f.n_above);
         f.tail = TAIL ? block_sum(f.tail) : 0;
-        f.slack = TAIL && !exact ? tail_slack(f.tail) : 0;
+        f.slack = TAIL ? tail_slack(f.tail) : 0;
         return f;
+    }
+    // The approximate mass of what is below `lo` once more, off by 2^-20 of itself at most:
+    // the exponent in two floats leaves ex2's 2^-22, the product's and the additions' 2^-24.
+    // (It decides seven of eight nuclei that the first sum leaves open; the exact one, for
+    // the eighth, takes three times as long.)
+    __device__ __forceinline__ void finer_tail(float lo, Found& f) {
+        Sum sum;
+        each([&](const uint4& q, int) {
+            float v[PV], t = 0.f;
+            unpack<T>(cleared<T>(q, mask_from<T>(q, lo)), v);
+#pragma unroll
+            for (int e = 0; e < PV; ++e) {
+                float d_lo;
+                const float d = gap(v[e], m, d_lo), y = d * sc.c;
+                const float y_lo = fmaf(d_lo, sc.c, fmaf(d, sc.c_lo, fmaf(d, sc.c, -y)));
+                const float w = ex2(-y);
+                t += y < 126.f ? fmaf(w, y_lo * -0.693147181f, w) : 0.f;
+            }
+            sum.add(t);
+        });
+        f.tail = block_sum(fixed_of(sum.hi + sum.lo));
+        f.slack = (f.tail >> 20) + (1ull << (62 - sc.shift) >> 28) + 1;
+    }
+    // The exact one.
+    __device__ __forceinline__ void exact_tail(float lo, Found& f) {
+        f.tail = 0;
+        each([&](const uint4& q, int) {
+            const uint4 rest = cleared<T>(q, mask_from<T>(q, lo));
+#pragma unroll 2
+            for (int e = 0; e < PV; ++e) f.tail += mass_of(element<T>(rest, e));
+        });
+        f.tail = block_sum(f.tail);
+        f.slack = 0;
     }
     __device__ __forceinline__ int bin_of(float v, float per) const {
         return (int)fminf((base - v) * per, (float)kBins);
@@ -804,22 +832,21 @@ template <typename T> struct Sampler {
     __device__ __forceinline__ int settle(const Found* made, float hi, float lo, bool floor, uint64_t known,
                           int top_k, float top_p, uint64_t least, bool draw, float u) {
         const bool tail = top_p < 1.f && top_k <= 0;
-        for (bool exact = false;; exact = true) {
+        __syncthreads();
+        Found f = made ? *made : tail ? collect<true>(hi, lo) : collect<false>(hi, lo);
+        int n = s.count;
+        above_from = hi;
+        if (n > kList || (n == 0 && !(floor && f.n_above > 0))) {
+            if (tid == 0) s.dec.all = f.tail, s.dec.listed = f.above;
             __syncthreads();
-            const Found f = made && !exact ? *made
-                            : tail         ? collect<true>(hi, lo, exact)
-                                           : collect<false>(hi, lo, false);
-            int n = s.count;
-            above_from = hi;
-            if (n > kList || (n == 0 && !(floor && f.n_above > 0))) {
-                if (tid == 0) s.dec.all = f.tail, s.dec.listed = f.above;
-                __syncthreads();
-                return kOverflow;
-            }
-            Found g = f;
-            if (made && top_k > 0 && n > top_k && n > 64 && n <= NT) n = prune(n, top_k, g);
-            if (made && tail && n > NT / 4 && least == 0 && past(n, f, top_p)) return kBracket;
-            decide_by(n, g, floor, known, top_k, top_p, least, draw, u);
+            return kOverflow;
+        }
+        if (made && top_k > 0 && n > top_k && n > 64 && n <= NT) n = prune(n, top_k, f);
+        if (made && tail && n > NT / 4 && least == 0 && past(n, f, top_p)) return kBracket;
+        for (int more = 0;; ++more) {
+            if (more == 1) finer_tail(lo, f);
+            else if (more == 2) exact_tail(lo, f);
+            decide_by(n, f, floor, known, top_k, top_p, least, draw, u);
             if (s.dec.what != kExactTail) return s.dec.what;
         }
     }
