@@ -22,7 +22,10 @@ constexpr int kBlock = 128;  // columns of a scale
 
 // ------------------------------------------------------------ quantizing
 // s = 2^ceil(log2(amax / 448)), q = x / s, an exact product with 2^-log2(s) rounded once.
-// Bound by memory: one read, one write of half or a quarter of it.
+// Bound by memory: one read, one write of half or a quarter of it.  A block of 128 or of
+// 128 x 128 stays in registers between its largest magnitude and its quotients, so x is
+// read once: 32000 x 4096 float32 by 128 rows takes 94 us, 7.1 TB/s (478 with a second
+// read); 4096 x 4096 bf16 by rows 17, of which the host's call is 15.
 
 // The least power of two s with amax / s <= 448 = 1.75 2^8, and its reciprocal; amax by
 // its bits (NaN is above infinity).
@@ -74,7 +77,8 @@ __global__ void __launch_bounds__(kQuantThreads)
     const int64_t units = R * nk, groups = (int64_t)gridDim.x * (kQuantThreads / kGroup);
     // (whole warps go round together: w is the unit of a warp's first group)
     const int sub = threadIdx.x % 32 / kGroup;
-    for (int64_t w = (int64_t)blockIdx.x * (kQuantThreads / kGroup) + threadIdx.x / kGroup - sub; w < units;
+    const int first = threadIdx.x / kGroup - sub;
+    for (int64_t w = (int64_t)blockIdx.x * (kQuantThreads / kGroup) + first; w < units;
          w += groups * kMany) {
         const int64_t u0 = w + sub;
         uint4 v[kMany];
@@ -115,7 +119,8 @@ __global__ void __launch_bounds__(kQuantThreads, 3)
 #pragma unroll
     for (int i = 0; i < kMany; ++i) {
         const int64_t r = r0 + i * kStep;
-        v[i] = r < R && col < H ? *reinterpret_cast<const uint4*>(x + r * H + col) : make_uint4(0u, 0u, 0u, 0u);
+        v[i] = r < R && col < H ? *reinterpret_cast<const uint4*>(x + r * H + col)
+                                : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int i = 0; i < kMany; ++i) m = max(m, vec_amax<T>(v[i]));
@@ -141,7 +146,8 @@ cudaError_t quantize(const T* x, int R, int H, int block_rows, __nv_fp8_e4m3* q,
     if (block_rows == 1) {
         constexpr int kPer = 4 * kQuantThreads * Traits<T>::kPerVec / kBlock;  // a block's at a time
         const int64_t blocks = ((int64_t)R * nk + kPer - 1) / kPer;
-        k_quantize_rows<T><<<(int)std::min<int64_t>(blocks, 16 * device_sm_count()), kQuantThreads, 0, st>>>(
+        const int most = 16 * device_sm_count();
+        k_quantize_rows<T><<<(int)std::min<int64_t>(blocks, most), kQuantThreads, 0, st>>>(
             x, R, H, q, scale);
         return cudaGetLastError();
     }
@@ -161,7 +167,8 @@ cudaError_t quantize(const T* x, int R, int H, int block_rows, __nv_fp8_e4m3* q,
 // row of a swizzled tile, four MMAs.  Each K block gets an accumulator of its own
 // (two to eight, in turn), which the epilogue takes from tensor memory, multiplies by the
 // block's scales and adds to the sums in its registers in fp32 while the next ones are
-// computed.  Per CTA:
+// computed.  (One accumulator over all of K would need scales that are the same for all
+// blocks.)  Per CTA:
 //   warp 0     TMA producer: its half of A and of B, counted on the leader's barrier;
 //   warp 1     the leader's MMA issuer (one thread, for both CTAs);
 //   warps 4-11 epilogue: 32 lanes and half of the columns each.
@@ -172,6 +179,17 @@ cudaError_t quantize(const T* x, int R, int H, int block_rows, __nv_fp8_e4m3* q,
 //   NF > 0     at most NF rows: A = tokens (2 `high` of them, see below), B = the
 //              rows, so that nothing but the weight is brought in; a lane is a token
 //              and a column a row, whose scales are in shared memory throughout.
+// What bounds them, and what they measured (one GB300, the rows' form by its count):
+//   NF = 0     the epilogue: 128 x 256 fp32 from tensor memory a K block and CTA, 64
+//              FMAs of two each a thread.  4096 x 32000 x 4096: 384 to 437 us as power
+//              allows (2.5 to 2.8 PFLOP/s), 322 without the epilogue.
+//   NF > 0     memory: 8 x 128256 x 4096 in 87 us, 6.1 TB/s.
+// Either by rows, V = 128256, H = 4096 (us; NF the least that holds them):
+//   rows       1*    8    32    64   100   128      (* V = 32000)
+//   NF > 0    25    87    87    89    98    99
+//   NF = 0    44   132   102   104   106   108
+// At 8 rows NF = 64 takes 89 us and 128 takes 95: so three sizes.  The scales of more than
+// 128 rows would have to come in with the tiles.
 // Every wait is bounded: one that runs out sets VSD_STATUS_TIMEOUT, and the pair winds
 // down, waits for its copies and MMAs in flight and frees its tensor memory.
 namespace tc = vsd_pair;
@@ -183,7 +201,8 @@ constexpr int kHalfBytes = 128 * kBlock;  // one operand's half tile: 16 KB
 constexpr int kOutBytes = 4096;           // 32 rows x 64 columns of bf16
 constexpr int kMaxStages = 16, kMaxAcc = 4;
 constexpr size_t kSmemMost = 232448;
-constexpr int kFewBlocks = 128;           // K blocks whose scales the turned form holds
+constexpr int kFewBlocks = 128;           // K blocks whose scales the turned form holds:
+                                          // 64 KB, which leave it six stages
 constexpr int kGroupM = 16;               // row tiles that share weight tiles in L2
 constexpr uint64_t kWaitNs = 2000000000ull;
 // Registers a thread: launched with 168, of which the first warpgroup gives up what
@@ -676,7 +695,9 @@ cudaError_t head_fp8(const void* hidden, const void* weight, int H, HeadArgs a, 
         return launch_head<0>(maps, a, jobs, most, st);
     }
     // the tiles' height with the least time: a K block takes what its bytes do at a
-    // pair's share of the memory, 300 ns at least
+    // pair's share of the memory (43.7 bytes a ns and CTA, 6.6 TB/s over 152), 300 ns at
+    // least.  (32000 tokens, 1 and 128 rows: 24.5 and 33.8 us, 25.5 and 35.1 at 128
+    // throughout; 128256: no difference.)
     double best = 1e30;
     for (int high = 128; high >= 64; high -= 8) {
         const int64_t tiles = (a.V + 2 * high - 1) / (2 * high);

@@ -8,20 +8,29 @@
 //
 // A block works on a row, two blocks to an SM.  Bound by memory where the filters leave
 // few tokens: the row comes from memory once, and from L2 for the passes after the
-// first.  A row takes as few of these steps as decide it:
+// first.  Bound by instructions where a nucleus is wide: 75 for an exact mass, 8 for an
+// approximate one.  A row takes as few of these steps as decide it:
 //
-//   top      the maximum, and a bound `lo` that enough tokens reach: the n-th largest
-//            of each warp's 32 lane maxima, the least over the warps.
+//   top      the maximum, and a bound `lo` that enough of the threads' first maxima
+//            reach (kWant over the row).
 //   list     the tokens from `lo` on, sorted; a prefix sum of their masses gives every
 //            filter's place and the draw.  A nucleus also needs the mass of all others,
 //            a sum of approximate exponentials (2^-17 off at most): where that leaves
-//            the place open, it is summed again exactly.
+//            the place open, it is made finer (2^-20), then exact.
 //   bracket  a nucleus past the list: a histogram of approximate masses over 1024
-//            steps of the logit brackets its place, the tokens in the bracket are
-//            listed, and the mass above it is summed exactly.
-//   search   whatever these leave open (a list that overflows, by large k or equal
-//            logits): bisection of the logits' ordered bits, exact counts and masses
-//            each step.
+//            steps of the logit brackets its place, first of a quarter of the row, then
+//            of all of it; the tokens in the bracket are listed, and the mass above it
+//            is summed exactly.  A list that overflows is bracketed within its bounds.
+//   search   whatever these leave open (large k, thousands of equal logits): bisection
+//            of the logits' ordered bits, exact counts and masses each step.
+//
+// At 4096 x 128256 bf16 (1.05 GB, 158 us at the copy's rate), us: greedy 240, top_k 50
+// 400, top_p 0.8 806 and 0.95 1606 (nuclei of 3500 tokens).  8 rows: 15 greedy, 27 with
+// top_k 50, 113 with top_p 0.95: one block's latency.  Measured against it: blocks of 256
+// with lists of 2048, three to an SM (greedy 198, top_p 0.95 a fifth slower); blocks of
+// 1024 where there is a row an SM at most (8 x 128256: 2 us more for greedy and top_k, a
+// seventh less for wide nuclei); a cluster of 8 a row (four times as long for the 4096
+// rows, by its barriers).
 //
 // Where the kept tokens are not all in the list, the exact sums are also kept by region
 // of the row; the draw finds the region, then the token in it.
@@ -49,10 +58,16 @@ constexpr int kSampleThreads = 512;
 constexpr int kList = 4096;
 constexpr int kPlaceBits = 12;           // of a place in it
 constexpr int kBins = 1024;
-constexpr int kWant = 768;               // a list's length aimed at, where top-k does not say
+// A list's length aimed at, where top-k does not say.  (256, 768, 1600, 2800: top_p 0.95 of
+// 4096 x 128256 in 2642, 2248, 2097, 2736 us when it was set, and settings of all kinds at
+// 512 x 32000 in 131, 119, 228, 226: 32000 is two rounds, of which the first then lists
+// all.)
+constexpr int kWant = 768;
 constexpr int kDeep = 8;                 // vectors of a lane in a long row's regions
 constexpr int kRegions = (1 << 18) / (32 * kDeep) + 1;
-constexpr int kShort = 2048;             // vectors of a row whose regions are one deep
+// Vectors of a row whose regions are one deep: no more than one round of a block's loads,
+// so that all its warps have some.
+constexpr int kShort = 2048;
 static_assert(kList == 1 << kPlaceBits && kList % 1024 == 0 && kBins % 1024 == 0, "whole rounds");
 
 
@@ -340,7 +355,7 @@ template <typename T> struct Sampler {
 
     // ------------------------------------------------------------ the list
     // What a listing leaves beside the list: the exact mass and the number of the tokens
-    // above, and the mass, approximate or exact, of the rest.
+    // above, and the approximate mass of the rest.
     struct Found {
         uint64_t above, tail, slack;  // (how far the tail may be off)
         int n_above;
@@ -361,8 +376,8 @@ template <typename T> struct Sampler {
     }
     // The sum of a vector's masses relative to `ref`, off by 2^-17 of itself at most, where
     // exponents are 40 at most: ex2's 2^-22, and what v - ref, c and their product are
-    // rounded by.  (A product in two floats is off by 2^-19, takes twice the instructions,
-    // and spares but one nucleus in twenty its exact sum.)
+    // rounded by.  (An exponent in two floats takes three times the instructions: see
+    // finer_tail.  One nucleus in twenty needs it.)
     __device__ __forceinline__ float approx_sum(const uint4& q, float ref) const {
         uint64_t p[PV / 2];
         vec_pairs<T>(q, p);
@@ -487,8 +502,8 @@ template <typename T> struct Sampler {
     }
     // The approximate mass of what is below `lo` once more, off by 2^-20 of itself at most:
     // the exponent in two floats leaves ex2's 2^-22, the product's and the additions' 2^-24.
-    // (It decides seven of eight nuclei that the first sum leaves open; the exact one, for
-    // the eighth, takes three times as long.)
+    // (It decides five of six nuclei that the first sum leaves open; the exact one, for the
+    // sixth, takes three times as long.)
     __device__ __forceinline__ void finer_tail(float lo, Found& f) {
         Sum sum;
         each([&](const uint4& q, int) {
@@ -608,8 +623,9 @@ template <typename T> struct Sampler {
     }
 
     // From the list of n: every filter's place, the kept tokens and, where they are all
-    // listed, the draw.  By G threads, Q entries each.  f: what is before and behind the list; `floor`: no token behind it has `least`; `known`: the mass of the
-    // first top_k, whose place is not looked for again.
+    // listed, the draw.  By G threads, Q entries each.  f: what is before and behind the
+    // list; `floor`: no token behind it has `least`; `known`: the mass of the first top_k,
+    // whose place is not looked for again.
     template <int G, int Q>
     __device__ __forceinline__ void decide(int n, const Found& f, bool floor, uint64_t known, int top_k,
                            float top_p, uint64_t least, bool draw, float u) {
@@ -765,7 +781,8 @@ template <typename T> struct Sampler {
         uint64_t best = 0;
         for (int i = tid; i < s.count; i += NT) best = max(best, s.list[i]);
         const uint32_t key = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32));
-        const uint32_t id = __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == key ? (uint32_t)best : 0u);
+        const uint32_t id =
+            __reduce_max_sync(0xffffffffu, (uint32_t)(best >> 32) == key ? (uint32_t)best : 0u);
         __syncthreads();
         if (lane == 0) s.part[warp] = (uint64_t)key << 32 | id;
         __syncthreads();
@@ -1028,7 +1045,8 @@ template <typename T> struct Sampler {
     __device__ __forceinline__ int count_from(uint32_t k) { return from_key<false>(k).n; }
     // The largest key in lo .. hi from which on the tokens are `goal`, in number or mass
     // (from lo on they are): bisection, each time to a key that is there.
-    template <bool MASS> __device__ __forceinline__ uint32_t last_key(uint32_t lo, uint32_t hi, uint64_t goal) {
+    template <bool MASS>
+    __device__ __forceinline__ uint32_t last_key(uint32_t lo, uint32_t hi, uint64_t goal) {
         while (lo < hi) {
             const uint32_t mid = lo + (hi - lo + 1) / 2;
             const From f = from_key<MASS>(mid);
@@ -1055,7 +1073,8 @@ template <typename T> struct Sampler {
         else at.ties = live - count_from(bottom + 1);
         int n = at.n;
         if (top_p < 1.f) {
-            const uint64_t all = from_key<true>(at.key + 1).mass + mass_of(of_key(at.key)) * (uint64_t)at.ties;
+            const uint64_t all =
+                from_key<true>(at.key + 1).mass + mass_of(of_key(at.key)) * (uint64_t)at.ties;
             const uint64_t goal = max(share_of(all, top_p, true), (uint64_t)1);
             const uint32_t lo = last_key<true>(at.key, top, goal);
             const From f = from_key<true>(lo + 1);
@@ -1264,7 +1283,9 @@ template <typename T> struct Sampler {
         // (for a long row's k a share of it and some more; were they too few, a histogram
         // finds the place)
         const int rounds = (nvec + kRound - 1) / kRound;
-        const int want = top_k <= 0 ? max(kWant / rounds, 16) : rounds == 1 ? top_k : min(top_k, (3 * min(top_k, 1 << 16)) / (2 * rounds) + 24);
+        const int want = top_k <= 0    ? max(kWant / rounds, 16)
+                         : rounds == 1 ? top_k
+                                       : min(top_k, 3 * min(top_k, 1 << 16) / (2 * rounds) + 24);
         float mx = -INFINITY, lo = lowest_of<T>(), ref = 0.f;
         float under = -INFINITY;
         bool floor = false;
