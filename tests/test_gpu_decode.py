@@ -378,6 +378,26 @@ def test_flat_and_peaked_rows(vsd, dtype, spread):
         check_sample(x, u, vsd.sample_filtered(x, u, filtered=True, **kw), **kw)
 
 
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("V,places", [(300, (1, 2, 40, 150, 299)), (5000, (3, 700, 2500, 4600)),
+                                      (128256, (4, 600, 6000, 30000))])
+def test_nuclei_that_end_at_a_border(vsd, V, places, dtype):
+    """top_p is a prefix's share of the mass, rounded to float32: within 2^-25 of the
+    border, where no approximate sum decides."""
+    R = 3 * len(places)
+    x, u = rows(R, V, dtype, 71)
+    xs = x.double().cpu().numpy()
+    share = []
+    for r in range(R):
+        cum = np.cumsum(reference(xs[r], 1.0, 0, 1.0, 0.0)[1])
+        share.append(cum[places[r % len(places)] - 1] / cum[-1])
+    top_p = torch.tensor(share, dtype=torch.float64).float().cuda()
+    check_sample(x, u, vsd.sample_filtered(x, u, top_p=top_p, filtered=True), top_p=top_p)
+    # and masked but for some: the rest has no mass
+    x[:, 1::2] = -INF
+    check_sample(x, u, vsd.sample_filtered(x, u, top_p=top_p, filtered=True), top_p=top_p)
+
+
 @pytest.mark.parametrize("V", (700, 40000))
 def test_settings_of_every_row(vsd, V):
     R = 48
