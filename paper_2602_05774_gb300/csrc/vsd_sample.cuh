@@ -880,6 +880,9 @@ template <typename T> struct Sampler {
     };
     template <bool COUNT, bool SAMPLE>
     __device__ __forceinline__ void histogram(float per, float unit, const Aim& aim) {
+        // (every thread has read the bins that the last one left: which way row() goes on
+        // hangs on them)
+        __syncthreads();
         for (int i = tid; i < kBins; i += NT) s.order[i] = 0;
         if (tid == 0) s.dec.bin0 = 0, s.dec.bin1 = kBins - 1;
         __syncthreads();

@@ -691,3 +691,80 @@ def test_gradients_of_a_head_that_drafts_in_8_bits(vsd):
         n = V if name == "d_hidden" else R
         # exact products summed in float32, one truncation of 2^-23 a term
         assert bool(((got[name].double() - want).abs() <= n * 2.0 ** -23 * mag + 1e-30).all()), name
+
+
+# ------------------------------------------------------------------ rows that leave the usual way
+def gpu_reference(x, T=1.0, top_p=1.0, min_p=0.0):
+    """Without top_k, in float64 on the GPU: per row the number kept, its nearest distance
+    from a border (relative), and the filtered logits."""
+    V = x.shape[1]
+    xs, order = torch.sort(x.double() + 0.0, dim=1, descending=True, stable=True)
+    e = torch.exp((xs - xs[:, :1]) / f32(T))
+    c = e.cumsum(1)
+    total = c[:, -1:]
+    kept = (xs > -INF).sum(1, keepdim=True)
+    near = torch.full_like(total, INF)
+    if top_p < 1:
+        gap = (c / total - f32(top_p)).abs()
+        near = gap.amin(1, keepdim=True)
+        kept = torch.minimum(kept, (c < f32(top_p) * total).sum(1, keepdim=True) + 1)
+    if min_p > 0:
+        near = torch.minimum(near, (e / min(f32(min_p), 1.0) - 1).abs().amin(1, keepdim=True))
+        kept = torch.minimum(kept, (e >= min(f32(min_p), 1.0)).sum(1, keepdim=True))
+    on = torch.zeros_like(x, dtype=torch.bool).scatter_(
+        1, order, torch.arange(V, device=x.device) < kept)
+    return kept[:, 0].int(), near[:, 0], torch.where(on, x, -INF)
+
+
+def check_on_gpu(x, u, out, **kw):
+    """Every row of a large call: kept tokens, filtered rows, and the draw by its prefix sums."""
+    V = x.shape[1]
+    kept, near, filtered = gpu_reference(x, **kw)
+    margin = 4 * (2.0 ** -41 + V * 2.0 ** -(63 - max(12, (V - 1).bit_length())))
+    sure = near > margin
+    assert int((~sure).sum()) <= len(x) // 50
+    assert torch.equal(out["kept"][sure], kept[sure])
+    assert torch.equal(out["filtered"][sure], filtered[sure])
+    f = out["filtered"].double()
+    e = torch.exp((f - x.double().amax(1, keepdim=True)) / f32(kw.get("T", 1.0)))
+    c = e.cumsum(1)
+    t = out["tokens"].long()[:, None]
+    goal, slack = u.double()[:, None] * c[:, -1:], c[:, -1:] * margin
+    assert bool((f.gather(1, t) > -INF).all())
+    assert bool((c.gather(1, t) > goal - slack).all())
+    assert bool((c.gather(1, t) - e.gather(1, t) <= goal + slack).all())
+
+
+def masked_by_id(R, V, dtype, seed, mask):
+    """Rows of normal logits whose ids are masked by a rule."""
+    x = torch.randn(R, V, generator=gen(seed), device="cuda")
+    ids = torch.arange(V, device="cuda")
+    if mask == "starts":       # the first quarter of each 2048 bf16, or 1024 float32
+        off = ids % (2048 if dtype == torch.bfloat16 else 1024) < (512 if dtype == torch.bfloat16 else 256)
+    elif mask == "ends":       # the other three quarters
+        off = ids % (2048 if dtype == torch.bfloat16 else 1024) >= (512 if dtype == torch.bfloat16 else 256)
+    elif mask == "bands":      # bands of allowed ids, elsewhere in every row
+        n = V // 24
+        at = torch.randint(0, n, (R, 1), generator=gen(seed + 1), device="cuda")
+        off = (ids + at) // n % 4 != 0
+    else:                      # heavy tokens at the regions' ends alone
+        x += 6 * (ids % 2048 >= 1500)
+        off = torch.zeros(V, dtype=torch.bool, device="cuda")
+    return x.masked_fill(off, -INF).to(dtype), torch.rand(R, generator=gen(seed + 2), device="cuda")
+
+
+@pytest.mark.parametrize("mask", ("starts", "ends", "bands", "heavy"))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("V", (40000, 128256))
+def test_nuclei_whose_tokens_a_sample_of_the_row_misses(vsd, V, dtype, mask):
+    """A nucleus past the list is looked for in a quarter of the row first, the first 512
+    bf16 or 256 float32 of each four times as many; masks by id leave that quarter without
+    mass, or without what the nucleus ends at, so that the whole row is asked."""
+    x, u = masked_by_id(608, V, dtype, V, mask)
+    for top_p in (0.5, 0.9, 0.95, 0.99):
+        out = vsd.sample_filtered(x, u, top_p=top_p, filtered=True)
+        check_on_gpu(x, u, out, top_p=top_p)
+        for _ in range(5):
+            again = vsd.sample_filtered(x, u, top_p=top_p, filtered=True)
+            for n in out:
+                assert torch.equal(again[n], out[n]), n
