@@ -53,8 +53,9 @@ vsd_status vsd_quantize_fp8(const void* x, vsd_dtype dtype, int32_t R, int32_t H
  *   logits  device, bf16 [R][V], written
  *   ws      device workspace of at least 256 bytes, its first word the status word,
  *           cleared here
- * Any finite scales, not only powers of two.  Products are exact; a block's 128 are
- * summed on the tensor cores, the blocks in fp32, and the sum is rounded once to
+ * Any finite scales, not only powers of two; the product of two may be past a float's
+ * range, or below it, where a block's scaled sum is not.  Products are exact; a block's
+ * 128 are summed on the tensor cores, the blocks in fp32, and the sum is rounded once to
  * bf16.  H a multiple of 16, hidden and weight 16-byte aligned, logits 2-byte;
  * 1 <= R <= 16777216, 1 <= V <= 1048576, H <= 1048576.  logits may not overlap an
  * input.  A device wait that runs out sets the timeout bit of the status word. */

@@ -3,11 +3,13 @@
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 #include <string.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "vsd_common.cuh"
 #include "vsd_decode.h"
@@ -165,7 +167,7 @@ cudaError_t quantize(const T* x, int R, int H, int block_rows, __nv_fp8_e4m3* q,
 // logits = hidden . weight^T on the tensor cores by pairs of CTAs (tcgen05,
 // kind::f8f6f4, cta_group::2).  A K block is a scale's 128 columns: one 128-byte
 // row of a swizzled tile, four MMAs.  Each K block gets an accumulator of its own
-// (two to eight, in turn), which the epilogue takes from tensor memory, multiplies by the
+// (two or four, in turn), which the epilogue takes from tensor memory, multiplies by the
 // block's scales and adds to the sums in its registers in fp32 while the next ones are
 // computed.  (One accumulator over all of K would need scales that are the same for all
 // blocks.)  Per CTA:
@@ -181,8 +183,10 @@ cudaError_t quantize(const T* x, int R, int H, int block_rows, __nv_fp8_e4m3* q,
 //              and a column a row, whose scales are in shared memory throughout.
 // What bounds them, and what they measured (one GB300, the rows' form by its count):
 //   NF = 0     the epilogue: 128 x 256 fp32 from tensor memory a K block and CTA, 64
-//              FMAs of two each a thread.  4096 x 32000 x 4096: 384 to 437 us as power
-//              allows (2.5 to 2.8 PFLOP/s), 322 without the epilogue.
+//              FMAs of two each a thread.  4096 x 32000 x 4096: 390 to 445 us as power
+//              allows (2.4 to 2.75 PFLOP/s), 322 without the epilogue.  2 % of that asks each
+//              K block whether a lane has a product of scales that is no normal
+//              number (NF > 0 asks once, in front).
 //   NF > 0     memory: 8 x 128256 x 4096 in 87 us, 6.1 TB/s.
 // Either by rows, V = 128256, H = 4096 (us; NF the least that holds them):
 //   rows       1*    8    32    64   100   128      (* V = 32000)
@@ -218,6 +222,8 @@ struct HeadBars {
     uint64_t drain;
     uint32_t tmem_base;
     int err;
+    uint32_t end[4];             // NF > 0: least and largest scale of the rows, and of the
+                                 // weight's blocks (their magnitudes' bits)
 };
 
 template <int NF> struct HeadCfg {
@@ -369,6 +375,24 @@ __device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
     return f2(__uint_as_float(lo), __uint_as_float(hi));
 }
 
+// A block's sum u is at most 2^25, and 2^-18 or more where it is not 0: h w u may be
+// within a float's range although h w is not, or is no normal number.
+__device__ __forceinline__ bool usual(float s) { return fabsf(s) >= FLT_MIN && fabsf(s) <= FLT_MAX; }
+// h w = first . second; (1, h w) where h w is a normal number.  Else the larger and the
+// smaller of them, brought nearer by powers of two: u first is a normal number, and second
+// one or less than 2^-126 where h w u is below 2^-115 (off by 2^-139 then); past a float's
+// range it is its end (u first is 2^30 then, or 0).
+__device__ __forceinline__ void split_scales(float h, float w, float& first, float& second) {
+    const float s = h * w;
+    const bool swap = fabsf(w) > fabsf(h);
+    const float large = swap ? w : h, little = swap ? h : w;
+    const bool over = fabsf(s) > 1.f;
+    const float end = little * 0x1p40f;
+    first = over ? large * 0x1p-40f : little * 0x1p56f;
+    second = over ? (fabsf(end) > FLT_MAX ? copysignf(FLT_MAX, end) : end) : large * 0x1p-56f;
+    if (usual(s)) first = 1.f, second = s;
+}
+
 // The warp's 32 rows x 128 columns, through its box of 32 x 64 (16-byte chunk j of row
 // i at chunk j ^ (i % 8)).
 __device__ __forceinline__ void store_rows(const HeadArgs& a, const CUtensorMap* map, int row0,
@@ -450,6 +474,50 @@ __device__ __forceinline__ void store_rows(const HeadArgs& a, const CUtensorMap*
     }
 }
 
+// NF > 0: whether a product of a row's scale and one of this CTA's tokens' may be no
+// normal number, by the ends of both.  By the epilogue warps, while the first tiles come.
+template <int NF>
+__device__ __forceinline__ bool scales_apart(const HeadArgs& a, HeadBars* sb, const float* row_scale,
+                                             int rank) {
+    const int tid = threadIdx.x - 128, nt = 32 * kEpilogueWarps;
+    uint32_t end[4] = {0x7F800000u, 0, 0x7F800000u, 0};  // by their bits; 0 is left out
+    auto add = [](float s, uint32_t& least, uint32_t& most) {
+        const uint32_t b = __float_as_uint(fabsf(s));
+        least = min(least, b - 1 < 0x7F800000u ? b : least);
+        most = max(most, b);
+    };
+    for (int i = tid; i < NF * a.nk; i += nt) add(row_scale[i], end[0], end[1]);
+    // a tile's tokens are of two blocks at most
+    const HeadJobs<NF> jobs(a);
+    const int tiles = (jobs.total - jobs.t + jobs.C - 1) / jobs.C, last = (a.V - 1) / kBlock;
+    const int64_t n = (int64_t)tiles * 2 * a.nk;
+    for (int64_t i0 = tid; i0 < n; i0 += 4 * nt) {
+        float w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t i = min(i0 + k * nt, n - 1);
+            const int t = (int)(i / (2 * a.nk)), j = (int)(i - (int64_t)t * 2 * a.nk);
+            const int m0 = (jobs.t + t * jobs.C) * 2 * a.high + a.high * rank;
+            const int b = min(min(m0, a.V - 1) / kBlock + (j >= a.nk), last);
+            w[k] = __ldg(a.ws + (size_t)b * a.nk + (j >= a.nk ? j - a.nk : j));
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) add(w[k], end[2], end[3]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        end[k] = k & 1 ? __reduce_max_sync(0xffffffffu, end[k]) : __reduce_min_sync(0xffffffffu, end[k]);
+        if (threadIdx.x % 32 == 0) {
+            if (k & 1) atomicMax(&sb->end[k], end[k]);
+            else atomicMin(&sb->end[k], end[k]);
+        }
+    }
+    asm volatile("bar.sync 1, %0;" :: "n"(32 * kEpilogueWarps) : "memory");
+    const volatile uint32_t* e = sb->end;
+    return !(__uint_as_float(e[0]) * __uint_as_float(e[2]) >= FLT_MIN &&
+             __uint_as_float(e[1]) * __uint_as_float(e[3]) <= FLT_MAX);
+}
+
 template <int NF>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
     k_head_fp8(const __grid_constant__ HeadMaps maps, const HeadArgs a) {
@@ -474,6 +542,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
         for (int b = 0; b < kAcc; ++b) mbar_init(&sb->acc_empty[b], 2 * kEpilogueWarps);
         mbar_init(&sb->drain, 1);
         sb->err = 0;
+        sb->end[0] = sb->end[2] = 0x7F800000u;
+        sb->end[1] = sb->end[3] = 0;
         mbar_init_fence();
     }
     if (NF)
@@ -558,74 +628,108 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kHeadThreads, 1)
         const int q = warp & 3;                          // TMEM lanes 32q .. 32q + 31
         const int h0 = ((warp - 4) >> 2) * kCols;        // its columns of the tile
         const uint32_t empty = tc::leader_addr(&sb->acc_empty[0]);
-        Ring at{0, 0, stages};
-        uint32_t it = 0;
-        bool ok = true;
-        while (ok && jobs.next(a, m0, n0)) {
-            const int in = 32 * q + lane;
-            const int top = m0 + high * rank + in;       // this lane's row (NF = 0) or token
-            // scales: of the lane (`lane_s`), and of the warp's columns
-            const float* lane_s = NF ? a.ws + (size_t)(min(top, a.V - 1) / kBlock) * a.nk
-                                     : a.hs + (size_t)min(top, a.R - 1) * a.nk;
-            const float* col_s =
-                NF ? nullptr : a.ws + (size_t)(min(n0 + h0, a.V - 1) / kBlock) * a.nk;
-            uint64_t x[kCols / 2];  // columns 2i and 2i + 1
+        // The tiles; split: by two factors throughout (NF > 0).
+        auto tiles = [&](auto split) {
+            Ring at{0, 0, stages};
+            uint32_t it = 0;
+            bool ok = true;
+            while (ok && jobs.next(a, m0, n0)) {
+                const int in = 32 * q + lane;
+                const int top = m0 + high * rank + in;       // this lane's row (NF = 0) or token
+                // scales: of the lane (`lane_s`), and of the warp's columns
+                const float* lane_s = NF ? a.ws + (size_t)(min(top, a.V - 1) / kBlock) * a.nk
+                                         : a.hs + (size_t)min(top, a.R - 1) * a.nk;
+                const float* col_s =
+                    NF ? nullptr : a.ws + (size_t)(min(n0 + h0, a.V - 1) / kBlock) * a.nk;
+                uint64_t x[kCols / 2];  // columns 2i and 2i + 1
 #pragma unroll
-            for (int i = 0; i < kCols / 2; ++i) x[i] = 0;
-            float ls = __ldg(lane_s), cs = NF ? 0.f : __ldg(col_s);
-            for (int kb = 0; kb < a.nk; ++kb, ++it, at.next()) {
-                const float s = NF ? ls : ls * cs;
-                if (kb + 1 < a.nk) {
-                    ls = __ldg(lane_s + kb + 1);
-                    if (!NF) cs = __ldg(col_s + kb + 1);
-                }
-                const int buf = (int)(it % kAcc);
-                const uint64_t s2 = f2(s, s);
-                uint64_t c2[NF ? kCols / 2 : 1];  // the products of the two sides' scales
-                if constexpr (NF != 0) {
-                    const float4* c = reinterpret_cast<const float4*>(row_scale + kb * NF + h0);
-#pragma unroll
-                    for (int i = 0; i < kCols / 4; ++i) {
-                        c2[2 * i] = f2mul(f2(c[i].x, c[i].y), s2);
-                        c2[2 * i + 1] = f2mul(f2(c[i].z, c[i].w), s2);
+                for (int i = 0; i < kCols / 2; ++i) x[i] = 0;
+                float ls = __ldg(lane_s), cs = NF ? 0.f : __ldg(col_s);
+                // NF = 0: whether a lane's product is no normal number
+                bool apart = NF == 0 && __any_sync(0xffffffffu, !usual(ls * cs));
+                for (int kb = 0; kb < a.nk; ++kb, ++it, at.next()) {
+                    const float s = NF ? ls : ls * cs;
+                    if (kb + 1 < a.nk) {
+                        ls = __ldg(lane_s + kb + 1);
+                        if (!NF) cs = __ldg(col_s + kb + 1);
                     }
-                }
-                if (!(ok = wait_warp(&sb->done[at.slot], at.round & 1u, sb, a.status))) break;
-                tc::tc_fence_after();
-                const uint32_t t = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * kN + h0);
-                uint32_t u[2][kStep];
-                tmem_ask(t, u[0]);
+                    const int buf = (int)(it % kAcc);
+                    const uint64_t s2 = f2(s, s);
+                    uint64_t c2[NF ? kCols / 2 : 1];  // the products of the two sides' scales
+                    if constexpr (NF != 0 && !split.value) {
+                        const float4* c = reinterpret_cast<const float4*>(row_scale + kb * NF + h0);
 #pragma unroll
-                for (int g = 0; g < kCols / kStep; ++g) {
-                    tmem_arrived(u[g & 1]);
-                    if (g + 1 < kCols / kStep) {
-                        tmem_ask(t + (uint32_t)(kStep * (g + 1)), u[(g + 1) & 1]);
-                    } else {  // all of it is in registers
-                        tc::tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) tc::arrive_remote(empty + 8u * buf);
+                        for (int i = 0; i < kCols / 4; ++i) {
+                            c2[2 * i] = f2mul(f2(c[i].x, c[i].y), s2);
+                            c2[2 * i + 1] = f2mul(f2(c[i].z, c[i].w), s2);
+                        }
                     }
+                    if (!(ok = wait_warp(&sb->done[at.slot], at.round & 1u, sb, a.status))) break;
+                    tc::tc_fence_after();
+                    const uint32_t t = tmem + ((uint32_t)(32 * q) << 16) + (uint32_t)(buf * kN + h0);
+                    bool next_apart = false;
+                    auto take = [&](auto twice) {
+                        float first = 1.f, second = s;
+                        if constexpr (NF == 0 && twice.value)
+                            split_scales(__ldg(lane_s + kb), __ldg(col_s + kb), first, second);
+                        uint32_t u[2][kStep];
+                        tmem_ask(t, u[0]);
 #pragma unroll
-                    for (int i = 0; i < kStep / 2; ++i) {
-                        const int c = kStep / 2 * g + i;
-                        x[c] = f2fma(pair_of(u[g & 1][2 * i], u[g & 1][2 * i + 1]), NF ? c2[NF ? c : 0] : s2,
-                                     x[c]);
-                    }
+                        for (int g = 0; g < kCols / kStep; ++g) {
+                            tmem_arrived(u[g & 1]);
+                            if (g + 1 < kCols / kStep) {
+                                tmem_ask(t + (uint32_t)(kStep * (g + 1)), u[(g + 1) & 1]);
+                            } else {  // all of it is in registers
+                                tc::tc_fence_before();
+                                __syncwarp();
+                                if (lane == 0) tc::arrive_remote(empty + 8u * buf);
+                                // (the next scales have come by now: 2 % less than asked
+                                // for before its wait)
+                                if (NF == 0) next_apart = __any_sync(0xffffffffu, !usual(ls * cs));
+                            }
+#pragma unroll
+                            for (int i = 0; i < kStep / 2; ++i) {
+                                const int c = kStep / 2 * g + i;
+                                uint64_t v = pair_of(u[g & 1][2 * i], u[g & 1][2 * i + 1]);
+                                uint64_t by = NF || twice.value ? 0 : s2;
+                                if constexpr (twice.value) {
+                                    float first1 = first, second1 = second;
+                                    if constexpr (NF != 0) {
+                                        const float* h = row_scale + kb * NF + h0 + 2 * c;
+                                        split_scales(h[0], s, first, second);
+                                        split_scales(h[1], s, first1, second1);
+                                    }
+                                    v = f2mul(v, f2(first, first1));
+                                    by = f2(second, second1);
+                                } else if constexpr (NF != 0) {
+                                    by = c2[c];
+                                }
+                                x[c] = f2fma(v, by, x[c]);
+                            }
+                        }
+                    };
+                    if constexpr (NF != 0) take(split);
+                    else if (apart) take(std::true_type{});
+                    else take(std::false_type{});
+                    apart = next_apart;
                 }
+                if (!ok) break;
+                if constexpr (NF == 0) {
+                    store_rows(a, &maps.o, m0 + 128 * rank + 32 * q, n0 + h0, lane, x,
+                               outs + (warp - 4) * kOutBytes);
+                } else if (in < high && top < a.V) {
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c)
+                        if (h0 + c < a.R)
+                            a.out[(size_t)(h0 + c) * a.V + top] = __float2bfloat16_rn(
+                                __uint_as_float((uint32_t)(x[c / 2] >> (c & 1 ? 32 : 0))));
+                }
+                __syncwarp();
             }
-            if (!ok) break;
-            if constexpr (NF == 0) {
-                store_rows(a, &maps.o, m0 + 128 * rank + 32 * q, n0 + h0, lane, x,
-                           outs + (warp - 4) * kOutBytes);
-            } else if (in < high && top < a.V) {
-#pragma unroll
-                for (int c = 0; c < kCols; ++c)
-                    if (h0 + c < a.R)
-                        a.out[(size_t)(h0 + c) * a.V + top] = __float2bfloat16_rn(
-                            __uint_as_float((uint32_t)(x[c / 2] >> (c & 1 ? 32 : 0))));
-            }
-            __syncwarp();
-        }
+        };
+        if constexpr (NF == 0) tiles(std::false_type{});
+        else if (scales_apart<NF>(a, sb, row_scale, rank)) tiles(std::true_type{});
+        else tiles(std::false_type{});
         if (NF == 0 && lane == 0) tc::bulk_wait_all();
     }
     __syncwarp();

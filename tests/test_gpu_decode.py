@@ -768,3 +768,52 @@ def test_nuclei_whose_tokens_a_sample_of_the_row_misses(vsd, V, dtype, mask):
             again = vsd.sample_filtered(x, u, top_p=top_p, filtered=True)
             for n in out:
                 assert torch.equal(again[n], out[n]), n
+
+
+# ------------------------------------------------------------------ scales whose product leaves float32
+@pytest.mark.parametrize("H", (128, 400))
+@pytest.mark.parametrize("R", (3, 33, 100, 300))
+def test_head_scales_whose_product_is_out_of_range(vsd, R, H):
+    """hidden_scale . weight_scale past float32's range, or below its normal numbers, where
+    the scaled sums are within it: by rows and by the weight's blocks, beside usual ones."""
+    V = 700
+    nk = -(-H // 128)
+    h, _, w, _ = operands(R, V, H, 3 * R + H)
+    g = gen(R)
+    near1 = lambda *n: 1 + torch.rand(*n, generator=g, device="cuda")
+    hs, ws = near1(R, nk), near1(6, nk)
+    # blocks whose sums are 0 under scales of any size: a zero row, a zero block of the weight
+    h[0] = 0
+    w[128:256] = 0
+    big, small = 2.0 ** 100, 2.0 ** -75
+    hs[0] *= big
+    ws[1] *= big
+    # a row of 2^-75: times a block of 2^-68 (normal), 2^-73 (subnormal) and 2^-90 (nothing)
+    hs[1] *= small
+    ws[2] *= 2.0 ** -68
+    ws[3] *= 2.0 ** -73
+    ws[4] *= 2.0 ** -90
+    # 2^-9 . 2^-9 under 2^127 . 2^8: 2^117
+    h[2], hs[2] = 0, hs[2] * 0 + 1.5 * 2.0 ** 126
+    h[2, 5] = 2.0 ** -9
+    w[640:, 5] = 2.0 ** -9
+    ws[5] *= 2.0 ** 8
+    h[2, 6:] = 0
+    w[0:128, 5] = 1.0
+    ws[0] *= 2.0 ** -20
+    out = vsd.lmhead_logits_fp8(h, hs, w, ws)
+    x, err = head_reference(h, hs, w, ws)
+    sure = x.abs() < 2.0 ** 127  # (the others are past bf16)
+    assert bool(sure[:2].all()) and bool(sure[2, 640:].all()) and bool(sure[2, :256].all())
+    assert float(x[2, 640:].abs().max()) > 2.0 ** 110 and float(x[1, 384:512].abs().max()) > 0
+    tol = err + 2.0 ** -8 * (x.abs() + err) + 2.0 ** -133
+    off = (out.double() - x).abs()
+    assert bool((off <= tol)[sure].all())
+    assert not bool(torch.isnan(out).any())
+    # a row's logits hang on its own scales alone
+    for r in range(3):
+        part = vsd.lmhead_logits_fp8(h[r:r + 1].contiguous(), hs[r:r + 1].contiguous(), w, ws)
+        assert torch.equal(part[0], out[r]), r
+    if R > 3:
+        plain = vsd.lmhead_logits_fp8(h[3:].contiguous(), hs[3:].contiguous(), w, ws)
+        assert torch.equal(plain, out[3:])
