@@ -407,10 +407,11 @@ template <typename T> struct Sampler {
         under = fmaxf(under, top);
         if (TAIL) sum.add(approx_sum(q, ref));
     }
-    // How far an approximate sum may be off (and 2^-28 of the first token, for terms of
-    // large exponents).
-    __device__ __forceinline__ uint64_t tail_slack(uint64_t tail) const {
-        return (tail >> 17) + (1ull << (62 - sc.shift) >> 28) + 1;
+    // How far an approximate sum, `bits` known, may be off the exact one: 2^-28 of the first
+    // token for terms of large exponents, and what whole numbers are off, a unit for each
+    // token.
+    __device__ __forceinline__ uint64_t slack_of(uint64_t tail, int bits) const {
+        return (tail >> bits) + (1ull << (62 - sc.shift) >> 28) + (uint64_t)a.V;
     }
     __device__ __forceinline__ uint64_t fixed_of(float v) const {
         return __float2ull_rn(v * ldexpf(1.f, 62 - sc.shift));
@@ -497,7 +498,7 @@ template <typename T> struct Sampler {
         f.above = block_sum(f.above);
         f.n_above = (int)block_sum((uint64_t)f.n_above);
         f.tail = TAIL ? block_sum(f.tail) : 0;
-        f.slack = TAIL ? tail_slack(f.tail) : 0;
+        f.slack = TAIL ? slack_of(f.tail, 17) : 0;
         return f;
     }
     // The approximate mass of what is below `lo` once more, off by 2^-20 of itself at most:
@@ -520,7 +521,7 @@ template <typename T> struct Sampler {
             sum.add(t);
         });
         f.tail = block_sum(fixed_of(sum.hi + sum.lo));
-        f.slack = (f.tail >> 20) + (1ull << (62 - sc.shift) >> 28) + 1;
+        f.slack = slack_of(f.tail, 20);
     }
     // The exact one.
     __device__ __forceinline__ void exact_tail(float lo, Found& f) {
@@ -1367,7 +1368,7 @@ template <typename T> struct Sampler {
                 f.tail = fixed_of(t);
                 made = !__syncthreads_or(!(t < 2e6f) || !(sum.hi < 1e30f) || !(ref > -INFINITY));
                 f.tail = block_sum(f.tail);
-                f.slack = tail_slack(f.tail);
+                f.slack = slack_of(f.tail, 17);
             }
             f.below = __syncthreads_or(under > -INFINITY);
             // A list from `low` on, behind what is from `high` on, until one decides.  First the

@@ -817,3 +817,27 @@ def test_head_scales_whose_product_is_out_of_range(vsd, R, H):
     if R > 3:
         plain = vsd.lmhead_logits_fp8(h[3:].contiguous(), hs[3:].contiguous(), w, ws)
         assert torch.equal(plain, out[3:])
+
+
+@pytest.mark.parametrize("top_p24", (3, 9, 12, 17, 22, 30))
+def test_a_nucleus_is_the_same_with_all_tokens_as_its_k(vsd, top_p24):
+    """top_k = V leaves all tokens, as top_k = 0 does, by another way through the row.  The
+    rest of this row, 2^20 tokens, weighs 1.49 units each: as whole numbers a third less."""
+    V = 1 << 20
+    x = torch.full((1, V), math.log(1.49) - 42 * math.log(2), device="cuda")
+    x[0, 16:16 * 201:16] = -26 * math.log(2) - torch.arange(200, device="cuda") * 1e-4
+    x[0, 5] = 0.0
+    u = torch.tensor([0.3], device="cuda")
+    p = 1 - top_p24 * 2.0 ** -24
+    a = vsd.sample_filtered(x, u, top_p=p, filtered=True)
+    b = vsd.sample_filtered(x, u, top_p=p, top_k=V, filtered=True)
+    for n in a:
+        assert torch.equal(a[n], b[n]), (n, a["kept"], b["kept"])
+    # and by whole numbers
+    e = np.exp(np.sort(x[0].double().cpu().numpy())[::-1])
+    m = np.rint(e * 2.0 ** 42)
+    goal, cum = p * m.sum(), np.cumsum(m)
+    n = int((cum < goal).sum()) + 1
+    if n <= 201:  # (else it ends among the small ones, whose number a unit decides)
+        assert np.abs(cum - goal).min() > 2 * n  # (a unit for each of the n)
+        assert int(a["kept"]) == n
