@@ -100,7 +100,8 @@ size_t vsd_sample_filtered_workspace_bytes(int32_t R, int32_t V);
  * are the first n = min(k, n_p, n_m):
  *   k    top_k, or all that are not at -inf
  *   n_p  the least n with e_1 + .. + e_n >= top_p (e_1 + .. + e_k)
- *   n_m  the number with e_i >= min_p
+ *   n_m  the number with e_i >= min_p (decided on the logits, to within 2^-39 of min_p,
+ *        however small)
  * Drawn is the first token v, in the vocabulary's order, with
  * sum of e over the kept tokens up to v  >  u[r] (sum of e over all kept);
  * u >= 1 draws the last kept token, u < 0 (or NaN) the first.

@@ -132,6 +132,22 @@ __host__ __device__ __forceinline__ uint64_t exp_fixed(float x, float m, const E
     return sh < 64 ? (v + (1ull << (sh - 1))) >> sh : 0;
 }
 
+// -ln(p) in two floats, for 0 < p < 1, off by 2^-40 at most (2^-42 from p = 1/2 on): p = f 2^-k with 1/2 <= f < 1,
+// ln(f) is the float l = logf(f) and what f exp(-l) is off 1.
+__host__ __device__ __forceinline__ float neg_log(float p, const uint64_t* tab, float& lo) {
+    int k;
+    const float f = frexpf(p, &k), l = logf(f), n = (float)-k;
+    const uint64_t near = exp_fixed(l, 0.f, exp_scale(1.f, 12), tab);  // exp(l) in 2^-50
+    const float t = (float)((int64_t)(uint64_t)(f * 0x1p50f) - (int64_t)near) * 0x1p-50f / f;
+    const float kLn2 = 0.693147182464599609375f, kLn2Lo = -1.904654300e-9f;
+    const float a = VSD_MUL(n, kLn2);
+    const float al = VSD_FMA(n, kLn2Lo, VSD_FMA(n, kLn2, -a));
+    const float s = VSD_ADD(a, -l), b = VSD_ADD(s, -a);
+    const float sl = VSD_ADD(VSD_ADD(a, -VSD_ADD(s, -b)), -VSD_ADD(l, b));
+    lo = VSD_ADD(VSD_ADD(sl, al), -t);
+    return s;
+}
+
 // ln(e / w) for e, w in such units, e = exp((x - m) / T) and w a sum of such with e
 // among them: -(m - x) / T - ln(w), rounded once but for some 2^-8 of a step.  ln(w)
 // is the float l = logf(w) and what w exp(-l) is off 1.

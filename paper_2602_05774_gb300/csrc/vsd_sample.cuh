@@ -243,6 +243,8 @@ template <typename T> struct Sampler {
     int depth;
     float m, T_, c, base;  // (base: where a histogram's bins begin)
     float above_from;      // of the list at hand
+    bool by_min;           // whether min_p is on: tokens as far below the first one as
+    float far, far_lo;     // T ln(1 / min_p), in two floats, or nearer have it
     ExpScale sc;
 
     __device__ Sampler(const SampleArgs& args, Shared& sh) : a(args), s(sh) {
@@ -333,6 +335,12 @@ template <typename T> struct Sampler {
     // The id of element 0 of vector j.
     __device__ __forceinline__ int id_of(int j) const { return j * PV - off; }
     __device__ __forceinline__ uint64_t mass_of(float v) const { return exp_fixed(v, m, sc, s.tab); }
+    // By the logits' distance, to within 2^-39 of min_p: a mass has a unit's precision only.
+    __device__ __forceinline__ bool has_min(float v) const {
+        float lo;
+        const float d = gap(v, m, lo);
+        return (d - far) + (lo - far_lo) <= 0.f;  // (NaN where m - v is past a float's range)
+    }
     __device__ __forceinline__ float approx(float v) const { return ex2((v - m) * c); }
     // f(vector, j) for this thread's vectors of the row, end(region) after a region's.
     template <typename F, typename E> __device__ __forceinline__ void each(F f, E end) const {
@@ -625,11 +633,11 @@ template <typename T> struct Sampler {
 
     // From the list of n: every filter's place, the kept tokens and, where they are all
     // listed, the draw.  By G threads, Q entries each.  f: what is before and behind the
-    // list; `floor`: no token behind it has `least`; `known`: the mass of the first top_k,
+    // list; `floor`: no token behind it has min_p; `known`: the mass of the first top_k,
     // whose place is not looked for again.
     template <int G, int Q>
     __device__ __forceinline__ void decide(int n, const Found& f, bool floor, uint64_t known, int top_k,
-                           float top_p, uint64_t least, bool draw, float u) {
+                           float top_p, bool draw, float u) {
         if constexpr (Q > 1) sort<Q, uint64_t, true>(s.list, n);  // (else it is sorted)
         // masses and their prefix sums, Q entries a thread
         uint64_t e[Q], own = 0;
@@ -637,10 +645,11 @@ template <typename T> struct Sampler {
 #pragma unroll
         for (int i = 0; i < Q; ++i) {
             const int p = tid * Q + i;
-            e[i] = p < n ? mass_of(of_key((uint32_t)(s.list[p] >> 32))) : 0;
+            const float v = p < n ? of_key((uint32_t)(s.list[p] >> 32)) : -INFINITY;
+            e[i] = p < n ? mass_of(v) : 0;
             if (p < n) s.mass[p] = e[i];
             own += e[i];
-            big += p < n && e[i] >= least;
+            big += by_min && p < n && has_min(v);
         }
         uint64_t listed;
         const uint64_t before = f.above + group_scan<G>(own, listed);
@@ -648,10 +657,10 @@ template <typename T> struct Sampler {
         const int A = f.n_above + n, kNone = INT_MAX;
         const int big_n = (int)group_sum<G>((uint64_t)big);
         const int pos_k = known ? kNone : top_k > 0 && top_k <= A ? top_k : f.below ? kNone : A;
-        const int pos_m = least == 0 || (big_n == n && f.below && !floor) ? kNone : f.n_above + big_n;
+        const int pos_m = !by_min || (big_n == n && f.below && !floor) ? kNone : f.n_above + big_n;
         int kept = min(pos_k, pos_m), what = kDone;
         // (known: those behind the first top_k are not kept; here they are behind the place)
-        if (pos_k <= f.n_above || (least != 0 && big_n == 0 && f.n_above > 0 && !floor)) {
+        if (pos_k <= f.n_above || (by_min && big_n == 0 && f.n_above > 0 && !floor)) {
             what = kSearch;  // a place is among those above
         } else if (top_p < 1.f) {
             uint64_t w0, w1;  // the mass that top_p is a share of, at least and at most
@@ -761,18 +770,18 @@ template <typename T> struct Sampler {
     // The same by as few threads as the list needs (what the others would do takes issue
     // slots from the SM's other block).
     __device__ __forceinline__ void decide_by(int n, const Found& f, bool floor, uint64_t known, int top_k,
-                              float top_p, uint64_t least, bool draw, float u) {
+                              float top_p, bool draw, float u) {
         __syncthreads();
         if (n <= NT / 2) sort_by_rank(n);
         else if (n <= NT) sort<1, uint64_t, true>(s.list, n);
         if (n <= 32) {
-            if (warp == 0) decide<32, 1>(n, f, floor, known, top_k, top_p, least, draw, u);
+            if (warp == 0) decide<32, 1>(n, f, floor, known, top_k, top_p, draw, u);
         } else if (n <= NT) {
-            decide<NT, 1>(n, f, floor, known, top_k, top_p, least, draw, u);
+            decide<NT, 1>(n, f, floor, known, top_k, top_p, draw, u);
         } else if (n <= 2 * NT) {
-            decide<NT, 2>(n, f, floor, known, top_k, top_p, least, draw, u);
+            decide<NT, 2>(n, f, floor, known, top_k, top_p, draw, u);
         } else {
-            decide<NT, kList / NT>(n, f, floor, known, top_k, top_p, least, draw, u);
+            decide<NT, kList / NT>(n, f, floor, known, top_k, top_p, draw, u);
         }
         __syncthreads();
     }
@@ -848,7 +857,7 @@ template <typename T> struct Sampler {
     // rest's mass made exact where that is needed.  (f: of a list that is there; else it is
     // made.)
     __device__ __forceinline__ int settle(const Found* made, float hi, float lo, bool floor, uint64_t known,
-                          int top_k, float top_p, uint64_t least, bool draw, float u) {
+                          int top_k, float top_p, bool draw, float u) {
         const bool tail = top_p < 1.f && top_k <= 0;
         __syncthreads();
         Found f = made ? *made : tail ? collect<true>(hi, lo) : collect<false>(hi, lo);
@@ -860,11 +869,11 @@ template <typename T> struct Sampler {
             return kOverflow;
         }
         if (made && top_k > 0 && n > top_k && n > 64 && n <= NT) n = prune(n, top_k, f);
-        if (made && tail && n > NT / 4 && least == 0 && past(n, f, top_p)) return kBracket;
+        if (made && tail && n > NT / 4 && !by_min && past(n, f, top_p)) return kBracket;
         for (int more = 0;; ++more) {
             if (more == 1) finer_tail(lo, f);
             else if (more == 2) exact_tail(lo, f);
-            decide_by(n, f, floor, known, top_k, top_p, least, draw, u);
+            decide_by(n, f, floor, known, top_k, top_p, draw, u);
             if (s.dec.what != kExactTail) return s.dec.what;
         }
     }
@@ -1069,7 +1078,7 @@ template <typename T> struct Sampler {
         return Place{k, n - count_from(k + 1), n};
     }
     // Every filter's place by bisection; leaves cut, limit and kept.
-    __device__ __forceinline__ void search(uint32_t top, int top_k, float top_p, uint64_t least) {
+    __device__ __forceinline__ void search(uint32_t top, int top_k, float top_p) {
         const uint32_t bottom = kKeyNone + 1;
         const int live = count_from(bottom);
         Place at{bottom, live, live};
@@ -1085,11 +1094,11 @@ template <typename T> struct Sampler {
             const uint64_t one = max(mass_of(of_key(lo)), (uint64_t)1);
             n = (int)min((uint64_t)n, (uint64_t)f.n + (goal - f.mass + one - 1) / one);
         }
-        if (least != 0) {
+        if (by_min) {
             uint32_t lo = bottom, hi = top;
-            while (lo < hi) {  // the lowest logit whose mass suffices
+            while (lo < hi) {  // the lowest logit that has min_p
                 const uint32_t mid = lo + (hi - lo) / 2;
-                if (mass_of(of_key(mid)) >= least) hi = mid;
+                if (has_min(of_key(mid))) hi = mid;
                 else lo = mid + 1;
             }
             n = min(n, count_from(lo));
@@ -1269,16 +1278,18 @@ template <typename T> struct Sampler {
         if (top_p <= 0.f) top_k = 1, top_p = 1.f;
         sc = exp_scale(T_, a.shift);
         c = sc.c;
-        // min_p as a mass
-        const uint64_t one = 1ull << (62 - sc.shift);
-        const uint64_t least = !(min_p > 0.f) ? 0
-                               : min_p >= 1.f ? one
-                                              : max(share_of(one, min_p, true), (uint64_t)1);
-        const bool filters = top_k > 0 || top_p < 1.f || least != 0;
+        by_min = min_p > 0.f;
+        far = far_lo = 0.f;
+        if (by_min && min_p < 1.f) {
+            float lo;
+            const float l = neg_log(min_p, s.tab, lo);
+            far = T_ * l;
+            far_lo = fmaf(T_, lo, fmaf(T_, l, -far));
+        }
+        const bool filters = top_k > 0 || top_p < 1.f || by_min;
         const bool tail = top_p < 1.f && top_k <= 0;
-        // how far below the maximum min_p reaches, and what rounding may make of it
-        const float span = least != 0 && least < one ? -T_ * logf(min_p) : 0.f;
-        auto rounding = [&](float top) { return (span + fabsf(top) + T_) * 1e-5f; };
+        // what rounding may make of the logit that min_p ends at
+        auto rounding = [&](float top) { return (far + fabsf(top) + T_) * 1e-5f; };
 
         constexpr int kRound = kWarps * 32 * kLoad;
         // one pass: the maximum, the list and the rest's mass.  After the first round of
@@ -1320,9 +1331,9 @@ template <typename T> struct Sampler {
                 const uint32_t lo_key = top_k == 1 ? top : t << 16 | ones;
                 ref = of_key(top);
                 lo = lo_key <= (kKeyNone | 0xFFFFu) ? lowest_of<T>() : of_key(lo_key);
-                if (least != 0 && top_p >= 1.f) {
+                if (by_min && top_p >= 1.f) {
                     // no token below max + T ln(min_p) is kept, and the maximum may grow
-                    const float bound = ref - span - rounding(ref);
+                    const float bound = ref - far - rounding(ref);
                     floor = top_k <= 0 || bound > lo;
                     if (floor) lo = down_to<T>(bound);
                 }
@@ -1383,8 +1394,8 @@ template <typename T> struct Sampler {
             for (;; made = false) {
                 what = step == kFirst && top_k == 1 && s.count <= kList
                            ? first_alone()
-                           : settle(made ? &f : nullptr, high, low, floor, known, top_k, top_p, least,
-                                    draw, u);
+                           : settle(made ? &f : nullptr, high, low, floor, known, top_k, top_p, draw,
+                                    u);
                 if (what == kDone) break;
                 if (step == kFirst && what == kOverflow && tail) {
                     // (a bound that a quarter of the entries at hand reach)
@@ -1393,13 +1404,13 @@ template <typename T> struct Sampler {
                     low = lo = raised;
                     continue;
                 }
-                if (step == kFirst && (what == kBracket ? least != 0
+                if (step == kFirst && (what == kBracket ? by_min
                                                         : what != kAbove && (floor || top_k > 0))) {
                     step = kNear;
                     whole = what == kBracket ? s.dec.all : 0;
                     listed = s.dec.listed;
-                    high = up_to<T>(m - span + rounding(m));
-                    low = down_to<T>(m - span - rounding(m));
+                    high = up_to<T>(m - far + rounding(m));
+                    low = down_to<T>(m - far - rounding(m));
                     floor = floor || what == kBracket;
                     if (floor) continue;
                     // the k-th token: among those at hand, or past them
@@ -1441,7 +1452,7 @@ template <typename T> struct Sampler {
                 edges(per, high, low);
             }
             if (what != kDone) {
-                search(top, top_k, top_p, least);
+                search(top, top_k, top_p);
                 if (tid == 0) s.dec.token = -1;
                 sums = true;
             }

@@ -841,3 +841,50 @@ def test_a_nucleus_is_the_same_with_all_tokens_as_its_k(vsd, top_p24):
     if n <= 201:  # (else it ends among the small ones, whose number a unit decides)
         assert np.abs(cum - goal).min() > 2 * n  # (a unit for each of the n)
         assert int(a["kept"]) == n
+
+
+TINY = (2.0 ** -149, 1e-38, 1e-30, 1e-20, 1e-15, 3e-13, 1e-12, 1e-9)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("V", (700, 5000, 40000, 1 << 20))
+def test_min_p_far_below_the_units_of_the_sums(vsd, V, dtype):
+    """Which tokens reach min_p of the first one's probability, where their masses are a
+    few units of the sums, or none: by the logits' distance."""
+    for i, min_p in enumerate(TINY):
+        g = gen(i)
+        x = -120 * torch.rand(2, V, generator=g, device="cuda")
+        x[1] = x[1] / 40 - 27.5  # many near 1e-12
+        x[:, V // 3] = 0.0
+        x[:, -1] = -INF
+        x = (x * 1.25).to(dtype)
+        u = torch.rand(2, generator=g, device="cuda")
+        for kw in (dict(), dict(top_k=300), dict(top_p=0.999)):
+            kw = dict(kw, min_p=min_p, T=1.25)
+            out = vsd.sample_filtered(x, u, filtered=True, **kw)
+            # (a log probability also has what the whole numbers of V masses are off, a unit
+            # each of a sum of 1 at least: taken out for the comparison of the others)
+            lq, units = out["logq_tok"].double().cpu(), V * 2.0 ** -(62 - max(12, (V - 1).bit_length()))
+            for r in range(2):
+                y = x[r].double().cpu().numpy() / 1.25
+                on = out["filtered"][r].float().cpu().numpy() > -INF
+                want = y[int(out["tokens"][r])] - y.max() - math.log(np.exp(y[on] - y.max()).sum())
+                assert abs(float(lq[r]) - want) <= U * abs(want) + 2.0 ** -38 * (1 + abs(want)) + units
+                out["logq_tok"][r] = want
+            check_sample(x, u, out, **kw)
+
+
+def test_min_p_next_to_a_logit(vsd):
+    """min_p on either side of a token's probability, by steps of float32."""
+    d = torch.tensor([0.0, 0.5, 3.0, 17.0, 29.0, 33.5, 60.0, 87.0], device="cuda")
+    for T in (0.7, 1.0, 3.0):
+        for m in (0.0, 11.25, -300.0):
+            x = (m - T * d)[None].contiguous()
+            e = np.exp((x[0].double().cpu().numpy() - float(x[0, 0])) / f32(T))
+            for i in range(1, 8):
+                p0 = np.float32(e[i])
+                for p in (np.nextafter(p0, np.float32(0)), p0, np.nextafter(p0, np.float32(1))):
+                    if abs(float(p) / e[i] - 1) < 2.0 ** -38:
+                        continue
+                    out = vsd.filter_logits(x, T=T, min_p=float(p))
+                    assert int(out["kept"]) == int((e >= float(p)).sum()), (T, m, i, p)
