@@ -12,6 +12,8 @@
 #pragma once
 
 #include <cuda_runtime.h>
+#include <float.h>
+#include <math.h>
 #include <stdint.h>
 
 namespace vsd {
@@ -156,6 +158,7 @@ __host__ __device__ __forceinline__ float log_share(float x, float m, float T, u
     float inv, inv_lo, e;
     over(1.f, 0.f, T, inv, inv_lo);
     const float d = gap(x, m, e), y = VSD_MUL(d, inv);
+    if (!(y <= FLT_MAX)) return -INFINITY;  // (past a float's range)
     const float yl = VSD_FMA(e, inv, VSD_FMA(d, inv_lo, VSD_FMA(d, inv, -y)));
     const float one = ldexpf(1.f, shift - 62);
     const float l = logf((float)w * one);

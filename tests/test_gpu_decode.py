@@ -888,3 +888,20 @@ def test_min_p_next_to_a_logit(vsd):
                         continue
                     out = vsd.filter_logits(x, T=T, min_p=float(p))
                     assert int(out["kept"]) == int((e >= float(p)).sum()), (T, m, i, p)
+
+
+def test_log_probability_past_a_floats_range(vsd):
+    """The last kept token (u = 1) of a row whose logits lie further apart than floats go."""
+    u = torch.ones(1, device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        top = torch.finfo(dtype).max
+        for x, T in (((top, -top), 1.0), ((0.9 * top, -0.3 * top), 1.0), ((0.0, -1e25), 2.0 ** -64),
+                     ((0.0, -top), 0.5)):
+            x = torch.tensor([x], device="cuda").to(dtype)
+            for kw in (dict(), dict(top_k=2)):
+                out = vsd.sample_filtered(x, u, T=T, **kw)
+                assert int(out["tokens"]) == 1 and int(out["kept"]) == 2
+                assert float(out["logq_tok"]) == -INF, (x, T, out["logq_tok"])
+        x = torch.tensor([[0.0, -1e30]], device="cuda").to(dtype)
+        out = vsd.sample_filtered(x, u, T=2.0)
+        assert float(out["logq_tok"]) == float(x[0, 1]) / 2
