@@ -150,11 +150,12 @@ template <> __device__ __forceinline__ float lowest_of<float>() { return -FLT_MA
 template <> __device__ __forceinline__ float lowest_of<__nv_bfloat16>() {
     return __uint_as_float(0xFF7F0000u);
 }
-// The nearest value of the type at or below, or above.
+// The nearest value of the type at or below, or above; down, the lowest finite one at least
+// (from -inf on, tokens without mass and what pads a row's ends would be listed).
 template <typename T> __device__ __forceinline__ float down_to(float v);
-template <> __device__ __forceinline__ float down_to<float>(float v) { return v; }
+template <> __device__ __forceinline__ float down_to<float>(float v) { return fmaxf(v, -FLT_MAX); }
 template <> __device__ __forceinline__ float down_to<__nv_bfloat16>(float v) {
-    return __bfloat162float(__float2bfloat16_rd(v));
+    return fmaxf(__bfloat162float(__float2bfloat16_rd(v)), lowest_of<__nv_bfloat16>());
 }
 template <typename T> __device__ __forceinline__ float up_to(float v);
 template <> __device__ __forceinline__ float up_to<float>(float v) { return v; }

@@ -905,3 +905,36 @@ def test_log_probability_past_a_floats_range(vsd):
         x = torch.tensor([[0.0, -1e30]], device="cuda").to(dtype)
         out = vsd.sample_filtered(x, u, T=2.0)
         assert float(out["logq_tok"]) == float(x[0, 1]) / 2
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("V", (20000, 128256))
+def test_rows_that_begin_masked(vsd, V, dtype):
+    """The first tokens, all that a block reads before it has a bound, are at -inf, or at
+    the type's lowest value; a row may end so too."""
+    x, u = rows(9, V, dtype, 17)
+    low = torch.finfo(dtype).min
+    lead = 16400
+    x[:3, :lead] = -INF
+    x[3:5, :lead] = low
+    x[5, :V - 1] = -INF
+    x[6, :] = low                    # equals at the lowest value
+    x[6, ::3] = -INF
+    x[7, :] = -INF                   # one token, at the lowest value
+    x[7, V - 2] = low
+    x[8, 7:] = -INF
+    for kw in SETTINGS:
+        check_sample(x, u, vsd.sample_filtered(x, u, filtered=True, **kw), **kw)
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("V", (3, 100, 1023, 4001))
+def test_rows_at_the_lowest_value_beside_masked_tokens(vsd, V, dtype):
+    """min_p's bound below a maximum at the type's lowest value is -inf."""
+    x = torch.full((4, V), torch.finfo(dtype).min, device="cuda", dtype=dtype)
+    x[1, ::2] = -INF
+    x[2, :-1] = -INF
+    x[3, 1:] = -INF
+    u = torch.tensor([0.0, 0.7, 1.0, 0.3], device="cuda")
+    for kw in SETTINGS + [dict(min_p=1e-30), dict(min_p=0.5, top_k=3)]:
+        check_sample(x, u, vsd.sample_filtered(x, u, filtered=True, **kw), **kw)
