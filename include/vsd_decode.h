@@ -13,8 +13,11 @@
  * from.  Under a policy both models' rows are filtered, and the filtered rows go to
  * vsd_verify_paths, vsd_estep_mstep and the tree calls, to which a logit of -inf is
  * a token without mass; at the policy's T their softmax is the renormalised kept
- * distribution.  vsd_lmhead_backward takes the logits of an 8-bit head as it takes
- * those of the bf16 one (a gradient straight through the rounding of the weight).
+ * distribution.  (A correction may be a token that the draft's policy leaves out: its
+ * logq_corr is -inf, the gradient, which has no log q in it, is finite, and the loss is
+ * infinite in vsd_tree_estep_mstep, while vsd_estep_mstep counts -2^20 for it.)
+ * vsd_lmhead_backward takes the logits of an 8-bit head as it takes those of the bf16
+ * one (a gradient straight through the rounding of the weight).
  *
  * The conventions of vsd.h hold: device pointers owned by the caller, work enqueued
  * on `stream`, argument checks before anything is enqueued, data errors in the

@@ -938,3 +938,130 @@ def test_rows_at_the_lowest_value_beside_masked_tokens(vsd, V, dtype):
     u = torch.tensor([0.0, 0.7, 1.0, 0.3], device="cuda")
     for kw in SETTINGS + [dict(min_p=1e-30), dict(min_p=0.5, top_k=3)]:
         check_sample(x, u, vsd.sample_filtered(x, u, filtered=True, **kw), **kw)
+
+
+# ------------------------------------------------------------------ lengths between the others
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("V", (4097, 8192, 8193, 16384, 200003, 262144))
+def test_rows_of_one_round_and_past_the_usual(vsd, V, dtype):
+    for i, kw in enumerate((dict(top_p=0.95), dict(top_p=0.8, T=1.5), dict(top_k=200, top_p=0.9), dict(top_k=2000),
+                            dict(top_p=0.9, min_p=1e-4), dict(T=0.0))):
+        x, u = rows(4, V, dtype, 300 + i)
+        check_sample(x, u, vsd.sample_filtered(x, u, filtered=True, **kw), **kw)
+
+
+def filtered_pair(vsd, R, V, dtype, seed, **kw):
+    """Draft and target rows that differ, both filtered in place by one policy."""
+    g = gen(seed)
+    q = 3 * torch.randn(R, V, generator=g, device="cuda")
+    p = (q + 1.5 * torch.randn(R, V, generator=g, device="cuda")).to(dtype)
+    q = q.to(dtype)
+    vsd.filter_logits(q, out=q, **kw)
+    vsd.filter_logits(p, out=p, **kw)
+    return q, p
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("kw", (dict(top_k=8), dict(top_p=0.6), dict(min_p=0.1, top_k=30, top_p=0.9)))
+def test_corrections_are_of_the_targets_kept_tokens(vsd, oracle, dtype, kw):
+    B, K, D, V, T = 2, 3, 4, 600, 0.9
+    R = B * K * D
+    q, p = filtered_pair(vsd, R, V, dtype, 41, T=T, **kw)
+    u = torch.rand(3, R, generator=gen(42), device="cuda")
+    z = vsd.sample_paths(q, u[0], K, D, T)
+    got = vsd.verify_paths(q, p, z["tokens"], u[1], u[2], K, D, T)
+    orc = oracle.linear(q.float().cpu().numpy(), p.float().cpu().numpy(), T, u[0].cpu().numpy(), u[1].cpu().numpy(),
+                        u[2].cpu().numpy(), K, D)
+    assert np.array_equal(orc["accept_len"].reshape(-1), got["accept_len"].cpu().numpy())
+    assert np.array_equal(orc["corr_tokens"].reshape(-1), got["corr_tokens"].cpu().numpy())
+    # every path's first token that was not accepted is drawn from the target's rows
+    corr = got["corr_tokens"].reshape(B * K, D).long()
+    n = got["accept_len"].reshape(B * K).long()
+    at = n.clamp(max=D - 1)[:, None]
+    rejected = (n < D)
+    assert bool(rejected.any())
+    kept = p.reshape(B * K, D, V).gather(1, at[..., None].expand(-1, 1, V))[:, 0]
+    assert bool((kept.gather(1, corr.gather(1, at))[rejected] > -INF).all())
+
+
+def filtered_tree(vsd, B, N, depth, topk, V, seed, dtype, **kw):
+    """A tree problem on the GPU whose rows are filtered; a node's token is its rank among
+    the kept ones of its parent's draft row."""
+    from paper_2602_05774_gb300 import inputs
+    p = inputs.tree_problem(B, N, depth, topk, V, seed=seed)
+    p = {k: v.cuda() if torch.is_tensor(v) else v for k, v in p.items()}
+    for n in ("draft", "target"):
+        p[n] = p[n].to(dtype)
+        vsd.filter_logits(p[n], out=p[n], **kw)
+    rows = (torch.arange(B, device="cuda").view(B, 1) * N + p["parent"].clamp(min=0).long()).view(-1)
+    q = p["draft"].float()[rows]
+    assert bool((q.gather(1, p["tokens"].long().view(-1, 1))[p["parent"].view(-1) >= 0] > -INF).all())
+    return p
+
+
+TREES = [(3, 12, 4, 3, 777), (2, 30, 6, 5, 4097), (4, 60, 8, 10, 1000)]
+
+
+@pytest.mark.parametrize("rule", (0, 1))
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+@pytest.mark.parametrize("shape", TREES)
+def test_filtered_rows_in_tree_verification(vsd, oracle, shape, dtype, rule):
+    from tests.parity import compare_tree, compare_tree_sequential
+    B, N = shape[:2]
+    for T, kw in ((1.0, dict(top_k=24)), (0.8, dict(top_k=40, top_p=0.995, min_p=1e-4))):
+        p = filtered_tree(vsd, *shape, 7, dtype, T=T, **dict(kw, top_p=1.0) if shape[3] > 3 else kw)
+        got = vsd.verify_tree(p["draft"], p["target"], p["parent"], p["tokens"], p["u_accept"], p["u_correct"], T,
+                              rule=rule)
+        c = {k: v.float().cpu().numpy() if v.dtype != torch.int32 else v.cpu().numpy()
+             for k, v in p.items() if torch.is_tensor(v)}
+        orc = oracle.tree(c["draft"], c["target"], T, c["parent"], c["tokens"], c["u_accept"], c["u_correct"], rule=rule)
+        (compare_tree_sequential if rule else compare_tree)(got, orc)
+        # the bonus token and what replaces a rejected one are the target's
+        bonus, rows = got["bonus"].long(), p["target"].view(B, N, -1)
+        at = got["deepest"].long()
+        assert bool((rows[torch.arange(B), at].gather(1, bonus[:, None]) > -INF).all())
+
+
+def check_em(got, orc, n_rows, V):
+    """The E/M step on filtered rows: a correction may be a token that the draft leaves out,
+    of log q = -inf; the gradient has no log q in it."""
+    from tests.parity import _grad_rows
+    assert np.array_equal(got["corr_tokens"].cpu().numpy().ravel(), orc["corr_tokens"].ravel())
+    for n, atol in (("logq_tok", 2e-5), ("logq_corr", 2e-5)):
+        assert np.allclose(got[n].cpu().numpy().ravel(), orc[n].ravel(), rtol=1e-6, atol=atol), n
+    a, b = got["grad"].float().cpu().numpy(), orc["grad"].reshape(n_rows, V)
+    assert np.isfinite(b).all() and np.isfinite(a).all()
+    _grad_rows("grad", a, b, "f32", float(np.abs(b).max()))
+    return np.isinf(orc["logq_corr"])
+
+
+@pytest.mark.parametrize("shape", TREES)
+def test_filtered_rows_in_the_trees_em(vsd, oracle, shape):
+    B, N = shape[:2]
+    V = shape[4]
+    p = filtered_tree(vsd, *shape, 9, torch.float32, T=0.8, top_k=24)
+    got = vsd.tree_estep_mstep(p["draft"], p["target"], p["parent"], p["tokens"], p["u_accept"], p["u_correct"], 0.8,
+                               prm=vsd.params(grad_dtype=torch.float32))
+    c = {k: v.float().cpu().numpy() if v.dtype != torch.int32 else v.cpu().numpy()
+         for k, v in p.items() if torch.is_tensor(v)}
+    orc = oracle.tree_em(c["draft"], c["target"], 0.8, c["parent"], c["tokens"], c["u_accept"], c["u_correct"])
+    check_em(got, orc, B * N, V)
+    # the loss of a tree with such a correction that counts is infinite
+    assert np.allclose(got["loss"].cpu().numpy(), orc["loss"], rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("top_k", (24, 300))
+def test_filtered_rows_in_the_em(vsd, oracle, top_k):
+    B, K, D, V, T = 4, 3, 4, 600, 0.9
+    R = B * K * D
+    q, p = filtered_pair(vsd, R, V, torch.float32, 43, T=T, top_k=top_k)
+    u = torch.rand(3, R, generator=gen(44), device="cuda")
+    got = vsd.estep_mstep(q, p, u[0], u[1], u[2], K, D, T, prm=vsd.params(grad_dtype=torch.float32))
+    orc = oracle.linear(q.cpu().numpy(), p.cpu().numpy(), T, u[0].cpu().numpy(), u[1].cpu().numpy(),
+                        u[2].cpu().numpy(), K, D)
+    assert check_em(got, orc, R, V).any() == (top_k == 24)
+    # a log q of -inf counts as -2^20, so that the loss stays finite
+    loss, want = got["loss"].cpu().numpy(), np.asarray(orc["loss"])
+    off = np.isinf(want)
+    assert off.any() == (top_k == 24) and (loss[off] > 1000).all() and np.isfinite(loss).all()
+    assert np.allclose(loss[~off], want[~off], rtol=1e-5, atol=1e-5)
