@@ -108,9 +108,10 @@ size_t vsd_sample_filtered_workspace_bytes(int32_t R, int32_t V);
  * Drawn is the first token v, in the vocabulary's order, with
  * sum of e over the kept tokens up to v  >  u[r] (sum of e over all kept);
  * u >= 1 draws the last kept token, u < 0 (or NaN) the first.
- * Sums are whole numbers (e in units of 2^-42 or finer, with a relative error of 2^-41
- * at most), so no result depends on an order of summation and equal calls give equal
- * bits.
+ * Sums are of whole numbers: each e is within 2^-41 of itself and one unit of
+ * 2^-(62 - s), s = max(12, ceil(log2 V)) (2^-45 at 128256 tokens, 2^-42 at 2^20).  So no
+ * result depends on an order of summation, equal calls give equal bits, and decisions by
+ * sums are those of real arithmetic but within 2^-41 of the sum and V units of a border.
  * A row with NaN or +inf, or all at -inf, sets VSD_STATUS_BAD_ROW; such a row, and one
  * whose parameters are refused, has token -1, logq_tok NaN, kept 0, and is all -inf in
  * `filtered`.

@@ -1,7 +1,9 @@
 // vsd_fixed.cuh -- exponentials as whole numbers: exp(-d / T) for d >= 0 in units
 // of 2^-S, so that sums of them are exact and in any order the same, and decisions
 // by them (which token a uniform number falls on, where a share of the mass is
-// reached) are those of real arithmetic but within some 2^-42 of a border.
+// reached) are those of real arithmetic but near a border: a mass is within 2^-41 of
+// itself and one unit (half of it by rounding, the rest by squares of the remainder's
+// lower half, left out), so a sum of V within 2^-41 of itself and V units.
 //
 //   y = d log2(e) / T in two floats,  y = n + j / 2048 + r,  |r| <= 2^-12,
 //   2^-y = 2^-n 2^-(j / 2048) (1 - z),  z = 1 - 2^-r = a - a^2/2 + a^3/6, a = r ln 2
@@ -151,8 +153,9 @@ __host__ __device__ __forceinline__ float neg_log(float p, const uint64_t* tab, 
 }
 
 // ln(e / w) for e, w in such units, e = exp((x - m) / T) and w a sum of such with e
-// among them: -(m - x) / T - ln(w), rounded once but for some 2^-8 of a step.  ln(w)
-// is the float l = logf(w) and what w exp(-l) is off 1.
+// among them: -(m - x) / T - ln(w), rounded once, of terms known to 2^-41 of each, and
+// 2^-50 w for exp(-l) in its units.  ln(w) is the float l = logf(w) and what w exp(-l) is
+// off 1.
 __host__ __device__ __forceinline__ float log_share(float x, float m, float T, uint64_t w, int shift,
                                                     const uint64_t* tab) {
     float inv, inv_lo, e;
