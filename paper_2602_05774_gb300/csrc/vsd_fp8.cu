@@ -26,7 +26,7 @@ constexpr int kBlock = 128;  // columns of a scale
 // s = 2^ceil(log2(amax / 448)), q = x / s, an exact product with 2^-log2(s) rounded once.
 // Bound by memory: one read, one write of half or a quarter of it.  A block of 128 or of
 // 128 x 128 stays in registers between its largest magnitude and its quotients, so x is
-// read once: 32000 x 4096 float32 by 128 rows takes 94 us, 7.1 TB/s (478 with a second
+// read once: 32000 x 4096 float32 by 128 rows takes 94 us, 7.0 TB/s (478 with a second
 // read); 4096 x 4096 bf16 by rows 17, of which the host's call is 15.
 
 // The least power of two s with amax / s <= 448 = 1.75 2^8, and its reciprocal; amax by

@@ -21,11 +21,12 @@
 //            steps of the logit brackets its place, first of a quarter of the row, then
 //            of all of it; the tokens in the bracket are listed, and the mass above it
 //            is summed exactly.  A list that overflows is bracketed within its bounds.
-//   search   whatever these leave open (large k, thousands of equal logits): bisection
+//   search   whatever these leave open (large k, thousands of equal logits, rows that
+//            begin with more masked tokens than a round of loads): bisection
 //            of the logits' ordered bits, exact counts and masses each step.
 //
-// At 4096 x 128256 bf16 (1.05 GB, 158 us at the copy's rate), us: greedy 240, top_k 50
-// 400, top_p 0.8 806 and 0.95 1606 (nuclei of 3500 tokens).  8 rows: 15 greedy, 27 with
+// At 4096 x 128256 bf16 (1.05 GB, 158 us at the copy's rate), us: greedy 245, top_k 50
+// 410, top_p 0.8 806 and 0.95 1630 (nuclei of 3500 tokens).  8 rows: 15 greedy, 27 with
 // top_k 50, 113 with top_p 0.95: one block's latency.  Measured against it: blocks of 256
 // with lists of 2048, three to an SM (greedy 198, top_p 0.95 a fifth slower); blocks of
 // 1024 where there is a row an SM at most (8 x 128256: 2 us more for greedy and top_k, a

@@ -771,7 +771,7 @@ def lmhead_logits_fp8(hidden, hidden_scale, weight, weight_scale, out=None, work
 
 
 def _policy(R, logits, T, top_k, top_p, min_p):
-    """The struct, and the tensors in it."""
+    """The struct; the tensors whose pointers it holds are the caller's."""
     values, rows = [], []
     for name, v, dtype, off in (("T", T, torch.float32, 1.0), ("top_k", top_k, torch.int32, 0),
                                 ("top_p", top_p, torch.float32, 1.0),
