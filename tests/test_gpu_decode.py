@@ -1065,3 +1065,25 @@ def test_filtered_rows_in_the_em(vsd, oracle, top_k):
     off = np.isinf(want)
     assert off.any() == (top_k == 24) and (loss[off] > 1000).all() and np.isfinite(loss).all()
     assert np.allclose(loss[~off], want[~off], rtol=1e-5, atol=1e-5)
+
+
+@pytest.mark.parametrize("R", (5, 60, 128, 300))
+def test_head_scales_out_of_range_in_some_tiles_alone(vsd, R):
+    """A few of a thousand blocks of the weight, in any of a block of threads' tiles."""
+    V, H = 128256, 272
+    h, hs, w, ws = operands(R, V, H, 7 * R, pow2=False)
+    want = vsd.lmhead_logits_fp8(h, hs, w, ws)
+    odd = torch.randperm(V // 128, generator=gen(R), device="cuda")[:40]
+    hs[R // 2] *= 2.0 ** -70
+    ws[odd[:20], 1] *= 2.0 ** 126
+    ws[odd[20:], 2] *= 2.0 ** -80
+    out = vsd.lmhead_logits_fp8(h, hs, w, ws)
+    x, err = head_reference(h, hs, w, ws)
+    sure = x.abs() < 2.0 ** 127
+    tol = err + 2.0 ** -8 * (x.abs() + err) + 2.0 ** -133
+    assert bool((((out.double() - x).abs() <= tol) | ~sure).all())
+    # what has usual scales keeps its bits
+    on = torch.ones(R, V, dtype=torch.bool, device="cuda")
+    on[R // 2] = False
+    on.view(R, -1, 128)[:, odd] = False
+    assert torch.equal(out[on], want[on])
