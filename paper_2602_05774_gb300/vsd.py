@@ -784,6 +784,9 @@ def _policy(R, logits, T, top_k, top_p, min_p):
             values.append(off)
             rows.append(v.data_ptr())
         else:
+            if name in ("T", "min_p") and v != 0 and C.c_float(v).value == 0:
+                # (0 would mean greedy, or off)
+                raise ValueError("%s must be 0 or within float32's range" % name)
             values.append(max(0, min(int(v), 2 ** 31 - 1)) if dtype == torch.int32 else float(v))
             rows.append(None)
     return Policy(*values, *rows)

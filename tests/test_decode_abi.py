@@ -173,3 +173,14 @@ def test_settings_reach_the_struct(vsd, monkeypatch):
     assert (p.top_p, p.min_p) == (0.5, 0.25)
     for given, held in ((-5, 0), (7, 7), (1 << 40, 2 ** 31 - 1)):  # (beyond 32 bits: off still)
         assert vsd._policy(3, x, 1.0, given, 1.0, 0.0).top_k == held
+
+
+def test_settings_that_round_to_zero_are_refused(vsd, monkeypatch):
+    """As float32 they would mean something else: greedy, or off."""
+    monkeypatch.setattr(vsd, "_need_cuda", lambda *ts: None)
+    x = torch.zeros(3, 8)
+    for kw in (dict(T=1e-46), dict(min_p=1e-46), dict(min_p=1e-300)):
+        with pytest.raises(ValueError, match="float32"):
+            vsd._policy(3, x, **dict(dict(T=1.0, top_k=0, top_p=1.0, min_p=0.0), **kw))
+    p = vsd._policy(3, x, 0, 0, 1e-46, 2.0 ** -149)
+    assert (p.T, p.top_p, p.min_p) == (0.0, 0.0, 2.0 ** -149)  # (top_p: the first token alone, either way)
